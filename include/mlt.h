@@ -32,6 +32,7 @@
 #ifndef MLT_H
 #define MLT_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -497,6 +498,91 @@ int mlt_tune_ordinal(int mode);
  * table, read wholly through L1/L2.  Model A always uses the compact
  * table.  Results never depend on the format.  Host-only. */
 int mlt_tune_head_levels(int levels);
+
+/* ---------------------------------------------------------------------------
+ * Sequence-model operators: a learned proposer beside the tree ensembles.
+ *
+ * The paper leaves the explorer's search open (Sec. 2, "Configuration
+ * Explorer") and retrains its models every tuning iteration.  These calls are
+ * what a proposer over knob digits and tuning histories needs next to
+ * screening: draws from scores instead of the top-k (mlt_sample), and digits
+ * or tokens to vectors with the gradient of the table (mlt_embed,
+ * mlt_embed_grad).  The paper has no counterpart.
+ *
+ * They keep no state between calls and use no library scratch: a call that
+ * needs a workspace takes it from the caller (device memory of at least the
+ * bytes its ..._workspace call gives, 256-byte aligned), so calls with
+ * workspaces of their own may run on different streams at once and be captured
+ * in graphs.  All are asynchronous on `stream`.  The first call on a device
+ * allocates the error word that mlt_sync_status reads; issue it outside a
+ * capture.
+ *
+ * Element types of the buffers that may be narrow.  Sums and states are held in
+ * fp32 and rounded once. */
+enum { MLT_F32 = 0, MLT_BF16 = 1, MLT_F16 = 2 };
+
+/* How a row is drawn from (16 bytes).  Out of range (temperature negative or
+ * not finite, top_p or min_p NaN): the row draws nothing, and the next
+ * mlt_sync_status reports MLT_EINVAL. */
+typedef struct {
+    float temperature; /* 0: the best alone, the other fields ignored        */
+    int32_t top_k;     /* the k best are kept; <= 0: all                     */
+    float top_p;       /* of these the fewest best with this share of their
+                          probability; >= 1: all                             */
+    float min_p;       /* of these those at least this probable, relative to
+                          the best; <= 0: all.  No cut drops the best.       */
+} mlt_sample_rule;
+
+/* Draw m different entries of every row of scores by their probability
+ * softmax(score / temperature), from given random numbers.
+ *   s_i    = clamp(fl(fl(1 / temperature) * score_i)) to the finite floats;
+ *            a NaN or -infinity score is never drawn (what mlt_screen gives
+ *            candidates that V rejects)
+ *   order    s descending, index ascending; the rule keeps a prefix of it
+ *   key_i  = clamp(fl(s_i + noise_i)) to the finite floats (NaN: the lowest)
+ *   out_index[r][j]   = the kept entry with the j-th largest (key, then
+ *            smallest index); -1 past the last kept one
+ *   out_logprob[r][j] = its s - ln(sum over the row's drawable entries of
+ *            exp s): the log-probability before the rule's cuts; 0 at
+ *            temperature 0; -infinity where out_index is -1
+ * With Gumbel noise, -ln(-ln u) of uniform u, these are m draws without
+ * replacement, the first one exactly a draw from the kept entries' softmax.
+ * Probability masses are summed in 64-bit fixed point (units of 2^-35 of the
+ * best entry's weight at n = 2^27, finer for shorter rows), so results do not
+ * depend on the order of summation.
+ *   scores   device [rows][n] of `dtype`, row_stride elements apart
+ *   noise    device [rows][n] fp32, noise_stride elements apart
+ *   rule     host, for every row; or `rules`, device [rows], instead of it
+ *            (the other one NULL)
+ *   rows     0 .. 2^31-1;  n  0 .. 2^27;  m  1 .. 2048
+ *   out_index device [rows][m] int64;  out_logprob device [rows][m] fp32 */
+int mlt_sample(void *stream, const void *scores, int dtype, int64_t rows, int64_t n, int64_t row_stride,
+               const float *noise, int64_t noise_stride, const mlt_sample_rule *rule,
+               const mlt_sample_rule *rules, int m, void *workspace, size_t workspace_bytes,
+               int64_t *out_index, float *out_logprob);
+int mlt_sample_workspace(int dtype, int64_t rows, int64_t n, int m, size_t *bytes_out);
+
+/* Embedding lookup: out[i][c] = round(scale * table[ids[i]][c]).  A negative
+ * id is padding (a row of zeros); an id >= vocab gives zeros too and is
+ * reported by the next mlt_sync_status (MLT_EINVAL).
+ *   table  device [vocab][dim] of `dtype`, table_stride elements apart
+ *   ids    device [tokens], int64 if ids_64 else int32
+ *   out    device [tokens][dim] of `out_dtype`, out_stride elements apart
+ *   tokens 0 .. 2^31-1;  vocab 1 .. 2^31-1;  dim 1 .. 2^20 */
+int mlt_embed(void *stream, const void *table, int dtype, int64_t vocab, int dim, int64_t table_stride,
+              const void *ids, int ids_64, int64_t tokens, float scale, void *out, int out_dtype,
+              int64_t out_stride);
+
+/* Its gradient: grad_table[v][c] = round(scale * sum over i with ids[i] = v of
+ * grad_out[i][c]), zero for rows no id names; every row is written.  The
+ * positions are sorted by id first and each row's sum has a fixed order, so
+ * the result is the same from call to call.
+ *   grad_out   device [tokens][dim] of `dtype`, grad_stride elements apart
+ *   grad_table device [vocab][dim] of `out_dtype`, out_stride elements apart */
+int mlt_embed_grad(void *stream, const void *grad_out, int dtype, int64_t grad_stride, const void *ids,
+                   int ids_64, int64_t tokens, int64_t vocab, int dim, float scale, void *workspace,
+                   size_t workspace_bytes, void *grad_table, int out_dtype, int64_t out_stride);
+int mlt_embed_grad_workspace(int64_t tokens, int64_t vocab, int dim, size_t *bytes_out);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

@@ -1,0 +1,537 @@
+// Embedding lookup and its gradient.
+//
+//   out[i][c]  = round(scale * table[id_i][c])              (one rounding)
+//   grad[v][c] = round(scale * sum over i with id_i = v of g[i][c])
+//
+// A negative id is padding: its output row is zero and it adds to no
+// gradient.  An id >= vocab does the same and sets the error word.
+//
+// Both are bound by memory: the lookup reads each distinct row and writes
+// tokens x dim values, the gradient reads tokens x dim values once and writes
+// vocab x dim.  The gradient sorts the token positions by id (stable radix
+// sort, 8 bits a pass, so equal ids keep the order of their positions) and adds each
+// run of equal ids in that order: no atomics on floating point, so the result
+// does not change from call to call, and every gradient row is written once.
+#include "seq.cuh"
+
+namespace mlt {
+namespace {
+
+template <typename I>
+__device__ __forceinline__ long long load_id(const void* ids, long long i) {
+  return static_cast<long long>(static_cast<const I*>(ids)[i]);
+}
+__device__ __forceinline__ long long id_of(const void* ids, int ids_64, long long i) {
+  return ids_64 ? load_id<long long>(ids, i) : load_id<int>(ids, i);
+}
+
+// ---------------------------------------------------------------------------
+// Lookup: `lanes` lanes of a warp per row (a power of two), kUnroll packs of V
+// elements a lane, so every lane has kUnroll independent loads in flight.
+// ---------------------------------------------------------------------------
+constexpr int kUnroll = 4;
+
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(256) k_embed(const TI* table, long long in_stride, const void* ids, int ids_64,
+                                               long long tokens, long long vocab, int dim, float scale, TO* out,
+                                               long long out_stride, int lanes, unsigned* err) {
+  const int lane = threadIdx.x & (lanes - 1);
+  const long long i = static_cast<long long>(blockIdx.x) * (256 / lanes) + threadIdx.x / lanes;
+  pdl_wait();
+  pdl_trigger();
+  if (i >= tokens) return;
+  const long long id = id_of(ids, ids_64, i);
+  const bool live = id >= 0 && id < vocab;
+  const int packs = dim / V;
+  const int first = blockIdx.y * lanes * kUnroll + lane;
+  if (id >= vocab && first == 0) atomicOr(err, kErrBadToken);
+  const TI* row = table + (live ? id : 0) * in_stride;
+  TO* dst = out + i * out_stride;
+  Pack<TI, V> p[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int c = first + u * lanes;
+    if (live && c < packs) p[u] = *reinterpret_cast<const Pack<TI, V>*>(row + static_cast<long long>(c) * V);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int c = first + u * lanes;
+    if (c >= packs) break;
+    Pack<TO, V> q;
+#pragma unroll
+    for (int e = 0; e < V; ++e) q.v[e] = from_f32<TO>(live ? __fmul_rn(to_f32(p[u].v[e]), scale) : 0.0f);
+    *reinterpret_cast<Pack<TO, V>*>(dst + static_cast<long long>(c) * V) = q;
+  }
+}
+
+// Widest pack (elements) that divides the row length, both strides and both
+// addresses; at most 16 bytes of the narrower type.
+int pack_width(const EmbedArgs& a) {
+  const size_t si = dtype_size(a.in_dtype), so = dtype_size(a.out_dtype);
+  for (int v = si == 4 && so == 4 ? 4 : 8; v > 1; v /= 2) {
+    const size_t bi = v * si > 16 ? 16 : v * si, bo = v * so > 16 ? 16 : v * so;
+    if (a.dim % v == 0 && a.in_stride % v == 0 && a.out_stride % v == 0 && aligned_to(a.table, bi) &&
+        aligned_to(a.out, bo))
+      return v;
+  }
+  return 1;
+}
+
+template <typename F>
+cudaError_t with_width(int v, F f) {
+  switch (v) {
+    case 8: return f(std::integral_constant<int, 8>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 2: return f(std::integral_constant<int, 2>());
+    default: return f(std::integral_constant<int, 1>());
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Stable radix sort of token positions by id
+// ---------------------------------------------------------------------------
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortPerLane = 8;
+constexpr int kSortTile = kSortThreads * kSortPerLane;
+constexpr int kDigits = 256;
+
+struct SortPass {
+  const void* ids;  // first pass: the ids themselves, else null
+  int ids_64;
+  const uint32_t* keys_in;
+  const uint32_t* pos_in;
+  uint32_t* keys_out;
+  uint32_t* pos_out;
+  uint32_t* counts;  // [kDigits][tiles], then prefixes over the tiles
+  uint32_t* totals;  // [kDigits]
+  long long tokens, vocab;
+  int tiles, shift;
+  unsigned* err;
+};
+
+// Ids outside [0, vocab) sort behind all others.
+__device__ __forceinline__ uint32_t sort_key(const SortPass& s, long long i) {
+  if (s.ids == nullptr) return s.keys_in[i];
+  const long long id = id_of(s.ids, s.ids_64, i);
+  return static_cast<uint32_t>(id < 0 || id >= s.vocab ? s.vocab : id);
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(SortPass s) {
+  __shared__ uint32_t hist[kDigits];
+  for (int d = threadIdx.x; d < kDigits; d += kSortThreads) hist[d] = 0;
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const long long base = static_cast<long long>(blockIdx.x) * kSortTile;
+#pragma unroll
+  for (int k = 0; k < kSortPerLane; ++k) {
+    const long long i = base + k * kSortThreads + threadIdx.x;
+    if (i >= s.tokens) break;
+    if (s.ids != nullptr && id_of(s.ids, s.ids_64, i) >= s.vocab) atomicOr(s.err, kErrBadToken);
+    atomicAdd(&hist[(sort_key(s, i) >> s.shift) & (kDigits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < kDigits; d += kSortThreads)
+    s.counts[static_cast<long long>(d) * s.tiles + blockIdx.x] = hist[d];
+}
+
+// One CTA per digit: exclusive prefix over its tiles.
+__global__ void __launch_bounds__(256) k_sort_scan(uint32_t* counts, uint32_t* totals, int tiles) {
+  __shared__ uint32_t part[8];
+  pdl_wait();
+  pdl_trigger();
+  uint32_t* row = counts + static_cast<long long>(blockIdx.x) * tiles;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t carry = 0;
+  for (int t0 = 0; t0 < tiles; t0 += 256) {
+    const int t = t0 + threadIdx.x;
+    const uint32_t c = t < tiles ? row[t] : 0;
+    uint32_t v = c;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const uint32_t w = __shfl_up_sync(~0u, v, o);
+      if (lane >= o) v += w;
+    }
+    if (lane == 31) part[warp] = v;
+    __syncthreads();
+    uint32_t below = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) below += part[w];
+      all += part[w];
+    }
+    if (t < tiles) row[t] = carry + below + v - c;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
+  __shared__ uint32_t cnt[kSortWarps][kDigits];
+  __shared__ uint32_t warp_sum[kDigits / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int d = lane; d < kDigits; d += 32) cnt[warp][d] = 0;
+  __syncwarp();
+  pdl_wait();
+  pdl_trigger();
+  // a warp owns kSortPerLane * 32 consecutive positions; rank[k] counts the
+  // equal digits before the lane's k-th one within the warp
+  const long long base = static_cast<long long>(blockIdx.x) * kSortTile + warp * (kSortPerLane * 32) + lane;
+  uint32_t key[kSortPerLane], rank[kSortPerLane];
+#pragma unroll
+  for (int k = 0; k < kSortPerLane; ++k) {
+    const long long i = base + k * 32;
+    key[k] = i < s.tokens ? sort_key(s, i) : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < kSortPerLane; ++k) {
+    const bool in = base + k * 32 < s.tokens;
+    const uint32_t d = in ? (key[k] >> s.shift) & (kDigits - 1) : kDigits;
+    const unsigned peers = __match_any_sync(~0u, d);
+    const unsigned before = peers & ((1u << lane) - 1u);
+    uint32_t seen = 0;
+    if (in) seen = cnt[warp][d];
+    __syncwarp();
+    rank[k] = seen + __popc(before);
+    if (in && before == 0) cnt[warp][d] = seen + __popc(peers);
+    __syncwarp();
+  }
+  __syncthreads();
+  // digit d's first place: digits below it, tiles before this one, warps before
+  const int d = threadIdx.x;
+  uint32_t total = 0, v = 0;
+  if (d < kDigits) {
+    total = s.totals[d];
+    v = total;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const uint32_t w = __shfl_up_sync(~0u, v, o);
+      if (lane >= o) v += w;
+    }
+    if (lane == 31) warp_sum[warp] = v;
+  }
+  __syncthreads();
+  if (d < kDigits) {
+    uint32_t at = v - total;
+    for (int w = 0; w < warp; ++w) at += warp_sum[w];
+    at += s.counts[static_cast<long long>(d) * s.tiles + blockIdx.x];
+    for (int w = 0; w < kSortWarps; ++w) {
+      const uint32_t c = cnt[w][d];
+      cnt[w][d] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSortPerLane; ++k) {
+    const long long i = base + k * 32;
+    if (i >= s.tokens) break;
+    const uint32_t to = cnt[warp][(key[k] >> s.shift) & (kDigits - 1)] + rank[k];
+    s.keys_out[to] = key[k];
+    s.pos_out[to] = s.ids != nullptr ? static_cast<uint32_t>(i) : s.pos_in[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Sums over runs of equal ids
+// ---------------------------------------------------------------------------
+// The sorted positions are cut into pieces of `piece`.  `lanes` lanes of a warp
+// (a power of two) add the rows of one piece for lanes x V columns.  A run that lies inside
+// a piece is finished there; of one that crosses pieces, `lead` takes the sum of
+// the part that began before the piece and `trail` of the part that begins in it
+// and goes on.  k_grad_join adds those in order.
+struct GradArgs {
+  const uint32_t* keys;
+  const uint32_t* pos;
+  long long tokens, vocab;
+  int dim, lanes, piece;
+  long long pieces;
+  float scale;
+  long long in_stride, out_stride;
+  float* lead;   // [pieces][dim]
+  float* trail;  // [pieces][dim]
+  long long sum_blocks;  // of k_grad_sum's grid.x; the rest clears rows no id names
+};
+
+__device__ __forceinline__ long long lower_bound(const uint32_t* keys, long long n, uint32_t v) {
+  long long lo = 0, hi = n;
+  while (lo < hi) {
+    const long long mid = (lo + hi) >> 1;
+    if (keys[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+constexpr int kSumThreads = 128;
+constexpr int kSumUnroll = 8;
+
+template <typename TG, int V>
+__device__ __forceinline__ void store_row(TG* out, const float (&acc)[V], float scale) {
+  Pack<TG, V> q;
+#pragma unroll
+  for (int e = 0; e < V; ++e) q.v[e] = from_f32<TG>(__fmul_rn(acc[e], scale));
+  *reinterpret_cast<Pack<TG, V>*>(out) = q;
+}
+
+template <typename TI, typename TG, int V>
+__global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradArgs a, const TI* grad, TG* out) {
+  const int groups = kSumThreads / a.lanes;
+  const int lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
+  const int col = (blockIdx.y * a.lanes + lane) * V;
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x >= a.sum_blocks) {
+    // rows that no id names
+    const long long v = (blockIdx.x - a.sum_blocks) * groups + group;
+    if (v >= a.vocab || col >= a.dim) return;
+    const long long at = lower_bound(a.keys, a.tokens, static_cast<uint32_t>(v));
+    if (at < a.tokens && a.keys[at] == static_cast<uint32_t>(v)) return;
+    const float zero[V] = {};
+    store_row<TG, V>(out + v * a.out_stride + col, zero, 1.0f);
+    return;
+  }
+  const long long p = static_cast<long long>(blockIdx.x) * groups + group;
+  if (p >= a.pieces || col >= a.dim) return;
+  const long long begin = p * a.piece, end = min(begin + a.piece, a.tokens);
+  const uint32_t none = static_cast<uint32_t>(a.vocab);
+  uint32_t run = a.keys[begin];
+  bool led = begin > 0 && a.keys[begin - 1] == run;  // the current run began before the piece
+  float acc[V] = {};
+  auto flush = [&]() {
+    if (run >= none) return;
+    if (led) {
+      Pack<float, V>* q = reinterpret_cast<Pack<float, V>*>(a.lead + p * a.dim + col);
+      Pack<float, V> w;
+#pragma unroll
+      for (int e = 0; e < V; ++e) w.v[e] = acc[e];
+      *q = w;
+    } else {
+      store_row<TG, V>(out + run * a.out_stride + col, acc, a.scale);
+    }
+  };
+  for (long long i = begin; i < end; i += kSumUnroll) {
+    uint32_t key[kSumUnroll];
+    Pack<TI, V> g[kSumUnroll];
+#pragma unroll
+    for (int u = 0; u < kSumUnroll; ++u) {
+      key[u] = i + u < end ? a.keys[i + u] : none;
+      if (key[u] < none)
+        g[u] = *reinterpret_cast<const Pack<TI, V>*>(grad + static_cast<long long>(a.pos[i + u]) * a.in_stride + col);
+    }
+#pragma unroll
+    for (int u = 0; u < kSumUnroll; ++u) {
+      if (i + u >= end) break;
+      if (key[u] != run) {
+        flush();
+        run = key[u];
+        led = false;
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+      }
+      if (key[u] < none) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += to_f32(g[u].v[e]);
+      }
+    }
+  }
+  if (run >= none) return;
+  const bool goes_on = end < a.tokens && a.keys[end] == run;
+  if (goes_on && !led) {
+    Pack<float, V> w;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w.v[e] = acc[e];
+    *reinterpret_cast<Pack<float, V>*>(a.trail + p * a.dim + col) = w;
+  } else {
+    flush();
+  }
+}
+
+// One CTA per piece and 32 x V columns: finishes the run that begins in the piece and goes on past it.
+// Warp w adds the pieces p + 1 + w, + 8, ...; the warps' sums are added in order.
+constexpr int kJoinWarps = 8;
+
+template <typename TG, int V>
+__global__ void __launch_bounds__(kJoinWarps * 32) k_grad_join(GradArgs a, TG* out) {
+  __shared__ float part[kJoinWarps][32 * V];
+  pdl_wait();
+  pdl_trigger();
+  const long long p = blockIdx.x;
+  const long long begin = p * a.piece, end = min(begin + a.piece, a.tokens);
+  if (end >= a.tokens) return;
+  const uint32_t run = a.keys[end - 1];
+  if (run >= static_cast<uint32_t>(a.vocab) || a.keys[end] != run) return;
+  if (a.keys[begin] == run && begin > 0 && a.keys[begin - 1] == run) return;  // it began earlier
+  // last piece that the run reaches into
+  const long long last = (end + lower_bound(a.keys + end, a.tokens - end, run + 1) - 1) / a.piece;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int col = (blockIdx.y * 32 + lane) * V;
+  const bool in = col < a.dim;
+  float acc[V] = {};
+  if (in) {
+    if (warp == 0) {
+      const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.trail + p * a.dim + col);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] = w.v[e];
+    }
+#pragma unroll 4
+    for (long long q = p + 1 + warp; q <= last; q += kJoinWarps) {
+      const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.lead + q * a.dim + col);
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[e] += w.v[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) part[warp][lane * V + e] = acc[e];
+  __syncthreads();
+  if (warp != 0 || !in) return;
+  for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] += part[w][lane * V + e];
+  store_row<TG, V>(out + run * a.out_stride + col, acc, a.scale);
+}
+
+int pow2_at_most_32(long long v) {
+  int l = 1;
+  while (l < 32 && l < v) l *= 2;
+  return l;
+}
+
+struct GradPlan {
+  int tiles, passes, piece;
+  long long pieces;
+  size_t off_keys[2], off_pos[2], off_counts, off_totals, off_lead, off_trail, bytes;
+};
+
+// Pieces: about 24 warps for each SM over all column chunks, 16 to 512 rows
+// each, so that a run's partial sums stay few beside the rows they stand for.
+GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
+  GradPlan g{};
+  const long long n = tokens < 1 ? 1 : tokens;
+  g.tiles = static_cast<int>((n + kSortTile - 1) / kSortTile);
+  int bits = 1;
+  while (bits < 32 && (vocab >> bits) != 0) ++bits;
+  g.passes = (bits + 7) / 8;
+  const long long work = n * ((dim + 127) / 128);
+  g.piece = 16;
+  while (g.piece < 512 && work / g.piece > 24LL * sms) g.piece *= 2;
+  g.pieces = (n + g.piece - 1) / g.piece;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += up256(bytes);
+    return o;
+  };
+  for (int k = 0; k < 2; ++k) {
+    g.off_keys[k] = take(n * 4);
+    g.off_pos[k] = take(n * 4);
+  }
+  g.off_counts = take(static_cast<size_t>(kDigits) * g.tiles * 4);
+  g.off_totals = take(kDigits * 4);
+  g.off_lead = take(static_cast<size_t>(g.pieces) * dim * 4);
+  g.off_trail = take(static_cast<size_t>(g.pieces) * dim * 4);
+  g.bytes = at;
+  return g;
+}
+
+}  // namespace
+
+cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t st) {
+  if (a.tokens == 0) return cudaSuccess;
+  ++*launches;
+  return with_width(pack_width(a), [&](auto width) {
+    constexpr int V = decltype(width)::value;
+    return with_dtype(a.in_dtype, [&](auto ti) {
+      return with_dtype(a.out_dtype, [&](auto to) {
+        using TI = decltype(ti);
+        using TO = decltype(to);
+        const int packs = a.dim / V;
+        const int lanes = pow2_at_most_32((packs + kUnroll - 1) / kUnroll);
+        const long long per = 256 / lanes;
+        const dim3 grid(static_cast<unsigned>((a.tokens + per - 1) / per),
+                        static_cast<unsigned>((packs + lanes * kUnroll - 1) / (lanes * kUnroll)));
+        return launch_pdl(k_embed<TI, TO, V>, grid, dim3(256), 0, st, static_cast<const TI*>(a.table), a.in_stride,
+                          a.ids, a.ids_64, a.tokens, a.vocab, a.dim, a.scale, static_cast<TO*>(a.out), a.out_stride,
+                          lanes, a.err);
+      });
+    });
+  });
+}
+
+size_t embed_grad_workspace(long long tokens, long long vocab, int dim, int sms) {
+  return grad_plan(tokens, vocab, dim, sms).bytes;
+}
+
+cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st) {
+  const GradPlan g = grad_plan(a.tokens, a.vocab, a.dim, sms);
+  unsigned char* ws = static_cast<unsigned char*>(a.ws);
+  auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
+  const uint32_t *keys = nullptr, *pos = nullptr;
+  if (a.tokens > 0) {
+    for (int k = 0; k < g.passes; ++k) {
+      SortPass s{};
+      s.ids = k == 0 ? a.ids : nullptr;
+      s.ids_64 = a.ids_64;
+      s.keys_in = keys;
+      s.pos_in = pos;
+      s.keys_out = u32(g.off_keys[k & 1]);
+      s.pos_out = u32(g.off_pos[k & 1]);
+      s.counts = u32(g.off_counts);
+      s.totals = u32(g.off_totals);
+      s.tokens = a.tokens;
+      s.vocab = a.vocab;
+      s.tiles = g.tiles;
+      s.shift = 8 * k;
+      s.err = a.err;
+      cudaError_t e = launch_pdl(k_sort_count, dim3(g.tiles), dim3(kSortThreads), 0, st, s);
+      if (e != cudaSuccess) return e;
+      e = launch_pdl(k_sort_scan, dim3(kDigits), dim3(256), 0, st, s.counts, s.totals, g.tiles);
+      if (e != cudaSuccess) return e;
+      e = launch_pdl(k_sort_scatter, dim3(g.tiles), dim3(kSortThreads), 0, st, s);
+      if (e != cudaSuccess) return e;
+      *launches += 3;
+      keys = s.keys_out;
+      pos = s.pos_out;
+    }
+  }
+  GradArgs q{};
+  q.keys = keys;
+  q.pos = pos;
+  q.tokens = a.tokens;
+  q.vocab = a.vocab;
+  q.dim = a.dim;
+  q.piece = g.piece;
+  q.pieces = a.tokens > 0 ? g.pieces : 0;
+  q.scale = a.scale;
+  q.in_stride = a.in_stride;
+  q.out_stride = a.out_stride;
+  q.lead = reinterpret_cast<float*>(ws + g.off_lead);
+  q.trail = reinterpret_cast<float*>(ws + g.off_trail);
+  return with_width(pack_width(a), [&](auto width) {
+    constexpr int V = decltype(width)::value;
+    return with_dtype(a.in_dtype, [&](auto ti) {
+      return with_dtype(a.out_dtype, [&](auto to) {
+        using TI = decltype(ti);
+        using TO = decltype(to);
+        const int packs = a.dim / V;
+        q.lanes = pow2_at_most_32(packs);
+        const long long groups = kSumThreads / q.lanes;
+        q.sum_blocks = (q.pieces + groups - 1) / groups;
+        const unsigned chunks = static_cast<unsigned>((packs + q.lanes - 1) / q.lanes);
+        const dim3 grid(static_cast<unsigned>(q.sum_blocks + (a.vocab + groups - 1) / groups), chunks);
+        cudaError_t e = launch_pdl(k_grad_sum<TI, TO, V>, grid, dim3(kSumThreads), 0, st, q,
+                                   static_cast<const TI*>(a.table), static_cast<TO*>(a.out));
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        if (q.pieces < 2) return cudaSuccess;
+        ++*launches;
+        return launch_pdl(k_grad_join<TO, V>, dim3(static_cast<unsigned>(q.pieces), (packs + 31) / 32),
+                          dim3(kJoinWarps * 32), 0, st, q, static_cast<TO*>(a.out));
+      });
+    });
+  });
+}
+
+}  // namespace mlt

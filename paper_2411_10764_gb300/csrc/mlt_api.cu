@@ -1332,6 +1332,36 @@ int install_model(int model_id, const std::vector<unsigned char>& packed, const 
 
 }  // namespace
 
+// What the sequence-model entry points (seq_api.cu) share with these.
+namespace mlt {
+
+int api_fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return fail(code, "%s", buf);
+}
+
+unsigned* api_error_word(int* rc) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  *rc = ensure_scratch(0);
+  return *rc == MLT_OK ? g_scr.err : nullptr;
+}
+
+void api_count_launches(long long n) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  g_launches += n;
+}
+
+int api_sm_count() {
+  std::lock_guard<std::mutex> lk(g_mu);
+  return sm_count();
+}
+
+}  // namespace mlt
+
 extern "C" {
 
 int mlt_set_num_features(int F) {
@@ -1806,6 +1836,8 @@ int mlt_sync_status(void* stream) {
   }
   if (word == 0) return MLT_OK;
   if (word & kErrWaitTimeout) return fail(MLT_ETIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
+  if (word & kErrBadRule) return fail(MLT_EINVAL, "a sampling rule was out of range (error word 0x%x)", word);
+  if (word & kErrBadToken) return fail(MLT_EINVAL, "an embedding id was not below vocab (error word 0x%x)", word);
   if (word & kErrBadIndex) return fail(MLT_EINVAL, "a rerank candidate index was outside [0, n) (error word 0x%x)", word);
   return fail(MLT_ECUDA, "device-side bookkeeping error (error word 0x%x)", word);
 }

@@ -22,6 +22,8 @@ constexpr int kMaxFullDepth = 10;  // deeper ensembles use the compact table
 constexpr unsigned kErrWaitTimeout = 1u;  // an mbarrier wait gave up
 constexpr unsigned kErrSelect = 2u;       // top-k bookkeeping out of range
 constexpr unsigned kErrBadIndex = 4u;     // a rerank candidate index outside [0, n)
+constexpr unsigned kErrBadRule = 8u;      // a sampling rule out of range
+constexpr unsigned kErrBadToken = 16u;    // an embedding id not below vocab
 
 // A bounded device wait gives up after this many nanoseconds.
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;

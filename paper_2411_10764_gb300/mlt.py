@@ -25,6 +25,14 @@ NODE_DTYPE = np.dtype(
 )
 OP_DTYPE = np.dtype([("op", "<i4"), ("a", "<i4"), ("b", "<i4"), ("c", "<f4")])
 
+MLT_F32, MLT_BF16, MLT_F16 = 0, 1, 2
+
+
+class SampleRule(C.Structure):
+    """mlt_sample_rule"""
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
+
+
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
 
 
@@ -87,6 +95,11 @@ def lib(build_if_missing: bool = True):
             "mlt_merge_topk": [P, P, P, i64, i32, P],
             "mlt_screen_until": [P, P, i64, i64, i64, f32, i32, P, P, P, P],
             "mlt_screen_until_decoded": [P, P, P, i32, P, i64, i64, i64, i64, f32, i32, P, P, P, P],
+            "mlt_sample": [P, P, i32, i64, i64, i64, P, i64, P, P, i32, P, C.c_size_t, P, P],
+            "mlt_sample_workspace": [i32, i64, i64, i32, P],
+            "mlt_embed": [P, P, i32, i64, i32, i64, P, i32, i64, f32, P, i32, i64],
+            "mlt_embed_grad": [P, P, i32, i64, P, i32, i64, i64, i32, f32, P, C.c_size_t, P, i32, i64],
+            "mlt_embed_grad_workspace": [i64, i64, i32, P],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -292,6 +305,185 @@ def merge_topk(scores, indices, k: int, out=None, stream=None):
     if out is None:
         out = torch.empty(int(k), dtype=torch.int64, device=indices.device)
     _check(lib().mlt_merge_topk(_stream_ptr(stream), _dptr(scores), _dptr(indices), m, int(k), _dptr(out)))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Sequence-model operators
+# ---------------------------------------------------------------------------
+
+_DTYPES = {}
+
+
+def _dtype_code(t) -> int:
+    if not _DTYPES:
+        import torch
+
+        _DTYPES.update({torch.float32: MLT_F32, torch.bfloat16: MLT_BF16, torch.float16: MLT_F16})
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"float32, bfloat16 or float16 wanted, got {t.dtype}") from None
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _cuda(t, name: str, dtype=None):
+    import torch
+
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and (dtype is None or t.dtype == dtype)):
+        raise TypeError(f"{name} must be a CUDA tensor" + (f" of {dtype}" if dtype is not None else ""))
+    return t
+
+
+def _rows(t, name: str) -> int:
+    """Elements between the rows of a matrix whose columns are adjacent."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have adjacent columns")
+    return t.stride(0)
+
+
+_ws_bytes: dict = {}
+
+
+def _workspace(key, query, device, stream):
+    """Device memory for one call (torch's allocator keeps it until the work
+    queued on the stream is done); the sizes that the library asks for are
+    remembered by the call's sizes."""
+    n = _ws_bytes.get(key)
+    if n is None:
+        out = C.c_size_t()
+        _check(query(out))
+        if len(_ws_bytes) > 4096:
+            _ws_bytes.clear()
+        n = _ws_bytes[key] = out.value
+    if n == 0:
+        return None, 0
+    import torch
+
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws, n
+
+
+def sample_rules(temperature, top_k=0, top_p=1.0, min_p=0.0, rows: int | None = None, device="cuda"):
+    """mlt_sample_rule records for mlt.sample's `rules`: an int32 CUDA tensor
+    [rows][4].  Each argument is a number or one value a row."""
+    import torch
+
+    cols = [torch.as_tensor(v, dtype=dt, device=device) for v, dt in
+            ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32))]
+    if rows is None:
+        rows = max([c.numel() for c in cols if c.dim() > 0], default=1)
+    cols = [c.expand(rows).contiguous().view(torch.int32) for c in cols]
+    return torch.stack(cols, 1).contiguous()
+
+
+def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+           m: int = 1, rules=None, out=None, stream=None):
+    """mlt_sample: m different entries of every row of `scores` ([rows][n], or
+    [n] for one row) drawn with the given noise (fp32, same shape; Gumbel
+    numbers -ln(-ln u)).  `rules` (sample_rules) gives every row its own
+    cuts instead of the four numbers.  Returns (index [rows][m] int64, -1
+    past the last kept entry, logprob [rows][m] fp32)."""
+    import torch
+
+    _cuda(scores, "scores")
+    code = _dtype_code(scores)
+    _cuda(noise, "noise", torch.float32)
+    one = scores.dim() == 1
+    if one:
+        scores, noise = scores[None], noise[None] if noise.dim() == 1 else noise
+    if noise.shape != scores.shape:
+        raise ValueError("scores and noise differ in shape")
+    stride, noise_stride = _rows(scores, "scores"), _rows(noise, "noise")
+    rows, n = scores.shape
+    m = int(m)
+    rule = None
+    if rules is None:
+        rule = C.byref(SampleRule(temperature, top_k, top_p, min_p))
+    else:
+        _cuda(rules, "rules", torch.int32)
+        if rules.shape != (rows, 4) or not rules.is_contiguous():
+            raise ValueError("rules must be a contiguous int32 tensor [rows][4]")
+    L = lib()
+    if out is None:
+        index = torch.empty((rows, m), dtype=torch.int64, device=scores.device)
+        logprob = torch.empty((rows, m), dtype=torch.float32, device=scores.device)
+    else:
+        index, logprob = out
+        for t, dt in ((index, torch.int64), (logprob, torch.float32)):
+            _cuda(t, "out", dt)
+            _need(t.is_contiguous() and t.numel() == rows * m, "out must be contiguous [rows][m] tensors")
+    ws, n_ws = _workspace(("sample", code, rows, n, m),
+                          lambda b: L.mlt_sample_workspace(code, rows, n, m, C.byref(b)), scores.device, stream)
+    _check(L.mlt_sample(_stream_ptr(stream), scores.data_ptr(), code, rows, n, stride, noise.data_ptr(), noise_stride,
+                        rule, None if rules is None else rules.data_ptr(), m, None if ws is None else ws.data_ptr(),
+                        n_ws, index.data_ptr(), logprob.data_ptr()))
+    return (index[0], logprob[0]) if one and out is None else (index, logprob)
+
+
+def _ids(ids):
+    import torch
+
+    _cuda(ids, "ids")
+    if ids.dtype not in (torch.int64, torch.int32):
+        raise TypeError("ids must be int32 or int64")
+    _need(ids.is_contiguous(), "ids must be contiguous")
+    return 1 if ids.dtype == torch.int64 else 0
+
+
+def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None):
+    """mlt_embed: scale * table[ids], rounded once to `out_dtype` (default: the
+    table's); ids of any shape, negative ones give zeros."""
+    import torch
+
+    ids_64 = _ids(ids)
+    _cuda(table, "table")
+    code, stride = _dtype_code(table), _rows(table, "table")
+    vocab, dim = table.shape
+    if out is None:
+        out = torch.empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
+        out_stride = dim
+    else:
+        _cuda(out, "out")
+        _need(tuple(out.shape) == (*ids.shape, dim), "out must have the shape of ids and one more dimension, dim")
+        flat = out if out.dim() == 2 else out.view(-1, dim)
+        out_stride = _rows(flat, "out")
+    _check(lib().mlt_embed(_stream_ptr(stream), table.data_ptr(), code, vocab, dim, stride, ids.data_ptr(), ids_64,
+                           ids.numel(), scale, out.data_ptr(), _dtype_code(out), out_stride))
+    return out
+
+
+def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, out=None, stream=None):
+    """mlt_embed_grad: the gradient [vocab][dim] of embed's table from that of
+    its output; the same from call to call."""
+    import torch
+
+    ids_64 = _ids(ids)
+    _cuda(grad_out, "grad_out")
+    dim = grad_out.shape[-1]
+    _need(tuple(grad_out.shape[:-1]) == tuple(ids.shape), "grad_out must have the shape of ids and one more dimension")
+    flat = grad_out if grad_out.dim() == 2 else grad_out.reshape(-1, dim)
+    code, stride = _dtype_code(flat), _rows(flat, "grad_out")
+    vocab, tokens = int(vocab), ids.numel()
+    if out is None:
+        out = torch.empty((vocab, dim), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
+    else:
+        _cuda(out, "out")
+        _need(tuple(out.shape) == (vocab, dim), "out must be [vocab][dim]")
+    L = lib()
+    ws, n_ws = _workspace(("embed_grad", tokens, vocab, dim),
+                          lambda b: L.mlt_embed_grad_workspace(tokens, vocab, dim, C.byref(b)), out.device, stream)
+    _check(L.mlt_embed_grad(_stream_ptr(stream), flat.data_ptr(), code, stride, ids.data_ptr(), ids_64, tokens, vocab,
+                            dim, scale, None if ws is None else ws.data_ptr(), n_ws, out.data_ptr(), _dtype_code(out),
+                            _rows(out, "out")))
     return out
 
 
