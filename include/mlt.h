@@ -505,9 +505,10 @@ int mlt_tune_head_levels(int levels);
  * The paper leaves the explorer's search open (Sec. 2, "Configuration
  * Explorer") and retrains its models every tuning iteration.  These calls are
  * what a proposer over knob digits and tuning histories needs next to
- * screening: draws from scores instead of the top-k (mlt_sample), and digits
- * or tokens to vectors with the gradient of the table (mlt_embed,
- * mlt_embed_grad).  The paper has no counterpart.
+ * screening: draws from scores instead of the top-k (mlt_sample), digits or
+ * tokens to vectors with the gradient of the table (mlt_embed,
+ * mlt_embed_grad), and a recurrent state over a sequence (mlt_scan).  The
+ * paper has no counterpart.
  *
  * They keep no state between calls and use no library scratch: a call that
  * needs a workspace takes it from the caller (device memory of at least the
@@ -583,6 +584,49 @@ int mlt_embed_grad(void *stream, const void *grad_out, int dtype, int64_t grad_s
                    int ids_64, int64_t tokens, int64_t vocab, int dim, float scale, void *workspace,
                    size_t workspace_bytes, void *grad_table, int out_dtype, int64_t out_stride);
 int mlt_embed_grad_workspace(int64_t tokens, int64_t vocab, int dim, size_t *bytes_out);
+
+/* Selective scan with a short causal convolution before it, for each sequence
+ * b, position t and channel c of group g = c / (dim / groups):
+ *   v   = conv_b + sum over j < taps of conv_w[c][j] x[t - taps + 1 + j]
+ *   u   = v sigmoid(v)                       (taps = 0: u = x)
+ *   d   = softplus(dt[t] + dt_bias)
+ *   h_t = exp(d A[c]) h_(t-1) + d u B[t][g]  (a vector of `states`)
+ *   y   = (C[t][g] . h_t + skip u) * z sigmoid(z)   (no z: without that factor)
+ * Positions t >= lengths[b] (clamped to 0 .. length) leave h as it is, give
+ * y = 0, and what the inputs hold there is not used.  x before the start comes
+ * from conv_state, or is 0 without one; h_(-1) is `state`, or 0.
+ *   x, dt, z, y        [batch][length][dim] of `dtype`: the *_batch strides
+ *                      between sequences and *_step strides between positions
+ *                      in elements, channels adjacent
+ *   B, C               [batch][length][groups][states] of `dtype`, with
+ *                      strides; groups and states adjacent
+ *   A [dim][states], skip, dt_bias, conv_b [dim], conv_w [dim][taps]: fp32
+ *   lengths            int32 [batch] or NULL
+ *   state, state_out   fp32 [batch][dim][states]
+ *   conv_state, conv_state_out  [batch][taps - 1][dim] of `dtype`: the inputs
+ *                      before the start / before each sequence's end
+ * z, skip, dt_bias, conv_b, lengths, state, state_out, conv_state and
+ * conv_state_out may be NULL.  state_out may be `state` and conv_state_out
+ * `conv_state`: length 1 is the single-token form that updates both in place.
+ *   batch 0 .. 65535;  length 0 .. 2^31-1;  dim 1 .. 2^20, a multiple of
+ *   groups;  states 1 .. 32;  taps 0 .. 4 */
+typedef struct {
+    int32_t dtype, batch, dim, states, groups, taps;
+    int64_t length;
+    const void *x, *dt, *z, *B, *C;
+    int64_t x_batch, x_step, dt_batch, dt_step, z_batch, z_step, B_batch, B_step, C_batch, C_step;
+    const float *A, *skip, *dt_bias, *conv_w, *conv_b;
+    const int32_t *lengths;
+    const float *state;
+    const void *conv_state;
+    void *y;
+    int64_t y_batch, y_step;
+    float *state_out;
+    void *conv_state_out;
+} mlt_scan_args;
+
+int mlt_scan(void *stream, const mlt_scan_args *args, void *workspace, size_t workspace_bytes);
+int mlt_scan_workspace(const mlt_scan_args *args, size_t *bytes_out);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

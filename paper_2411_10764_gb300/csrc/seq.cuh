@@ -93,4 +93,9 @@ cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t s
 size_t embed_grad_workspace(long long tokens, long long vocab, int dim, int sms);
 cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st);
 
+// --- scan.cu -------------------------------------------------
+constexpr int kScanMaxStates = 32;
+constexpr int kScanMaxTaps = 4;
+size_t scan_workspace(const mlt_scan_args& a, int sms);
+cudaError_t launch_scan(const mlt_scan_args& a, void* ws, int sms, long long* launches, cudaStream_t st);
 }  // namespace mlt

@@ -1,5 +1,5 @@
 // C entry points of the sequence-model operators: argument checks, then the
-// launches of sample.cu and embed.cu.  Nothing here
+// launches of sample.cu, embed.cu, and scan.cu.  Nothing here
 // allocates device memory but the error word at the first call.
 #include <cmath>
 
@@ -46,6 +46,46 @@ int check_embed(int dtype, int out_dtype, int64_t tokens, int64_t vocab, int dim
 
 // A row stride that keeps rows apart (one row needs none).
 bool stride_ok(int64_t stride, int64_t width, int64_t rows) { return rows <= 1 || stride >= width; }
+
+int check_scan(const mlt_scan_args* a) {
+  if (a == nullptr) return api_fail(MLT_EINVAL, "args must be non-NULL");
+  if (!dtype_ok(a->dtype)) return api_fail(MLT_EINVAL, "unknown element type %d", a->dtype);
+  if (a->batch < 0 || a->batch > 65535) return api_fail(MLT_EINVAL, "batch must lie in [0, 65535], got %d", a->batch);
+  if (a->length < 0 || a->length > kMaxCount) return api_fail(MLT_EINVAL, "length must lie in [0, 2^31-1]");
+  if (a->dim < 1 || a->dim > kMaxDim) return api_fail(MLT_EINVAL, "dim must lie in [1, %d], got %d", kMaxDim, a->dim);
+  if (a->states < 1 || a->states > kScanMaxStates)
+    return api_fail(MLT_EINVAL, "states must lie in [1, %d], got %d", kScanMaxStates, a->states);
+  if (a->groups < 1 || a->dim % a->groups != 0)
+    return api_fail(MLT_EINVAL, "dim must be a multiple of groups, got %d and %d", a->dim, a->groups);
+  if (a->taps < 0 || a->taps > kScanMaxTaps)
+    return api_fail(MLT_EINVAL, "taps must lie in [0, %d], got %d", kScanMaxTaps, a->taps);
+  return MLT_OK;
+}
+
+int check_scan_inputs(const mlt_scan_args* a) {
+  const int64_t L = a->length, bs = static_cast<int64_t>(a->groups) * a->states;
+  if (a->A == nullptr) return api_fail(MLT_EINVAL, "A must be non-NULL");
+  if (a->taps > 0 && a->conv_w == nullptr) return api_fail(MLT_EINVAL, "conv_w must be non-NULL with %d taps", a->taps);
+  if (L > 0 && (a->x == nullptr || a->dt == nullptr || a->B == nullptr || a->C == nullptr))
+    return api_fail(MLT_EINVAL, "x, dt, B and C must be non-NULL");
+  struct {
+    const char* name;
+    const void* p;
+    int64_t step, batch, width;
+  } in[] = {{"x", a->x, a->x_step, a->x_batch, a->dim},
+            {"dt", a->dt, a->dt_step, a->dt_batch, a->dim},
+            {"z", a->z, a->z_step, a->z_batch, a->dim},
+            {"B", a->B, a->B_step, a->B_batch, bs},
+            {"C", a->C, a->C_step, a->C_batch, bs}};
+  for (const auto& t : in) {
+    if (t.p == nullptr) continue;
+    if (!stride_ok(t.step, t.width, L) || t.batch < 0)
+      return api_fail(MLT_EINVAL, "%s: positions must be at least %lld elements apart", t.name,
+                      static_cast<long long>(t.width));
+    if (!aligned_to(t.p, dtype_size(a->dtype))) return api_fail(MLT_EINVAL, "%s is not aligned to its elements", t.name);
+  }
+  return MLT_OK;
+}
 
 }  // namespace
 
@@ -177,6 +217,32 @@ int mlt_embed_grad(void* stream, const void* grad_out, int dtype, int64_t grad_s
   long long launches = 0;
   const cudaError_t e = launch_embed_grad(a, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "embedding gradient launch");
+}
+
+int mlt_scan_workspace(const mlt_scan_args* args, size_t* bytes_out) {
+  if (bytes_out == nullptr) return api_fail(MLT_EINVAL, "bytes_out must be non-NULL");
+  const int rc = check_scan(args);
+  if (rc != MLT_OK) return rc;
+  *bytes_out = scan_workspace(*args, api_sm_count());
+  return MLT_OK;
+}
+
+int mlt_scan(void* stream, const mlt_scan_args* args, void* workspace, size_t workspace_bytes) {
+  int rc = check_scan(args);
+  if (rc != MLT_OK) return rc;
+  if (args->batch == 0) return MLT_OK;
+  rc = check_scan_inputs(args);
+  if (rc != MLT_OK) return rc;
+  if (args->length > 0 && args->y == nullptr) return api_fail(MLT_EINVAL, "y must be non-NULL");
+  if (!stride_ok(args->y_step, args->dim, args->length) || !stride_ok(args->y_batch, args->dim, args->batch))
+    return api_fail(MLT_EINVAL, "y: positions and sequences must be at least dim elements apart");
+  if (!aligned_to(args->y, dtype_size(args->dtype))) return api_fail(MLT_EINVAL, "y is not aligned to its elements");
+  const int sms = api_sm_count();
+  rc = check_ws(workspace, workspace_bytes, scan_workspace(*args, sms));
+  if (rc != MLT_OK) return rc;
+  long long launches = 0;
+  const cudaError_t e = launch_scan(*args, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "scan launch");
 }
 
 }  // extern "C"

@@ -33,6 +33,18 @@ class SampleRule(C.Structure):
     _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
+class ScanArgs(C.Structure):
+    """mlt_scan_args"""
+    _fields_ = ([(k, C.c_int32) for k in ("dtype", "batch", "dim", "states", "groups", "taps")]
+                + [("length", C.c_int64)]
+                + [(k, C.c_void_p) for k in ("x", "dt", "z", "B", "C")]
+                + [(f"{k}_{s}", C.c_int64) for k in ("x", "dt", "z", "B", "C") for s in ("batch", "step")]
+                + [(k, C.c_void_p) for k in ("A", "skip", "dt_bias", "conv_w", "conv_b", "lengths", "state",
+                                             "conv_state", "y")]
+                + [("y_batch", C.c_int64), ("y_step", C.c_int64), ("state_out", C.c_void_p),
+                   ("conv_state_out", C.c_void_p)])
+
+
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
 
 
@@ -100,6 +112,8 @@ def lib(build_if_missing: bool = True):
             "mlt_embed": [P, P, i32, i64, i32, i64, P, i32, i64, f32, P, i32, i64],
             "mlt_embed_grad": [P, P, i32, i64, P, i32, i64, i64, i32, f32, P, C.c_size_t, P, i32, i64],
             "mlt_embed_grad_workspace": [i64, i64, i32, P],
+            "mlt_scan": [P, P, P, C.c_size_t],
+            "mlt_scan_workspace": [P, P],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -485,6 +499,89 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
                             dim, scale, None if ws is None else ws.data_ptr(), n_ws, out.data_ptr(), _dtype_code(out),
                             _rows(out, "out")))
     return out
+
+
+def _scan_args(x, dt, B, Cm, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state):
+    import torch
+
+    _cuda(x, "x")
+    a = ScanArgs()
+    a.dtype = _dtype_code(x)
+    _need(x.dim() == 3, "x must be [batch][length][dim]")
+    b, L, d = x.shape
+    if B.dim() == 3:
+        B = B.unsqueeze(2)
+    if Cm.dim() == 3:
+        Cm = Cm.unsqueeze(2)
+    _need(B.dim() == 4, "B must be [batch][length][groups][states]")
+    g, n = B.shape[2:]
+    taps = 0 if conv_w is None else conv_w.shape[1]
+    a.batch, a.length, a.dim, a.states, a.groups, a.taps = b, L, d, n, g, taps
+    wide, narrow = (b, L, d), (b, L, g, n)
+    for name, t, shape in (("x", x, wide), ("dt", dt, wide), ("z", z, wide), ("B", B, narrow), ("C", Cm, narrow)):
+        if t is None:
+            continue
+        if not (t.is_cuda and t.dtype == x.dtype):
+            raise TypeError(f"{name} must be a CUDA tensor of x's type")
+        _need(tuple(t.shape) == shape, f"{name} must have the shape {shape}")
+        s = t.stride()
+        _need(t.numel() == 0 or ((shape[-1] == 1 or s[-1] == 1) and (t.dim() == 3 or g == 1 or s[2] == n)),
+              f"the channels of {name} must be adjacent")
+        setattr(a, name, t.data_ptr())
+        setattr(a, name + "_batch", s[0])
+        setattr(a, name + "_step", s[1])
+    f32 = torch.float32
+    for name, t, shape, dtype in (("A", A, (d, n), f32), ("skip", skip, (d,), f32), ("dt_bias", dt_bias, (d,), f32),
+                                  ("conv_w", conv_w, (d, taps), f32), ("conv_b", conv_b, (d,), f32),
+                                  ("lengths", lengths, (b,), torch.int32), ("state", state, (b, d, n), f32),
+                                  ("conv_state", conv_state, (b, max(0, taps - 1), d), x.dtype)):
+        if t is None:
+            continue
+        if not (t.is_cuda and t.dtype == dtype):
+            raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
+        _need(tuple(t.shape) == shape and t.is_contiguous(), f"{name} must be contiguous, of the shape {shape}")
+        setattr(a, name, t.data_ptr())
+    return a
+
+
+def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=None, lengths=None, state=None,
+         conv_state=None, out=None, state_out=None, conv_state_out=None, stream=None):
+    """mlt_scan: selective scan with its short causal convolution.  x, dt, z
+    [batch][length][dim]; B, C_ [batch][length][groups][states] (or without
+    the groups dimension); the rest fp32 (see mlt_scan in include/mlt.h).
+    Returns (y, state, conv_state), the last None with fewer than two taps.
+    For single tokens (length 1) pass state_out=state and
+    conv_state_out=conv_state to update them in place."""
+    import torch
+
+    a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
+    b, L, d = x.shape
+    y = torch.empty((b, L, d), dtype=x.dtype, device=x.device) if out is None else out
+    if out is not None:
+        _need(tuple(y.shape) == (b, L, d) and y.dtype == x.dtype and y.is_cuda and (d == 1 or y.stride(2) == 1),
+              "out must be like x, its channels adjacent")
+    if state_out is None:
+        state_out = torch.empty((b, d, a.states), dtype=torch.float32, device=x.device)
+    else:
+        _cuda(state_out, "state_out", torch.float32)
+        _need(state_out.is_contiguous() and tuple(state_out.shape) == (b, d, a.states),
+              "state_out must be contiguous [batch][dim][states]")
+    if a.taps < 2:
+        conv_state_out = None
+    elif conv_state_out is None:
+        conv_state_out = torch.empty((b, a.taps - 1, d), dtype=x.dtype, device=x.device)
+    else:
+        _cuda(conv_state_out, "conv_state_out", x.dtype)
+        _need(conv_state_out.is_contiguous() and tuple(conv_state_out.shape) == (b, a.taps - 1, d),
+              "conv_state_out must be contiguous [batch][taps - 1][dim]")
+    a.y, a.y_batch, a.y_step = y.data_ptr(), y.stride(0), y.stride(1)
+    a.state_out = state_out.data_ptr()
+    a.conv_state_out = None if conv_state_out is None else conv_state_out.data_ptr()
+    lb = lib()
+    ws, n_ws = _workspace(("scan", a.dtype, b, L, d, a.states, a.groups, a.taps),
+                          lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)), x.device, stream)
+    _check(lb.mlt_scan(_stream_ptr(stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws))
+    return y, state_out, conv_state_out
 
 
 def screen_host(feats: np.ndarray, thr: float, k: int, out=None, stream=None):
