@@ -507,8 +507,8 @@ int mlt_tune_head_levels(int levels);
  * what a proposer over knob digits and tuning histories needs next to
  * screening: draws from scores instead of the top-k (mlt_sample), digits or
  * tokens to vectors with the gradient of the table (mlt_embed,
- * mlt_embed_grad), and a recurrent state over a sequence (mlt_scan).  The
- * paper has no counterpart.
+ * mlt_embed_grad), and a recurrent state over a sequence (mlt_scan,
+ * mlt_scan_grad).  The paper has no counterpart.
  *
  * They keep no state between calls and use no library scratch: a call that
  * needs a workspace takes it from the caller (device memory of at least the
@@ -627,6 +627,26 @@ typedef struct {
 
 int mlt_scan(void *stream, const mlt_scan_args *args, void *workspace, size_t workspace_bytes);
 int mlt_scan_workspace(const mlt_scan_args *args, size_t *bytes_out);
+
+/* Gradients of mlt_scan, from those of y (gy, with strides) and of state_out
+ * (g_state_out, fp32 [batch][dim][states], NULL: 0).  `args` as for the
+ * forward call; its outputs (y, state_out, conv_state_out) are not read or
+ * written, and conv_state_out is taken to have no gradient.  Every output may
+ * be NULL; x, dt, z, B, C: contiguous, of `dtype`, zero past a sequence's end;
+ * g_conv_state of `dtype`; the rest fp32, summed over sequences and positions
+ * in a fixed order. */
+typedef struct {
+    const void *gy;
+    int64_t gy_batch, gy_step;
+    const float *g_state_out;
+    void *x, *dt, *z, *B, *C;
+    float *A, *skip, *dt_bias, *conv_w, *conv_b, *state;
+    void *conv_state;
+} mlt_scan_grads;
+
+int mlt_scan_grad(void *stream, const mlt_scan_args *args, const mlt_scan_grads *grads, void *workspace,
+                  size_t workspace_bytes);
+int mlt_scan_grad_workspace(const mlt_scan_args *args, size_t *bytes_out);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

@@ -1,0 +1,744 @@
+// Gradients of the selective scan (scan.cu has the forward formulas).
+//
+// With gc_t the gradient of C_t . h_t + skip u_t, g_t that of h_t from position t on, and
+// a_t = exp(d_t A):
+//   g_t = gc_t C_t + a_(t+1) g_(t+1)          e_t = g_t a_t h_(t-1)
+//   dB_t = sum over the group's channels of g_t d_t u_t       dC_t likewise of gc_t h_t
+//   d(d_t) = u_t (g_t . B_t) + e_t . A        d(u_t) = d_t (g_t . B_t) + gc_t skip
+//   dA = sum of d_t e_t                       d(h_(-1)) = a_0 g_0
+// then through softplus, the gates and the convolution.
+//
+// Sequences are cut into chunks, all at once in the first and third step:
+//   k_grad_local   per chunk: end state from zero, sum of d, and the chunk's own gradient
+//                  of the state before it (sum over t of gc_t C_t exp(A sum of d up to t))
+//   k_grad_carry   the state before and the gradient after each chunk, chunk by chunk
+//   k_grad_chunk   per chunk: states recomputed from the one before it, then backwards
+//   k_grad_finish  sums over chunks, sequences and channel blocks, in a fixed order, and
+//                  the inputs whose convolution reaches into the next chunk
+// No state is kept from the forward pass and none but a chunk's first is written: inside
+// a chunk every kSub-th state is kept in shared memory and the others, with their decays,
+// in registers while their kSub positions are walked backwards.
+//
+// Bound: issue.  A position and channel takes about 60 instructions in each of its four lanes.
+#include "scan.cuh"
+
+namespace mlt {
+namespace {
+
+using namespace scan;
+
+// Positions of a chunk and of the part that is walked backwards at a time, by states a lane:
+// the states kept of a chunk take 32 KB (S = 4) or 64 KB (S = 8) of shared memory.
+template <int S>
+struct Shape {
+  static constexpr int kChunk = S > 4 ? 32 : 64;
+  static constexpr int kSub = S > 4 ? 4 : 8;
+  static constexpr int kSubs = kChunk / kSub;
+};
+int chunk_of(int states) { return states > 16 ? 32 : 64; }
+
+constexpr int kTimes = kThreads / kChannels;  // threads that share a channel outside the walk
+constexpr int kRing = 16;                     // rows of dv kept for the convolution
+constexpr int kVecs = kScanMaxTaps + 3;       // per channel: conv_w (4), conv_b, skip, dt_bias
+constexpr int kHalo = kScanMaxTaps - 1;
+
+struct GradPlan {
+  int chunk;
+  long long chunks;
+  int blocks;  // channel blocks of a group
+  size_t off_e, off_g, off_sum, off_A, off_vec, off_head, off_part, off_bc, bytes;
+};
+
+template <int S>
+struct alignas(16) Staged {
+  float2 du[Shape<S>::kChunk][kChannels];  // (d, u)
+  float gc[Shape<S>::kChunk][kChannels];
+  float B[Shape<S>::kChunk * 4 * S];
+  float C[Shape<S>::kChunk * 4 * S];
+};
+
+template <int S>
+struct alignas(16) Walk {
+  Staged<S> in;
+  float kept[Shape<S>::kSubs][kChannels * 4 * S];  // the state before each part
+  float y[Shape<S>::kSub][kChannels + 4];          // C . h
+  float gp[Shape<S>::kSub][kChannels + 4];         // g . B
+  float ga[Shape<S>::kSub][kChannels + 4];         // e . A, times log2 e
+  float bc[kThreads / 32][Shape<S>::kSub][2 * 4 * S];  // each warp's share of dB, dC
+  float dv[kRing][kChannels];
+};
+
+// A channel's convolution weights, last tap first.
+struct ChannelTaps {
+  float w[kScanMaxTaps], b;
+};
+__device__ __forceinline__ ChannelTaps channel_taps(const mlt_scan_args& a, int ch, bool in) {
+  ChannelTaps q;
+  q.b = in && a.taps > 0 && a.conv_b != nullptr ? a.conv_b[ch] : 0.0f;
+#pragma unroll
+  for (int j = 0; j < kScanMaxTaps; ++j)
+    q.w[j] = in && j < a.taps ? a.conv_w[static_cast<long long>(ch) * a.taps + a.taps - 1 - j] : 0.0f;
+  return q;
+}
+// Input at position t of the sequence (before the start: conv_state, or 0).
+template <typename T>
+__device__ __forceinline__ float input_at(const mlt_scan_args& a, int b, long long t, int ch) {
+  if (t >= 0) return to_f32(static_cast<const T*>(a.x)[b * a.x_batch + t * a.x_step + ch]);
+  if (a.conv_state == nullptr || t < -(a.taps - 1)) return 0.0f;
+  return to_f32(static_cast<const T*>(a.conv_state)[(static_cast<long long>(b) * (a.taps - 1) + t + a.taps - 1) * a.dim +
+                                                    ch]);
+}
+__device__ __forceinline__ float conv_of(const mlt_scan_args& a, const ChannelTaps& q, const float (&x)[kScanMaxTaps]) {
+  if (a.taps == 0) return x[0];
+  float v = fmaf(q.w[0], x[0], q.b);
+#pragma unroll
+  for (int j = 1; j < kScanMaxTaps; ++j)
+    if (j < a.taps) v = fmaf(q.w[j], x[j], v);
+  return v;
+}
+
+// The chunk's (d, u), gc, B and C in shared memory; zero from `live` on.  A thread stages one
+// channel's kChunk / kTimes consecutive positions.
+template <typename T, int S>
+__device__ __forceinline__ void stage_chunk(const mlt_scan_args& a, const mlt_scan_grads& g, const Block& k,
+                                            long long begin, int live, Staged<S>& st) {
+  constexpr int kRun = Shape<S>::kChunk / kTimes;
+  const int c = threadIdx.x % kChannels, t0 = threadIdx.x / kChannels * kRun;
+  const bool in = c < k.cn;
+  const int ch = k.c0 + c;
+  const ChannelTaps taps = channel_taps(a, ch, in);
+  const float bias = in && a.dt_bias != nullptr ? a.dt_bias[ch] : 0.0f;
+  float x[kScanMaxTaps] = {};
+  if (in && t0 < live) {
+#pragma unroll
+    for (int j = 1; j < kScanMaxTaps; ++j)
+      if (j < a.taps) x[j] = input_at<T>(a, k.b, begin + t0 - j, ch);
+  }
+  const T* xp = static_cast<const T*>(a.x) + k.b * a.x_batch + ch;
+  const T* dp = static_cast<const T*>(a.dt) + k.b * a.dt_batch + ch;
+  const T* zp = static_cast<const T*>(a.z) + k.b * a.z_batch + ch;
+  const T* gp = static_cast<const T*>(g.gy) + k.b * g.gy_batch + ch;
+#pragma unroll 4
+  for (int i = 0; i < kRun; ++i) {
+    const int t = t0 + i;
+    float2 du = make_float2(0.0f, 0.0f);
+    float gc = 0.0f;
+    if (in && t < live) {
+      const long long at = begin + t;
+      x[0] = to_f32(xp[at * a.x_step]);
+      du.x = softplus(to_f32(dp[at * a.dt_step]) + bias);
+      const float v = conv_of(a, taps, x);
+      du.y = a.taps > 0 ? v * sigmoid(v) : v;
+      gc = to_f32(gp[at * g.gy_step]);
+      if (a.z != nullptr) {
+        const float z = to_f32(zp[at * a.z_step]);
+        gc *= z * sigmoid(z);
+      }
+#pragma unroll
+      for (int j = kScanMaxTaps - 1; j > 0; --j) x[j] = x[j - 1];
+    }
+    st.du[t][c] = du;
+    st.gc[t][c] = gc;
+  }
+  const T* Bp = static_cast<const T*>(a.B) + k.b * a.B_batch + begin * a.B_step + static_cast<long long>(k.g) * a.states;
+  const T* Cp = static_cast<const T*>(a.C) + k.b * a.C_batch + begin * a.C_step + static_cast<long long>(k.g) * a.states;
+  for (int i = threadIdx.x; i < Shape<S>::kChunk * 4 * S; i += kThreads) {
+    const int t = i / (4 * S), s = i - t * (4 * S);
+    const bool ok = t < live && s < a.states;
+    st.B[i] = ok ? to_f32(Bp[t * a.B_step + s]) : 0.0f;
+    st.C[i] = ok ? to_f32(Cp[t * a.C_step + s]) : 0.0f;
+  }
+}
+
+// blockIdx.x counts (chunk, channel block), blockIdx.y sequences.
+struct Where {
+  Block k;
+  long long chunk, begin, len;
+  int live;  // positions of the chunk before the sequence's end
+};
+__device__ __forceinline__ Where where(const mlt_scan_args& a, int chunk_positions) {
+  Where w;
+  const int blocks = a.groups * blocks_per_group(a);
+  w.chunk = blockIdx.x / blocks;
+  w.k = block_of(a, static_cast<int>(blockIdx.x - w.chunk * blocks), blockIdx.y);
+  w.begin = w.chunk * chunk_positions;
+  w.len = length_of(a, w.k.b);
+  w.live = static_cast<int>(min(static_cast<long long>(chunk_positions), max(0ll, w.len - w.begin)));
+  return w;
+}
+
+template <typename T, int S>
+__global__ void __launch_bounds__(kThreads) k_grad_local(mlt_scan_args a, mlt_scan_grads g, GradPlan p,
+                                                         unsigned char* ws) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  Staged<S>& st = *reinterpret_cast<Staged<S>*>(smem);
+  pdl_wait();
+  pdl_trigger();
+  const Where w = where(a, Shape<S>::kChunk);
+  if (w.live == 0) return;  // k_grad_carry stops before it
+  stage_chunk<T, S>(a, g, w.k, w.begin, w.live, st);
+  const int lane = threadIdx.x & 3, ch = threadIdx.x >> 2;
+  const bool in = ch < w.k.cn;
+  const long long at = static_cast<long long>(w.k.c0 + ch) * a.states + lane * S;
+  Lane<S> A = lane_zero<S>(), h = A, acc = A, prod = A;
+  if (in) A = lane_load<S>(a.A + at, lane * S, a.states);
+#pragma unroll
+  for (int s = 0; s < Lane<S>::H; ++s) {
+    A.v[s] = mul2(A.v[s], f2(kLog2E, kLog2E));
+    prod.v[s] = f2(1.0f, 1.0f);
+  }
+  float sum = 0.0f;
+  __syncthreads();
+#pragma unroll 4
+  for (int t = 0; t < Shape<S>::kChunk; ++t) {
+    const float2 du = st.du[t][ch];
+    const float gc = st.gc[t][ch];
+    const Lane<S> B = lane_shared<S>(st.B + (t * 4 + lane) * S), C = lane_shared<S>(st.C + (t * 4 + lane) * S);
+    const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y), gg = f2(gc, gc);
+#pragma unroll
+    for (int s = 0; s < Lane<S>::H; ++s) {
+      const F2 decay = ex2_2(mul2(d, A.v[s]));
+      h.v[s] = fma2(decay, h.v[s], mul2(push, B.v[s]));
+      prod.v[s] = mul2(prod.v[s], decay);
+      acc.v[s] = fma2(prod.v[s], mul2(gg, C.v[s]), acc.v[s]);
+    }
+    sum += du.x;
+  }
+  if (!in) return;
+  const long long seq = static_cast<long long>(w.k.b) * p.chunks + w.chunk;
+  const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  lane_store<S>(reinterpret_cast<float*>(ws + p.off_e) + seq * of_seq + at, lane * S, a.states, h);
+  lane_store<S>(reinterpret_cast<float*>(ws + p.off_g) + seq * of_seq + at, lane * S, a.states, acc);
+  if (lane == 0) reinterpret_cast<float*>(ws + p.off_sum)[seq * a.dim + w.k.c0 + ch] = sum;
+}
+
+// In place: a chunk's end state becomes the state before it, its own gradient the one after it.
+__global__ void __launch_bounds__(256) k_grad_carry(mlt_scan_args a, mlt_scan_grads g, GradPlan p, unsigned char* ws) {
+  pdl_wait();
+  pdl_trigger();
+  const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= of_seq) return;
+  const int b = blockIdx.y;
+  const long long chunks = (length_of(a, b) + p.chunk - 1) / p.chunk;
+  float* e = reinterpret_cast<float*>(ws + p.off_e) + b * p.chunks * of_seq + i;
+  float* q = reinterpret_cast<float*>(ws + p.off_g) + b * p.chunks * of_seq + i;
+  const float* sum = reinterpret_cast<const float*>(ws + p.off_sum) + b * p.chunks * a.dim + i / a.states;
+  const float A = a.A[i] * kLog2E;
+  float h = a.state != nullptr ? a.state[b * of_seq + i] : 0.0f;
+#pragma unroll 8
+  for (long long c = 0; c < chunks; ++c) {
+    const float end = e[c * of_seq], decay = ex2(A * sum[c * a.dim]);
+    e[c * of_seq] = h;
+    h = fmaf(decay, h, end);
+  }
+  float r = g.g_state_out != nullptr ? g.g_state_out[b * of_seq + i] : 0.0f;
+#pragma unroll 8
+  for (long long c = chunks - 1; c >= 0; --c) {
+    const float own = q[c * of_seq], decay = ex2(A * sum[c * a.dim]);
+    q[c * of_seq] = r;
+    r = fmaf(decay, r, own);
+  }
+}
+
+// Sums over the eight channels of a warp of each lane's M values: halves of the values are
+// exchanged with the lane whose channel differs in one bit, so M / 8 (at least 1) remain in
+// a lane: with M >= 8, the values from (lane >> 2) M / 8 on.
+template <int M>
+struct ChannelSums {
+  static constexpr int kLeft = M > 8 ? M / 8 : 1;
+};
+template <int M>
+__device__ __forceinline__ int channel_sums(float (&v)[M]) {
+  const int lane = threadIdx.x & 31;
+  int first = 0;
+  int left = M;
+#pragma unroll
+  for (int bit = 16; bit >= 4; bit /= 2) {
+    if (left > 1) {
+      const int half = left / 2;
+      const bool hi = lane & bit;
+#pragma unroll
+      for (int i = 0; i < M / 2; ++i)
+        if (i < half) {
+          const float mine = hi ? v[i + half] : v[i], other = hi ? v[i] : v[i + half];
+          v[i] = mine + __shfl_xor_sync(~0u, other, bit);
+        }
+      if (hi) first += half;
+      left = half;
+    } else {
+      v[0] += __shfl_xor_sync(~0u, v[0], bit);
+    }
+  }
+  return first;
+}
+
+template <typename T, int S>
+__global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt_scan_grads g, GradPlan p,
+                                                            unsigned char* ws) {
+  using Sh = Shape<S>;
+  constexpr int kSub = Sh::kSub;
+  extern __shared__ __align__(16) unsigned char smem[];
+  Walk<S>& sm = *reinterpret_cast<Walk<S>*>(smem);
+  pdl_wait();
+  pdl_trigger();
+  const Where w = where(a, Sh::kChunk);
+  const Block& k = w.k;
+  const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  const long long seq = static_cast<long long>(k.b) * p.chunks + w.chunk;
+  const int positions = static_cast<int>(min(static_cast<long long>(Sh::kChunk), a.length - w.begin));
+  // a lane's channel and states in the walk
+  const int lane = threadIdx.x & 3, ch = threadIdx.x >> 2;
+  const bool in = ch < k.cn;
+  const long long at = static_cast<long long>(k.c0 + ch) * a.states + lane * S;
+  // a thread's channel and first position (then every kTimes-th) elsewhere
+  const int c = threadIdx.x % kChannels, tl = threadIdx.x / kChannels;
+  const bool cin = c < k.cn;
+  const int cc = k.c0 + c;
+  T* gx = static_cast<T*>(g.x) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
+  T* gdt = static_cast<T*>(g.dt) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
+  T* gz = static_cast<T*>(g.z) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
+  if (w.live == 0) {
+    // past the sequence's end
+    const T zero = from_f32<T>(0.0f);
+    if (cin)
+      for (int t = tl; t < positions; t += kTimes) {
+        const long long o = static_cast<long long>(t) * a.dim;
+        if (g.x != nullptr) gx[o] = zero;
+        if (g.dt != nullptr) gdt[o] = zero;
+        if (g.z != nullptr) gz[o] = zero;
+      }
+    if (w.chunk == 0 && in && g.state != nullptr) {
+      Lane<S> r = lane_zero<S>();
+      if (g.g_state_out != nullptr) r = lane_load<S>(g.g_state_out + k.b * of_seq + at, lane * S, a.states);
+      lane_store<S>(g.state + k.b * of_seq + at, lane * S, a.states, r);
+    }
+    return;
+  }
+  stage_chunk<T, S>(a, g, k, w.begin, w.live, sm.in);
+  for (int i = threadIdx.x; i < kRing * kChannels; i += kThreads) sm.dv[i / kChannels][i % kChannels] = 0.0f;
+  Lane<S> A = lane_zero<S>(), h = A, r = A, dA = A;
+  if (in) {
+    A = lane_load<S>(a.A + at, lane * S, a.states);
+    const bool one = p.chunks == 1;
+    const float* hp = one ? (a.state != nullptr ? a.state + k.b * of_seq : nullptr)
+                          : reinterpret_cast<const float*>(ws + p.off_e) + seq * of_seq;
+    const float* rp = one ? (g.g_state_out != nullptr ? g.g_state_out + k.b * of_seq : nullptr)
+                          : reinterpret_cast<const float*>(ws + p.off_g) + seq * of_seq;
+    if (hp != nullptr) h = lane_load<S>(hp + at, lane * S, a.states);
+    if (rp != nullptr) r = lane_load<S>(rp + at, lane * S, a.states);
+  }
+#pragma unroll
+  for (int s = 0; s < Lane<S>::H; ++s) A.v[s] = mul2(A.v[s], f2(kLog2E, kLog2E));
+  __syncthreads();
+
+  // forwards: the state before each part
+  float* kept = sm.kept[0] + (ch * 4 + lane) * S;
+  const int parts = (w.live + kSub - 1) / kSub;  // later ones hold no live position
+#pragma unroll 1
+  for (int part = 0; part < parts; ++part) {
+    lane_store<S>(kept + part * (kChannels * 4 * S), 0, S, h);
+    if (part + 1 == parts) break;
+#pragma unroll
+    for (int t = 0; t < kSub; ++t) {
+      const float2 du = sm.in.du[part * kSub + t][ch];
+      const Lane<S> B = lane_shared<S>(sm.in.B + ((part * kSub + t) * 4 + lane) * S);
+      const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y);
+#pragma unroll
+      for (int s = 0; s < Lane<S>::H; ++s) h.v[s] = fma2(ex2_2(mul2(d, A.v[s])), h.v[s], mul2(push, B.v[s]));
+    }
+  }
+
+  const ChannelTaps taps = channel_taps(a, cc, cin);
+  const float skip = cin && a.skip != nullptr ? a.skip[cc] : 0.0f;
+  const float bias = cin && a.dt_bias != nullptr ? a.dt_bias[cc] : 0.0f;
+  const bool next_live = w.begin + Sh::kChunk < w.len;  // its convolution reads this chunk's last inputs
+  const int halo = a.taps > 1 ? a.taps - 1 : 0;
+  float vec[kVecs] = {};
+  const T zero = from_f32<T>(0.0f);
+  // parts past the sequence's end
+  if (cin)
+    for (int t = parts * kSub + tl; t < positions; t += kTimes) {
+      const long long o = static_cast<long long>(t) * a.dim;
+      if (g.x != nullptr) gx[o] = zero;
+      if (g.dt != nullptr) gdt[o] = zero;
+      if (g.z != nullptr) gz[o] = zero;
+    }
+
+#pragma unroll 1
+  for (int part = parts - 1; part >= 0; --part) {
+    const int t0 = part * kSub;
+    {
+      Lane<S> hs[kSub + 1], decay[kSub];
+      hs[0] = lane_shared<S>(kept + part * (kChannels * 4 * S));
+      float y[kSub], gp[kSub], ga[kSub];
+#pragma unroll
+      for (int t = 0; t < kSub; ++t) {
+        const float2 du = sm.in.du[t0 + t][ch];
+        const Lane<S> B = lane_shared<S>(sm.in.B + ((t0 + t) * 4 + lane) * S);
+        const Lane<S> C = lane_shared<S>(sm.in.C + ((t0 + t) * 4 + lane) * S);
+        const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y);
+        Lane<S> o;
+#pragma unroll
+        for (int s = 0; s < Lane<S>::H; ++s) {
+          decay[t].v[s] = ex2_2(mul2(d, A.v[s]));
+          hs[t + 1].v[s] = fma2(decay[t].v[s], hs[t].v[s], mul2(push, B.v[s]));
+          o.v[s] = mul2(C.v[s], hs[t + 1].v[s]);
+        }
+        y[t] = lane_sum(o);
+      }
+#pragma unroll
+      for (int t = kSub - 1; t >= 0; --t) {
+        const float2 du = sm.in.du[t0 + t][ch];
+        const float gc = sm.in.gc[t0 + t][ch];
+        const Lane<S> B = lane_shared<S>(sm.in.B + ((t0 + t) * 4 + lane) * S);
+        const Lane<S> C = lane_shared<S>(sm.in.C + ((t0 + t) * 4 + lane) * S);
+        const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y), gg = f2(gc, gc);
+        float bc[2 * S];
+        Lane<S> ob, oa;
+#pragma unroll
+        for (int s = 0; s < Lane<S>::H; ++s) {
+          r.v[s] = fma2(gg, C.v[s], r.v[s]);
+          const F2 db = mul2(r.v[s], push), dc = mul2(gg, hs[t + 1].v[s]);
+          float v0, v1;
+          un2(db, v0, v1);
+          bc[2 * s < S ? 2 * s : 0] = v0;
+          if (2 * s + 1 < S) bc[2 * s + 1] = v1;
+          un2(dc, v0, v1);
+          bc[S + (2 * s < S ? 2 * s : 0)] = v0;
+          if (2 * s + 1 < S) bc[S + 2 * s + 1] = v1;
+          ob.v[s] = mul2(r.v[s], B.v[s]);
+          r.v[s] = mul2(r.v[s], decay[t].v[s]);
+          const F2 e = mul2(r.v[s], hs[t].v[s]);
+          oa.v[s] = mul2(e, A.v[s]);
+          dA.v[s] = fma2(e, d, dA.v[s]);
+        }
+        gp[t] = lane_sum(ob);
+        ga[t] = lane_sum(oa);
+        // dB and dC: sums over the warp's channels
+        const int first = channel_sums(bc);
+        constexpr int kLeft = ChannelSums<2 * S>::kLeft;
+        if (2 * S >= 8 || (threadIdx.x & 31 & (S == 2 ? 4 : 12)) == 0) {
+#pragma unroll
+          for (int i = 0; i < kLeft; ++i) {
+            const int v = first + i;  // < S: dB, else dC
+            sm.bc[threadIdx.x >> 5][t][(v < S ? 0 : 4 * S) + lane * S + (v < S ? v : v - S)] = bc[i];
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kSub; t += 4) {
+        const float yy[4] = {y[t], y[t + 1], y[t + 2], y[t + 3]};
+        const float pp[4] = {gp[t], gp[t + 1], gp[t + 2], gp[t + 3]};
+        const float aa[4] = {ga[t], ga[t + 1], ga[t + 2], ga[t + 3]};
+        sm.y[t + lane][ch] = quad_sums(yy, lane);
+        sm.gp[t + lane][ch] = quad_sums(pp, lane);
+        sm.ga[t + lane][ch] = quad_sums(aa, lane);
+      }
+    }
+    __syncthreads();
+    // the CTA's share of dB and dC
+    if (g.B != nullptr || g.C != nullptr) {
+      float* to = reinterpret_cast<float*>(ws + p.off_bc);
+      const long long row = (static_cast<long long>(k.b) * a.groups * p.blocks +
+                             (blockIdx.x - w.chunk * (a.groups * p.blocks))) * a.length + w.begin + t0;
+      for (int i = threadIdx.x; i < kSub * 8 * S; i += kThreads) {
+        const int t = i / (8 * S), v = i - t * (8 * S);
+        const int s = v % (4 * S);
+        if (t0 + t >= w.live || s >= a.states) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kThreads / 32; ++q) sum += sm.bc[q][t][v];
+        to[((row + t) * 2 + v / (4 * S)) * a.states + s] = sum;
+      }
+    }
+    // through the gate, softplus and the convolution's activation
+#pragma unroll
+    for (int i = 0; i < kSub / kTimes; ++i) {
+      const int t = i * kTimes + tl;  // of the part
+      const int ct = t0 + t;          // of the chunk
+      float dv = 0.0f;
+      if (cin && ct < w.live) {
+        const long long pos = w.begin + ct, o = static_cast<long long>(ct) * a.dim;
+        const float2 du = sm.in.du[ct][c];
+        const float gc = sm.in.gc[ct][c];
+        const float gp = sm.gp[t][c];
+        if (g.z != nullptr) {
+          const float z = to_f32(static_cast<const T*>(a.z)[k.b * a.z_batch + pos * a.z_step + cc]);
+          const float go = to_f32(static_cast<const T*>(g.gy)[k.b * g.gy_batch + pos * g.gy_step + cc]);
+          const float sz = sigmoid(z);
+          gz[o] = from_f32<T>(go * (sm.y[t][c] + skip * du.y) * sz * fmaf(z, 1.0f - sz, 1.0f));
+        }
+        const float raw = to_f32(static_cast<const T*>(a.dt)[k.b * a.dt_batch + pos * a.dt_step + cc]) + bias;
+        const float graw = fmaf(gp, du.y, sm.ga[t][c] * (1.0f / kLog2E)) * sigmoid(raw);
+        if (g.dt != nullptr) gdt[o] = from_f32<T>(graw);
+        vec[kScanMaxTaps + 1] = fmaf(gc, du.y, vec[kScanMaxTaps + 1]);
+        vec[kScanMaxTaps + 2] += graw;
+        dv = fmaf(gp, du.x, gc * skip);
+        if (a.taps > 0) {
+          float x[kScanMaxTaps];
+#pragma unroll
+          for (int j = 0; j < kScanMaxTaps; ++j) x[j] = j < a.taps ? input_at<T>(a, k.b, pos - j, cc) : 0.0f;
+          const float v = conv_of(a, taps, x), sv = sigmoid(v);
+          dv *= sv * fmaf(v, 1.0f - sv, 1.0f);
+#pragma unroll
+          for (int j = 0; j < kScanMaxTaps; ++j) vec[j] = fmaf(dv, x[j], vec[j]);
+          vec[kScanMaxTaps] += dv;
+        }
+      } else if (cin && ct < positions) {
+        const long long o = static_cast<long long>(ct) * a.dim;
+        if (g.z != nullptr) gz[o] = zero;
+        if (g.dt != nullptr) gdt[o] = zero;
+      }
+      sm.dv[ct % kRing][c] = dv;
+      if (halo > 0 && cin && ct < kHalo)
+        reinterpret_cast<float*>(ws + p.off_head)[(seq * kHalo + ct) * a.dim + cc] = dv;
+    }
+    __syncthreads();
+    // x[t] meets weight j in v[t + j]
+    if (g.x != nullptr && cin) {
+#pragma unroll
+      for (int i = 0; i < kSub / kTimes; ++i) {
+        const int ct = t0 + i * kTimes + tl;
+        if (ct >= positions) continue;
+        float d = sm.dv[ct % kRing][c];
+        if (a.taps > 0) {
+          d *= taps.w[0];
+#pragma unroll
+          for (int j = 1; j < kScanMaxTaps; ++j)
+            if (j < a.taps && ct + j < Sh::kChunk) d = fmaf(taps.w[j], sm.dv[(ct + j) % kRing][c], d);
+        }
+        if (next_live && ct >= Sh::kChunk - halo)
+          reinterpret_cast<float*>(ws + p.off_part)[(seq * kHalo + ct - (Sh::kChunk - halo)) * a.dim + cc] = d;
+        else
+          gx[static_cast<long long>(ct) * a.dim] = from_f32<T>(ct < w.live ? d : 0.0f);
+      }
+    }
+  }
+  if (in) {
+    lane_store<S>(reinterpret_cast<float*>(ws + p.off_A) + seq * of_seq + at, lane * S, a.states, dA);
+    if (w.chunk == 0 && g.state != nullptr) lane_store<S>(g.state + k.b * of_seq + at, lane * S, a.states, r);
+  }
+  // the channel's sums over the chunk: kTimes threads each, through the staging memory
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) red[(v * kTimes + tl) * kChannels + c] = vec[v];
+  __syncthreads();
+  if (cin)
+    for (int v = tl; v < kVecs; v += kTimes) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int q = 0; q < kTimes; ++q) sum += red[(v * kTimes + q) * kChannels + c];
+      reinterpret_cast<float*>(ws + p.off_vec)[(seq * kVecs + v) * a.dim + cc] = sum;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums and chunk borders
+// ---------------------------------------------------------------------------
+struct Finish {
+  long long bc_blocks, sum_blocks, edge_blocks;
+};
+
+// Sum over the sequences' live chunks of p[(b chunks + chunk) stride], by 8 threads of a column.
+__device__ __forceinline__ float sum_chunks(const mlt_scan_args& a, const GradPlan& p, const float* at, long long stride,
+                                            int part) {
+  float sum = 0.0f;
+  for (int b = 0; b < a.batch; ++b) {
+    const long long live = (length_of(a, b) + p.chunk - 1) / p.chunk;
+    const float* q = at + b * p.chunks * stride;
+#pragma unroll 4
+    for (long long k = part; k < live; k += 8) sum += q[k * stride];
+  }
+  return sum;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_grad_finish(mlt_scan_args a, mlt_scan_grads g, GradPlan p, Finish f,
+                                                     const unsigned char* ws) {
+  __shared__ float red[8][33];
+  pdl_wait();
+  pdl_trigger();
+  long long block = blockIdx.x;
+  if (block < f.bc_blocks) {
+    // dB, dC over the group's channel blocks
+    const long long n = a.states, i = block * 256 + threadIdx.x;
+    const long long rows = static_cast<long long>(a.batch) * a.length;
+    if (i >= rows * a.groups * n) return;
+    const long long s = i % n, gr = i / n % a.groups, row = i / n / a.groups;
+    const long long b = row / a.length, t = row - b * a.length;
+    float sb = 0.0f, sc = 0.0f;
+    if (t < length_of(a, static_cast<int>(b))) {
+      const float* q = reinterpret_cast<const float*>(ws + p.off_bc);
+#pragma unroll 4
+      for (int k = 0; k < p.blocks; ++k) {
+        const float* r = q + (((b * a.groups + gr) * p.blocks + k) * a.length + t) * 2 * n + s;
+        sb += r[0];
+        sc += r[n];
+      }
+    }
+    if (g.B != nullptr) static_cast<T*>(g.B)[i] = from_f32<T>(sb);
+    if (g.C != nullptr) static_cast<T*>(g.C)[i] = from_f32<T>(sc);
+    return;
+  }
+  block -= f.bc_blocks;
+  if (block < f.sum_blocks) {
+    // dA and the channels' vectors: 32 columns, 8 threads each
+    const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const long long of_seq = static_cast<long long>(a.dim) * a.states;
+    const long long i = block * 32 + col, all = of_seq + static_cast<long long>(kVecs) * a.dim;
+    float sum = 0.0f;
+    if (i < of_seq)
+      sum = sum_chunks(a, p, reinterpret_cast<const float*>(ws + p.off_A) + i, of_seq, part);
+    else if (i < all)
+      sum = sum_chunks(a, p, reinterpret_cast<const float*>(ws + p.off_vec) + (i - of_seq),
+                       static_cast<long long>(kVecs) * a.dim, part);
+    red[part][col] = sum;
+    __syncthreads();
+    if (part != 0 || i >= all) return;
+#pragma unroll
+    for (int q = 1; q < 8; ++q) sum += red[q][col];
+    if (i < of_seq) {
+      if (g.A != nullptr) g.A[i] = sum;
+      return;
+    }
+    const int v = static_cast<int>((i - of_seq) / a.dim), ch = static_cast<int>((i - of_seq) % a.dim);
+    if (v < kScanMaxTaps) {
+      if (v < a.taps && g.conv_w != nullptr) g.conv_w[static_cast<long long>(ch) * a.taps + a.taps - 1 - v] = sum;
+    } else {
+      float* to = v == kScanMaxTaps ? g.conv_b : v == kScanMaxTaps + 1 ? g.skip : g.dt_bias;
+      if (to != nullptr) to[ch] = sum;
+    }
+    return;
+  }
+  block -= f.sum_blocks;
+  // inputs that the next chunk's convolution reads too, and those before the start (chunk -1)
+  const long long i = block * 256 + threadIdx.x;
+  const int halo = a.taps - 1;
+  const long long per_seq = p.chunks * halo * a.dim;
+  if (i >= a.batch * per_seq) return;
+  const int b = static_cast<int>(i / per_seq);
+  const long long rest = i - b * per_seq;
+  const int ch = static_cast<int>(rest % a.dim), row = static_cast<int>(rest / a.dim % halo);
+  const long long chunk = rest / a.dim / halo - 1;  // the next one is chunk + 1
+  const long long len = length_of(a, b);
+  const bool next_live = (chunk + 1) * p.chunk < len;
+  if (chunk >= 0 && (!next_live || g.x == nullptr)) return;  // k_grad_chunk wrote them
+  if (chunk < 0 && g.conv_state == nullptr) return;
+  const long long seq = b * p.chunks + chunk;
+  float d = 0.0f;
+  if (next_live) {
+    if (chunk >= 0) d = reinterpret_cast<const float*>(ws + p.off_part)[(seq * kHalo + row) * a.dim + ch];
+    const float* head = reinterpret_cast<const float*>(ws + p.off_head) + (seq + 1) * kHalo * a.dim + ch;
+    // row is halo - row positions before the next chunk: weight j meets its position j - (halo - row)
+    for (int j = halo - row; j < a.taps; ++j)
+      d = fmaf(a.conv_w[static_cast<long long>(ch) * a.taps + a.taps - 1 - j],
+               head[static_cast<long long>(j - (halo - row)) * a.dim], d);
+  }
+  if (chunk < 0)
+    static_cast<T*>(g.conv_state)[(static_cast<long long>(b) * halo + row) * a.dim + ch] = from_f32<T>(d);
+  else
+    static_cast<T*>(g.x)[(b * a.length + (chunk + 1) * p.chunk - halo + row) * a.dim + ch] = from_f32<T>(d);
+}
+
+// No positions or no sequences: sums are zero, the state's gradient passes through.
+__global__ void __launch_bounds__(256) k_grad_nothing(mlt_scan_args a, mlt_scan_grads g, int elem) {
+  pdl_wait();
+  pdl_trigger();
+  const long long stride = static_cast<long long>(gridDim.x) * 256;
+  const long long first = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  auto clear = [&](float* p, long long n) {
+    if (p == nullptr) return;
+    for (long long i = first; i < n; i += stride) p[i] = 0.0f;
+  };
+  clear(g.A, of_seq);
+  clear(g.skip, a.dim);
+  clear(g.dt_bias, a.dim);
+  clear(g.conv_b, a.dim);
+  clear(g.conv_w, static_cast<long long>(a.dim) * a.taps);
+  if (g.state != nullptr)
+    for (long long i = first; i < a.batch * of_seq; i += stride)
+      g.state[i] = g.g_state_out != nullptr ? g.g_state_out[i] : 0.0f;
+  if (g.conv_state != nullptr)
+    for (long long i = first; i < static_cast<long long>(a.batch) * (a.taps - 1) * a.dim * (elem / 2); i += stride)
+      static_cast<unsigned short*>(g.conv_state)[i] = 0;
+}
+
+GradPlan grad_plan(const mlt_scan_args& a) {
+  GradPlan p{};
+  p.chunk = chunk_of(a.states);
+  p.chunks = (a.length + p.chunk - 1) / p.chunk;
+  p.blocks = blocks_per_group(a);
+  const size_t seqs = static_cast<size_t>(a.batch) * static_cast<size_t>(p.chunks), dim = a.dim;
+  size_t at = 0;
+  auto take = [&](size_t floats) {
+    const size_t o = at;
+    at += up256(floats * 4);
+    return o;
+  };
+  if (p.chunks > 1) {
+    p.off_e = take(seqs * dim * a.states);
+    p.off_g = take(seqs * dim * a.states);
+    p.off_sum = take(seqs * dim);
+  }
+  p.off_A = take(seqs * dim * a.states);
+  p.off_vec = take(seqs * dim * kVecs);
+  p.off_head = take(seqs * dim * kHalo);
+  p.off_part = take(seqs * dim * kHalo);
+  p.off_bc = take(static_cast<size_t>(a.batch) * a.groups * p.blocks * a.length * 2 * a.states);
+  p.bytes = at;
+  return p;
+}
+
+}  // namespace
+
+size_t scan_grad_workspace(const mlt_scan_args& a, int) {
+  return a.length == 0 || a.batch == 0 ? 0 : grad_plan(a).bytes;
+}
+
+cudaError_t launch_scan_grad(const mlt_scan_args& a, const mlt_scan_grads& g, void* ws, int sms, long long* launches,
+                             cudaStream_t st) {
+  if (a.length == 0 || a.batch == 0) {
+    ++*launches;
+    return launch_pdl(k_grad_nothing, dim3(sms), dim3(256), 0, st, a, g, static_cast<int>(dtype_size(a.dtype)));
+  }
+  const GradPlan p = grad_plan(a);
+  unsigned char* w = static_cast<unsigned char*>(ws);
+  const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  return with_dtype(a.dtype, [&](auto tag) {
+    return with_states(a.states, [&](auto states) -> cudaError_t {
+      using T = decltype(tag);
+      constexpr int S = decltype(states)::value;
+      const dim3 grid(static_cast<unsigned>(p.chunks * a.groups * p.blocks), a.batch);
+      auto go = [&](auto kernel, size_t smem) {
+        ++*launches;
+        const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), smem);
+        if (e != cudaSuccess) return e;
+        return launch_pdl(kernel, grid, dim3(kThreads), smem, st, a, g, p, w);
+      };
+      cudaError_t e;
+      if (p.chunks > 1) {
+        e = go(k_grad_local<T, S>, sizeof(Staged<S>));
+        if (e != cudaSuccess) return e;
+        ++*launches;
+        e = launch_pdl(k_grad_carry, dim3(static_cast<unsigned>((of_seq + 255) / 256), a.batch), dim3(256), 0, st, a, g,
+                       p, w);
+        if (e != cudaSuccess) return e;
+      }
+      e = go(k_grad_chunk<T, S>, sizeof(Walk<S>));
+      if (e != cudaSuccess) return e;
+      Finish f{};
+      if (g.B != nullptr || g.C != nullptr)
+        f.bc_blocks = (a.batch * a.length * a.groups * a.states + 255) / 256;
+      f.sum_blocks = (of_seq + static_cast<long long>(kVecs) * a.dim + 31) / 32;
+      if (a.taps > 1) f.edge_blocks = (a.batch * p.chunks * (a.taps - 1) * a.dim + 255) / 256;
+      ++*launches;
+      return launch_pdl(k_grad_finish<T>, dim3(static_cast<unsigned>(f.bc_blocks + f.sum_blocks + f.edge_blocks)),
+                        dim3(256), 0, st, a, g, p, f, static_cast<const unsigned char*>(w));
+    });
+  });
+}
+
+}  // namespace mlt

@@ -93,9 +93,13 @@ cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t s
 size_t embed_grad_workspace(long long tokens, long long vocab, int dim, int sms);
 cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st);
 
-// --- scan.cu -------------------------------------------------
+// --- scan.cu, scan_grad.cu -------------------------------------------------
 constexpr int kScanMaxStates = 32;
 constexpr int kScanMaxTaps = 4;
 size_t scan_workspace(const mlt_scan_args& a, int sms);
 cudaError_t launch_scan(const mlt_scan_args& a, void* ws, int sms, long long* launches, cudaStream_t st);
+size_t scan_grad_workspace(const mlt_scan_args& a, int sms);
+cudaError_t launch_scan_grad(const mlt_scan_args& a, const mlt_scan_grads& g, void* ws, int sms, long long* launches,
+                             cudaStream_t st);
+
 }  // namespace mlt

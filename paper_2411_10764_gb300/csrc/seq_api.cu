@@ -1,5 +1,5 @@
 // C entry points of the sequence-model operators: argument checks, then the
-// launches of sample.cu, embed.cu, and scan.cu.  Nothing here
+// launches of sample.cu, embed.cu, scan.cu and scan_grad.cu.  Nothing here
 // allocates device memory but the error word at the first call.
 #include <cmath>
 
@@ -243,6 +243,37 @@ int mlt_scan(void* stream, const mlt_scan_args* args, void* workspace, size_t wo
   long long launches = 0;
   const cudaError_t e = launch_scan(*args, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "scan launch");
+}
+
+int mlt_scan_grad_workspace(const mlt_scan_args* args, size_t* bytes_out) {
+  if (bytes_out == nullptr) return api_fail(MLT_EINVAL, "bytes_out must be non-NULL");
+  const int rc = check_scan(args);
+  if (rc != MLT_OK) return rc;
+  *bytes_out = scan_grad_workspace(*args, api_sm_count());
+  return MLT_OK;
+}
+
+int mlt_scan_grad(void* stream, const mlt_scan_args* args, const mlt_scan_grads* grads, void* workspace,
+                  size_t workspace_bytes) {
+  int rc = check_scan(args);
+  if (rc != MLT_OK) return rc;
+  if (grads == nullptr) return api_fail(MLT_EINVAL, "grads must be non-NULL");
+  rc = check_scan_inputs(args);
+  if (rc != MLT_OK) return rc;
+  if (args->length > 0 && args->batch > 0 && grads->gy == nullptr) return api_fail(MLT_EINVAL, "gy must be non-NULL");
+  if (!stride_ok(grads->gy_step, args->dim, args->length) || grads->gy_batch < 0)
+    return api_fail(MLT_EINVAL, "gy: positions must be at least dim elements apart");
+  if (!aligned_to(grads->gy, dtype_size(args->dtype))) return api_fail(MLT_EINVAL, "gy is not aligned to its elements");
+  if ((grads->z != nullptr && args->z == nullptr) || (grads->skip != nullptr && args->skip == nullptr) ||
+      (grads->dt_bias != nullptr && args->dt_bias == nullptr) || (grads->conv_b != nullptr && args->conv_b == nullptr) ||
+      (grads->conv_w != nullptr && args->taps == 0) || (grads->conv_state != nullptr && args->taps < 2))
+    return api_fail(MLT_EINVAL, "a gradient was asked for of an input that is not there");
+  const int sms = api_sm_count();
+  rc = check_ws(workspace, workspace_bytes, scan_grad_workspace(*args, sms));
+  if (rc != MLT_OK) return rc;
+  long long launches = 0;
+  const cudaError_t e = launch_scan_grad(*args, *grads, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "scan gradient launch");
 }
 
 }  // extern "C"

@@ -45,6 +45,12 @@ class ScanArgs(C.Structure):
                    ("conv_state_out", C.c_void_p)])
 
 
+class ScanGrads(C.Structure):
+    """mlt_scan_grads"""
+    _fields_ = ([("gy", C.c_void_p), ("gy_batch", C.c_int64), ("gy_step", C.c_int64)]
+                + [(k, C.c_void_p) for k in ("g_state_out", "x", "dt", "z", "B", "C", "A", "skip", "dt_bias", "conv_w",
+                                             "conv_b", "state", "conv_state")])
+
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
 
 
@@ -114,6 +120,8 @@ def lib(build_if_missing: bool = True):
             "mlt_embed_grad_workspace": [i64, i64, i32, P],
             "mlt_scan": [P, P, P, C.c_size_t],
             "mlt_scan_workspace": [P, P],
+            "mlt_scan_grad": [P, P, P, P, C.c_size_t],
+            "mlt_scan_grad_workspace": [P, P],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -582,6 +590,41 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
                           lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)), x.device, stream)
     _check(lb.mlt_scan(_stream_ptr(stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws))
     return y, state_out, conv_state_out
+
+
+def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=None, lengths=None, state=None,
+              conv_state=None, g_state=None, stream=None):
+    """mlt_scan_grad: the gradients of scan's inputs from those of y (`gy`) and
+    of the returned state (`g_state`, or None).  Returns a dict by the names of
+    the arguments (C_'s as "C"); None for inputs that were not given."""
+    import torch
+
+    a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
+    _cuda(gy, "gy", x.dtype)
+    _need(gy.shape == x.shape, "gy must have x's shape")
+    s = gy.stride()
+    _need(gy.numel() == 0 or x.shape[2] == 1 or s[2] == 1, "the channels of gy must be adjacent")
+    q = ScanGrads()
+    q.gy, q.gy_batch, q.gy_step = gy.data_ptr(), s[0], s[1]
+    if g_state is not None:
+        _cuda(g_state, "g_state", torch.float32)
+        _need(g_state.is_contiguous() and tuple(g_state.shape) == (a.batch, a.dim, a.states),
+              "g_state must be contiguous [batch][dim][states]")
+        q.g_state_out = g_state.data_ptr()
+    g = {}
+    for name, t in (("x", x), ("dt", dt), ("z", z), ("B", B), ("C", C_), ("A", A), ("skip", skip),
+                    ("dt_bias", dt_bias), ("conv_w", conv_w), ("conv_b", conv_b), ("state", state),
+                    ("conv_state", conv_state)):
+        if t is None or t.numel() == 0:
+            g[name] = None if t is None else torch.empty_like(t)
+            continue
+        g[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        setattr(q, name, g[name].data_ptr())
+    lb = lib()
+    ws, n_ws = _workspace(("scan_grad", a.dtype, *x.shape, a.states, a.groups, a.taps),
+                          lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device, stream)
+    _check(lb.mlt_scan_grad(_stream_ptr(stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws))
+    return g
 
 
 def screen_host(feats: np.ndarray, thr: float, k: int, out=None, stream=None):

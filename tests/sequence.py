@@ -60,68 +60,158 @@ def embed_grad(ids, grad, vocab, scale):
     return out * c, mag * abs(c)
 
 
-def sigmoid(v):
-    return 0.5 * (1 + np.tanh(0.5 * v))
+U = 2.0 ** -23  # an operation in 32 bits is off by at most half of U, an approximate one by a few
 
 
-U = 2.0 ** -23  # an approximate operation in 32 bits: one unit in the last place
+class Approx:
+    """A 64-bit value with a bound on how far a 32-bit evaluation of the same formula may be off."""
+
+    def __init__(self, v, e=None):
+        self.v = np.asarray(v, np.float64)
+        self.e = np.zeros_like(self.v) if e is None else e
+
+    def __add__(self, o):
+        o = o if isinstance(o, Approx) else Approx(o)
+        v = self.v + o.v
+        return Approx(v, self.e + o.e + U * np.abs(v))
+
+    def __mul__(self, o):
+        o = o if isinstance(o, Approx) else Approx(o)
+        v = self.v * o.v
+        return Approx(v, np.abs(self.v) * o.e + np.abs(o.v) * self.e + self.e * o.e + U * np.abs(v))
+
+    def __getitem__(self, i):
+        return Approx(self.v[i], self.e[i])
+
+    def exp(self):  # 2^(x log2 e): the argument is off by U of itself, the power by a few U
+        v = np.exp(self.v)
+        return Approx(v, v * np.expm1(self.e + U * (4 + 2 * np.abs(self.v))))
+
+    def sigmoid(self):  # slope at most a quarter and at most the value
+        v = 0.5 * (1 + np.tanh(0.5 * self.v))
+        return Approx(v, np.minimum(0.25, v) * (self.e + 2 * U * np.abs(self.v)) + 6 * U * v)
+
+    def softplus(self):  # slope sigmoid(x) <= the value where x < 0
+        v = np.logaddexp(0, self.v)
+        return Approx(v, np.minimum(1.0, v) * (self.e + 2 * U * np.abs(self.v)) + 8 * U * v)
+
+    def sum(self, axis):
+        n = np.prod([self.v.shape[i] for i in np.atleast_1d(axis)])
+        return Approx(self.v.sum(axis), self.e.sum(axis) + U * min(n, 64) * np.abs(self.v).sum(axis))
+
+    def where(self, on):
+        return Approx(np.where(on, self.v, 0), np.where(on, self.e, 0))
+
+    def pick(self, on, other):
+        return Approx(np.where(on, self.v, other.v), np.where(on, self.e, other.e))
 
 
-def scan(p):
-    """The recurrence of one call in 64 bits, position by position, with a bound on what 32-bit
-    arithmetic may add: every factor and term is off by a few units U of its magnitude, the
-    exponential's argument by U of it.  p: dict of numpy arrays (None where absent); returns a
-    dict with y, state, conv_state, their bounds y_tol, state_tol, and what the gradient needs."""
-    f = lambda k: None if p.get(k) is None else p[k].astype(np.float64)  # noqa: E731
+def _cat(parts, axis):
+    return Approx(np.concatenate([p.v for p in parts], axis), np.concatenate([p.e for p in parts], axis))
+
+
+def scan(p, gy=None, g_state=None):
+    """One call, position by position, as Approx values: y, state, conv_state; with gy also the
+    gradients of every input, by the chain rule on the recurrence.  p: numpy arrays by name
+    (absent ones missing)."""
+    f = lambda k: Approx(p[k]) if p.get(k) is not None else None  # noqa: E731
     x, dt, B, C, A = (f(k) for k in ("x", "dt", "B", "C", "A"))
-    nb, L, d = x.shape
-    n = A.shape[1]
-    group = np.arange(d) // (d // B.shape[2])
+    nb, L, d = x.v.shape
+    n, gr = A.v.shape[1], B.v.shape[2]
+    group = np.arange(d) // (d // gr)
     taps = 0 if p.get("conv_w") is None else p["conv_w"].shape[1]
-    z, w, cb, skip, bias = f("z"), f("conv_w"), f("conv_b"), f("skip"), f("dt_bias")
+    z, w, skip, bias, cb = f("z"), f("conv_w"), f("skip"), f("dt_bias"), f("conv_b")
     lengths = np.full(nb, L) if p.get("lengths") is None else np.clip(p["lengths"], 0, L)
-    live = np.arange(L)[None] < lengths[:, None]
-    x = np.where(live[..., None], x, 0)
+    live = (np.arange(L)[None] < lengths[:, None])[..., None]
+    x, dt, B, C = x.where(live), dt.where(live), B.where(live[..., None]), C.where(live[..., None])
     k1 = max(0, taps - 1)
-    old = np.zeros((nb, k1, d)) if p.get("conv_state") is None else f("conv_state")
-    past = np.concatenate([old, x], 1)
+    old = Approx(np.zeros((nb, k1, d))) if p.get("conv_state") is None else f("conv_state")
+    past = _cat([old, x], 1)
     if taps:
-        v = sum(past[:, j:j + L] * w[:, j] for j in range(taps)) + (0 if cb is None else cb)
-        vm = sum(np.abs(past[:, j:j + L] * w[:, j]) for j in range(taps)) + (0 if cb is None else np.abs(cb))
-        u = v * sigmoid(v)
-        um = np.abs(u) * (4 + np.abs(v)) + 1.1 * vm * (taps + 1)  # units of U; silu's slope is at most 1.1
+        v = Approx(np.zeros((nb, L, d))) if cb is None else cb + np.zeros((nb, L, d))
+        for j in range(taps):
+            v = v + past[:, j:j + L] * w[:, j]
+        sv = v.sigmoid()
+        u = v * sv
     else:
-        v, u, um = x, x, 0 * x
-    raw = np.where(live[..., None], dt, 0) + (0 if bias is None else bias)
-    step = np.logaddexp(0, raw)
-    stepm = step * (8 + np.abs(raw))  # units
-    h = np.zeros((nb, d, n)) if p.get("state") is None else f("state")
-    mag, err = np.abs(h), np.zeros_like(h)
-    hs, y, tol = [h], np.zeros((nb, L, d)), np.zeros((nb, L, d))
+        u = x
+    raw = dt if bias is None else dt + bias
+    step, u = raw.softplus().where(live), u.where(live)
+    push = step * u
+    sk = skip if skip is not None else Approx(np.zeros(d))
+    h = f("state") or Approx(np.zeros((nb, d, n)))
+    hs, decay, core = [h], [], []
     for t in range(L):
-        on = live[:, t][:, None, None]
-        arg = step[:, t][..., None] * A
-        a = np.exp(arg)
-        Bt, Ct = np.where(on, B[:, t], 0)[:, group], np.where(on, C[:, t], 0)[:, group]
-        push = (step[:, t] * u[:, t])[..., None] * Bt
-        pm = np.abs(push) * 4 + (stepm[:, t] * np.abs(u[:, t]) + step[:, t] * um[:, t])[..., None] * np.abs(Bt)
-        am = a * (4 + 2 * np.abs(arg) + np.abs(A) * stepm[:, t][..., None])
-        h2 = np.where(on, a * h + push, h)
-        err = np.where(on, a * err + U * (am * mag + pm), err)
-        mag = np.where(on, a * mag + np.abs(push), mag)
-        h = h2
+        on = live[:, t][..., None]
+        a = (step[:, t][..., None] * A).exp()
+        new = a * h + push[:, t][..., None] * B[:, t][:, group]
+        h = new.pick(on, h)
+        core.append((h * C[:, t][:, group]).sum(-1) + sk * u[:, t])
         hs.append(h)
-        su = (0 if skip is None else skip) * u[:, t]
-        y[:, t] = (h * Ct).sum(-1) + su
-        tol[:, t] = (np.abs(Ct) * (err + U * (n + 4) * mag)).sum(-1) + U * (
-            np.abs(su) * 4 + (0 if skip is None else np.abs(skip)) * um[:, t])
-    core, gate = y, 1.0
+        decay.append(a)
+    stack = lambda q: Approx(np.stack([i.v for i in q], 1), np.stack([i.e for i in q], 1))  # noqa: E731
+    core = stack(core) if L else Approx(np.zeros((nb, 0, d)))
+    out = {}
     if z is not None:
-        zz = np.where(live[..., None], z, 0)
-        gate = zz * sigmoid(zz)
-        tol = tol * np.abs(gate) + U * np.abs(y * gate) * (6 + np.abs(zz))
-    y = np.where(live[..., None], y * gate, 0)
-    idx = lengths[:, None] + np.arange(k1)
-    conv = np.take_along_axis(past, np.broadcast_to(idx[..., None], (nb, k1, d)), 1) if k1 else None
-    return dict(y=y, y_tol=np.where(live[..., None], tol, 0), state=h, state_tol=err + U * 4 * mag, conv_state=conv,
-                hs=hs, u=u, v=v, step=step, raw=raw, past=past, core=core, live=live, group=group, taps=taps)
+        z = z.where(live)
+        sz = z.sigmoid()
+        gate = z * sz
+    else:
+        gate = Approx(np.ones((nb, L, d)))
+    out["y"] = (core * gate).where(live)
+    out["state"] = h
+    if k1:
+        at = np.broadcast_to((lengths[:, None] + np.arange(k1))[..., None], (nb, k1, d))
+        out["conv_state"] = Approx(np.take_along_axis(past.v, at, 1))
+    if gy is None:
+        return out
+    go = Approx(gy).where(live)
+    gc = go * gate
+    g = Approx(np.zeros((nb, d, n)) if g_state is None else g_state)
+    G = {}
+    if z is not None:
+        G["z"] = go * core * sz * (z * (sz * -1.0 + 1.0) + 1.0)
+    gB, gC, gp, ga = [None] * L, [None] * L, [None] * L, [None] * L
+    gA = Approx(np.zeros((nb, d, n)))
+    per = (nb, gr, d // gr, n)
+    shape = lambda q, s: Approx(q.v.reshape(s), q.e.reshape(s))  # noqa: E731
+    for t in range(L - 1, -1, -1):
+        on = live[:, t][..., None]
+        gt = g + gc[:, t][..., None] * C[:, t][:, group]
+        gC[t] = shape(gc[:, t][..., None] * hs[t + 1], per).sum(2)
+        gB[t] = shape(gt * push[:, t][..., None], per).sum(2)
+        gp[t] = (gt * B[:, t][:, group]).sum(-1)
+        r = gt * decay[t]
+        e = r * hs[t]
+        ga[t] = (e * A).sum(-1)
+        gA = (gA + e * step[:, t][..., None]).pick(on, gA)
+        g = r.pick(on, g)
+    gp, ga = stack(gp), stack(ga)
+    G.update(state=g, A=gA.sum(0), B=stack(gB).where(live[..., None]), C=stack(gC).where(live[..., None]))
+    if skip is not None:
+        G["skip"] = (gc * u).sum((0, 1))
+    graw = ((gp * u + ga) * raw.sigmoid()).where(live)
+    G["dt"] = graw
+    if bias is not None:
+        G["dt_bias"] = graw.sum((0, 1))
+    gu = (gp * step + gc * sk).where(live)
+    if not taps:
+        G["x"] = gu
+    else:
+        gv = gu * sv * (v * (sv * -1.0 + 1.0) + 1.0)
+        gpast = Approx(np.zeros_like(past.v))
+        cols = []
+        for j in range(taps):
+            part = gv * w[:, j]
+            gpast = Approx(gpast.v.copy(), gpast.e.copy())
+            new = gpast[:, j:j + L] + part
+            gpast.v[:, j:j + L], gpast.e[:, j:j + L] = new.v, new.e
+            cols.append((gv * past[:, j:j + L]).sum((0, 1)))
+        G["conv_w"] = Approx(np.stack([c.v for c in cols], 1), np.stack([c.e for c in cols], 1))
+        if cb is not None:
+            G["conv_b"] = gv.sum((0, 1))
+        if p.get("conv_state") is not None:
+            G["conv_state"] = gpast[:, :k1]
+        G["x"] = gpast[:, k1:].where(live)
+    out["grad"] = {k: q for k, q in G.items() if p.get(k) is not None}
+    return out
