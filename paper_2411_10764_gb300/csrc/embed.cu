@@ -92,9 +92,10 @@ cudaError_t with_width(int v, F f) {
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortPerLane = 8;
-constexpr int kSortTile = kSortThreads * kSortPerLane;
 constexpr int kDigits = 256;
+// Positions a lane takes: a tile of 4,096 a CTA, or of 1,024 where there are too few
+// positions to give every SM a large one.
+int sort_per_lane(long long tokens) { return tokens > (1 << 18) ? 8 : 2; }
 
 struct SortPass {
   const void* ids;  // first pass: the ids themselves, else null
@@ -107,6 +108,7 @@ struct SortPass {
   uint32_t* totals;  // [kDigits]
   long long tokens, vocab;
   int tiles, shift;
+  unsigned char* named;  // first pass: 1 for ids that occur, else 0
   unsigned* err;
 };
 
@@ -117,15 +119,20 @@ __device__ __forceinline__ uint32_t sort_key(const SortPass& s, long long i) {
   return static_cast<uint32_t>(id < 0 || id >= s.vocab ? s.vocab : id);
 }
 
+template <int kPerLane>
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortPass s) {
   __shared__ uint32_t hist[kDigits];
   for (int d = threadIdx.x; d < kDigits; d += kSortThreads) hist[d] = 0;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const long long base = static_cast<long long>(blockIdx.x) * kSortTile;
+  if (s.named != nullptr)
+    for (long long v = (static_cast<long long>(blockIdx.x) * kSortThreads + threadIdx.x) * 16; v < s.vocab;
+         v += static_cast<long long>(gridDim.x) * kSortThreads * 16)
+      *reinterpret_cast<uint4*>(s.named + v) = make_uint4(0, 0, 0, 0);  // the array is padded
+  const long long base = static_cast<long long>(blockIdx.x) * (kSortThreads * kPerLane);
 #pragma unroll
-  for (int k = 0; k < kSortPerLane; ++k) {
+  for (int k = 0; k < kPerLane; ++k) {
     const long long i = base + k * kSortThreads + threadIdx.x;
     if (i >= s.tokens) break;
     if (s.ids != nullptr && id_of(s.ids, s.ids_64, i) >= s.vocab) atomicOr(s.err, kErrBadToken);
@@ -168,6 +175,7 @@ __global__ void __launch_bounds__(256) k_sort_scan(uint32_t* counts, uint32_t* t
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
+template <int kPerLane>
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
   __shared__ uint32_t cnt[kSortWarps][kDigits];
   __shared__ uint32_t warp_sum[kDigits / 32];
@@ -176,17 +184,17 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
   __syncwarp();
   pdl_wait();
   pdl_trigger();
-  // a warp owns kSortPerLane * 32 consecutive positions; rank[k] counts the
+  // a warp owns kPerLane * 32 consecutive positions; rank[k] counts the
   // equal digits before the lane's k-th one within the warp
-  const long long base = static_cast<long long>(blockIdx.x) * kSortTile + warp * (kSortPerLane * 32) + lane;
-  uint32_t key[kSortPerLane], rank[kSortPerLane];
+  const long long base = static_cast<long long>(blockIdx.x) * (kSortThreads * kPerLane) + warp * (kPerLane * 32) + lane;
+  uint32_t key[kPerLane], rank[kPerLane];
 #pragma unroll
-  for (int k = 0; k < kSortPerLane; ++k) {
+  for (int k = 0; k < kPerLane; ++k) {
     const long long i = base + k * 32;
     key[k] = i < s.tokens ? sort_key(s, i) : 0;
   }
 #pragma unroll
-  for (int k = 0; k < kSortPerLane; ++k) {
+  for (int k = 0; k < kPerLane; ++k) {
     const bool in = base + k * 32 < s.tokens;
     const uint32_t d = in ? (key[k] >> s.shift) & (kDigits - 1) : kDigits;
     const unsigned peers = __match_any_sync(~0u, d);
@@ -225,11 +233,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kSortPerLane; ++k) {
+  for (int k = 0; k < kPerLane; ++k) {
     const long long i = base + k * 32;
     if (i >= s.tokens) break;
     const uint32_t to = cnt[warp][(key[k] >> s.shift) & (kDigits - 1)] + rank[k];
     s.keys_out[to] = key[k];
+    // (looked at first: a million stores to 64 flags took 37 us)
+    if (s.named != nullptr && key[k] < s.vocab && s.named[key[k]] == 0) s.named[key[k]] = 1;
     s.pos_out[to] = s.ids != nullptr ? static_cast<uint32_t>(i) : s.pos_in[i];
   }
 }
@@ -253,6 +263,7 @@ struct GradArgs {
   float* lead;   // [pieces][dim]
   float* trail;  // [pieces][dim]
   long long sum_blocks;  // of k_grad_sum's grid.x; the rest clears rows no id names
+  const unsigned char* named;
 };
 
 __device__ __forceinline__ long long lower_bound(const uint32_t* keys, long long n, uint32_t v) {
@@ -266,6 +277,7 @@ __device__ __forceinline__ long long lower_bound(const uint32_t* keys, long long
 }
 
 constexpr int kSumThreads = 128;
+constexpr int kClearRows = 16;  // rows a group of lanes looks at
 constexpr int kSumUnroll = 8;
 
 template <typename TG, int V>
@@ -285,12 +297,14 @@ __global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradArgs a, const TI* 
   pdl_trigger();
   if (blockIdx.x >= a.sum_blocks) {
     // rows that no id names
-    const long long v = (blockIdx.x - a.sum_blocks) * groups + group;
-    if (v >= a.vocab || col >= a.dim) return;
-    const long long at = lower_bound(a.keys, a.tokens, static_cast<uint32_t>(v));
-    if (at < a.tokens && a.keys[at] == static_cast<uint32_t>(v)) return;
+    if (col >= a.dim) return;
+    const long long first = (blockIdx.x - a.sum_blocks) * groups * kClearRows + group;
     const float zero[V] = {};
-    store_row<TG, V>(out + v * a.out_stride + col, zero, 1.0f);
+#pragma unroll
+    for (int i = 0; i < kClearRows; ++i) {
+      const long long v = first + i * groups;
+      if (v < a.vocab && (a.named == nullptr || a.named[v] == 0)) store_row<TG, V>(out + v * a.out_stride + col, zero, 1.0f);
+    }
     return;
   }
   const long long p = static_cast<long long>(blockIdx.x) * groups + group;
@@ -400,23 +414,24 @@ int pow2_at_most_32(long long v) {
 }
 
 struct GradPlan {
-  int tiles, passes, piece;
+  int per_lane, tiles, passes, piece;
   long long pieces;
-  size_t off_keys[2], off_pos[2], off_counts, off_totals, off_lead, off_trail, bytes;
+  size_t off_keys[2], off_pos[2], off_counts, off_totals, off_named, off_lead, off_trail, bytes;
 };
 
-// Pieces: about 24 warps for each SM over all column chunks, 16 to 512 rows
-// each, so that a run's partial sums stay few beside the rows they stand for.
+// Pieces: 24 to 96 warps for each SM over all column chunks, 16 to 512 rows each, so that a
+// run's partial sums stay few beside the rows they stand for.
 GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
   GradPlan g{};
   const long long n = tokens < 1 ? 1 : tokens;
-  g.tiles = static_cast<int>((n + kSortTile - 1) / kSortTile);
+  g.per_lane = sort_per_lane(n);
+  g.tiles = static_cast<int>((n + kSortThreads * g.per_lane - 1) / (kSortThreads * g.per_lane));
   int bits = 1;
   while (bits < 32 && (vocab >> bits) != 0) ++bits;
   g.passes = (bits + 7) / 8;
   const long long work = n * ((dim + 127) / 128);
   g.piece = 16;
-  while (g.piece < 512 && work / g.piece > 24LL * sms) g.piece *= 2;
+  while (g.piece < 512 && work / g.piece > 96LL * sms) g.piece *= 2;
   g.pieces = (n + g.piece - 1) / g.piece;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -430,6 +445,7 @@ GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
   }
   g.off_counts = take(static_cast<size_t>(kDigits) * g.tiles * 4);
   g.off_totals = take(kDigits * 4);
+  g.off_named = take(vocab);
   g.off_lead = take(static_cast<size_t>(g.pieces) * dim * 4);
   g.off_trail = take(static_cast<size_t>(g.pieces) * dim * 4);
   g.bytes = at;
@@ -485,11 +501,15 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
       s.tiles = g.tiles;
       s.shift = 8 * k;
       s.err = a.err;
-      cudaError_t e = launch_pdl(k_sort_count, dim3(g.tiles), dim3(kSortThreads), 0, st, s);
+      s.named = k == 0 ? ws + g.off_named : nullptr;
+      const dim3 grid(g.tiles), block(kSortThreads);
+      cudaError_t e = g.per_lane == 8 ? launch_pdl(k_sort_count<8>, grid, block, 0, st, s)
+                                      : launch_pdl(k_sort_count<2>, grid, block, 0, st, s);
       if (e != cudaSuccess) return e;
       e = launch_pdl(k_sort_scan, dim3(kDigits), dim3(256), 0, st, s.counts, s.totals, g.tiles);
       if (e != cudaSuccess) return e;
-      e = launch_pdl(k_sort_scatter, dim3(g.tiles), dim3(kSortThreads), 0, st, s);
+      e = g.per_lane == 8 ? launch_pdl(k_sort_scatter<8>, grid, block, 0, st, s)
+                          : launch_pdl(k_sort_scatter<2>, grid, block, 0, st, s);
       if (e != cudaSuccess) return e;
       *launches += 3;
       keys = s.keys_out;
@@ -504,6 +524,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
   q.dim = a.dim;
   q.piece = g.piece;
   q.pieces = a.tokens > 0 ? g.pieces : 0;
+  q.named = a.tokens > 0 ? ws + g.off_named : nullptr;
   q.scale = a.scale;
   q.in_stride = a.in_stride;
   q.out_stride = a.out_stride;
@@ -520,7 +541,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
         const long long groups = kSumThreads / q.lanes;
         q.sum_blocks = (q.pieces + groups - 1) / groups;
         const unsigned chunks = static_cast<unsigned>((packs + q.lanes - 1) / q.lanes);
-        const dim3 grid(static_cast<unsigned>(q.sum_blocks + (a.vocab + groups - 1) / groups), chunks);
+        const dim3 grid(static_cast<unsigned>(q.sum_blocks + (a.vocab + groups * kClearRows - 1) / (groups * kClearRows)), chunks);
         cudaError_t e = launch_pdl(k_grad_sum<TI, TO, V>, grid, dim3(kSumThreads), 0, st, q,
                                    static_cast<const TI*>(a.table), static_cast<TO*>(a.out));
         if (e != cudaSuccess) return e;

@@ -1,10 +1,15 @@
 // What the selective scan and its gradient share (not part of the C ABI).
 //
-// Four lanes share a channel, each with S of its states (N <= 4 S); a CTA has 64
-// channels of one group, so it reads one B and C row a position.  Per tile of
-// positions the CTA first turns the inputs into what the recurrence
-// uses (step size, pushed input, gate) in shared memory, once per
-// (position, channel), then each lane walks its states through the tile.
+// Four lanes share a channel (or two of them), each with S of its states (N <= 4 S); a CTA
+// has CH channels of one group, so it reads one B and C row a position.
+// Inputs are first turned into what the recurrence uses (step size, pushed input, gate) in
+// shared memory, once per (position, channel): a thread does this for two adjacent
+// channels and a run of consecutive positions, whose convolution windows overlap.
+// Then each lane walks its states through the staged positions.
+//
+// Arithmetic on states goes through two-float instructions: they do not raise the rate of
+// fp32 operations (128 a cycle and SM either way, measured) but take half the issue slots.
+// They take no immediate operands, so formulas full of constants stay scalar.
 #pragma once
 
 #include <cmath>
@@ -15,11 +20,7 @@
 namespace mlt {
 namespace scan {
 
-constexpr int kChannels = 64;          // of a CTA
-constexpr int kThreads = 4 * kChannels;
-constexpr int kTile = 16;              // positions staged at a time
-constexpr int kPackC = 4;              // channels a thread stages at once
-static_assert(kTile * kChannels == kThreads * kPackC, "a thread stages one pack of a tile");
+constexpr int kGroups = 8;  // runs of positions staged side by side: 4 CH threads / (CH / 2) pairs
 
 constexpr float kLog2E = 1.4426950408889634f;
 
@@ -27,20 +28,22 @@ struct Block {
   int b, c0, cn, g;  // sequence, first channel, channels, group
 };
 
-// blockIdx.x counts channel blocks, group by group (a block never spans two groups).
+// Channel blocks are counted group by group (a block never spans two groups).
+template <int CH>
 __host__ __device__ inline int blocks_per_group(const mlt_scan_args& a) {
-  return (a.dim / a.groups + kChannels - 1) / kChannels;
+  return (a.dim / a.groups + CH - 1) / CH;
 }
 
 #ifdef __CUDACC__
+template <int CH>
 __device__ __forceinline__ Block block_of(const mlt_scan_args& a, int block, int b) {
   Block k;
-  const int per = blocks_per_group(a), width = a.dim / a.groups;
+  const int per = blocks_per_group<CH>(a), width = a.dim / a.groups;
   k.b = b;
   k.g = block / per;
-  const int first = (block - k.g * per) * kChannels;
+  const int first = (block - k.g * per) * CH;
   k.c0 = k.g * width + first;
-  k.cn = min(kChannels, width - first);
+  k.cn = min(CH, width - first);
   return k;
 }
 __device__ __forceinline__ long long length_of(const mlt_scan_args& a, int b) {
@@ -62,16 +65,14 @@ __device__ __forceinline__ float rcp(float x) {
 __device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-kLog2E * x)); }
 
 // ln(1 + e^x) = max(x, 0) + ln(1 + e), e = e^-|x| in (0, 1].  With s = e / (2 + e) <= 1/3,
-// ln(1 + e) = 2 atanh s = 2 (s + s^3/3 + s^5/5 + ...): nine terms leave 2 s^19/19 < 1e-10, so
+// ln(1 + e) = 2 atanh s = 2 (s + s^3/3 + s^5/5 + ...): seven terms leave 2 s^15/15 < 1e-8, so
 // the result keeps its relative precision where e is small (the usual step sizes are
 // 0.001 .. 0.1), which log2 of 1 + e would lose.
 __device__ __forceinline__ float softplus(float x) {
   const float e = ex2(-kLog2E * fabsf(x));
   const float s = e * rcp(2.0f + e);
   const float q = s * s;
-  float p = 2.0f / 17.0f;
-  p = fmaf(p, q, 2.0f / 15.0f);
-  p = fmaf(p, q, 2.0f / 13.0f);
+  float p = 2.0f / 13.0f;
   p = fmaf(p, q, 2.0f / 11.0f);
   p = fmaf(p, q, 2.0f / 9.0f);
   p = fmaf(p, q, 2.0f / 7.0f);
@@ -190,110 +191,221 @@ __device__ __forceinline__ float quad_sums(const float (&v)[4], int j) {
   return r;
 }
 
-// kPackC channels of a row: one access where the call's strides and addresses allow, else
-// element by element; nothing past the block's channels is read or written.
-template <typename T, bool kVec>
-__device__ __forceinline__ Pack<T, kPackC> load_pack(const T* row, int c, int cn) {
-  Pack<T, kPackC> p;
-  if (kVec) {
-    if (c < cn) p = *reinterpret_cast<const Pack<T, kPackC>*>(row + c);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kPackC; ++e)
-      if (c + e < cn) p.v[e] = row[c + e];
-  }
-  return p;
+// ---------------------------------------------------------------------------
+// Staging
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ F2 dup2(float a) { return f2(a, a); }
+__device__ __forceinline__ F2 rcp_2(F2 a) {
+  float x, y;
+  un2(a, x, y);
+  return f2(rcp(x), rcp(y));
 }
-template <typename T, bool kVec>
-__device__ __forceinline__ void store_pack(T* row, int c, int cn, const Pack<T, kPackC>& p) {
-  if (kVec) {
-    if (c < cn) *reinterpret_cast<Pack<T, kPackC>*>(row + c) = p;
-  } else {
-#pragma unroll
-    for (int e = 0; e < kPackC; ++e)
-      if (c + e < cn) row[c + e] = p.v[e];
-  }
-}
-
-// Input x at position t - back (before the start: conv_state, or zeros).
-template <typename T, bool kVec>
-__device__ __forceinline__ Pack<T, kPackC> load_x(const mlt_scan_args& a, const Block& k, long long t, int c) {
-  if (t >= 0)
-    return load_pack<T, kVec>(static_cast<const T*>(a.x) + k.b * a.x_batch + t * a.x_step + k.c0, c, k.cn);
-  Pack<T, kPackC> p;
-#pragma unroll
-  for (int e = 0; e < kPackC; ++e) p.v[e] = from_f32<T>(0.0f);
-  if (a.conv_state != nullptr)
-    p = load_pack<T, kVec>(static_cast<const T*>(a.conv_state) +
-                               (static_cast<long long>(k.b) * (a.taps - 1) + t + a.taps - 1) * a.dim + k.c0,
-                           c, k.cn);
-  return p;
+__device__ __forceinline__ F2 sigmoid2(F2 x) { return rcp_2(add2(ex2_2(mul2(x, dup2(-kLog2E))), dup2(1.0f))); }
+__device__ __forceinline__ F2 softplus2(F2 x) {  // as softplus
+  float a, b;
+  un2(x, a, b);
+  const F2 e = f2(ex2(-kLog2E * fabsf(a)), ex2(-kLog2E * fabsf(b)));
+  const F2 s = mul2(e, rcp_2(add2(e, dup2(2.0f))));
+  const F2 q = mul2(s, s);
+  F2 p = dup2(2.0f / 13.0f);
+  p = fma2(p, q, dup2(2.0f / 11.0f));
+  p = fma2(p, q, dup2(2.0f / 9.0f));
+  p = fma2(p, q, dup2(2.0f / 7.0f));
+  p = fma2(p, q, dup2(2.0f / 5.0f));
+  p = fma2(p, q, dup2(2.0f / 3.0f));
+  p = fma2(p, q, dup2(2.0f));
+  return fma2(p, s, f2(fmaxf(a, 0.0f), fmaxf(b, 0.0f)));
 }
 
-// The convolution's weights of a thread's channels, last tap first: w[0] meets x[t].
-struct Taps {
-  float w[kScanMaxTaps][kPackC];
-  float b[kPackC];
+// Two adjacent channels of a row, as they are in memory: 16-bit types stay packed in one
+// register until they are used.  (Held as two values they would be taken apart right
+// after the load, which then waits for memory there.)
+template <typename T>
+struct Two {
+  uint32_t w;
+  __device__ __forceinline__ F2 f32() const {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      return f2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    } else {
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+      return f2(v.x, v.y);
+    }
+  }
 };
-__device__ __forceinline__ Taps load_taps(const mlt_scan_args& a, const Block& k, int c) {
-  Taps q;
+template <>
+struct Two<float> {
+  F2 v;
+  __device__ __forceinline__ F2 f32() const { return v; }
+};
+// kVec: one access (rows and addresses allow it), else element by element; `n` (1 or 2) of
+// them belong to the block.
+template <typename T, bool kVec>
+__device__ __forceinline__ Two<T> load_two(const T* p, int n) {
+  Two<T> r;
+  if constexpr (sizeof(T) == 4) {
+    if (kVec)
+      r.v.v = *reinterpret_cast<const unsigned long long*>(p);
+    else
+      r.v = f2(p[0], n > 1 ? p[1] : 0.0f);
+  } else {
+    if (kVec) {
+      r.w = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+      r.w = h[0];
+      if (n > 1) r.w |= static_cast<uint32_t>(h[1]) << 16;
+    }
+  }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ Two<T> two_zero() {
+  Two<T> r;
+  if constexpr (sizeof(T) == 4) r.v = f2(0.0f, 0.0f);
+  else r.w = 0;
+  return r;
+}
+template <typename T, bool kVec>
+__device__ __forceinline__ void store_two(T* p, int n, F2 v) {
+  float a, b;
+  un2(v, a, b);
+  Pack<T, 2> r;
+  r.v[0] = from_f32<T>(a);
+  r.v[1] = from_f32<T>(b);
+  if (kVec) {
+    *reinterpret_cast<Pack<T, 2>*>(p) = r;
+  } else {
+    p[0] = r.v[0];
+    if (n > 1) p[1] = r.v[1];
+  }
+}
+template <typename T>
+__device__ __forceinline__ F2 two_f32(const Two<T>& p) {
+  return p.f32();
+}
+
+// A thread's two channels and what staging needs of their parameters.
+struct PairParams {
+  int c, n;     // first channel within the block; how many of the two belong to it
+  F2 w[kScanMaxTaps], conv_b, bias;  // w[0] meets x[t]
+};
+template <int CH>
+__device__ __forceinline__ PairParams pair_params(const mlt_scan_args& a, const Block& k) {
+  PairParams q;
+  q.c = threadIdx.x % (CH / 2) * 2;
+  q.n = max(0, min(2, k.cn - q.c));
+  const int ch = k.c0 + q.c;
+  auto two = [&](const float* p) {
+    return p == nullptr ? dup2(0.0f) : f2(q.n > 0 ? p[ch] : 0.0f, q.n > 1 ? p[ch + 1] : 0.0f);
+  };
+  q.conv_b = two(a.taps > 0 ? a.conv_b : nullptr);
+  q.bias = two(a.dt_bias);
 #pragma unroll
-  for (int e = 0; e < kPackC; ++e) {
-    const int ch = k.c0 + c + e;
-    const bool in = c + e < k.cn;
-    q.b[e] = in && a.conv_b != nullptr && a.taps > 0 ? a.conv_b[ch] : 0.0f;
-#pragma unroll
-    for (int j = 0; j < kScanMaxTaps; ++j)
-      q.w[j][e] = in && j < a.taps ? a.conv_w[static_cast<long long>(ch) * a.taps + a.taps - 1 - j] : 0.0f;
+  for (int j = 0; j < kScanMaxTaps; ++j) {
+    const long long at = static_cast<long long>(ch) * a.taps + a.taps - 1 - j;
+    const bool on = j < a.taps;
+    q.w[j] = f2(on && q.n > 0 ? a.conv_w[at] : 0.0f, on && q.n > 1 ? a.conv_w[at + a.taps] : 0.0f);
   }
   return q;
 }
-// The inputs that position t's convolution reads; [0] is x[t].
-template <typename T>
-struct Window {
-  Pack<T, kPackC> x[kScanMaxTaps];
+
+// Inputs of a run of positions; x[kScanMaxTaps - 1 + i] belongs to position i.
+template <typename T, int RUN>
+struct RawRun {
+  Two<T> x[RUN + kScanMaxTaps - 1], dt[RUN], z[RUN];
 };
-template <typename T, bool kVec>
-__device__ __forceinline__ Window<T> load_window(const mlt_scan_args& a, const Block& k, long long t, int c) {
-  Window<T> w;
-  w.x[0] = load_x<T, kVec>(a, k, t, c);
+
+// Positions first .. first + RUN - 1 below `end`; what lies before the start comes from
+// conv_state.
+template <typename T, int RUN, bool kVec, bool kGate>
+__device__ __forceinline__ void load_run(const mlt_scan_args& a, const Block& k, const PairParams& q, long long first,
+                                         long long end, RawRun<T, RUN>& r) {
+  if (q.n == 0 || first >= end) return;
+  const int ch = k.c0 + q.c;
+  const long long left = end - first;
+  const T* x = static_cast<const T*>(a.x) + k.b * a.x_batch + first * a.x_step + ch;
+  if (a.taps > 1) {
+    if (first >= kScanMaxTaps - 1) {
+      const T* p = x;
 #pragma unroll
-  for (int j = 1; j < kScanMaxTaps; ++j)
-    if (j < a.taps) w.x[j] = load_x<T, kVec>(a, k, t - j, c);
-  return w;
+      for (int j = 1; j < kScanMaxTaps; ++j) {
+        p -= a.x_step;
+        if (j < a.taps) r.x[kScanMaxTaps - 1 - j] = load_two<T, kVec>(p, q.n);
+      }
+    } else {
+#pragma unroll
+      for (int j = 1; j < kScanMaxTaps; ++j) {
+        if (j >= a.taps) break;
+        const long long t = first - j;
+        Two<T> v = two_zero<T>();
+        if (t >= 0)
+          v = load_two<T, kVec>(x - j * a.x_step, q.n);
+        else if (a.conv_state != nullptr && t + a.taps - 1 >= 0)
+          v = load_two<T, kVec>(static_cast<const T*>(a.conv_state) +
+                                    (static_cast<long long>(k.b) * (a.taps - 1) + t + a.taps - 1) * a.dim + ch,
+                                q.n);
+        r.x[kScanMaxTaps - 1 - j] = v;
+      }
+    }
+  }
+  const T* d = static_cast<const T*>(a.dt) + k.b * a.dt_batch + first * a.dt_step + ch;
+  const T* z = static_cast<const T*>(a.z) + k.b * a.z_batch + first * a.z_step + ch;
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) {
+    if (i < left) {
+      r.x[kScanMaxTaps - 1 + i] = load_two<T, kVec>(x, q.n);
+      r.dt[i] = load_two<T, kVec>(d, q.n);
+      if (kGate && a.z != nullptr) r.z[i] = load_two<T, kVec>(z, q.n);
+    }
+    x += a.x_step;
+    d += a.dt_step;
+    z += a.z_step;
+  }
 }
-// The convolution's output before its activation (x itself without taps).
-template <typename T>
-__device__ __forceinline__ float conv_at(const mlt_scan_args& a, const Taps& q, const Window<T>& w, int e) {
-  if (a.taps == 0) return to_f32(w.x[0].v[e]);
-  float v = fmaf(q.w[0][e], to_f32(w.x[0].v[e]), q.b[e]);
+
+// Convolution of position i of the run, before its activation (x itself without taps).
+template <typename T, int RUN>
+__device__ __forceinline__ F2 conv_run(const mlt_scan_args& a, const PairParams& q, const RawRun<T, RUN>& r, int i) {
+  const F2 x0 = two_f32(r.x[kScanMaxTaps - 1 + i]);
+  if (a.taps == 0) return x0;
+  F2 v = fma2(q.w[0], x0, q.conv_b);
 #pragma unroll
   for (int j = 1; j < kScanMaxTaps; ++j)
-    if (j < a.taps) v = fmaf(q.w[j][e], to_f32(w.x[j].v[e]), v);
+    if (j < a.taps) v = fma2(q.w[j], two_f32(r.x[kScanMaxTaps - 1 + i - j]), v);
   return v;
 }
 
-// A tile's rows of B (or C) as floats, [kTile][4 S], zero past `live` positions and N states.
-template <typename T, int S>
-__device__ __forceinline__ void stage_rows(float* to, const T* rows, long long step, int n, int live) {
-  for (int i = threadIdx.x; i < kTile * 4 * S; i += kThreads) {
-    const int t = i / (4 * S), s = i - t * (4 * S);
-    to[i] = t < live && s < n ? to_f32(rows[t * step + s]) : 0.0f;
-  }
+// Input at position t of the sequence (before the start: conv_state, or 0).
+template <typename T>
+__device__ __forceinline__ float input_at(const mlt_scan_args& a, int b, long long t, int ch) {
+  if (t >= 0) return t < a.length ? to_f32(static_cast<const T*>(a.x)[b * a.x_batch + t * a.x_step + ch]) : 0.0f;
+  if (a.conv_state == nullptr || t < -(a.taps - 1)) return 0.0f;
+  return to_f32(static_cast<const T*>(a.conv_state)[(static_cast<long long>(b) * (a.taps - 1) + t + a.taps - 1) * a.dim +
+                                                    ch]);
+}
+// Two adjacent elements of shared memory, aligned to both.
+template <typename T>
+__device__ __forceinline__ F2 shared_two(const T* p) {
+  Two<T> r;
+  if constexpr (sizeof(T) == 4) r.v.v = *reinterpret_cast<const unsigned long long*>(p);
+  else r.w = *reinterpret_cast<const uint32_t*>(p);
+  return r.f32();
+}
+template <typename T>
+__device__ __forceinline__ void copy_two(T* to, const T* from) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<unsigned long long*>(to) = *reinterpret_cast<const unsigned long long*>(from);
+  else *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
 }
 #endif
 
-// Whether packs of kPackC channels are aligned in every row.
-inline bool packs_ok(const mlt_scan_args& a) {
-  const size_t e = dtype_size(a.dtype), bytes = e * kPackC;
-  const int64_t w = kPackC;
-  bool ok = a.dim / a.groups % w == 0 && aligned_to(a.conv_state, bytes) && aligned_to(a.conv_state_out, bytes);
-  ok = ok && aligned_to(a.x, bytes) && a.x_step % w == 0 && a.x_batch % w == 0;
-  ok = ok && aligned_to(a.dt, bytes) && a.dt_step % w == 0 && a.dt_batch % w == 0;
-  ok = ok && (a.z == nullptr || (aligned_to(a.z, bytes) && a.z_step % w == 0 && a.z_batch % w == 0));
-  return ok;
+// Whether two adjacent channels are one aligned access in every row.
+inline bool pairs_ok(const mlt_scan_args& a) {
+  const size_t bytes = 2 * dtype_size(a.dtype);
+  bool ok = a.dim / a.groups % 2 == 0 && aligned_to(a.conv_state, bytes);
+  ok = ok && aligned_to(a.x, bytes) && a.x_step % 2 == 0 && a.x_batch % 2 == 0;
+  ok = ok && aligned_to(a.dt, bytes) && a.dt_step % 2 == 0 && a.dt_batch % 2 == 0;
+  return ok && (a.z == nullptr || (aligned_to(a.z, bytes) && a.z_step % 2 == 0 && a.z_batch % 2 == 0));
 }
-
 // Calls f with the number of states a lane takes.
 template <typename F>
 auto with_states(int n, F f) {
@@ -303,12 +415,6 @@ auto with_states(int n, F f) {
   return f(std::integral_constant<int, 8>());
 }
 inline int states_padded(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : 32; }
-
-// Sequences are cut into `chunks` of `chunk` positions (a multiple of kTile).
-struct Chunks {
-  long long chunk;
-  int chunks;
-};
 
 }  // namespace scan
 }  // namespace mlt

@@ -37,8 +37,10 @@ struct Shape {
 };
 int chunk_of(int states) { return states > 16 ? 32 : 64; }
 
-constexpr int kTimes = kThreads / kChannels;  // threads that share a channel outside the walk
-constexpr int kRing = 16;                     // rows of dv kept for the convolution
+constexpr int kChannels = 64;   // of a CTA
+constexpr int kThreads = 4 * kChannels;
+constexpr int kPairs = kChannels / 2;
+constexpr int kRing = 16;       // rows of dv kept for the convolution
 constexpr int kVecs = kScanMaxTaps + 3;       // per channel: conv_w (4), conv_b, skip, dt_bias
 constexpr int kHalo = kScanMaxTaps - 1;
 
@@ -68,80 +70,52 @@ struct alignas(16) Walk {
   float dv[kRing][kChannels];
 };
 
-// A channel's convolution weights, last tap first.
-struct ChannelTaps {
-  float w[kScanMaxTaps], b;
-};
-__device__ __forceinline__ ChannelTaps channel_taps(const mlt_scan_args& a, int ch, bool in) {
-  ChannelTaps q;
-  q.b = in && a.taps > 0 && a.conv_b != nullptr ? a.conv_b[ch] : 0.0f;
+// Two channels of gy at `count` positions from t on.
+template <typename T, int RUN, bool kVec>
+__device__ __forceinline__ void load_gy(const mlt_scan_grads& g, const Block& k, const PairParams& q, long long t,
+                                        int count, Two<T> (&gy)[RUN]) {
+  const T* p = static_cast<const T*>(g.gy) + k.b * g.gy_batch + t * g.gy_step + k.c0 + q.c;
 #pragma unroll
-  for (int j = 0; j < kScanMaxTaps; ++j)
-    q.w[j] = in && j < a.taps ? a.conv_w[static_cast<long long>(ch) * a.taps + a.taps - 1 - j] : 0.0f;
-  return q;
-}
-// Input at position t of the sequence (before the start: conv_state, or 0).
-template <typename T>
-__device__ __forceinline__ float input_at(const mlt_scan_args& a, int b, long long t, int ch) {
-  if (t >= 0) return to_f32(static_cast<const T*>(a.x)[b * a.x_batch + t * a.x_step + ch]);
-  if (a.conv_state == nullptr || t < -(a.taps - 1)) return 0.0f;
-  return to_f32(static_cast<const T*>(a.conv_state)[(static_cast<long long>(b) * (a.taps - 1) + t + a.taps - 1) * a.dim +
-                                                    ch]);
-}
-__device__ __forceinline__ float conv_of(const mlt_scan_args& a, const ChannelTaps& q, const float (&x)[kScanMaxTaps]) {
-  if (a.taps == 0) return x[0];
-  float v = fmaf(q.w[0], x[0], q.b);
-#pragma unroll
-  for (int j = 1; j < kScanMaxTaps; ++j)
-    if (j < a.taps) v = fmaf(q.w[j], x[j], v);
-  return v;
+  for (int i = 0; i < RUN; ++i) {
+    if (q.n > 0 && i < count) gy[i] = load_two<T, kVec>(p, q.n);
+    p += g.gy_step;
+  }
 }
 
-// The chunk's (d, u), gc, B and C in shared memory; zero from `live` on.  A thread stages one
-// channel's kChunk / kTimes consecutive positions.
-template <typename T, int S>
+// The chunk's (d, u), gc, B and C in shared memory; zero from `live` on.
+template <typename T, int S, bool kVec>
 __device__ __forceinline__ void stage_chunk(const mlt_scan_args& a, const mlt_scan_grads& g, const Block& k,
-                                            long long begin, int live, Staged<S>& st) {
-  constexpr int kRun = Shape<S>::kChunk / kTimes;
-  const int c = threadIdx.x % kChannels, t0 = threadIdx.x / kChannels * kRun;
-  const bool in = c < k.cn;
-  const int ch = k.c0 + c;
-  const ChannelTaps taps = channel_taps(a, ch, in);
-  const float bias = in && a.dt_bias != nullptr ? a.dt_bias[ch] : 0.0f;
-  float x[kScanMaxTaps] = {};
-  if (in && t0 < live) {
+                                            const PairParams& q, long long begin, int live, Staged<S>& st) {
+  constexpr int kRun = Shape<S>::kChunk / kGroups;
+  const int run = threadIdx.x / kPairs * kRun;
+  RawRun<T, kRun> raw;
+  Two<T> gy[kRun];
+  load_run<T, kRun, kVec, true>(a, k, q, begin + run, begin + live, raw);
+  load_gy<T, kRun, kVec>(g, k, q, begin + run, live - run, gy);
 #pragma unroll
-    for (int j = 1; j < kScanMaxTaps; ++j)
-      if (j < a.taps) x[j] = input_at<T>(a, k.b, begin + t0 - j, ch);
-  }
-  const T* xp = static_cast<const T*>(a.x) + k.b * a.x_batch + ch;
-  const T* dp = static_cast<const T*>(a.dt) + k.b * a.dt_batch + ch;
-  const T* zp = static_cast<const T*>(a.z) + k.b * a.z_batch + ch;
-  const T* gp = static_cast<const T*>(g.gy) + k.b * g.gy_batch + ch;
-#pragma unroll 4
   for (int i = 0; i < kRun; ++i) {
-    const int t = t0 + i;
-    float2 du = make_float2(0.0f, 0.0f);
-    float gc = 0.0f;
-    if (in && t < live) {
-      const long long at = begin + t;
-      x[0] = to_f32(xp[at * a.x_step]);
-      du.x = softplus(to_f32(dp[at * a.dt_step]) + bias);
-      const float v = conv_of(a, taps, x);
-      du.y = a.taps > 0 ? v * sigmoid(v) : v;
-      gc = to_f32(gp[at * g.gy_step]);
+    F2 d = dup2(0.0f), u = d, gc = d;
+    if (run + i < live && q.n > 0) {
+      u = conv_run(a, q, raw, i);
+      if (a.taps > 0) u = mul2(u, sigmoid2(u));
+      d = softplus2(add2(two_f32(raw.dt[i]), q.bias));
+      gc = two_f32(gy[i]);
       if (a.z != nullptr) {
-        const float z = to_f32(zp[at * a.z_step]);
-        gc *= z * sigmoid(z);
+        const F2 z = two_f32(raw.z[i]);
+        gc = mul2(gc, mul2(z, sigmoid2(z)));
       }
-#pragma unroll
-      for (int j = kScanMaxTaps - 1; j > 0; --j) x[j] = x[j - 1];
     }
-    st.du[t][c] = du;
-    st.gc[t][c] = gc;
+    float4 o;
+    un2(d, o.x, o.z);
+    un2(u, o.y, o.w);
+    *reinterpret_cast<float4*>(&st.du[run + i][q.c]) = o;
+    float2 c;
+    un2(gc, c.x, c.y);
+    *reinterpret_cast<float2*>(&st.gc[run + i][q.c]) = c;
   }
   const T* Bp = static_cast<const T*>(a.B) + k.b * a.B_batch + begin * a.B_step + static_cast<long long>(k.g) * a.states;
   const T* Cp = static_cast<const T*>(a.C) + k.b * a.C_batch + begin * a.C_step + static_cast<long long>(k.g) * a.states;
+#pragma unroll 4
   for (int i = threadIdx.x; i < Shape<S>::kChunk * 4 * S; i += kThreads) {
     const int t = i / (4 * S), s = i - t * (4 * S);
     const bool ok = t < live && s < a.states;
@@ -158,16 +132,16 @@ struct Where {
 };
 __device__ __forceinline__ Where where(const mlt_scan_args& a, int chunk_positions) {
   Where w;
-  const int blocks = a.groups * blocks_per_group(a);
+  const int blocks = a.groups * blocks_per_group<kChannels>(a);
   w.chunk = blockIdx.x / blocks;
-  w.k = block_of(a, static_cast<int>(blockIdx.x - w.chunk * blocks), blockIdx.y);
+  w.k = block_of<kChannels>(a, static_cast<int>(blockIdx.x - w.chunk * blocks), blockIdx.y);
   w.begin = w.chunk * chunk_positions;
   w.len = length_of(a, w.k.b);
   w.live = static_cast<int>(min(static_cast<long long>(chunk_positions), max(0ll, w.len - w.begin)));
   return w;
 }
 
-template <typename T, int S>
+template <typename T, int S, bool kVec>
 __global__ void __launch_bounds__(kThreads) k_grad_local(mlt_scan_args a, mlt_scan_grads g, GradPlan p,
                                                          unsigned char* ws) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -176,7 +150,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_local(mlt_scan_args a, mlt_sc
   pdl_trigger();
   const Where w = where(a, Shape<S>::kChunk);
   if (w.live == 0) return;  // k_grad_carry stops before it
-  stage_chunk<T, S>(a, g, w.k, w.begin, w.live, st);
+  stage_chunk<T, S, kVec>(a, g, w.k, pair_params<kChannels>(a, w.k), w.begin, w.live, st);
   const int lane = threadIdx.x & 3, ch = threadIdx.x >> 2;
   const bool in = ch < w.k.cn;
   const long long at = static_cast<long long>(w.k.c0 + ch) * a.states + lane * S;
@@ -226,18 +200,37 @@ __global__ void __launch_bounds__(256) k_grad_carry(mlt_scan_args a, mlt_scan_gr
   const float* sum = reinterpret_cast<const float*>(ws + p.off_sum) + b * p.chunks * a.dim + i / a.states;
   const float A = a.A[i] * kLog2E;
   float h = a.state != nullptr ? a.state[b * of_seq + i] : 0.0f;
-#pragma unroll 8
-  for (long long c = 0; c < chunks; ++c) {
-    const float end = e[c * of_seq], decay = ex2(A * sum[c * a.dim]);
-    e[c * of_seq] = h;
-    h = fmaf(decay, h, end);
+  // loads of eight chunks first: the stores go to the same memory
+  for (long long c0 = 0; c0 < chunks; c0 += 8) {
+    float end[8], d[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c0 + k < chunks) {
+        end[k] = e[(c0 + k) * of_seq];
+        d[k] = sum[(c0 + k) * a.dim];
+      }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c0 + k < chunks) {
+        e[(c0 + k) * of_seq] = h;
+        h = fmaf(ex2(A * d[k]), h, end[k]);
+      }
   }
   float r = g.g_state_out != nullptr ? g.g_state_out[b * of_seq + i] : 0.0f;
-#pragma unroll 8
-  for (long long c = chunks - 1; c >= 0; --c) {
-    const float own = q[c * of_seq], decay = ex2(A * sum[c * a.dim]);
-    q[c * of_seq] = r;
-    r = fmaf(decay, r, own);
+  for (long long c0 = chunks - 1; c0 >= 0; c0 -= 8) {
+    float own[8], d[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c0 - k >= 0) {
+        own[k] = q[(c0 - k) * of_seq];
+        d[k] = sum[(c0 - k) * a.dim];
+      }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c0 - k >= 0) {
+        q[(c0 - k) * of_seq] = r;
+        r = fmaf(ex2(A * d[k]), r, own[k]);
+      }
   }
 }
 
@@ -273,7 +266,7 @@ __device__ __forceinline__ int channel_sums(float (&v)[M]) {
   return first;
 }
 
-template <typename T, int S>
+template <typename T, int S, bool kVec>
 __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt_scan_grads g, GradPlan p,
                                                             unsigned char* ws) {
   using Sh = Shape<S>;
@@ -291,23 +284,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
   const int lane = threadIdx.x & 3, ch = threadIdx.x >> 2;
   const bool in = ch < k.cn;
   const long long at = static_cast<long long>(k.c0 + ch) * a.states + lane * S;
-  // a thread's channel and first position (then every kTimes-th) elsewhere
-  const int c = threadIdx.x % kChannels, tl = threadIdx.x / kChannels;
-  const bool cin = c < k.cn;
-  const int cc = k.c0 + c;
+  // a thread's two channels and first position (then every kGroups-th) elsewhere
+  const PairParams q = pair_params<kChannels>(a, k);
+  const int tl = threadIdx.x / kPairs, cc = k.c0 + q.c;
+  const bool cin = q.n > 0;
   T* gx = static_cast<T*>(g.x) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
   T* gdt = static_cast<T*>(g.dt) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
   T* gz = static_cast<T*>(g.z) + (static_cast<long long>(k.b) * a.length + w.begin) * a.dim + cc;
+  auto clear = [&](long long o) {
+    if (g.x != nullptr) store_two<T, kVec>(gx + o, q.n, dup2(0.0f));
+    if (g.dt != nullptr) store_two<T, kVec>(gdt + o, q.n, dup2(0.0f));
+    if (g.z != nullptr) store_two<T, kVec>(gz + o, q.n, dup2(0.0f));
+  };
   if (w.live == 0) {
     // past the sequence's end
-    const T zero = from_f32<T>(0.0f);
     if (cin)
-      for (int t = tl; t < positions; t += kTimes) {
-        const long long o = static_cast<long long>(t) * a.dim;
-        if (g.x != nullptr) gx[o] = zero;
-        if (g.dt != nullptr) gdt[o] = zero;
-        if (g.z != nullptr) gz[o] = zero;
-      }
+      for (int t = tl; t < positions; t += kGroups) clear(static_cast<long long>(t) * a.dim);
     if (w.chunk == 0 && in && g.state != nullptr) {
       Lane<S> r = lane_zero<S>();
       if (g.g_state_out != nullptr) r = lane_load<S>(g.g_state_out + k.b * of_seq + at, lane * S, a.states);
@@ -315,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     }
     return;
   }
-  stage_chunk<T, S>(a, g, k, w.begin, w.live, sm.in);
+  stage_chunk<T, S, kVec>(a, g, k, q, w.begin, w.live, sm.in);
   for (int i = threadIdx.x; i < kRing * kChannels; i += kThreads) sm.dv[i / kChannels][i % kChannels] = 0.0f;
   Lane<S> A = lane_zero<S>(), h = A, r = A, dA = A;
   if (in) {
@@ -349,21 +341,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     }
   }
 
-  const ChannelTaps taps = channel_taps(a, cc, cin);
-  const float skip = cin && a.skip != nullptr ? a.skip[cc] : 0.0f;
-  const float bias = cin && a.dt_bias != nullptr ? a.dt_bias[cc] : 0.0f;
+  F2 skip = dup2(0.0f);
+  if (cin && a.skip != nullptr) skip = f2(a.skip[cc], q.n > 1 ? a.skip[cc + 1] : 0.0f);
   const bool next_live = w.begin + Sh::kChunk < w.len;  // its convolution reads this chunk's last inputs
   const int halo = a.taps > 1 ? a.taps - 1 : 0;
-  float vec[kVecs] = {};
-  const T zero = from_f32<T>(0.0f);
+  F2 vec[kVecs];
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) vec[v] = dup2(0.0f);
   // parts past the sequence's end
   if (cin)
-    for (int t = parts * kSub + tl; t < positions; t += kTimes) {
-      const long long o = static_cast<long long>(t) * a.dim;
-      if (g.x != nullptr) gx[o] = zero;
-      if (g.dt != nullptr) gdt[o] = zero;
-      if (g.z != nullptr) gz[o] = zero;
-    }
+    for (int t = parts * kSub + tl; t < positions; t += kGroups) clear(static_cast<long long>(t) * a.dim);
 
 #pragma unroll 1
   for (int part = parts - 1; part >= 0; --part) {
@@ -453,65 +440,78 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
       }
     }
     // through the gate, softplus and the convolution's activation
-#pragma unroll
-    for (int i = 0; i < kSub / kTimes; ++i) {
-      const int t = i * kTimes + tl;  // of the part
-      const int ct = t0 + t;          // of the chunk
-      float dv = 0.0f;
-      if (cin && ct < w.live) {
-        const long long pos = w.begin + ct, o = static_cast<long long>(ct) * a.dim;
-        const float2 du = sm.in.du[ct][c];
-        const float gc = sm.in.gc[ct][c];
-        const float gp = sm.gp[t][c];
+    static_assert(kSub <= kGroups, "a thread has one position of a part");
+    const int ct = t0 + tl;  // position in the chunk
+    const long long o = static_cast<long long>(ct) * a.dim;
+    const bool mine = tl < kSub && cin;
+    if (mine) {
+      F2 dv = dup2(0.0f);
+      if (ct < w.live) {
+        RawRun<T, 1> raw;
+        Two<T> gy[1];
+        load_run<T, 1, kVec, true>(a, k, q, w.begin + ct, w.begin + w.live, raw);
+        load_gy<T, 1, kVec>(g, k, q, w.begin + ct, 1, gy);
+        const float4 in4 = *reinterpret_cast<const float4*>(&sm.in.du[ct][q.c]);
+        const F2 d = f2(in4.x, in4.z), u = f2(in4.y, in4.w);
+        auto two = [&](const float* p) {
+          const float2 v = *reinterpret_cast<const float2*>(p);
+          return f2(v.x, v.y);
+        };
+        const F2 gc = two(&sm.in.gc[ct][q.c]), gp = two(&sm.gp[tl][q.c]);
         if (g.z != nullptr) {
-          const float z = to_f32(static_cast<const T*>(a.z)[k.b * a.z_batch + pos * a.z_step + cc]);
-          const float go = to_f32(static_cast<const T*>(g.gy)[k.b * g.gy_batch + pos * g.gy_step + cc]);
-          const float sz = sigmoid(z);
-          gz[o] = from_f32<T>(go * (sm.y[t][c] + skip * du.y) * sz * fmaf(z, 1.0f - sz, 1.0f));
+          const F2 z = two_f32(raw.z[0]), sz = sigmoid2(z);
+          const F2 slope = mul2(sz, fma2(z, fma2(sz, dup2(-1.0f), dup2(1.0f)), dup2(1.0f)));
+          store_two<T, kVec>(gz + o, q.n, mul2(mul2(two_f32(gy[0]), fma2(skip, u, two(&sm.y[tl][q.c]))), slope));
         }
-        const float raw = to_f32(static_cast<const T*>(a.dt)[k.b * a.dt_batch + pos * a.dt_step + cc]) + bias;
-        const float graw = fmaf(gp, du.y, sm.ga[t][c] * (1.0f / kLog2E)) * sigmoid(raw);
-        if (g.dt != nullptr) gdt[o] = from_f32<T>(graw);
-        vec[kScanMaxTaps + 1] = fmaf(gc, du.y, vec[kScanMaxTaps + 1]);
-        vec[kScanMaxTaps + 2] += graw;
-        dv = fmaf(gp, du.x, gc * skip);
+        const F2 graw = mul2(fma2(gp, u, mul2(two(&sm.ga[tl][q.c]), dup2(1.0f / kLog2E))),
+                             sigmoid2(add2(two_f32(raw.dt[0]), q.bias)));
+        if (g.dt != nullptr) store_two<T, kVec>(gdt + o, q.n, graw);
+        vec[kScanMaxTaps + 1] = fma2(gc, u, vec[kScanMaxTaps + 1]);
+        vec[kScanMaxTaps + 2] = add2(graw, vec[kScanMaxTaps + 2]);
+        dv = fma2(gp, d, mul2(gc, skip));
         if (a.taps > 0) {
-          float x[kScanMaxTaps];
+          const F2 v = conv_run(a, q, raw, 0), sv = sigmoid2(v);
+          dv = mul2(dv, mul2(sv, fma2(v, fma2(sv, dup2(-1.0f), dup2(1.0f)), dup2(1.0f))));
 #pragma unroll
-          for (int j = 0; j < kScanMaxTaps; ++j) x[j] = j < a.taps ? input_at<T>(a, k.b, pos - j, cc) : 0.0f;
-          const float v = conv_of(a, taps, x), sv = sigmoid(v);
-          dv *= sv * fmaf(v, 1.0f - sv, 1.0f);
-#pragma unroll
-          for (int j = 0; j < kScanMaxTaps; ++j) vec[j] = fmaf(dv, x[j], vec[j]);
-          vec[kScanMaxTaps] += dv;
+          for (int j = 0; j < kScanMaxTaps; ++j)
+            if (j < a.taps) vec[j] = fma2(dv, two_f32(raw.x[kScanMaxTaps - 1 - j]), vec[j]);
+          vec[kScanMaxTaps] = add2(dv, vec[kScanMaxTaps]);
         }
-      } else if (cin && ct < positions) {
-        const long long o = static_cast<long long>(ct) * a.dim;
-        if (g.z != nullptr) gz[o] = zero;
-        if (g.dt != nullptr) gdt[o] = zero;
+      } else if (ct < positions) {
+        if (g.z != nullptr) store_two<T, kVec>(gz + o, q.n, dup2(0.0f));
+        if (g.dt != nullptr) store_two<T, kVec>(gdt + o, q.n, dup2(0.0f));
       }
-      sm.dv[ct % kRing][c] = dv;
-      if (halo > 0 && cin && ct < kHalo)
-        reinterpret_cast<float*>(ws + p.off_head)[(seq * kHalo + ct) * a.dim + cc] = dv;
+      float2 v;
+      un2(dv, v.x, v.y);
+      *reinterpret_cast<float2*>(&sm.dv[ct % kRing][q.c]) = v;
+      if (halo > 0 && ct < kHalo) {
+        float* head = reinterpret_cast<float*>(ws + p.off_head) + (seq * kHalo + ct) * a.dim + cc;
+        head[0] = v.x;
+        if (q.n > 1) head[1] = v.y;
+      }
     }
     __syncthreads();
     // x[t] meets weight j in v[t + j]
-    if (g.x != nullptr && cin) {
+    if (g.x != nullptr && mine && ct < positions) {
+      auto dv = [&](int j) {
+        const float2 v = *reinterpret_cast<const float2*>(&sm.dv[(ct + j) % kRing][q.c]);
+        return f2(v.x, v.y);
+      };
+      F2 d = dv(0);
+      if (a.taps > 0) {
+        d = mul2(d, q.w[0]);
 #pragma unroll
-      for (int i = 0; i < kSub / kTimes; ++i) {
-        const int ct = t0 + i * kTimes + tl;
-        if (ct >= positions) continue;
-        float d = sm.dv[ct % kRing][c];
-        if (a.taps > 0) {
-          d *= taps.w[0];
-#pragma unroll
-          for (int j = 1; j < kScanMaxTaps; ++j)
-            if (j < a.taps && ct + j < Sh::kChunk) d = fmaf(taps.w[j], sm.dv[(ct + j) % kRing][c], d);
-        }
-        if (next_live && ct >= Sh::kChunk - halo)
-          reinterpret_cast<float*>(ws + p.off_part)[(seq * kHalo + ct - (Sh::kChunk - halo)) * a.dim + cc] = d;
-        else
-          gx[static_cast<long long>(ct) * a.dim] = from_f32<T>(ct < w.live ? d : 0.0f);
+        for (int j = 1; j < kScanMaxTaps; ++j)
+          if (j < a.taps && ct + j < Sh::kChunk) d = fma2(q.w[j], dv(j), d);
+      }
+      if (next_live && ct >= Sh::kChunk - halo) {
+        float v0, v1;
+        un2(d, v0, v1);
+        float* part_x = reinterpret_cast<float*>(ws + p.off_part) + (seq * kHalo + ct - (Sh::kChunk - halo)) * a.dim + cc;
+        part_x[0] = v0;
+        if (q.n > 1) part_x[1] = v1;
+      } else {
+        store_two<T, kVec>(gx + o, q.n, ct < w.live ? d : dup2(0.0f));
       }
     }
   }
@@ -519,19 +519,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     lane_store<S>(reinterpret_cast<float*>(ws + p.off_A) + seq * of_seq + at, lane * S, a.states, dA);
     if (w.chunk == 0 && g.state != nullptr) lane_store<S>(g.state + k.b * of_seq + at, lane * S, a.states, r);
   }
-  // the channel's sums over the chunk: kTimes threads each, through the staging memory
+  // the channels' sums over the chunk: kGroups threads each, through the staging memory
   __syncthreads();
   float* red = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int v = 0; v < kVecs; ++v) red[(v * kTimes + tl) * kChannels + c] = vec[v];
+  for (int v = 0; v < kVecs; ++v) {
+    float2 f;
+    un2(vec[v], f.x, f.y);
+    *reinterpret_cast<float2*>(&red[(v * kGroups + tl) * kChannels + q.c]) = f;
+  }
   __syncthreads();
-  if (cin)
-    for (int v = tl; v < kVecs; v += kTimes) {
-      float sum = 0.0f;
+  for (int i = threadIdx.x; i < kVecs * kChannels; i += kThreads) {
+    const int v = i / kChannels, c = i % kChannels;
+    if (c >= k.cn) continue;
+    float sum = 0.0f;
 #pragma unroll
-      for (int q = 0; q < kTimes; ++q) sum += red[(v * kTimes + q) * kChannels + c];
-      reinterpret_cast<float*>(ws + p.off_vec)[(seq * kVecs + v) * a.dim + cc] = sum;
-    }
+    for (int e = 0; e < kGroups; ++e) sum += red[(v * kGroups + e) * kChannels + c];
+    reinterpret_cast<float*>(ws + p.off_vec)[(seq * kVecs + v) * a.dim + k.c0 + c] = sum;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -670,7 +675,7 @@ GradPlan grad_plan(const mlt_scan_args& a) {
   GradPlan p{};
   p.chunk = chunk_of(a.states);
   p.chunks = (a.length + p.chunk - 1) / p.chunk;
-  p.blocks = blocks_per_group(a);
+  p.blocks = blocks_per_group<kChannels>(a);
   const size_t seqs = static_cast<size_t>(a.batch) * static_cast<size_t>(p.chunks), dim = a.dim;
   size_t at = 0;
   auto take = [&](size_t floats) {
@@ -707,6 +712,9 @@ cudaError_t launch_scan_grad(const mlt_scan_args& a, const mlt_scan_grads& g, vo
   const GradPlan p = grad_plan(a);
   unsigned char* w = static_cast<unsigned char*>(ws);
   const long long of_seq = static_cast<long long>(a.dim) * a.states;
+  const size_t two = 2 * dtype_size(a.dtype);
+  const bool vec = pairs_ok(a) && aligned_to(g.gy, two) && g.gy_step % 2 == 0 && g.gy_batch % 2 == 0 &&
+                   aligned_to(g.x, two) && aligned_to(g.dt, two) && aligned_to(g.z, two);
   return with_dtype(a.dtype, [&](auto tag) {
     return with_states(a.states, [&](auto states) -> cudaError_t {
       using T = decltype(tag);
@@ -720,14 +728,14 @@ cudaError_t launch_scan_grad(const mlt_scan_args& a, const mlt_scan_grads& g, vo
       };
       cudaError_t e;
       if (p.chunks > 1) {
-        e = go(k_grad_local<T, S>, sizeof(Staged<S>));
+        e = vec ? go(k_grad_local<T, S, true>, sizeof(Staged<S>)) : go(k_grad_local<T, S, false>, sizeof(Staged<S>));
         if (e != cudaSuccess) return e;
         ++*launches;
         e = launch_pdl(k_grad_carry, dim3(static_cast<unsigned>((of_seq + 255) / 256), a.batch), dim3(256), 0, st, a, g,
                        p, w);
         if (e != cudaSuccess) return e;
       }
-      e = go(k_grad_chunk<T, S>, sizeof(Walk<S>));
+      e = vec ? go(k_grad_chunk<T, S, true>, sizeof(Walk<S>)) : go(k_grad_chunk<T, S, false>, sizeof(Walk<S>));
       if (e != cudaSuccess) return e;
       Finish f{};
       if (g.B != nullptr || g.C != nullptr)
