@@ -2,17 +2,23 @@
 // m largest of score + noise among the kept entries (with Gumbel noise, m draws
 // without replacement from the kept entries' softmax).
 //
-// Every cut keeps a prefix of the order (scaled score descending, index
-// ascending), so the kept set is {key > tau} and the first `ties` entries with
-// key = tau, where key is the scaled score as an ordered 32-bit integer.  tau is found by
-// radix selection: histograms over 11, 11 and 10 bits of the key, of entry counts for
-// top-k and of probability mass for top-p.  No row is sorted.  Masses are added
-// as 64-bit integers (fixed point), so neither atomics nor the split of a row
-// over CTAs changes a result.
+// Entries are ordered by a 59-bit composite: the scaled score as an ordered integer, then the
+// index, lower ones first.  No two are equal, and every cut keeps a prefix of this order, so
+// the kept set is {composite >= edge}.  An edge is found without sorting the row: one
+// pass counts entries (top-k) or adds their probability mass (top-p) in 2,048 bins, linear in
+// the score from the row's best down; the bin where the sum reaches its target is
+// collected (a few dozen entries as a rule, at most 4,096) and sorted, which settles
+// ties by index too.  A bin with more entries (equal or nearly equal scores) is first
+// narrowed down by digits of the composite.  The m draws are found the same way from
+// composites of score + noise.  Linear bins matter: the leading bits of a float put most
+// scores of a vocabulary in two dozen bins, and shared-memory atomics to one address
+// take turns (64 rows x 50,021: 177 us with leading bits and 64-bit atomics).
+// Masses are added as integers (fixed point), so neither atomics nor the split of a
+// row over CTAs changes a result.
 //
-// Bound: the scores are read from HBM once and from L1 or L2 by the later
-// passes; noise is read for kept entries only.  What is left beside the first
-// read is latency: a pass over a CTA's share and a barrier for each digit.
+// Bound: the scores are read from HBM once and from L1 or L2 by the later passes;
+// noise is read for kept entries only.  What is left beside the first read is latency: two
+// to five passes over a CTA's share and a barrier for each.
 //
 // Two kernels:
 //   k_sample_warp  rows of up to 512 entries and m <= 32: a warp per row, the row in
@@ -31,7 +37,7 @@ namespace {
 constexpr int kWarpMaxN = 512;
 constexpr int kWarpMaxM = 32;
 constexpr int kBins = 2048;
-constexpr int kList = 4096;  // composite keys that the last step sorts
+constexpr int kList = 4096;  // composites that are sorted
 constexpr int kIndexBits = 27;
 constexpr unsigned kNoTies = 0xFFFFFFFFu;
 
@@ -235,29 +241,30 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
 // ---------------------------------------------------------------------------
 // A team of CTAs per row
 // ---------------------------------------------------------------------------
+constexpr int kMaxTeam = 160;
+constexpr int kUses = 3;  // selections of a row: top-k, top-p, draws
+
 // Global memory of a team; teams of one CTA use none of it.
 struct TeamMem {
-  unsigned arrivals;  // barrier: CTAs arrived, over all barriers of the call (zeroed before the launch)
-  unsigned listed;    // entries in list
-  unsigned long long best;
-  float2 stats[160];       // each CTA's (max, sum of exp)
-  unsigned long long best_of[160];
-  unsigned ties[160];
-  unsigned long long hist[3][kBins];
-  unsigned long long list[kList];
+  unsigned arrivals;      // barrier: CTAs arrived, over all barriers of the call (zeroed before the launch)
+  unsigned listed[kUses]; // entries in list
+  float4 stats[kMaxTeam]; // each CTA's (max, sum of exp, min)
+  unsigned long long best[kMaxTeam];
+  unsigned long long mass[3][kBins];
+  unsigned count[3][kBins];
+  unsigned long long list[kUses][kList];
 };
-constexpr int kMaxTeam = 160;
 
 struct Shared {
-  unsigned long long hist[kBins];
   unsigned long long list[kList];
+  unsigned long long mass[kBins];  // merged
+  unsigned count[kBins];
+  unsigned lo[kBins], hi[kBins];   // of the CTA's masses
   unsigned long long warp_u64[32];
-  float warp_f[32][2];
-  unsigned warp_u32[32];
-  unsigned long long found_above, found_in;
-  unsigned found_bin;
-  unsigned count;
-  float top, z;
+  float warp_f[32][3];
+  unsigned long long above, edge;
+  unsigned in, bin, listed;
+  float top, z, low;
   int dead;
 };
 
@@ -299,114 +306,327 @@ __device__ bool team_sync(Team& t, Shared& sh) {
   return sh.dead == 0;
 }
 
-// f(i0, x, valid) for every 16-byte group of the row that the warp owns, in order of
-// index: x[v] is entry i0 + v where bit v of valid is set.  Called by whole warps.
-// A warp's groups are consecutive, so (CTA, warp, call, lane, v) is the order of indices.
+// f(i0, x, valid) for every 16-byte group of the row that the thread owns: x[v] is entry
+// i0 + v where bit v of valid is set.
 template <typename T, typename F>
 __device__ __forceinline__ void walk(const T* row, long long n, const Team& t, F f) {
   constexpr int V = 16 / sizeof(T);
-  constexpr int U = 4;
-  const int lane = threadIdx.x & 31;
-  const int warps = blockDim.x >> 5;
+  constexpr int U = sizeof(T) == 4 ? 4 : 2;
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
-  const long long groups = (skew + n + V - 1) / V;
-  const long long all = static_cast<long long>(t.size) * warps;
-  const long long per = ((groups + all - 1) / all + 31) / 32 * 32;
-  const long long begin = (static_cast<long long>(t.rank) * warps + (threadIdx.x >> 5)) * per;
-  const long long end = min(begin + per, groups);
+  const int groups = static_cast<int>((skew + n + V - 1) / V);  // n <= 2^27
+  const int stride = t.size * static_cast<int>(blockDim.x);
   const T* base = row - skew;  // 16-byte aligned; entries before `row` are not read
-  for (long long q0 = begin; q0 < end; q0 += 32 * U) {
+  for (int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x; q0 < groups; q0 += stride * U) {
     Pack<T, V> p[U];
-    unsigned valid[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long q = q0 + u * 32 + lane;
-      const long long i0 = q * V - skew;
-      valid[u] = 0;
-      if (q < end) {
-        if (i0 >= 0 && i0 + V <= n) {
-          p[u] = *reinterpret_cast<const Pack<T, V>*>(base + q * V);
-          valid[u] = (1u << V) - 1u;
-        } else {
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            if (i0 + v >= 0 && i0 + v < n) {
-              p[u].v[v] = row[i0 + v];
-              valid[u] |= 1u << v;
-            }
-        }
-      }
+      const int q = q0 + u * stride, i0 = q * V - skew;
+      if (q < groups && i0 >= 0 && i0 + V <= n)
+        p[u] = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (q0 + u * 32 >= end) break;
+      const int q = q0 + u * stride, i0 = q * V - skew;
+      if (q >= groups) break;
       float x[V];
+      unsigned valid = (1u << V) - 1u;
+      if (i0 >= 0 && i0 + V <= n) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) x[v] = (valid[u] >> v & 1u) ? to_f32(p[u].v[v]) : -INFINITY;
-      f((q0 + u * 32 + lane) * V - skew, x, valid[u]);
+        for (int v = 0; v < V; ++v) x[v] = to_f32(p[u].v[v]);
+      } else {
+        // a row's ends
+        valid = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          x[v] = -INFINITY;
+          if (i0 + v >= 0 && i0 + v < n) {
+            x[v] = to_f32(row[i0 + v]);
+            valid |= 1u << v;
+          }
+        }
+      }
+      f(i0, x, valid);
     }
   }
 }
 
-// The team's histogram of this stage into sh.hist; then the bin from the top where the
-// running sum first reaches `need` (found_bin, the sum above it and the bin's own).
-// found_in = 0 where the whole histogram does not reach it.
-__device__ bool team_find(Team& t, Shared& sh, unsigned long long need) {
-  if (t.size > 1) {
-    unsigned long long* h = t.g->hist[t.stage % 3];
-    unsigned long long* next = t.g->hist[(t.stage + 1) % 3];  // last read before the previous barrier
-    ++t.stage;
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
-      if (sh.hist[b] != 0) atomicAdd(&h[b], sh.hist[b]);
-      if (t.rank == 0) next[b] = 0;
-    }
-    if (!team_sync(t, sh)) return false;
-    for (int b = threadIdx.x; b < kBins; b += blockDim.x) sh.hist[b] = __ldcg(&h[b]);
-  }
-  if (threadIdx.x == 0) {
-    sh.found_in = 0;
-    sh.found_above = 0;
-    sh.found_bin = 0;
+__device__ __forceinline__ void clear_bins(Shared& sh, bool mass) {
+  __syncthreads();
+  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+    sh.count[b] = 0;
+    if (mass) sh.lo[b] = sh.hi[b] = 0;
   }
   __syncthreads();
-  // thread j sums `span` bins from the top down
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int span = kBins / blockDim.x;
-  unsigned long long mine = 0;
-  for (int j = 0; j < span; ++j) mine += sh.hist[kBins - 1 - (threadIdx.x * span + j)];
+}
+
+__device__ __forceinline__ void add_mass(Shared& sh, int b, unsigned long long w) {
+  // shared memory adds 32 bits at a time: the carry goes to the upper half
+  const unsigned lo = static_cast<unsigned>(w);
+  const unsigned old = atomicAdd(&sh.lo[b], lo);
+  const unsigned hi = static_cast<unsigned>(w >> 32) + (old + lo < old ? 1u : 0u);
+  if (hi != 0) atomicAdd(&sh.hi[b], hi);
+}
+
+// The team's bins of this stage, merged, in sh.count and (kMass) sh.mass.
+template <bool kMass>
+__device__ bool merge_bins(Team& t, Shared& sh) {
+  __syncthreads();
+  if (t.size == 1) {
+    if (kMass) {
+      for (int b = threadIdx.x; b < kBins; b += blockDim.x)
+        sh.mass[b] = (static_cast<unsigned long long>(sh.hi[b]) << 32) + sh.lo[b];
+      __syncthreads();
+    }
+    return true;
+  }
+  const int now = t.stage % 3, next = (t.stage + 1) % 3;  // `next` was last read before the previous barrier
+  ++t.stage;
+  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+    if (sh.count[b] != 0) {
+      atomicAdd(&t.g->count[now][b], sh.count[b]);
+      if (kMass) atomicAdd(&t.g->mass[now][b], (static_cast<unsigned long long>(sh.hi[b]) << 32) + sh.lo[b]);
+    }
+    if (t.rank == 0) {
+      t.g->count[next][b] = 0;
+      t.g->mass[next][b] = 0;
+    }
+  }
+  if (!team_sync(t, sh)) return false;
+  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+    sh.count[b] = __ldcg(&t.g->count[now][b]);
+    if (kMass) sh.mass[b] = __ldcg(&t.g->mass[now][b]);
+  }
+  __syncthreads();
+  return true;
+}
+
+// Sum over the CTA, on every thread.
+__device__ __forceinline__ unsigned long long block_sum(unsigned long long v, Shared& sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh.warp_u64[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v += sh.warp_u64[w];
+  return v;
+}
+__device__ __forceinline__ unsigned long long block_max(unsigned long long v, Shared& sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v = max(v, __shfl_xor_sync(~0u, v, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh.warp_u64[threadIdx.x >> 5] = v;
+  __syncthreads();
+  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v = max(v, sh.warp_u64[w]);
+  return v;
+}
+// The CTA's sum over lower threads; *all: over every thread.
+__device__ __forceinline__ unsigned long long block_below(unsigned long long mine, Shared& sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned long long v = mine;
 #pragma unroll
   for (int o = 1; o < 32; o *= 2) {
     const unsigned long long w = __shfl_up_sync(~0u, v, o);
     if (lane >= o) v += w;
   }
+  __syncthreads();
   if (lane == 31) sh.warp_u64[warp] = v;
   __syncthreads();
-  unsigned long long above = v - mine;
-  for (int w = 0; w < warps; ++w)
-    if (w < warp) above += sh.warp_u64[w];
+  v -= mine;
+  for (int w = 0; w < warp; ++w) v += sh.warp_u64[w];
+  return v;
+}
+
+// The first bin where the running sum of counts (or masses) reaches `need`: sh.bin, the sum
+// before it sh.above, its count sh.in (0 where the sum stays below).
+template <bool kMass>
+__device__ void find_bin(Shared& sh, unsigned long long need) {
+  const int span = kBins / blockDim.x, first = threadIdx.x * span;
+  unsigned long long mine = 0;
+  for (int j = 0; j < span; ++j) mine += kMass ? sh.mass[first + j] : sh.count[first + j];
+  unsigned long long above = block_below(mine, sh);
+  if (threadIdx.x == 0) sh.in = 0;
+  __syncthreads();
   if (above < need && above + mine >= need) {
     for (int j = 0; j < span; ++j) {
-      const int b = kBins - 1 - (threadIdx.x * span + j);
-      const unsigned long long c = sh.hist[b];
+      const unsigned long long c = kMass ? sh.mass[first + j] : sh.count[first + j];
       if (above + c >= need) {
-        sh.found_bin = b;
-        sh.found_above = above;
-        sh.found_in = c;
+        sh.bin = first + j;
+        sh.above = above;
+        sh.in = sh.count[first + j];
         break;
       }
       above += c;
     }
   }
   __syncthreads();
-  return true;
 }
 
-__device__ __forceinline__ void clear_hist(Shared& sh) {
+// Composite: larger key first, then the lower index.
+__device__ __forceinline__ unsigned long long composite(uint32_t key, int i) {
+  return (static_cast<unsigned long long>(key) << kIndexBits) |
+         static_cast<unsigned long long>((1 << kIndexBits) - 1 - i);
+}
+__device__ __forceinline__ int index_of(unsigned long long c) {
+  return (1 << kIndexBits) - 1 - static_cast<int>(c & ((1ull << kIndexBits) - 1));
+}
+__device__ __forceinline__ float score_of(unsigned long long c) {
+  return from_ordered(static_cast<uint32_t>(c >> kIndexBits));
+}
+
+// sh.list[0 .. n), descending.
+__device__ void sort_list(Shared& sh, unsigned n) {
+  unsigned width = 1;
+  while (width < n) width *= 2;
+  for (unsigned j = n + threadIdx.x; j < width; j += blockDim.x) sh.list[j] = 0;
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += blockDim.x) sh.hist[b] = 0;
+  for (unsigned k = 2; k <= width; k *= 2)
+    for (unsigned j = k / 2; j > 0; j /= 2) {
+      for (unsigned q = threadIdx.x; q < width / 2; q += blockDim.x) {
+        const unsigned i = 2 * q - (q & (j - 1)), o = i + j;  // the pairs that differ in bit j
+        const unsigned long long u = sh.list[i], w = sh.list[o];
+        if ((i & k) == 0 ? u < w : u > w) {
+          sh.list[i] = w;
+          sh.list[o] = u;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// Bins of a selection: linear from `from` down, kBins / range a unit; what lies outside goes to
+// the first or last one.  Rounded steps of it are monotone, so a bin is an interval.
+struct Bins {
+  float from, scale;
+  __device__ __forceinline__ int of(float v) const {
+    return static_cast<int>(fminf(fmaxf(__fmul_rn(__fsub_rn(from, v), scale), 0.0f), static_cast<float>(kBins - 1)));
+  }
+};
+
+// Selects from the entries that get() gives: get(i0, x, valid, key) -> bits of the entries that
+// take part, with their keys.
+//   kMass = false: the `need`-th largest composite; kAbove: the `need` largest
+//   kMass = true:  the composite at which the mass reaches `share` of all
+// Leaves a sorted list in sh.list.  *edge: the composite found (0: the entries do not
+// reach that far, all are kept).  kAbove: sh.listed entries, on rank 0 only, and no edge.
+template <typename T, bool kMass, bool kAbove, typename Get>
+__device__ bool select(const T* x, long long n, Team& t, Shared& sh, int use, Bins bins, unsigned long long need,
+                       float share, float top, float unit, Get get, unsigned long long* edge) {
+  constexpr int V = 16 / sizeof(T);
+  *edge = 0;
+  if (threadIdx.x == 0) sh.listed = 0;
+  clear_bins(sh, kMass);
+  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
+    uint32_t key[V];
+    const unsigned in = get(i0, xs, valid, key);
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (in >> e & 1u) {
+        const float v = from_ordered(key[e]);
+        const int b = bins.of(v);
+        atomicAdd(&sh.count[b], 1u);
+        if (kMass) add_mass(sh, b, fixed_weight(v, top, unit));
+      }
+  });
+  if (!merge_bins<kMass>(t, sh)) return false;
+  if (kMass) {
+    unsigned long long sum = 0;
+    for (int b = threadIdx.x; b < kBins; b += blockDim.x) sum += sh.mass[b];
+    sum = block_sum(sum, sh);
+    need = share > 0.0f ? max(1ull, static_cast<unsigned long long>(static_cast<double>(share) *
+                                                                    static_cast<double>(sum)))
+                        : 1ull;
+  }
+  find_bin<kMass>(sh, need);
+  int bin = static_cast<int>(sh.bin);
+  unsigned in = sh.in;
+  unsigned above_n = 0;  // kAbove: entries above the bin (the list takes them too)
+  if (in == 0) {
+    if (!kAbove) return true;
+    bin = kBins - 1;  // fewer than `need`: all of them
+  } else {
+    need -= sh.above;
+    if (kAbove) above_n = static_cast<unsigned>(sh.above);
+  }
+  // a bin that does not fit the list: digits of the composite
+  int shift = kIndexBits + 32;
+  unsigned long long prefix = 0;
+#pragma unroll 1
+  while (in + above_n > kList) {
+    const int bits = min(11, shift);
+    shift -= bits;
+    clear_bins(sh, kMass);
+    walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
+      uint32_t key[V];
+      const unsigned on = get(i0, xs, valid, key);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const unsigned long long c = composite(key[e], i0 + e);
+        if ((on >> e & 1u) && bins.of(from_ordered(key[e])) == bin && (c >> (shift + bits)) == prefix) {
+          const int b = kBins - 1 - static_cast<int>((c >> shift) & ((1u << bits) - 1u));
+          atomicAdd(&sh.count[b], 1u);
+          if (kMass) add_mass(sh, b, fixed_weight(from_ordered(key[e]), top, unit));
+        }
+      }
+    });
+    if (!merge_bins<kMass>(t, sh)) return false;
+    find_bin<kMass>(sh, need);
+    prefix = (prefix << bits) | static_cast<unsigned>(kBins - 1 - sh.bin);
+    in = sh.in;
+    need -= sh.above;
+    if (kAbove) above_n += static_cast<unsigned>(sh.above);
+  }
+  unsigned long long* list = t.size > 1 ? t.g->list[use] : sh.list;
+  unsigned* listed = t.size > 1 ? &t.g->listed[use] : &sh.listed;
+  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
+    uint32_t key[V];
+    const unsigned on = get(i0, xs, valid, key);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      if (!(on >> e & 1u)) continue;
+      const int b = bins.of(from_ordered(key[e]));
+      if (b > bin || (!kAbove && b != bin)) continue;
+      const unsigned long long c = composite(key[e], i0 + e), high = c >> shift;
+      if (b < bin || (kAbove ? high >= prefix : high == prefix)) {
+        const unsigned at = atomicAdd(listed, 1u);
+        if (at < kList) list[at] = c;
+      }
+    }
+  });
+  if (!team_sync(t, sh)) return false;
+  if (kAbove && t.rank != 0) return true;
+  if (t.size > 1) {
+    const unsigned have = min(__ldcg(listed), static_cast<unsigned>(kList));
+    for (unsigned j = threadIdx.x; j < have; j += blockDim.x) sh.list[j] = __ldcg(&list[j]);
+    if (threadIdx.x == 0) sh.listed = have;
+    __syncthreads();
+  }
+  const unsigned have = min(sh.listed, static_cast<unsigned>(kList));
+  sort_list(sh, have);
+  if (kAbove) return true;
+  if (!kMass) {
+    *edge = sh.list[need - 1];
+  } else {
+    // the entry at which the running mass reaches `need` (the last one if rounding leaves less)
+    const unsigned span = (have + blockDim.x - 1) / blockDim.x, first = threadIdx.x * span;
+    unsigned long long mine = 0;
+    for (unsigned j = first; j < min(first + span, have); ++j) mine += fixed_weight(score_of(sh.list[j]), top, unit);
+    unsigned long long at = block_below(mine, sh);
+    if (threadIdx.x == 0) sh.edge = sh.list[have - 1];
+    __syncthreads();
+    if (at < need && at + mine >= need)
+      for (unsigned j = first; j < min(first + span, have); ++j) {
+        at += fixed_weight(score_of(sh.list[j]), top, unit);
+        if (at >= need) {
+          sh.edge = sh.list[j];
+          break;
+        }
+      }
+    __syncthreads();
+    *edge = sh.edge;
+  }
   __syncthreads();
+  return true;
 }
 
 __device__ __forceinline__ void none_drawn(const SampleArgs& a, long long row, int from) {
@@ -416,53 +636,6 @@ __device__ __forceinline__ void none_drawn(const SampleArgs& a, long long row, i
   }
 }
 
-// Row state after the cuts.
-struct Cut {
-  uint32_t tau;       // kept: key > tau, and the first `ties` with key = tau
-  unsigned ties;
-  bool ranked;        // more than `ties` entries have key = tau
-  float top, log_min;
-  unsigned rank0;     // entries with key = tau before the warp's first group
-};
-
-// Bits of the group's entries that are kept; `seen` counts the ties passed so far.
-template <int V>
-__device__ __forceinline__ unsigned kept_bits(const Cut& c, const float (&s)[V], unsigned alive, unsigned& seen) {
-  unsigned keep = 0, eq = 0;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const uint32_t k = ordered(s[v]);
-    if (k > c.tau) keep |= 1u << v;
-    if (k == c.tau) eq |= 1u << v;
-  }
-  keep &= alive;
-  eq &= alive;
-  if (!c.ranked) {
-    keep |= eq;
-  } else if (__any_sync(~0u, eq != 0)) {
-    const unsigned mine = __popc(eq);
-    unsigned v = mine;
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const unsigned w = __shfl_up_sync(~0u, v, o);
-      if (lane >= o) v += w;
-    }
-    unsigned rank = seen + v - mine;
-    seen += __shfl_sync(~0u, v, 31);
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (eq >> e & 1u) {
-        if (rank < c.ties) keep |= 1u << e;
-        ++rank;
-      }
-  }
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (!(__fsub_rn(s[e], c.top) >= c.log_min)) keep &= ~(1u << e);
-  return keep;
-}
-
 template <int V>
 __device__ __forceinline__ unsigned scale_group(const float (&x)[V], unsigned valid, float inv, float (&s)[V]) {
   unsigned alive = 0;
@@ -470,26 +643,6 @@ __device__ __forceinline__ unsigned scale_group(const float (&x)[V], unsigned va
   for (int v = 0; v < V; ++v)
     if (scaled(x[v], inv, &s[v])) alive |= 1u << v;
   return alive & valid;
-}
-
-// Composite of a draw: larger key first, then the lower index.
-__device__ __forceinline__ unsigned long long composite(uint32_t key, long long i) {
-  return (static_cast<unsigned long long>(key) << kIndexBits) |
-         static_cast<unsigned long long>((1ll << kIndexBits) - 1 - i);
-}
-__device__ __forceinline__ long long index_of(unsigned long long c) {
-  return (1ll << kIndexBits) - 1 - static_cast<long long>(c & ((1ull << kIndexBits) - 1));
-}
-
-__device__ __forceinline__ unsigned long long block_max(unsigned long long v, Shared& sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 16; o > 0; o /= 2) v = max(v, __shfl_xor_sync(~0u, v, o));
-  __syncthreads();
-  if (lane == 0) sh.warp_u64[warp] = v;
-  __syncthreads();
-  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v = max(v, sh.warp_u64[w]);
-  return v;
 }
 
 __device__ __forceinline__ void join_stats(float& m, float& z, float m2, float z2) {
@@ -514,19 +667,22 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
     return true;
   }
-  // One draw from an uncut row needs no threshold: it is found in the first pass.
-  const bool direct = a.m == 1 && r.k == 0 && r.p >= 1.0f && r.log_min == -INFINITY;
+  // One draw from an uncut row needs no edge: it is found in the first pass.
+  const bool direct = (a.m == 1 || r.greedy) && r.k == 0 && r.p >= 1.0f && r.log_min == -INFINITY;
 
-  // Pass 1: maximum and sum of exponentials, each lane's own, then joined in a fixed order.
-  float top = -INFINITY, z = 0.0f;
+  // Pass 1: maximum, minimum and sum of exponentials, each lane's own, then joined in a fixed order.
+  float top = -INFINITY, z = 0.0f, low = INFINITY;
   unsigned long long best = 0;
-  walk(x, n, t, [&](long long i0, const float(&xs)[V], unsigned valid) {
+  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
     float s[V];
     const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
     float b = top;
 #pragma unroll
     for (int v = 0; v < V; ++v)
-      if (alive >> v & 1u) b = fmaxf(b, s[v]);
+      if (alive >> v & 1u) {
+        b = fmaxf(b, s[v]);
+        low = fminf(low, s[v]);
+      }
     if (b > top) {
       z *= __expf(top - b);
       top = b;
@@ -542,39 +698,68 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
   });
 #pragma unroll
-  for (int o = 16; o > 0; o /= 2) join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
+  for (int o = 16; o > 0; o /= 2) {
+    join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
+    low = fminf(low, __shfl_xor_sync(~0u, low, o));
+  }
   if (lane == 0) {
     sh.warp_f[warp][0] = top;
     sh.warp_f[warp][1] = z;
+    sh.warp_f[warp][2] = low;
   }
   if (direct) best = block_max(best, sh);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < warps; ++w) join_stats(top, z, sh.warp_f[w][0], sh.warp_f[w][1]);
-    sh.top = top;
-    sh.z = z;
-    if (t.size > 1) {
-      t.g->stats[t.rank] = make_float2(top, z);
-      t.g->best_of[t.rank] = best;
+  if (warp == 0) {
+    // one warp joins, by a tree too: its shape is fixed
+    top = lane < warps ? sh.warp_f[lane][0] : -INFINITY;
+    z = lane < warps ? sh.warp_f[lane][1] : 0.0f;
+    low = lane < warps ? sh.warp_f[lane][2] : INFINITY;
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+      join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
+      low = fminf(low, __shfl_xor_sync(~0u, low, o));
+    }
+    if (lane == 0) {
+      sh.top = top;
+      sh.z = z;
+      sh.low = low;
+      if (t.size > 1) {
+        t.g->stats[t.rank] = make_float4(top, z, low, 0.0f);
+        t.g->best[t.rank] = best;
+      }
     }
   }
   if (t.size > 1) {
     if (t.rank == 0) {
-      for (int b = threadIdx.x; b < kBins; b += blockDim.x) t.g->hist[t.stage % 3][b] = 0;
-      if (threadIdx.x == 0) t.g->listed = 0;
+      for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+        t.g->count[t.stage % 3][b] = 0;
+        t.g->mass[t.stage % 3][b] = 0;
+      }
+      if (threadIdx.x < kUses) t.g->listed[threadIdx.x] = 0;
     }
     if (!team_sync(t, sh)) return false;
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
       top = -INFINITY;
       z = 0.0f;
+      low = INFINITY;
       best = 0;
-      for (int c = 0; c < t.size; ++c) {
-        const float2 q = __ldcg(&t.g->stats[c]);
+      for (int c = lane; c < t.size; c += 32) {
+        const float4 q = __ldcg(&t.g->stats[c]);
         join_stats(top, z, q.x, q.y);
-        best = max(best, __ldcg(&t.g->best_of[c]));
+        low = fminf(low, q.z);
+        best = max(best, __ldcg(&t.g->best[c]));
       }
-      sh.top = top;
-      sh.z = z;
+#pragma unroll
+      for (int o = 16; o > 0; o /= 2) {
+        join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
+        low = fminf(low, __shfl_xor_sync(~0u, low, o));
+        best = max(best, __shfl_xor_sync(~0u, best, o));
+      }
+      if (lane == 0) {
+        sh.top = top;
+        sh.z = z;
+        sh.low = low;
+      }
     }
   }
   __syncthreads();
@@ -583,177 +768,80 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
   if (direct || top == -INFINITY) {
     if (t.rank == 0) {
       if (threadIdx.x == 0 && top != -INFINITY) {
-        const long long i = index_of(best);
+        const int i = index_of(best);
         float s;
         scaled(to_f32(x[i]), r.inv, &s);
-        a.out_index[row] = i;
-        a.out_logprob[row] = r.greedy ? 0.0f : __fsub_rn(s, top) - logf(z);
+        a.out_index[row * a.m] = i;
+        a.out_logprob[row * a.m] = r.greedy ? 0.0f : __fsub_rn(s, top) - logf(z);
       }
-      if (top == -INFINITY) none_drawn(a, row, 0);
+      none_drawn(a, row, top != -INFINITY ? 1 : 0);
     }
     return true;
   }
 
-  Cut cut;
-  cut.tau = 0;
-  cut.ties = kNoTies;
-  cut.ranked = false;
-  cut.top = top;
-  cut.log_min = r.log_min;
-  cut.rank0 = 0;
-
-  // top-k: three digits of the key, counted.
-  if (r.k != 0) {
-    uint32_t prefix = 0;
-    unsigned long long need = r.k;
-    bool all = false;
-#pragma unroll 1
-    for (int level = 0; level < 3 && !all; ++level) {
-      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-      clear_hist(sh);
-      walk(x, n, t, [&](long long, const float(&xs)[V], unsigned valid) {
-        float s[V];
-        const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
+  // The cuts.  Scores more than 40 below the best share the last bin: their mass is
+  // nothing, and only a top-k of a very peaked row looks there.
+  const float range = fminf(__fsub_rn(top, sh.low), 40.0f);
+  const Bins by_score = {top, range > 0.0f ? fminf(static_cast<float>(kBins - 1) / range, 1e30f) : 0.0f};
+  unsigned long long edge = 0;
+  // an entry's composite is at or above the edge
+  auto kept = [&](uint32_t key, int i) {
+    const uint32_t ek = static_cast<uint32_t>(edge >> kIndexBits);
+    return key > ek || (key == ek && i <= index_of(edge));
+  };
+  auto scores = [&](int i0, const float(&xs)[V], unsigned valid, uint32_t(&key)[V]) {
+    float s[V];
+    unsigned in = scale_group<V>(xs, valid, r.inv, s);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const uint32_t k = ordered(s[v]);
-          if ((alive >> v & 1u) && (level == 0 || (k >> (shift + bits)) == prefix))
-            atomicAdd(reinterpret_cast<unsigned*>(&sh.hist[(k >> shift) & ((1u << bits) - 1u)]), 1u);
-        }
-      });
-      if (!team_find(t, sh, need)) return false;
-      if (sh.found_in == 0) {
-        all = true;  // fewer than k entries can be drawn
-      } else {
-        prefix = (prefix << bits) | sh.found_bin;
-        need -= sh.found_above;
-        cut.ranked = sh.found_in > need;
-      }
+    for (int v = 0; v < V; ++v) {
+      key[v] = ordered(s[v]);
+      if (!kept(key[v], i0 + v)) in &= ~(1u << v);
     }
-    if (!all) {
-      cut.tau = prefix;
-      cut.ties = static_cast<unsigned>(need);
-    } else {
-      cut.ranked = false;
-    }
+    return in;
+  };
+  unsigned long long found;
+  if (r.k != 0) {
+    if (!select<T, false, false>(x, n, t, sh, 0, by_score, r.k, 0.0f, top, 0.0f, scores, &found)) return false;
+    edge = found;
   }
-
-  // top-p: the same digits, weighed.  Of the ties at the top-k cut only the kept number counts.
   if (r.p < 1.0f) {
     int log_n = 0;
     while ((1ll << log_n) < n) ++log_n;
     const float unit = static_cast<float>(1ull << (62 - log_n));
-    uint32_t prefix = 0;
-    unsigned long long need = 0;
-    bool all = false;
-#pragma unroll 1
-    for (int level = 0; level < 3 && !all; ++level) {
-      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-      clear_hist(sh);
-      auto add = [&](uint32_t k, unsigned long long times) {
-        if (level == 0 || (k >> (shift + bits)) == prefix)
-          atomicAdd(&sh.hist[(k >> shift) & ((1u << bits) - 1u)], times * fixed_weight(from_ordered(k), top, unit));
-      };
-      walk(x, n, t, [&](long long, const float(&xs)[V], unsigned valid) {
-        float s[V];
-        const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const uint32_t k = ordered(s[v]);
-          if ((alive >> v & 1u) && (k > cut.tau || (k == cut.tau && cut.ties == kNoTies))) add(k, 1);
-        }
-      });
-      if (cut.ties != kNoTies && t.rank == 0 && threadIdx.x == 0) add(cut.tau, cut.ties);
-      __syncthreads();
-      if (level == 0) {
-        // the target is a share of what the first histogram holds
-        if (!team_find(t, sh, ~0ull)) return false;
-        unsigned long long sum = 0;
-        for (int b = threadIdx.x; b < kBins; b += blockDim.x) sum += sh.hist[b];
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-        if (lane == 0) sh.warp_u64[warp] = sum;
-        __syncthreads();
-        sum = 0;
-        for (int w = 0; w < warps; ++w) sum += sh.warp_u64[w];
-        need = r.p > 0.0f ? max(1ull, static_cast<unsigned long long>(static_cast<double>(r.p) *
-                                                                      static_cast<double>(sum)))
-                          : 1ull;
-        Team one = t;  // the histogram is whole by now
-        one.size = 1;
-        team_find(one, sh, need);
-      } else if (!team_find(t, sh, need)) {
-        return false;
-      }
-      if (sh.found_in == 0) {
-        all = true;
-      } else {
-        prefix = (prefix << bits) | sh.found_bin;
-        need -= sh.found_above;
-      }
-    }
-    if (!all) {
-      const unsigned long long each = max(1ull, fixed_weight(from_ordered(prefix), top, unit));
-      const unsigned long long ties = (need + each - 1) / each, held = sh.found_in / each;
-      if (prefix == cut.tau && cut.ties != kNoTies) {
-        cut.ranked = cut.ranked || ties < cut.ties;
-        cut.ties = static_cast<unsigned>(min(static_cast<unsigned long long>(cut.ties), ties));
-      } else {
-        cut.ranked = held > ties;
-        cut.tau = prefix;
-        cut.ties = static_cast<unsigned>(ties);
-      }
-    }
+    if (!select<T, true, false>(x, n, t, sh, 1, by_score, 0, r.p, top, unit, scores, &found)) return false;
+    edge = max(edge, found);
   }
 
-  // Where not all ties are kept, each warp needs the number of ties before its groups.
-  if (cut.ranked) {
-    unsigned mine = 0;
-    walk(x, n, t, [&](long long, const float(&xs)[V], unsigned valid) {
-      float s[V];
-      const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
+  // Bits of the group's kept entries and their draw keys.
+  auto draws = [&](int i0, const float(&xs)[V], unsigned valid, uint32_t(&key)[V]) {
+    float s[V];
+    unsigned in = scale_group<V>(xs, valid, r.inv, s);
 #pragma unroll
-      for (int v = 0; v < V; ++v) mine += (alive >> v & 1u) && ordered(s[v]) == cut.tau;
-    });
-    mine = __reduce_add_sync(~0u, mine);
-    __syncthreads();
-    if (lane == 0) sh.warp_u32[warp] = mine;
-    __syncthreads();
-    unsigned before = 0, total = 0;
-    for (int w = 0; w < warps; ++w) {
-      if (w < warp) before += sh.warp_u32[w];
-      total += sh.warp_u32[w];
+    for (int v = 0; v < V; ++v) {
+      if (!kept(ordered(s[v]), i0 + v) || !(__fsub_rn(s[v], top) >= r.log_min)) in &= ~(1u << v);
+      key[v] = in >> v & 1u ? draw_key(s[v], noise[i0 + v]) : 0;
     }
-    if (t.size > 1) {
-      if (threadIdx.x == 0) t.g->ties[t.rank] = total;
-      if (!team_sync(t, sh)) return false;
-      for (int c = 0; c < t.rank; ++c) before += __ldcg(&t.g->ties[c]);
-    }
-    cut.rank0 = before;
-  }
-
+    return in;
+  };
   const float logz = logf(z);
   if (a.m == 1) {
     best = 0;
-    unsigned seen = cut.rank0;
-    walk(x, n, t, [&](long long i0, const float(&xs)[V], unsigned valid) {
-      float s[V];
-      const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
-      const unsigned keep = kept_bits<V>(cut, s, alive, seen);
-      if (keep == 0) return;
+    walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
+      uint32_t key[V];
+      const unsigned in = draws(i0, xs, valid, key);
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (keep >> v & 1u) best = max(best, composite(draw_key(s[v], noise[i0 + v]), i0 + v));
+        if (in >> v & 1u) best = max(best, composite(key[v], i0 + v));
     });
     best = block_max(best, sh);
     if (t.size > 1) {
-      if (threadIdx.x == 0) t.g->best_of[t.rank] = best;
+      if (threadIdx.x == 0) t.g->best[t.rank] = best;
       if (!team_sync(t, sh)) return false;
       if (t.rank == 0 && threadIdx.x == 0)
-        for (int c = 0; c < t.size; ++c) best = max(best, __ldcg(&t.g->best_of[c]));
+        for (int c = 0; c < t.size; ++c) best = max(best, __ldcg(&t.g->best[c]));
     }
     if (t.rank == 0 && threadIdx.x == 0) {
-      const long long i = index_of(best);  // the best entry is always kept
+      const int i = index_of(best);  // no cut drops the best entry
       float s;
       scaled(to_f32(x[i]), r.inv, &s);
       a.out_index[row] = i;
@@ -761,96 +849,20 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
     return true;
   }
-
-  // The m largest composites: histograms narrow them down until what lies at or above
-  // the edge fits the list.  Composites differ, so the last digit leaves exactly m.
-  unsigned long long edge = 0, need = a.m, above = 0;
-  int shift = kIndexBits + 32;
-  bool enough = false;
-#pragma unroll 1
-  while (!enough && shift > 0) {
-    const int bits = min(11, shift);
-    const unsigned long long high = edge >> shift;
-    shift -= bits;
-    clear_hist(sh);
-    unsigned seen = cut.rank0;
-    walk(x, n, t, [&](long long i0, const float(&xs)[V], unsigned valid) {
-      float s[V];
-      const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
-      const unsigned keep = r.greedy ? alive : kept_bits<V>(cut, s, alive, seen);
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (keep >> v & 1u) {
-          const unsigned long long c =
-              composite(r.greedy ? ordered(s[v]) : draw_key(s[v], noise[i0 + v]), i0 + v);
-          if ((c >> (shift + bits)) == high)
-            atomicAdd(reinterpret_cast<unsigned*>(&sh.hist[(c >> shift) & ((1u << bits) - 1u)]), 1u);
-        }
-    });
-    if (!team_find(t, sh, need)) return false;
-    if (sh.found_in == 0) {
-      enough = true;  // fewer than m: all at or above the edge (only at the first digit)
-    } else {
-      edge |= static_cast<unsigned long long>(sh.found_bin) << shift;
-      need -= sh.found_above;
-      above += sh.found_above;
-      enough = above + sh.found_in <= kList;
-    }
-  }
-  if (threadIdx.x == 0) sh.count = 0;
-  __syncthreads();
-  unsigned seen = cut.rank0;
-  unsigned long long* list = t.size > 1 ? t.g->list : sh.list;
-  unsigned* count = t.size > 1 ? &t.g->listed : &sh.count;
-  walk(x, n, t, [&](long long i0, const float(&xs)[V], unsigned valid) {
-    float s[V];
-    const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
-    const unsigned keep = r.greedy ? alive : kept_bits<V>(cut, s, alive, seen);
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (keep >> v & 1u) {
-        const unsigned long long c = composite(r.greedy ? ordered(s[v]) : draw_key(s[v], noise[i0 + v]), i0 + v);
-        if (c >= edge) {
-          const unsigned at = atomicAdd(count, 1u);
-          if (at < kList) list[at] = c;
-        }
-      }
-  });
-  if (!team_sync(t, sh)) return false;
+  // Gumbel noise puts the largest keys within a few units of the best score, and ln n above it.
+  const Bins by_key = {top + 24.0f, static_cast<float>(kBins) / 48.0f};
+  if (!select<T, false, true>(x, n, t, sh, 2, by_key, a.m, 0.0f, top, 0.0f, draws, &found)) return false;
   if (t.rank != 0) return true;
-  unsigned total = t.size > 1 ? __ldcg(count) : sh.count;
-  if (total > kList) total = kList;
-  unsigned width = 1;
-  while (width < total) width *= 2;
-  for (unsigned j = threadIdx.x; j < width; j += blockDim.x) {
-    if (j >= total) sh.list[j] = 0;
-    else if (t.size > 1) sh.list[j] = __ldcg(&t.g->list[j]);
-  }
-  __syncthreads();
-  for (unsigned k = 2; k <= width; k *= 2)
-    for (unsigned j = k / 2; j > 0; j /= 2) {
-      for (unsigned q = threadIdx.x; q < width; q += blockDim.x) {
-        const unsigned o = q ^ j;
-        if (o > q) {
-          const unsigned long long u = sh.list[q], w = sh.list[o];
-          const bool desc = (q & k) == 0;
-          if (desc ? u < w : u > w) {
-            sh.list[q] = w;
-            sh.list[o] = u;
-          }
-        }
-      }
-      __syncthreads();
-    }
-  const int drawn = r.greedy ? 1 : static_cast<int>(min(total, static_cast<unsigned>(a.m)));
+  const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
   for (int j = threadIdx.x; j < drawn; j += blockDim.x) {
-    const long long i = index_of(sh.list[j]);
+    const int i = index_of(sh.list[j]);
     float s;
     scaled(to_f32(x[i]), r.inv, &s);
     a.out_index[row * a.m + j] = i;
-    a.out_logprob[row * a.m + j] = r.greedy ? 0.0f : __fsub_rn(s, top) - logz;
+    a.out_logprob[row * a.m + j] = __fsub_rn(s, top) - logz;
   }
   none_drawn(a, row, drawn);
+  __syncthreads();
   return true;
 }
 
@@ -865,12 +877,7 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
   t.err = a.err;
   t.barriers = 0;
   t.stage = 0;
-  const long long teams = gridDim.x / team_size;
-  for (long long row = blockIdx.x / team_size; row < a.rows; row += teams) {
-    if (!sample_row<T>(a, t, sh, row)) return;
-    // the next row's first writes to the team's memory come after all reads of this row's
-    if (row + teams < a.rows && !team_sync(t, sh)) return;
-  }
+  sample_row<T>(a, t, sh, blockIdx.x / team_size);
 }
 
 bool by_warp(long long n, int m) { return n <= kWarpMaxN && m <= kWarpMaxM; }
