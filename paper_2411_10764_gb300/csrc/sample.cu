@@ -41,9 +41,9 @@ constexpr int kList = 4096;  // composites that are sorted
 constexpr int kIndexBits = 27;
 constexpr unsigned kNoTies = 0xFFFFFFFFu;
 
-// Order-preserving map of finite floats (no -0: the caller adds +0).
+// Order-preserving map of finite floats; -0 as +0.
 __device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t b = __float_as_uint(v);
+  const uint32_t b = __float_as_uint(v + 0.0f);
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t k) {
@@ -51,15 +51,15 @@ __device__ __forceinline__ float from_ordered(uint32_t k) {
 }
 __device__ __forceinline__ float clamp_finite(float v) { return fminf(fmaxf(v, -FLT_MAX), FLT_MAX); }
 
-// Scaled score; false where the entry can never be drawn.
-__device__ __forceinline__ bool scaled(float x, float inv, float* s) {
-  const float v = __fmul_rn(x, inv);
-  *s = clamp_finite(v) + 0.0f;
-  return v == v && x != -INFINITY;
+// Scaled score, finite; -infinity where the entry can never be drawn.
+__device__ __forceinline__ float scaled(float x, float inv) {
+  const float s = clamp_finite(__fmul_rn(x, inv));
+  return x > -INFINITY ? s : -INFINITY;
 }
-__device__ __forceinline__ uint32_t draw_key(float s, float noise) {
+// s + noise, finite (NaN: the lowest).
+__device__ __forceinline__ float draw_value(float s, float noise) {
   const float k = __fadd_rn(s, noise);
-  return ordered(k == k ? clamp_finite(k) + 0.0f : -FLT_MAX);
+  return clamp_finite(k);  // fmaxf takes the number where the other is NaN
 }
 
 struct Rule {
@@ -74,7 +74,7 @@ __device__ __forceinline__ Rule read_rule(const mlt_sample_rule& q, long long n)
   Rule r;
   r.bad = !(q.temperature >= 0.0f) || isinf(q.temperature) || isnan(q.top_p) || isnan(q.min_p);
   r.greedy = q.temperature == 0.0f;
-  r.inv = r.greedy ? 1.0f : __fdiv_rn(1.0f, q.temperature);
+  r.inv = r.greedy ? 1.0f : fminf(__fdiv_rn(1.0f, q.temperature), FLT_MAX);
   r.k = r.greedy || q.top_k <= 0 || q.top_k >= n ? 0u : static_cast<unsigned>(q.top_k);
   r.p = r.greedy ? 1.0f : q.top_p;
   r.log_min = r.greedy || q.min_p <= 0.0f ? -INFINITY : fminf(logf(q.min_p), 0.0f);  // the best stays
@@ -113,9 +113,8 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = j * 32 + lane;
-    s[j] = 0.0f;
-    key[j] = 0;
-    if (i < n && scaled(to_f32(x[i]), r.inv, &s[j])) key[j] = ordered(s[j]);
+    s[j] = i < n ? scaled(to_f32(x[i]), r.inv) : -INFINITY;
+    key[j] = s[j] > -INFINITY ? ordered(s[j]) : 0;
     best = max(best, key[j]);
   }
   best = __reduce_max_sync(~0u, best);
@@ -203,7 +202,7 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
                       __fsub_rn(s[j], top) >= r.log_min;
     seen += __popc(eq);
     draw[j] = 0;
-    if (keep) draw[j] = r.greedy ? key[j] : draw_key(s[j], noise[j * 32 + lane]);
+    if (keep) draw[j] = r.greedy ? key[j] : ordered(draw_value(s[j], noise[j * 32 + lane]));
   }
   const float logz = logf(z);
   for (int d = 0; d < a.m; ++d) {
@@ -242,28 +241,34 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
 // A team of CTAs per row
 // ---------------------------------------------------------------------------
 constexpr int kMaxTeam = 160;
-constexpr int kUses = 3;  // selections of a row: top-k, top-p, draws
+constexpr int kUses = 4;  // selections of a row: top-k, top-p, draws; candidates for the top-k
+constexpr int kLarge = 16384;  // candidates that one CTA finishes without the team
 
 // Global memory of a team; teams of one CTA use none of it.
 struct TeamMem {
   unsigned arrivals;      // barrier: CTAs arrived, over all barriers of the call (zeroed before the launch)
-  unsigned listed[kUses]; // entries in list
+  unsigned listed[kUses]; // entries in list (the last: in large)
   float4 stats[kMaxTeam]; // each CTA's (max, sum of exp, min)
   unsigned long long best[kMaxTeam];
   unsigned long long mass[3][kBins];
   unsigned count[3][kBins];
   unsigned long long list[kUses][kList];
+  unsigned long long large[kLarge];
 };
 
 struct Shared {
-  unsigned long long list[kList];
-  unsigned long long mass[kBins];  // merged
+  union {  // a list is made once its bin is found
+    unsigned long long list[kList];
+    struct {
+      unsigned long long mass[kBins];  // merged
+      unsigned lo[kBins], hi[kBins];   // of the CTA's masses
+    };
+  };
   unsigned count[kBins];
-  unsigned lo[kBins], hi[kBins];   // of the CTA's masses
   unsigned long long warp_u64[32];
   float warp_f[32][3];
-  unsigned long long above, edge;
-  unsigned in, bin, listed;
+  unsigned long long above;
+  unsigned in, bin, listed, found;
   float top, z, low;
   int dead;
 };
@@ -274,6 +279,7 @@ struct Team {
   int size, rank;
   unsigned barriers;
   int stage;  // histograms used so far
+  int bins;   // in use: a multiple of the CTA's threads, at most kBins
 };
 
 // All CTAs of the team; false where the wait gave up (then on every thread of the CTA).
@@ -306,53 +312,82 @@ __device__ bool team_sync(Team& t, Shared& sh) {
   return sh.dead == 0;
 }
 
-// f(i0, x, valid) for every 16-byte group of the row that the thread owns: x[v] is entry
-// i0 + v where bit v of valid is set.
-template <typename T, typename F>
-__device__ __forceinline__ void walk(const T* row, long long n, const Team& t, F f) {
-  constexpr int V = 16 / sizeof(T);
-  constexpr int U = sizeof(T) == 4 ? 4 : 2;
-  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
-  const int groups = static_cast<int>((skew + n + V - 1) / V);  // n <= 2^27
-  const int stride = t.size * static_cast<int>(blockDim.x);
-  const T* base = row - skew;  // 16-byte aligned; entries before `row` are not read
-  for (int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x; q0 < groups; q0 += stride * U) {
-    Pack<T, V> p[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int q = q0 + u * stride, i0 = q * V - skew;
-      if (q < groups && i0 >= 0 && i0 + V <= n)
-        p[u] = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int q = q0 + u * stride, i0 = q * V - skew;
-      if (q >= groups) break;
-      float x[V];
-      unsigned valid = (1u << V) - 1u;
-      if (i0 >= 0 && i0 + V <= n) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = to_f32(p[u].v[v]);
-      } else {
-        // a row's ends
-        valid = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          x[v] = -INFINITY;
-          if (i0 + v >= 0 && i0 + v < n) {
-            x[v] = to_f32(row[i0 + v]);
-            valid |= 1u << v;
-          }
-        }
-      }
-      f(i0, x, valid);
-    }
-  }
+// Composite: larger key first, then the lower index.
+__device__ __forceinline__ unsigned long long composite(uint32_t key, int i) {
+  return (static_cast<unsigned long long>(key) << kIndexBits) |
+         static_cast<unsigned long long>((1 << kIndexBits) - 1 - i);
+}
+__device__ __forceinline__ int index_of(unsigned long long c) {
+  return (1 << kIndexBits) - 1 - static_cast<int>(c & ((1ull << kIndexBits) - 1));
+}
+__device__ __forceinline__ float score_of(unsigned long long c) {
+  return from_ordered(static_cast<uint32_t>(c >> kIndexBits));
 }
 
-__device__ __forceinline__ void clear_bins(Shared& sh, bool mass) {
+// A row of scores.  walk: f(i0, s) for every 16-byte group that the thread owns, the same ones
+// at each walk: s[v] is the scaled score of entry i0 + v, -infinity where it cannot be
+// drawn or is outside the row.  U groups are loaded at once.
+template <typename T>
+struct Row {
+  static constexpr int V = 16 / sizeof(T);
+  const T* row;
+  int n;
+  float inv;
+
+  __device__ __forceinline__ float score(int i) const { return scaled(to_f32(row[i]), inv); }
+  template <int U, typename F>
+  __device__ __forceinline__ void walk(const Team& t, F f) const {
+    const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
+    const int groups = (skew + n + V - 1) / V;
+    const int stride = t.size * static_cast<int>(blockDim.x), last = n - V;
+    const T* base = row - skew;  // 16-byte aligned; entries before `row` are not read
+#pragma unroll 1
+    for (int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x; q0 < groups; q0 += stride * U) {
+      Pack<T, V> p[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int q = q0 + u * stride, i0 = q * V - skew;
+        if (i0 >= 0 && i0 <= last) p[u] = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int q = q0 + u * stride, i0 = q * V - skew;
+        if (q >= groups) break;
+        float s[V];
+        if (i0 >= 0 && i0 <= last) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) s[v] = scaled(to_f32(p[u].v[v]), inv);
+        } else {
+          // a row's ends
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            s[v] = i0 + v >= 0 && i0 + v < n ? scaled(to_f32(row[i0 + v]), inv) : -INFINITY;
+        }
+        f(i0, s);
+      }
+    }
+  }
+};
+// Candidates that were collected from a row, as composites; walked by one CTA.
+struct Candidates {
+  static constexpr int V = 1;
+  const unsigned long long* list;
+  int n;
+
+  template <int U, typename F>
+  __device__ __forceinline__ void walk(const Team&, F f) const {
+#pragma unroll 1
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+      const unsigned long long c = __ldcg(&list[j]);
+      float s[1] = {score_of(c)};
+      f(index_of(c), s);
+    }
+  }
+};
+
+__device__ __forceinline__ void clear_bins(const Team& t, Shared& sh, bool mass) {
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+  for (int b = threadIdx.x; b < t.bins; b += blockDim.x) {
     sh.count[b] = 0;
     if (mass) sh.lo[b] = sh.hi[b] = 0;
   }
@@ -373,7 +408,7 @@ __device__ bool merge_bins(Team& t, Shared& sh) {
   __syncthreads();
   if (t.size == 1) {
     if (kMass) {
-      for (int b = threadIdx.x; b < kBins; b += blockDim.x)
+      for (int b = threadIdx.x; b < t.bins; b += blockDim.x)
         sh.mass[b] = (static_cast<unsigned long long>(sh.hi[b]) << 32) + sh.lo[b];
       __syncthreads();
     }
@@ -381,7 +416,7 @@ __device__ bool merge_bins(Team& t, Shared& sh) {
   }
   const int now = t.stage % 3, next = (t.stage + 1) % 3;  // `next` was last read before the previous barrier
   ++t.stage;
-  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+  for (int b = threadIdx.x; b < t.bins; b += blockDim.x) {
     if (sh.count[b] != 0) {
       atomicAdd(&t.g->count[now][b], sh.count[b]);
       if (kMass) atomicAdd(&t.g->mass[now][b], (static_cast<unsigned long long>(sh.hi[b]) << 32) + sh.lo[b]);
@@ -392,7 +427,7 @@ __device__ bool merge_bins(Team& t, Shared& sh) {
     }
   }
   if (!team_sync(t, sh)) return false;
-  for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+  for (int b = threadIdx.x; b < t.bins; b += blockDim.x) {
     sh.count[b] = __ldcg(&t.g->count[now][b]);
     if (kMass) sh.mass[b] = __ldcg(&t.g->mass[now][b]);
   }
@@ -400,27 +435,32 @@ __device__ bool merge_bins(Team& t, Shared& sh) {
   return true;
 }
 
-// Sum over the CTA, on every thread.
+// Each warp's value of `mine` over the CTA's warps, lane w having warp w's.
+__device__ __forceinline__ unsigned long long warps_of(unsigned long long mine, int from_lane, Shared& sh) {
+  const int lane = threadIdx.x & 31;
+  __syncthreads();
+  if (lane == from_lane) sh.warp_u64[threadIdx.x >> 5] = mine;
+  __syncthreads();
+  return lane < static_cast<int>(blockDim.x >> 5) ? sh.warp_u64[lane] : 0;
+}
+// Sum (maximum) over the CTA, on every thread.
 __device__ __forceinline__ unsigned long long block_sum(unsigned long long v, Shared& sh) {
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(~0u, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh.warp_u64[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0;
-  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v += sh.warp_u64[w];
+  v = warps_of(v, 0, sh);
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(~0u, v, o);
   return v;
 }
 __device__ __forceinline__ unsigned long long block_max(unsigned long long v, Shared& sh) {
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) v = max(v, __shfl_xor_sync(~0u, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh.warp_u64[threadIdx.x >> 5] = v;
-  __syncthreads();
-  for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v = max(v, sh.warp_u64[w]);
+  v = warps_of(v, 0, sh);
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v = max(v, __shfl_xor_sync(~0u, v, o));
   return v;
 }
-// The CTA's sum over lower threads; *all: over every thread.
+// The sum over the CTA's lower threads.
 __device__ __forceinline__ unsigned long long block_below(unsigned long long mine, Shared& sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned long long v = mine;
@@ -429,19 +469,21 @@ __device__ __forceinline__ unsigned long long block_below(unsigned long long min
     const unsigned long long w = __shfl_up_sync(~0u, v, o);
     if (lane >= o) v += w;
   }
-  __syncthreads();
-  if (lane == 31) sh.warp_u64[warp] = v;
-  __syncthreads();
-  v -= mine;
-  for (int w = 0; w < warp; ++w) v += sh.warp_u64[w];
-  return v;
+  unsigned long long all = warps_of(v, 31, sh);
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const unsigned long long w = __shfl_up_sync(~0u, all, o);
+    if (lane >= o) all += w;
+  }
+  const unsigned long long below = __shfl_sync(~0u, all, warp > 0 ? warp - 1 : 0);
+  return v - mine + (warp > 0 ? below : 0);
 }
 
 // The first bin where the running sum of counts (or masses) reaches `need`: sh.bin, the sum
 // before it sh.above, its count sh.in (0 where the sum stays below).
 template <bool kMass>
-__device__ void find_bin(Shared& sh, unsigned long long need) {
-  const int span = kBins / blockDim.x, first = threadIdx.x * span;
+__device__ void find_bin(const Team& t, Shared& sh, unsigned long long need) {
+  const int span = t.bins / blockDim.x, first = threadIdx.x * span;
   unsigned long long mine = 0;
   for (int j = 0; j < span; ++j) mine += kMass ? sh.mass[first + j] : sh.count[first + j];
   unsigned long long above = block_below(mine, sh);
@@ -460,18 +502,6 @@ __device__ void find_bin(Shared& sh, unsigned long long need) {
     }
   }
   __syncthreads();
-}
-
-// Composite: larger key first, then the lower index.
-__device__ __forceinline__ unsigned long long composite(uint32_t key, int i) {
-  return (static_cast<unsigned long long>(key) << kIndexBits) |
-         static_cast<unsigned long long>((1 << kIndexBits) - 1 - i);
-}
-__device__ __forceinline__ int index_of(unsigned long long c) {
-  return (1 << kIndexBits) - 1 - static_cast<int>(c & ((1ull << kIndexBits) - 1));
-}
-__device__ __forceinline__ float score_of(unsigned long long c) {
-  return from_ordered(static_cast<uint32_t>(c >> kIndexBits));
 }
 
 // sh.list[0 .. n), descending.
@@ -494,56 +524,140 @@ __device__ void sort_list(Shared& sh, unsigned n) {
     }
 }
 
-// Bins of a selection: linear from `from` down, kBins / range a unit; what lies outside goes to
+// The team's list into sh.list (a lone CTA's is there).
+__device__ __forceinline__ void take_list(const Team& t, Shared& sh, const unsigned long long* list,
+                                          const unsigned* listed) {
+  if (t.size > 1) {
+    const unsigned have = min(__ldcg(listed), static_cast<unsigned>(kList));
+    for (unsigned j = threadIdx.x; j < have; j += blockDim.x) sh.list[j] = __ldcg(&list[j]);
+    if (threadIdx.x == 0) sh.listed = have;
+  } else if (threadIdx.x == 0) {
+    sh.listed = min(sh.listed, static_cast<unsigned>(kList));
+  }
+  __syncthreads();
+}
+// Mass of the first `n` entries of sh.list.
+__device__ __forceinline__ unsigned long long list_mass(Shared& sh, unsigned n, float top, float unit) {
+  unsigned long long sum = 0;
+  for (unsigned j = threadIdx.x; j < n; j += blockDim.x) sum += fixed_weight(score_of(sh.list[j]), top, unit);
+  return block_sum(sum, sh);
+}
+// The entry of the sorted list (of n >= 1) at which the running mass reaches `need`; the last one
+// where rounding leaves less.
+__device__ __forceinline__ unsigned mass_reaches(Shared& sh, unsigned n, unsigned long long need, float top, float unit) {
+  const unsigned span = (n + blockDim.x - 1) / blockDim.x, first = threadIdx.x * span;
+  unsigned long long mine = 0;
+  for (unsigned j = first; j < min(first + span, n); ++j) mine += fixed_weight(score_of(sh.list[j]), top, unit);
+  unsigned long long at = block_below(mine, sh);
+  if (threadIdx.x == 0) sh.found = n - 1;
+  __syncthreads();
+  if (at < need && at + mine >= need)
+    for (unsigned j = first; j < min(first + span, n); ++j) {
+      at += fixed_weight(score_of(sh.list[j]), top, unit);
+      if (at >= need) {
+        sh.found = j;
+        break;
+      }
+    }
+  __syncthreads();
+  return sh.found;
+}
+__device__ __forceinline__ unsigned long long share_of(float share, unsigned long long sum) {
+  return share > 0.0f
+             ? max(1ull, static_cast<unsigned long long>(static_cast<double>(share) * static_cast<double>(sum)))
+             : 1ull;
+}
+
+// Bins of a selection: linear from `from` down, `scale` a unit; what lies outside goes to
 // the first or last one.  Rounded steps of it are monotone, so a bin is an interval.
 struct Bins {
-  float from, scale;
+  float from, scale, last;
   __device__ __forceinline__ int of(float v) const {
-    return static_cast<int>(fminf(fmaxf(__fmul_rn(__fsub_rn(from, v), scale), 0.0f), static_cast<float>(kBins - 1)));
+    return static_cast<int>(fminf(fmaxf(__fmul_rn(__fsub_rn(from, v), scale), 0.0f), last));
   }
 };
 
-// Selects from the entries that get() gives: get(i0, x, valid, key) -> bits of the entries that
-// take part, with their keys.
+// The bin that holds the `need`-th largest of the threads' own maxima (-infinity: none), one a
+// thread; all entries in bins up to it are at least `need`.  -1 where there are not so many.
+__device__ bool bin_of_maxima(Team& t, Shared& sh, Bins bins, unsigned long long need, float mine, int* bin) {
+  clear_bins(t, sh, false);
+  if (mine > -INFINITY) atomicAdd(&sh.count[bins.of(mine)], 1u);
+  if (!merge_bins<false>(t, sh)) return false;
+  find_bin<false>(t, sh, need);
+  *bin = sh.in > 0 ? static_cast<int>(sh.bin) : -1;
+  return true;
+}
+// Collects the composites of all values in bins up to `bin` (kAbove) or in it, of these only those whose
+// leading digits (above `shift`) are at least (are) `prefix`.  mine: the thread's largest value.
+template <bool kAbove, typename Src, typename Get>
+__device__ __forceinline__ void collect(const Src& src, const Team& t, Bins bins, int bin, float mine, int shift,
+                                        unsigned long long prefix, Get get, unsigned long long* list, unsigned* listed,
+                                        unsigned capacity) {
+  constexpr int V = Src::V;
+  if (!(mine > -INFINITY) || bins.of(mine) > bin) return;  // nor is any other of its values that large
+  src.template walk<1>(t, [&](int i0, float(&s)[V]) {
+    get(i0, s);
+    unsigned hit = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (s[v] > -INFINITY) {
+        const int b = bins.of(s[v]);
+        if (kAbove ? b <= bin : b == bin) hit |= 1u << v;
+      }
+    if (hit == 0) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (!(hit >> v & 1u)) continue;
+      const unsigned long long c = composite(ordered(s[v]), i0 + v), high = c >> shift;
+      if ((kAbove && bins.of(s[v]) < bin) || (kAbove ? high >= prefix : high == prefix)) {
+        const unsigned at = atomicAdd(listed, 1u);
+        if (at < capacity) list[at] = c;
+      }
+    }
+  });
+}
+
+// Selects from the values that get() gives: get(i0, s) turns the scores of a group into
+// values, -infinity for entries that do not take part.
 //   kMass = false: the `need`-th largest composite; kAbove: the `need` largest
 //   kMass = true:  the composite at which the mass reaches `share` of all
+// mine: the thread's largest value, or +infinity where it is not known.
 // Leaves a sorted list in sh.list.  *edge: the composite found (0: the entries do not
 // reach that far, all are kept).  kAbove: sh.listed entries, on rank 0 only, and no edge.
-template <typename T, bool kMass, bool kAbove, typename Get>
-__device__ bool select(const T* x, long long n, Team& t, Shared& sh, int use, Bins bins, unsigned long long need,
-                       float share, float top, float unit, Get get, unsigned long long* edge) {
-  constexpr int V = 16 / sizeof(T);
+template <bool kMass, bool kAbove, typename Src, typename Get>
+__device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use, Bins bins, unsigned long long need,
+                                    float share, float top, float unit, float mine, Get get,
+                                    unsigned long long* edge) {
+  constexpr int V = Src::V;
   *edge = 0;
+  unsigned long long* list = t.size > 1 ? t.g->list[use] : sh.list;
+  unsigned* listed = t.size > 1 ? &t.g->listed[use] : &sh.listed;
   if (threadIdx.x == 0) sh.listed = 0;
-  clear_bins(sh, kMass);
-  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
-    uint32_t key[V];
-    const unsigned in = get(i0, xs, valid, key);
+  clear_bins(t, sh, kMass);
+  src.template walk<1>(t, [&](int i0, float(&s)[V]) {
+    get(i0, s);
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (in >> e & 1u) {
-        const float v = from_ordered(key[e]);
-        const int b = bins.of(v);
+    for (int v = 0; v < V; ++v)
+      if (s[v] > -INFINITY) {
+        const int b = bins.of(s[v]);
         atomicAdd(&sh.count[b], 1u);
-        if (kMass) add_mass(sh, b, fixed_weight(v, top, unit));
+        if (kMass) add_mass(sh, b, fixed_weight(s[v], top, unit));
       }
   });
   if (!merge_bins<kMass>(t, sh)) return false;
   if (kMass) {
     unsigned long long sum = 0;
-    for (int b = threadIdx.x; b < kBins; b += blockDim.x) sum += sh.mass[b];
+    for (int b = threadIdx.x; b < t.bins; b += blockDim.x) sum += sh.mass[b];
     sum = block_sum(sum, sh);
-    need = share > 0.0f ? max(1ull, static_cast<unsigned long long>(static_cast<double>(share) *
-                                                                    static_cast<double>(sum)))
-                        : 1ull;
+    need = share_of(share, sum);
   }
-  find_bin<kMass>(sh, need);
+  find_bin<kMass>(t, sh, need);
   int bin = static_cast<int>(sh.bin);
   unsigned in = sh.in;
   unsigned above_n = 0;  // kAbove: entries above the bin (the list takes them too)
   if (in == 0) {
     if (!kAbove) return true;
-    bin = kBins - 1;  // fewer than `need`: all of them
+    bin = t.bins - 1;  // fewer than `need`: all of them
   } else {
     need -= sh.above;
     if (kAbove) above_n = static_cast<unsigned>(sh.above);
@@ -553,78 +667,36 @@ __device__ bool select(const T* x, long long n, Team& t, Shared& sh, int use, Bi
   unsigned long long prefix = 0;
 #pragma unroll 1
   while (in + above_n > kList) {
-    const int bits = min(11, shift);
+    const int bits = min(31 - __clz(t.bins), shift);
     shift -= bits;
-    clear_bins(sh, kMass);
-    walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
-      uint32_t key[V];
-      const unsigned on = get(i0, xs, valid, key);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const unsigned long long c = composite(key[e], i0 + e);
-        if ((on >> e & 1u) && bins.of(from_ordered(key[e])) == bin && (c >> (shift + bits)) == prefix) {
-          const int b = kBins - 1 - static_cast<int>((c >> shift) & ((1u << bits) - 1u));
-          atomicAdd(&sh.count[b], 1u);
-          if (kMass) add_mass(sh, b, fixed_weight(from_ordered(key[e]), top, unit));
-        }
+    clear_bins(t, sh, kMass);
+    src.template walk<1>(t, [&](int i0, float(&s)[V]) {
+      get(i0, s);
+#pragma unroll 1
+      for (int v = 0; v < V; ++v) {
+        if (!(s[v] > -INFINITY) || bins.of(s[v]) != bin) continue;
+        const unsigned long long c = composite(ordered(s[v]), i0 + v);
+        if ((c >> (shift + bits)) != prefix) continue;
+        const int b = t.bins - 1 - static_cast<int>((c >> shift) & ((1u << bits) - 1u));
+        atomicAdd(&sh.count[b], 1u);
+        if (kMass) add_mass(sh, b, fixed_weight(s[v], top, unit));
       }
     });
     if (!merge_bins<kMass>(t, sh)) return false;
-    find_bin<kMass>(sh, need);
-    prefix = (prefix << bits) | static_cast<unsigned>(kBins - 1 - sh.bin);
+    find_bin<kMass>(t, sh, need);
+    prefix = (prefix << bits) | static_cast<unsigned>(t.bins - 1 - sh.bin);
     in = sh.in;
     need -= sh.above;
     if (kAbove) above_n += static_cast<unsigned>(sh.above);
   }
-  unsigned long long* list = t.size > 1 ? t.g->list[use] : sh.list;
-  unsigned* listed = t.size > 1 ? &t.g->listed[use] : &sh.listed;
-  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
-    uint32_t key[V];
-    const unsigned on = get(i0, xs, valid, key);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      if (!(on >> e & 1u)) continue;
-      const int b = bins.of(from_ordered(key[e]));
-      if (b > bin || (!kAbove && b != bin)) continue;
-      const unsigned long long c = composite(key[e], i0 + e), high = c >> shift;
-      if (b < bin || (kAbove ? high >= prefix : high == prefix)) {
-        const unsigned at = atomicAdd(listed, 1u);
-        if (at < kList) list[at] = c;
-      }
-    }
-  });
+  collect<kAbove>(src, t, bins, bin, mine, shift, prefix, get, list, listed, kList);
   if (!team_sync(t, sh)) return false;
   if (kAbove && t.rank != 0) return true;
-  if (t.size > 1) {
-    const unsigned have = min(__ldcg(listed), static_cast<unsigned>(kList));
-    for (unsigned j = threadIdx.x; j < have; j += blockDim.x) sh.list[j] = __ldcg(&list[j]);
-    if (threadIdx.x == 0) sh.listed = have;
-    __syncthreads();
-  }
-  const unsigned have = min(sh.listed, static_cast<unsigned>(kList));
+  take_list(t, sh, list, listed);
+  const unsigned have = sh.listed;
   sort_list(sh, have);
   if (kAbove) return true;
-  if (!kMass) {
-    *edge = sh.list[need - 1];
-  } else {
-    // the entry at which the running mass reaches `need` (the last one if rounding leaves less)
-    const unsigned span = (have + blockDim.x - 1) / blockDim.x, first = threadIdx.x * span;
-    unsigned long long mine = 0;
-    for (unsigned j = first; j < min(first + span, have); ++j) mine += fixed_weight(score_of(sh.list[j]), top, unit);
-    unsigned long long at = block_below(mine, sh);
-    if (threadIdx.x == 0) sh.edge = sh.list[have - 1];
-    __syncthreads();
-    if (at < need && at + mine >= need)
-      for (unsigned j = first; j < min(first + span, have); ++j) {
-        at += fixed_weight(score_of(sh.list[j]), top, unit);
-        if (at >= need) {
-          sh.edge = sh.list[j];
-          break;
-        }
-      }
-    __syncthreads();
-    *edge = sh.edge;
-  }
+  *edge = kMass ? sh.list[mass_reaches(sh, have, need, top, unit)] : sh.list[need - 1];
   __syncthreads();
   return true;
 }
@@ -636,15 +708,6 @@ __device__ __forceinline__ void none_drawn(const SampleArgs& a, long long row, i
   }
 }
 
-template <int V>
-__device__ __forceinline__ unsigned scale_group(const float (&x)[V], unsigned valid, float inv, float (&s)[V]) {
-  unsigned alive = 0;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-    if (scaled(x[v], inv, &s[v])) alive |= 1u << v;
-  return alive & valid;
-}
-
 __device__ __forceinline__ void join_stats(float& m, float& z, float m2, float z2) {
   const float b = fmaxf(m, m2);
   if (b == -INFINITY) return;
@@ -652,56 +715,219 @@ __device__ __forceinline__ void join_stats(float& m, float& z, float m2, float z
   m = b;
 }
 
+// What the steps of a row share.
+struct Ctx {
+  const float* noise;
+  Rule r;
+  float top, logz, unit;
+  long long row;
+};
+
+// Kept entries of the row lie above (value, index) of the edge's entry, or are it.
+struct Edge {
+  unsigned long long c = 0;
+  float s = -FLT_MAX;
+  int i = (1 << kIndexBits) - 1;
+  __device__ __forceinline__ void raise(unsigned long long to) {
+    if (to <= c) return;
+    c = to;
+    s = score_of(to);
+    i = index_of(to);
+  }
+  __device__ __forceinline__ bool keeps(float v, int at) const { return v > s || (v == s && at <= i); }
+};
+
+__device__ __forceinline__ void put(const SampleArgs& a, const Ctx& x, int j, int index, float s) {
+  a.out_index[x.row * a.m + j] = index;
+  a.out_logprob[x.row * a.m + j] = x.r.greedy ? 0.0f : __fsub_rn(s, x.top) - x.logz;
+}
+
+// Cuts and draws from sh.list, sorted, which holds the row's best entries: at least the top k.
 template <typename T>
-__device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long row) {
-  constexpr int V = 16 / sizeof(T);
-  const long long n = a.n;
+__device__ void finish_list(const SampleArgs& a, Shared& sh, const Ctx& x, const Row<T>& src) {
+  unsigned keep = min(sh.listed, x.r.k);
+  if (x.r.p < 1.0f)
+    keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.top, x.unit)), x.top, x.unit) + 1;
+  if (x.r.log_min > -INFINITY) {
+    unsigned long long mine = 0;
+    for (unsigned j = threadIdx.x; j < keep; j += blockDim.x)
+      mine += __fsub_rn(score_of(sh.list[j]), x.top) >= x.r.log_min;
+    keep = static_cast<unsigned>(block_sum(mine, sh));
+  }
+  unsigned long long best = 0;
+  for (unsigned j = threadIdx.x; j < keep; j += blockDim.x) {
+    const int i = index_of(sh.list[j]);
+    const unsigned long long c = composite(ordered(draw_value(score_of(sh.list[j]), x.noise[i])), i);
+    sh.list[j] = c;
+    best = max(best, c);
+  }
+  if (a.m == 1) {
+    best = block_max(best, sh);
+    if (threadIdx.x == 0) put(a, x, 0, index_of(best), src.score(index_of(best)));
+    return;
+  }
+  __syncthreads();
+  sort_list(sh, keep);
+  const int drawn = static_cast<int>(min(keep, static_cast<unsigned>(a.m)));
+  for (int j = threadIdx.x; j < drawn; j += blockDim.x)
+    put(a, x, j, index_of(sh.list[j]), src.score(index_of(sh.list[j])));
+  none_drawn(a, x.row, drawn);
+}
+
+// Cuts and draws by selection from `src` (the row, or candidates that hold its top k).  mine: the
+// thread's largest score there; mine_key: its largest draw value where nothing is cut (else NaN).
+template <typename T, typename Src>
+__device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ctx& x, const Row<T>& row, const Src& src,
+                              Bins by_score, float mine, float mine_key) {
+  constexpr int V = Src::V;
+  Edge edge;
+  unsigned long long found;
+  if (x.r.k != 0) {
+    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.top, 0.0f, mine, [](int, float(&)[V]) {}, &found))
+      return false;
+    edge.raise(found);
+  }
+  if (x.r.p < 1.0f) {
+    auto scores = [=](int i0, float(&s)[V]) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (!edge.keeps(s[v], i0 + v)) s[v] = -INFINITY;
+    };
+    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.top, x.unit, mine, scores, &found)) return false;
+    edge.raise(found);
+  }
+  // Draw values of the kept entries.
+  auto draws = [edge, noise = x.noise, top = x.top, log_min = x.r.log_min](int i0, float(&s)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool in = edge.keeps(s[v], i0 + v) && __fsub_rn(s[v], top) >= log_min;
+      s[v] = in ? draw_value(s[v], noise[i0 + v]) : -INFINITY;
+    }
+  };
+  // The thread's largest draw value.  A thread whose largest score is cut has none.
+  int at = 0;
+  if (mine_key != mine_key) {
+    mine_key = -INFINITY;
+    if (mine >= edge.s && __fsub_rn(mine, x.top) >= x.r.log_min)
+      src.template walk<1>(t, [&](int i0, float(&s)[V]) {
+        draws(i0, s);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (s[v] > mine_key || (V == 1 && s[v] == mine_key && i0 < at)) {  // a row's indices grow
+            mine_key = s[v];
+            at = i0 + v;
+          }
+      });
+  }
+  if (a.m == 1) {
+    unsigned long long best = mine_key > -INFINITY ? composite(ordered(mine_key), at) : 0;
+    best = block_max(best, sh);
+    if (t.size > 1) {
+      if (threadIdx.x == 0) t.g->best[t.rank] = best;
+      if (!team_sync(t, sh)) return false;
+      if (t.rank == 0 && threadIdx.x == 0)
+        for (int c = 0; c < t.size; ++c) best = max(best, __ldcg(&t.g->best[c]));
+    }
+    if (t.rank == 0 && threadIdx.x == 0) put(a, x, 0, index_of(best), row.score(index_of(best)));
+    return true;
+  }
+  // Gumbel noise puts the largest keys within a few units of the best score, and ln n above it.
+  const float last = static_cast<float>(t.bins - 1);
+  const Bins by_key = {x.top + 24.0f, last / 48.0f, last};
+  // More than m threads: the m-th of their maxima bounds the m-th draw from below, and few
+  // entries beside the draws lie above it.
+  bool done = false;
+  if (a.m <= t.size * static_cast<int>(blockDim.x) / 2) {
+    int bin;
+    if (!bin_of_maxima(t, sh, by_key, a.m, mine_key, &bin)) return false;
+    if (bin >= 0) {
+      unsigned long long* list = t.size > 1 ? t.g->list[1] : sh.list;  // top-p's is read by now
+      unsigned* listed = t.size > 1 ? &t.g->listed[3] : &sh.listed;
+      if (threadIdx.x == 0) sh.listed = 0;
+      __syncthreads();
+      collect<true>(src, t, by_key, bin, mine_key, kIndexBits + 32, 0, draws, list, listed, kList);
+      if (!team_sync(t, sh)) return false;
+      done = (t.size > 1 ? __ldcg(listed) : sh.listed) <= kList;
+      if (done) {
+        if (t.rank != 0) return true;
+        take_list(t, sh, list, listed);
+        sort_list(sh, sh.listed);
+      }
+      __syncthreads();
+    }
+  }
+  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.top, 0.0f, mine_key, draws, &found))
+    return false;
+  if (t.rank != 0) return true;
+  const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
+  for (int j = threadIdx.x; j < drawn; j += blockDim.x)
+    put(a, x, j, index_of(sh.list[j]), row.score(index_of(sh.list[j])));
+  none_drawn(a, x.row, drawn);
+  return true;
+}
+
+template <typename T>
+__device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long row_at) {
+  constexpr int V = Row<T>::V;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const Rule r = read_rule(a.rules != nullptr ? a.rules[row] : a.rule, n);
-  const T* x = static_cast<const T*>(a.scores) + row * a.row_stride;
-  const float* noise = a.noise + row * a.noise_stride;
-  if (r.bad) {
+  Ctx x;
+  x.r = read_rule(a.rules != nullptr ? a.rules[row_at] : a.rule, a.n);
+  x.noise = a.noise + row_at * a.noise_stride;
+  x.row = row_at;
+  const Row<T> row = {static_cast<const T*>(a.scores) + row_at * a.row_stride, static_cast<int>(a.n), x.r.inv};
+  if (x.r.bad) {
     if (t.rank == 0) {
       if (threadIdx.x == 0) atomicOr(a.err, kErrBadRule);
-      none_drawn(a, row, 0);
+      none_drawn(a, row_at, 0);
     }
     return true;
   }
-  // One draw from an uncut row needs no edge: it is found in the first pass.
-  const bool direct = (a.m == 1 || r.greedy) && r.k == 0 && r.p >= 1.0f && r.log_min == -INFINITY;
+  // Where nothing is cut the first pass finds the draws too: one, or every thread's largest.
+  const bool uncut = x.r.k == 0 && x.r.p >= 1.0f && x.r.log_min == -INFINITY;
+  const bool direct = uncut && (a.m == 1 || x.r.greedy);
 
   // Pass 1: maximum, minimum and sum of exponentials, each lane's own, then joined in a fixed order.
   float top = -INFINITY, z = 0.0f, low = INFINITY;
-  unsigned long long best = 0;
-  walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
-    float s[V];
-    const unsigned alive = scale_group<V>(xs, valid, r.inv, s);
+  float best_key = -INFINITY;
+  int best_at = 0;
+  auto first = [&](int i0, float(&s)[V]) {
     float b = top;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (alive >> v & 1u) {
-        b = fmaxf(b, s[v]);
-        low = fminf(low, s[v]);
-      }
+    for (int v = 0; v < V; ++v) {
+      b = fmaxf(b, s[v]);
+      low = fminf(low, s[v] > -INFINITY ? s[v] : INFINITY);
+    }
+    if (b == -INFINITY) return;
     if (b > top) {
       z *= __expf(top - b);
       top = b;
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (alive >> v & 1u) z += __expf(s[v] - top);
-    if (direct) {
+    for (int v = 0; v < V; ++v) z += __expf(s[v] - top);
+    if (uncut) {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (alive >> v & 1u)
-          best = max(best, composite(r.greedy ? ordered(s[v]) : draw_key(s[v], noise[i0 + v]), i0 + v));
+        if (s[v] > -INFINITY) {
+          const float k = x.r.greedy ? s[v] : draw_value(s[v], x.noise[i0 + v]);
+          if (k > best_key) {  // indices grow: the first of equal ones stays
+            best_key = k;
+            best_at = i0 + v;
+          }
+        }
     }
-  });
+  };
+  if (uncut) row.template walk<2>(t, first);
+  else row.template walk<sizeof(T) == 4 ? 4 : 2>(t, first);
+  const float mine = top;
+  unsigned long long best = best_key > -INFINITY ? composite(ordered(best_key), best_at) : 0;
+  auto join_lanes = [&]() {
 #pragma unroll
-  for (int o = 16; o > 0; o /= 2) {
-    join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
-    low = fminf(low, __shfl_xor_sync(~0u, low, o));
-  }
+    for (int o = 16; o > 0; o /= 2) {
+      join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
+      low = fminf(low, __shfl_xor_sync(~0u, low, o));
+    }
+  };
+  join_lanes();
   if (lane == 0) {
     sh.warp_f[warp][0] = top;
     sh.warp_f[warp][1] = z;
@@ -710,15 +936,10 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
   if (direct) best = block_max(best, sh);
   __syncthreads();
   if (warp == 0) {
-    // one warp joins, by a tree too: its shape is fixed
     top = lane < warps ? sh.warp_f[lane][0] : -INFINITY;
     z = lane < warps ? sh.warp_f[lane][1] : 0.0f;
     low = lane < warps ? sh.warp_f[lane][2] : INFINITY;
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
-      join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
-      low = fminf(low, __shfl_xor_sync(~0u, low, o));
-    }
+    join_lanes();
     if (lane == 0) {
       sh.top = top;
       sh.z = z;
@@ -731,7 +952,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
   }
   if (t.size > 1) {
     if (t.rank == 0) {
-      for (int b = threadIdx.x; b < kBins; b += blockDim.x) {
+      for (int b = threadIdx.x; b < t.bins; b += blockDim.x) {
         t.g->count[t.stage % 3][b] = 0;
         t.g->mass[t.stage % 3][b] = 0;
       }
@@ -749,12 +970,9 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
         low = fminf(low, q.z);
         best = max(best, __ldcg(&t.g->best[c]));
       }
+      join_lanes();
 #pragma unroll
-      for (int o = 16; o > 0; o /= 2) {
-        join_stats(top, z, __shfl_xor_sync(~0u, top, o), __shfl_xor_sync(~0u, z, o));
-        low = fminf(low, __shfl_xor_sync(~0u, low, o));
-        best = max(best, __shfl_xor_sync(~0u, best, o));
-      }
+      for (int o = 16; o > 0; o /= 2) best = max(best, __shfl_xor_sync(~0u, best, o));
       if (lane == 0) {
         sh.top = top;
         sh.z = z;
@@ -763,111 +981,73 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
   }
   __syncthreads();
-  top = sh.top;
-  z = sh.z;
-  if (direct || top == -INFINITY) {
+  x.top = sh.top;
+  if (x.top == -INFINITY) {
+    if (t.rank == 0) none_drawn(a, row_at, 0);
+    return true;
+  }
+  x.logz = logf(sh.z);
+  if (direct) {
     if (t.rank == 0) {
-      if (threadIdx.x == 0 && top != -INFINITY) {
-        const int i = index_of(best);
-        float s;
-        scaled(to_f32(x[i]), r.inv, &s);
-        a.out_index[row * a.m] = i;
-        a.out_logprob[row * a.m] = r.greedy ? 0.0f : __fsub_rn(s, top) - logf(z);
-      }
-      none_drawn(a, row, top != -INFINITY ? 1 : 0);
+      if (threadIdx.x == 0) put(a, x, 0, index_of(best), row.score(index_of(best)));
+      none_drawn(a, row_at, 1);
     }
     return true;
   }
+  int log_n = 0;
+  while ((1ll << log_n) < a.n) ++log_n;
+  x.unit = static_cast<float>(1ull << (62 - log_n));
 
-  // The cuts.  Scores more than 40 below the best share the last bin: their mass is
-  // nothing, and only a top-k of a very peaked row looks there.
-  const float range = fminf(__fsub_rn(top, sh.low), 40.0f);
-  const Bins by_score = {top, range > 0.0f ? fminf(static_cast<float>(kBins - 1) / range, 1e30f) : 0.0f};
-  unsigned long long edge = 0;
-  // an entry's composite is at or above the edge
-  auto kept = [&](uint32_t key, int i) {
-    const uint32_t ek = static_cast<uint32_t>(edge >> kIndexBits);
-    return key > ek || (key == ek && i <= index_of(edge));
-  };
-  auto scores = [&](int i0, const float(&xs)[V], unsigned valid, uint32_t(&key)[V]) {
-    float s[V];
-    unsigned in = scale_group<V>(xs, valid, r.inv, s);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      key[v] = ordered(s[v]);
-      if (!kept(key[v], i0 + v)) in &= ~(1u << v);
-    }
-    return in;
-  };
-  unsigned long long found;
-  if (r.k != 0) {
-    if (!select<T, false, false>(x, n, t, sh, 0, by_score, r.k, 0.0f, top, 0.0f, scores, &found)) return false;
-    edge = found;
-  }
-  if (r.p < 1.0f) {
-    int log_n = 0;
-    while ((1ll << log_n) < n) ++log_n;
-    const float unit = static_cast<float>(1ull << (62 - log_n));
-    if (!select<T, true, false>(x, n, t, sh, 1, by_score, 0, r.p, top, unit, scores, &found)) return false;
-    edge = max(edge, found);
-  }
+  // Scores more than 40 below the best share the last bin: their mass is nothing, and only
+  // a top-k of a very peaked row looks there.
+  const float range = fminf(__fsub_rn(x.top, sh.low), 40.0f), last = static_cast<float>(t.bins - 1);
+  const Bins by_score = {x.top, range > 0.0f ? fminf(last / range, 1e30f) : 0.0f, last};
 
-  // Bits of the group's kept entries and their draw keys.
-  auto draws = [&](int i0, const float(&xs)[V], unsigned valid, uint32_t(&key)[V]) {
-    float s[V];
-    unsigned in = scale_group<V>(xs, valid, r.inv, s);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!kept(ordered(s[v]), i0 + v) || !(__fsub_rn(s[v], top) >= r.log_min)) in &= ~(1u << v);
-      key[v] = in >> v & 1u ? draw_key(s[v], noise[i0 + v]) : 0;
-    }
-    return in;
-  };
-  const float logz = logf(z);
-  if (a.m == 1) {
-    best = 0;
-    walk(x, n, t, [&](int i0, const float(&xs)[V], unsigned valid) {
-      uint32_t key[V];
-      const unsigned in = draws(i0, xs, valid, key);
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (in >> v & 1u) best = max(best, composite(key[v], i0 + v));
-    });
-    best = block_max(best, sh);
-    if (t.size > 1) {
-      if (threadIdx.x == 0) t.g->best[t.rank] = best;
+  // A top-k of less than half as many entries as threads: the k-th of the threads' maxima bounds the
+  // k-th entry from below.  Few entries beside the k lie above it; they are collected in one
+  // more pass, which most threads skip, and one CTA does the rest from the list.
+  const long long threads = static_cast<long long>(t.size) * blockDim.x;
+  if (x.r.k != 0 && 2ll * x.r.k <= threads) {
+    int bin;
+    if (!bin_of_maxima(t, sh, by_score, x.r.k, mine, &bin)) return false;
+    if (bin >= 0) {
+      unsigned long long* list = t.size > 1 ? t.g->large : sh.list;
+      unsigned* listed = t.size > 1 ? &t.g->listed[0] : &sh.listed;
+      const unsigned capacity = t.size > 1 ? kLarge : kList;
+      if (threadIdx.x == 0) sh.listed = 0;
+      __syncthreads();
+      collect<true>(row, t, by_score, bin, mine, kIndexBits + 32, 0, [](int, float(&)[V]) {}, list, listed, capacity);
       if (!team_sync(t, sh)) return false;
-      if (t.rank == 0 && threadIdx.x == 0)
-        for (int c = 0; c < t.size; ++c) best = max(best, __ldcg(&t.g->best[c]));
+      const unsigned have = t.size > 1 ? __ldcg(listed) : sh.listed;
+      if (have <= capacity) {
+        if (t.rank != 0) return true;
+        if (have <= kList) {
+          take_list(t, sh, list, listed);
+          sort_list(sh, have);
+          finish_list(a, sh, x, row);
+          return true;
+        }
+        // more than can be sorted: the same selections, from the candidates and by this CTA alone
+        const Candidates src = {list, static_cast<int>(have)};
+        float own = -INFINITY;
+        src.walk<1>(t, [&](int, float(&s)[1]) { own = fmaxf(own, s[0]); });
+        Team alone = t;
+        alone.size = 1;
+        return finish_select(a, alone, sh, x, row, src, by_score, own, __int_as_float(0x7FFFFFFF));
+      }
+      if (t.size > 1) {
+        // a crowded bin: the list's counter starts anew
+        if (!team_sync(t, sh)) return false;
+        if (t.rank == 0 && threadIdx.x == 0) t.g->listed[0] = 0;
+        if (!team_sync(t, sh)) return false;
+      }
     }
-    if (t.rank == 0 && threadIdx.x == 0) {
-      const int i = index_of(best);  // no cut drops the best entry
-      float s;
-      scaled(to_f32(x[i]), r.inv, &s);
-      a.out_index[row] = i;
-      a.out_logprob[row] = __fsub_rn(s, top) - logz;
-    }
-    return true;
   }
-  // Gumbel noise puts the largest keys within a few units of the best score, and ln n above it.
-  const Bins by_key = {top + 24.0f, static_cast<float>(kBins) / 48.0f};
-  if (!select<T, false, true>(x, n, t, sh, 2, by_key, a.m, 0.0f, top, 0.0f, draws, &found)) return false;
-  if (t.rank != 0) return true;
-  const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
-  for (int j = threadIdx.x; j < drawn; j += blockDim.x) {
-    const int i = index_of(sh.list[j]);
-    float s;
-    scaled(to_f32(x[i]), r.inv, &s);
-    a.out_index[row * a.m + j] = i;
-    a.out_logprob[row * a.m + j] = __fsub_rn(s, top) - logz;
-  }
-  none_drawn(a, row, drawn);
-  __syncthreads();
-  return true;
+  return finish_select(a, t, sh, x, row, row, by_score, mine, uncut ? best_key : __int_as_float(0x7FFFFFFF));
 }
 
 template <typename T>
-__global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size) {
+__global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size, int bins) {
   extern __shared__ __align__(16) unsigned char smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   Team t;
@@ -877,13 +1057,14 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
   t.err = a.err;
   t.barriers = 0;
   t.stage = 0;
+  t.bins = bins;
   sample_row<T>(a, t, sh, blockIdx.x / team_size);
 }
 
 bool by_warp(long long n, int m) { return n <= kWarpMaxN && m <= kWarpMaxM; }
 
-// CTAs per row: all SMs divided over the rows, but no CTA with less than 4,096 entries
-// (a barrier of a team costs about as much as a CTA's passes over that many).
+// CTAs per row: all SMs divided over the rows, but no CTA with less than 4,096 entries (one row of
+// 50,021 with top-p: 35 us by 13 CTAs, 55 by two).
 int team_of(long long rows, long long n, int sms) {
   if (rows * 2 > sms) return 1;
   long long t = sms / rows;
@@ -916,15 +1097,17 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
     const size_t smem = sizeof(Shared);
     cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_sample_row<T>), smem);
     if (e != cudaSuccess) return e;
-    const int threads = a.n <= 2048 ? 256 : a.n <= 8192 ? 512 : 1024;
+    // small CTAs for short rows: several share an SM, and barriers take fewer warps
+    const int threads = a.n <= 4096 ? 128 : a.n <= 16384 ? 256 : a.n <= 32768 ? 512 : 1024;
+    const int bins = a.n <= 16384 ? 512 : kBins;
     cudaLaunchConfig_t cfg{};
-    cfg.blockDim = dim3(team > 1 ? 1024 : threads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     if (team == 1) {
       cfg.gridDim = dim3(static_cast<unsigned>(a.rows));
       ++*launches;
-      return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, 1);
+      return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, 1, bins);
     }
     // the barriers' counters start from zero
     e = cudaMemset2DAsync(a.ws, sizeof(TeamMem), 0, 16, static_cast<size_t>(a.rows), st);
@@ -936,7 +1119,7 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     ++*launches;
-    return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, team);
+    return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, team, bins);
   });
 }
 
