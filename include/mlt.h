@@ -536,7 +536,8 @@ typedef struct {
 
 /* Draw m different entries of every row of scores by their probability
  * softmax(score / temperature), from given random numbers.
- *   s_i    = clamp(fl(fl(1 / temperature) * score_i)) to the finite floats;
+ *   s_i    = clamp(fl(c * score_i)) to the finite floats, c = fl(1 / temperature)
+ *            or the largest float;
  *            a NaN or -infinity score is never drawn (what mlt_screen gives
  *            candidates that V rejects)
  *   order    s descending, index ascending; the rule keeps a prefix of it
@@ -548,9 +549,8 @@ typedef struct {
  *            temperature 0; -infinity where out_index is -1
  * With Gumbel noise, -ln(-ln u) of uniform u, these are m draws without
  * replacement, the first one exactly a draw from the kept entries' softmax.
- * Probability masses are summed in 64-bit fixed point (units of 2^-35 of the
- * best entry's weight at n = 2^27, finer for shorter rows), so results do not
- * depend on the order of summation.
+ * Probability masses are summed as 64-bit integers in units of 2^-31 of the
+ * best entry's weight, so results do not depend on the order of summation.
  *   scores   device [rows][n] of `dtype`, row_stride elements apart
  *   noise    device [rows][n] fp32, noise_stride elements apart
  *   rule     host, for every row; or `rules`, device [rows], instead of it

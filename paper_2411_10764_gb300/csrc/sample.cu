@@ -24,9 +24,11 @@
 //   k_sample_warp  rows of up to 512 entries and m <= 32: a warp per row, the row in
 //                  registers, selection by ballots and warp sums, no barrier;
 //   k_sample_row   longer rows: a team of CTAs per row.  Where there are fewer
-//                  rows than SMs the team has several CTAs, which meet at a
-//                  barrier in global memory (cooperative launch, so all are
-//                  resident; the wait is bounded).
+//                  rows than SMs the team has several CTAs: a cluster, or where a few
+//                  rows have more than 32 each CTAs that meet at a barrier in
+//                  global memory (cooperative launch, so all are resident; the wait is
+//                  bounded).
+#include <atomic>
 #include <cfloat>
 
 #include "seq.cuh"
@@ -81,16 +83,16 @@ __device__ __forceinline__ Rule read_rule(const mlt_sample_rule& q, long long n)
   return r;
 }
 
-// Weight of an entry in fixed point: exp(s - top) * 2^shift.
-__device__ __forceinline__ unsigned long long fixed_weight(float s, float top, float unit) {
-  return __float2ull_rn(expf(__fsub_rn(s, top)) * unit);
+// Weight of an entry in fixed point, units of 2^-31 of the best one's.
+__device__ __forceinline__ uint32_t fixed_weight(float s, float top) {
+  return __float2uint_rn(__expf(__fsub_rn(s, top)) * 2147483648.0f);
 }
 
 // ---------------------------------------------------------------------------
 // A warp per row
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ unsigned long long warp_sum_fixed(unsigned long long v) {
-  // lanes hold up to 2^48 (16 weights of 2^44): 32 halves of 22 and of 26 bits add up below 2^32
+  // lanes hold up to 2^35 (16 weights of 2^31): 32 halves of 22 and of 13 bits add up below 2^32
   const unsigned lo = __reduce_add_sync(~0u, static_cast<unsigned>(v) & 0x3FFFFFu);
   const unsigned hi = __reduce_add_sync(~0u, static_cast<unsigned>(v >> 22));
   return (static_cast<unsigned long long>(hi) << 22) + lo;
@@ -155,8 +157,7 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
     }
   }
   if (r.p < 1.0f) {
-    const float unit = static_cast<float>(1ull << 44);
-    unsigned long long w[PER];
+    uint32_t w[PER];
     unsigned long long sum = 0;
     unsigned seen = 0;
 #pragma unroll
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
       const unsigned eq = __ballot_sync(~0u, key[j] == tau);
       const bool keep = key[j] > tau || (key[j] == tau && seen + __popc(eq & ((1u << lane) - 1u)) < ties);
       seen += __popc(eq);
-      w[j] = keep ? fixed_weight(s[j], top, unit) : 0;
+      w[j] = keep ? fixed_weight(s[j], top) : 0;
       sum += w[j];
     }
     sum = warp_sum_fixed(sum);
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
       at = best;
     }
     if (at > 0) {
-      const unsigned long long each = max(1ull, fixed_weight(from_ordered(at), top, unit));
+      const unsigned long long each = max(1u, fixed_weight(from_ordered(at), top));
       const unsigned long long need = (target - min(target, above) + each - 1) / each;
       const unsigned cap = at == tau ? ties : kNoTies;
       tau = at;
@@ -250,6 +251,7 @@ struct TeamMem {
   unsigned listed[kUses]; // entries in list (the last: in large)
   float4 stats[kMaxTeam]; // each CTA's (max, sum of exp, min)
   unsigned long long best[kMaxTeam];
+  unsigned entries[kMaxTeam];
   unsigned long long mass[3][kBins];
   unsigned count[3][kBins];
   unsigned long long list[kUses][kList];
@@ -266,7 +268,7 @@ struct Shared {
   };
   unsigned count[kBins];
   unsigned long long warp_u64[32];
-  float warp_f[32][3];
+  float warp_f[32][3];  // maximum, sum of exponentials, least of the lanes' maxima
   unsigned long long above;
   unsigned in, bin, listed, found;
   float top, z, low;
@@ -274,6 +276,7 @@ struct Shared {
 };
 
 struct Team {
+  bool cluster;  // the team is a thread-block cluster
   TeamMem* g;
   unsigned* err;
   int size, rank;
@@ -286,6 +289,10 @@ struct Team {
 __device__ bool team_sync(Team& t, Shared& sh) {
   __syncthreads();
   if (t.size == 1) return true;
+  if (t.cluster) {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    return true;
+  }
   ++t.barriers;
   if (threadIdx.x == 0) {
     __threadfence();
@@ -324,12 +331,14 @@ __device__ __forceinline__ float score_of(unsigned long long c) {
   return from_ordered(static_cast<uint32_t>(c >> kIndexBits));
 }
 
-// A row of scores.  walk: f(i0, s) for every 16-byte group that the thread owns, the same ones
-// at each walk: s[v] is the scaled score of entry i0 + v, -infinity where it cannot be
-// drawn or is outside the row.  U groups are loaded at once.
+// A row of scores.  walk: f(at, s) for every group of eight that the thread owns, the same ones
+// at each walk: s[v] is the scaled score of entry at[v], -infinity where it cannot be
+// drawn or is outside the row.  U groups are loaded at once.  What f loads or adds by
+// atomics it does for all of a group before it uses any of it: one after another, each
+// would wait for memory (64 rows x 50,021 with min-p: 10 us a pass).
 template <typename T>
 struct Row {
-  static constexpr int V = 16 / sizeof(T);
+  static constexpr int V = 8;  // of 16-bit scores 16 bytes, of fp32 twice that
   const T* row;
   int n;
   float inv;
@@ -340,7 +349,7 @@ struct Row {
     const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
     const int groups = (skew + n + V - 1) / V;
     const int stride = t.size * static_cast<int>(blockDim.x), last = n - V;
-    const T* base = row - skew;  // 16-byte aligned; entries before `row` are not read
+    const T* base = row - skew;  // aligned to the group; entries before `row` are not read
 #pragma unroll 1
     for (int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x; q0 < groups; q0 += stride * U) {
       Pack<T, V> p[U];
@@ -363,24 +372,34 @@ struct Row {
           for (int v = 0; v < V; ++v)
             s[v] = i0 + v >= 0 && i0 + v < n ? scaled(to_f32(row[i0 + v]), inv) : -INFINITY;
         }
-        f(i0, s);
+        int at[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) at[v] = i0 + v;
+        f(at, s);
       }
     }
   }
 };
 // Candidates that were collected from a row, as composites; walked by one CTA.
 struct Candidates {
-  static constexpr int V = 1;
+  static constexpr int V = 4;
   const unsigned long long* list;
   int n;
 
   template <int U, typename F>
   __device__ __forceinline__ void walk(const Team&, F f) const {
 #pragma unroll 1
-    for (int j = threadIdx.x; j < n; j += blockDim.x) {
-      const unsigned long long c = __ldcg(&list[j]);
-      float s[1] = {score_of(c)};
-      f(index_of(c), s);
+    for (int j = threadIdx.x; j < n; j += V * blockDim.x) {
+      unsigned long long c[V];
+      float s[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = j + v * static_cast<int>(blockDim.x) < n ? __ldcg(&list[j + v * blockDim.x]) : 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[v] = c[v] != 0 ? score_of(c[v]) : -INFINITY;
+      int at[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) at[v] = index_of(c[v]);
+      f(at, s);
     }
   }
 };
@@ -392,14 +411,6 @@ __device__ __forceinline__ void clear_bins(const Team& t, Shared& sh, bool mass)
     if (mass) sh.lo[b] = sh.hi[b] = 0;
   }
   __syncthreads();
-}
-
-__device__ __forceinline__ void add_mass(Shared& sh, int b, unsigned long long w) {
-  // shared memory adds 32 bits at a time: the carry goes to the upper half
-  const unsigned lo = static_cast<unsigned>(w);
-  const unsigned old = atomicAdd(&sh.lo[b], lo);
-  const unsigned hi = static_cast<unsigned>(w >> 32) + (old + lo < old ? 1u : 0u);
-  if (hi != 0) atomicAdd(&sh.hi[b], hi);
 }
 
 // The team's bins of this stage, merged, in sh.count and (kMass) sh.mass.
@@ -504,15 +515,80 @@ __device__ void find_bin(const Team& t, Shared& sh, unsigned long long need) {
   __syncthreads();
 }
 
-// sh.list[0 .. n), descending.
+// sh.list[0 .. n), descending; entries differ.
+constexpr unsigned kRanked = 256;
+
+// Bitonic, E entries a thread (entry e blockDim + thread): exchanges within a warp by
+// shuffles, within a thread in registers, others through sh.list.
+template <int E>
+__device__ void sort_registers(Shared& sh, unsigned n) {
+  unsigned long long v[E];
+  const unsigned threads = blockDim.x, width = E * threads;
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = e * threads + threadIdx.x < n ? sh.list[e * threads + threadIdx.x] : 0;
+  for (unsigned k = 2; k <= width; k *= 2)
+    for (unsigned j = k / 2; j > 0; j /= 2) {
+      if (j >= threads) {
+        // both are this thread's
+#pragma unroll
+        for (int d = 1; d < E; d *= 2) {
+          if (j != d * threads) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int o = e ^ d;
+            if (o < e) continue;
+            const unsigned long long lo = min(v[e], v[o]), hi = max(v[e], v[o]);
+            const bool desc = ((e * threads + threadIdx.x) & k) == 0;
+            v[e] = desc ? hi : lo;
+            v[o] = desc ? lo : hi;
+          }
+        }
+        continue;
+      }
+      if (j >= 32) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) sh.list[e * threads + threadIdx.x] = v[e];
+        __syncthreads();
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const unsigned i = e * threads + threadIdx.x;
+        const unsigned long long w = j >= 32 ? sh.list[i ^ j] : __shfl_xor_sync(~0u, v[e], j);
+        // the lower of a descending pair keeps the larger value, and so does the upper of an ascending one
+        v[e] = ((i & k) == 0) == ((i & j) == 0) ? max(v[e], w) : min(v[e], w);
+      }
+    }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) sh.list[e * threads + threadIdx.x] = v[e];
+  __syncthreads();
+}
+
 __device__ void sort_list(Shared& sh, unsigned n) {
+  const unsigned threads = blockDim.x;
+  if (n <= kRanked && n <= threads) {
+    // an entry's place is the number of larger ones
+    const unsigned long long v = threadIdx.x < n ? sh.list[threadIdx.x] : 0;
+    unsigned rank = 0;
+    if (threadIdx.x < n)
+      for (unsigned j = 0; j < n; ++j) rank += sh.list[j] > v;
+    __syncthreads();
+    if (threadIdx.x < n) sh.list[rank] = v;
+    __syncthreads();
+    return;
+  }
+  if (n <= threads) return sort_registers<1>(sh, n);
+  if (n <= 2 * threads) return sort_registers<2>(sh, n);
+  if (n <= 4 * threads) return sort_registers<4>(sh, n);
+  if (n <= 8 * threads && 8 * threads <= kList) return sort_registers<8>(sh, n);
   unsigned width = 1;
   while (width < n) width *= 2;
-  for (unsigned j = n + threadIdx.x; j < width; j += blockDim.x) sh.list[j] = 0;
+  for (unsigned j = n + threadIdx.x; j < width; j += threads) sh.list[j] = 0;
   __syncthreads();
   for (unsigned k = 2; k <= width; k *= 2)
     for (unsigned j = k / 2; j > 0; j /= 2) {
-      for (unsigned q = threadIdx.x; q < width / 2; q += blockDim.x) {
+      for (unsigned q = threadIdx.x; q < width / 2; q += threads) {
         const unsigned i = 2 * q - (q & (j - 1)), o = i + j;  // the pairs that differ in bit j
         const unsigned long long u = sh.list[i], w = sh.list[o];
         if ((i & k) == 0 ? u < w : u > w) {
@@ -537,23 +613,23 @@ __device__ __forceinline__ void take_list(const Team& t, Shared& sh, const unsig
   __syncthreads();
 }
 // Mass of the first `n` entries of sh.list.
-__device__ __forceinline__ unsigned long long list_mass(Shared& sh, unsigned n, float top, float unit) {
+__device__ __forceinline__ unsigned long long list_mass(Shared& sh, unsigned n, float top) {
   unsigned long long sum = 0;
-  for (unsigned j = threadIdx.x; j < n; j += blockDim.x) sum += fixed_weight(score_of(sh.list[j]), top, unit);
+  for (unsigned j = threadIdx.x; j < n; j += blockDim.x) sum += fixed_weight(score_of(sh.list[j]), top);
   return block_sum(sum, sh);
 }
 // The entry of the sorted list (of n >= 1) at which the running mass reaches `need`; the last one
 // where rounding leaves less.
-__device__ __forceinline__ unsigned mass_reaches(Shared& sh, unsigned n, unsigned long long need, float top, float unit) {
+__device__ __forceinline__ unsigned mass_reaches(Shared& sh, unsigned n, unsigned long long need, float top) {
   const unsigned span = (n + blockDim.x - 1) / blockDim.x, first = threadIdx.x * span;
   unsigned long long mine = 0;
-  for (unsigned j = first; j < min(first + span, n); ++j) mine += fixed_weight(score_of(sh.list[j]), top, unit);
+  for (unsigned j = first; j < min(first + span, n); ++j) mine += fixed_weight(score_of(sh.list[j]), top);
   unsigned long long at = block_below(mine, sh);
   if (threadIdx.x == 0) sh.found = n - 1;
   __syncthreads();
   if (at < need && at + mine >= need)
     for (unsigned j = first; j < min(first + span, n); ++j) {
-      at += fixed_weight(score_of(sh.list[j]), top, unit);
+      at += fixed_weight(score_of(sh.list[j]), top);
       if (at >= need) {
         sh.found = j;
         break;
@@ -579,10 +655,27 @@ struct Bins {
 
 // The bin that holds the `need`-th largest of the threads' own maxima (-infinity: none), one a
 // thread; all entries in bins up to it are at least `need`.  -1 where there are not so many.
-__device__ bool bin_of_maxima(Team& t, Shared& sh, Bins bins, unsigned long long need, float mine, int* bin) {
+// all: the CTA's number of entries (kList + 1 or more where it is not known); where the team's
+// are not many more than `need`, the bin is the last one: all of them.
+__device__ bool bin_of_maxima(Team& t, Shared& sh, Bins bins, unsigned long long need, float mine, unsigned all,
+                              int* bin) {
   clear_bins(t, sh, false);
   if (mine > -INFINITY) atomicAdd(&sh.count[bins.of(mine)], 1u);
+  __syncthreads();
+  const unsigned entries = min(all, static_cast<unsigned>(kList) + 1u);
+  if (t.size > 1) {
+    if (threadIdx.x == 0) t.g->entries[t.rank] = entries;
+  }
   if (!merge_bins<false>(t, sh)) return false;
+  unsigned total = entries;
+  if (t.size > 1) {
+    unsigned long long v = threadIdx.x < static_cast<unsigned>(t.size) ? __ldcg(&t.g->entries[threadIdx.x]) : 0;
+    total = static_cast<unsigned>(block_sum(v, sh));
+  }
+  if (total <= max(2ull * need, static_cast<unsigned long long>(kRanked)) && total <= kList) {
+    *bin = t.bins - 1;
+    return true;
+  }
   find_bin<false>(t, sh, need);
   *bin = sh.in > 0 ? static_cast<int>(sh.bin) : -1;
   return true;
@@ -595,29 +688,36 @@ __device__ __forceinline__ void collect(const Src& src, const Team& t, Bins bins
                                         unsigned capacity) {
   constexpr int V = Src::V;
   if (!(mine > -INFINITY) || bins.of(mine) > bin) return;  // nor is any other of its values that large
-  src.template walk<1>(t, [&](int i0, float(&s)[V]) {
-    get(i0, s);
+  // most values are told apart by an interval half a bin wider
+  const float from = kAbove || bin == 0 ? INFINITY : bins.from - (static_cast<float>(bin) - 0.5f) / bins.scale;
+  const float to = static_cast<float>(bin) == bins.last || bins.scale == 0.0f
+                       ? -FLT_MAX
+                       : bins.from - (static_cast<float>(bin) + 1.5f) / bins.scale;
+  src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+    get(at, s);
     unsigned hit = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v)
-      if (s[v] > -INFINITY) {
-        const int b = bins.of(s[v]);
-        if (kAbove ? b <= bin : b == bin) hit |= 1u << v;
-      }
-    if (hit == 0) return;
+      if (s[v] >= to && s[v] <= from) hit |= 1u << v;
+    while (hit != 0) {
+      const int v = __ffs(hit) - 1;
+      hit &= hit - 1;
+      float value = s[0];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!(hit >> v & 1u)) continue;
-      const unsigned long long c = composite(ordered(s[v]), i0 + v), high = c >> shift;
-      if ((kAbove && bins.of(s[v]) < bin) || (kAbove ? high >= prefix : high == prefix)) {
-        const unsigned at = atomicAdd(listed, 1u);
-        if (at < capacity) list[at] = c;
+      for (int e = 1; e < V; ++e)
+        if (e == v) value = s[e];
+      const int b = bins.of(value);
+      if (b > bin || (!kAbove && b != bin)) continue;
+      const unsigned long long c = composite(ordered(value), at[v]), high = c >> shift;
+      if (b < bin || (kAbove ? high >= prefix : high == prefix)) {
+        const unsigned to_at = atomicAdd(listed, 1u);
+        if (to_at < capacity) list[to_at] = c;
       }
     }
   });
 }
 
-// Selects from the values that get() gives: get(i0, s) turns the scores of a group into
+// Selects from the values that get() gives: get(at, s) turns the scores of a group into
 // values, -infinity for entries that do not take part.
 //   kMass = false: the `need`-th largest composite; kAbove: the `need` largest
 //   kMass = true:  the composite at which the mass reaches `share` of all
@@ -626,7 +726,7 @@ __device__ __forceinline__ void collect(const Src& src, const Team& t, Bins bins
 // reach that far, all are kept).  kAbove: sh.listed entries, on rank 0 only, and no edge.
 template <bool kMass, bool kAbove, typename Src, typename Get>
 __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use, Bins bins, unsigned long long need,
-                                    float share, float top, float unit, float mine, Get get,
+                                    float share, float top, float mine, Get get,
                                     unsigned long long* edge) {
   constexpr int V = Src::V;
   *edge = 0;
@@ -634,15 +734,29 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   unsigned* listed = t.size > 1 ? &t.g->listed[use] : &sh.listed;
   if (threadIdx.x == 0) sh.listed = 0;
   clear_bins(t, sh, kMass);
-  src.template walk<1>(t, [&](int i0, float(&s)[V]) {
-    get(i0, s);
+  src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+    get(at, s);
+    int b[V];
+    uint32_t w[V], old[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+      b[v] = bins.of(s[v]);
+      if (kMass) w[v] = fixed_weight(s[v], top);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      old[v] = 0;
       if (s[v] > -INFINITY) {
-        const int b = bins.of(s[v]);
-        atomicAdd(&sh.count[b], 1u);
-        if (kMass) add_mass(sh, b, fixed_weight(s[v], top, unit));
+        atomicAdd(&sh.count[b[v]], 1u);
+        if (kMass) old[v] = atomicAdd(&sh.lo[b[v]], w[v]);
       }
+    }
+    if (kMass) {
+      // shared memory adds 32 bits at a time: carries go to the upper half
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (s[v] > -INFINITY && old[v] + w[v] < old[v]) atomicAdd(&sh.hi[b[v]], 1u);
+    }
   });
   if (!merge_bins<kMass>(t, sh)) return false;
   if (kMass) {
@@ -670,16 +784,19 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
     const int bits = min(31 - __clz(t.bins), shift);
     shift -= bits;
     clear_bins(t, sh, kMass);
-    src.template walk<1>(t, [&](int i0, float(&s)[V]) {
-      get(i0, s);
+    src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+      get(at, s);
 #pragma unroll 1
       for (int v = 0; v < V; ++v) {
         if (!(s[v] > -INFINITY) || bins.of(s[v]) != bin) continue;
-        const unsigned long long c = composite(ordered(s[v]), i0 + v);
+        const unsigned long long c = composite(ordered(s[v]), at[v]);
         if ((c >> (shift + bits)) != prefix) continue;
         const int b = t.bins - 1 - static_cast<int>((c >> shift) & ((1u << bits) - 1u));
         atomicAdd(&sh.count[b], 1u);
-        if (kMass) add_mass(sh, b, fixed_weight(s[v], top, unit));
+        if (kMass) {
+          const uint32_t w = fixed_weight(s[v], top), old = atomicAdd(&sh.lo[b], w);
+          if (old + w < old) atomicAdd(&sh.hi[b], 1u);
+        }
       }
     });
     if (!merge_bins<kMass>(t, sh)) return false;
@@ -696,7 +813,7 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   const unsigned have = sh.listed;
   sort_list(sh, have);
   if (kAbove) return true;
-  *edge = kMass ? sh.list[mass_reaches(sh, have, need, top, unit)] : sh.list[need - 1];
+  *edge = kMass ? sh.list[mass_reaches(sh, have, need, top)] : sh.list[need - 1];
   __syncthreads();
   return true;
 }
@@ -719,7 +836,7 @@ __device__ __forceinline__ void join_stats(float& m, float& z, float m2, float z
 struct Ctx {
   const float* noise;
   Rule r;
-  float top, logz, unit;
+  float top, logz;
   long long row;
 };
 
@@ -737,6 +854,39 @@ struct Edge {
   __device__ __forceinline__ bool keeps(float v, int at) const { return v > s || (v == s && at <= i); }
 };
 
+// What a selection goes by: scores as they are, those of kept entries, draw values of kept ones.
+struct All {
+  template <int V>
+  __device__ __forceinline__ void operator()(const int (&)[V], float (&)[V]) const {}
+};
+struct Kept {
+  Edge edge;
+  template <int V>
+  __device__ __forceinline__ void operator()(const int (&at)[V], float (&s)[V]) const {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (!edge.keeps(s[v], at[v])) s[v] = -INFINITY;
+  }
+};
+struct Draws {
+  Edge edge;
+  const float* noise;
+  float top, log_min;
+  template <int V>
+  __device__ __forceinline__ void operator()(const int (&at)[V], float (&s)[V]) const {
+    float g[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (!(edge.keeps(s[v], at[v]) && __fsub_rn(s[v], top) >= log_min)) s[v] = -INFINITY;
+      g[v] = 0.0f;
+      if (s[v] > -INFINITY) g[v] = __ldg(noise + at[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (s[v] > -INFINITY) s[v] = draw_value(s[v], g[v]);
+  }
+};
+
 __device__ __forceinline__ void put(const SampleArgs& a, const Ctx& x, int j, int index, float s) {
   a.out_index[x.row * a.m + j] = index;
   a.out_logprob[x.row * a.m + j] = x.r.greedy ? 0.0f : __fsub_rn(s, x.top) - x.logz;
@@ -747,7 +897,7 @@ template <typename T>
 __device__ void finish_list(const SampleArgs& a, Shared& sh, const Ctx& x, const Row<T>& src) {
   unsigned keep = min(sh.listed, x.r.k);
   if (x.r.p < 1.0f)
-    keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.top, x.unit)), x.top, x.unit) + 1;
+    keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.top)), x.top) + 1;
   if (x.r.log_min > -INFINITY) {
     unsigned long long mine = 0;
     for (unsigned j = threadIdx.x; j < keep; j += blockDim.x)
@@ -783,44 +933,36 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
   Edge edge;
   unsigned long long found;
   if (x.r.k != 0) {
-    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.top, 0.0f, mine, [](int, float(&)[V]) {}, &found))
+    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.top, mine, All(), &found))
       return false;
     edge.raise(found);
   }
   if (x.r.p < 1.0f) {
-    auto scores = [=](int i0, float(&s)[V]) {
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (!edge.keeps(s[v], i0 + v)) s[v] = -INFINITY;
-    };
-    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.top, x.unit, mine, scores, &found)) return false;
+    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.top, mine, Kept{edge}, &found)) return false;
     edge.raise(found);
   }
-  // Draw values of the kept entries.
-  auto draws = [edge, noise = x.noise, top = x.top, log_min = x.r.log_min](int i0, float(&s)[V]) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const bool in = edge.keeps(s[v], i0 + v) && __fsub_rn(s[v], top) >= log_min;
-      s[v] = in ? draw_value(s[v], noise[i0 + v]) : -INFINITY;
-    }
-  };
+  const Draws draws = {edge, x.noise, x.top, x.r.log_min};
   // The thread's largest draw value.  A thread whose largest score is cut has none.
-  int at = 0;
+  int key_at = 0;
+  unsigned long long entries = kList + 1;
   if (mine_key != mine_key) {
+    entries = 0;
     mine_key = -INFINITY;
     if (mine >= edge.s && __fsub_rn(mine, x.top) >= x.r.log_min)
-      src.template walk<1>(t, [&](int i0, float(&s)[V]) {
-        draws(i0, s);
+      src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+        draws(at, s);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (s[v] > mine_key || (V == 1 && s[v] == mine_key && i0 < at)) {  // a row's indices grow
+        for (int v = 0; v < V; ++v) {
+          entries += s[v] > -INFINITY;
+          if (s[v] > mine_key || (s[v] == mine_key && s[v] > -INFINITY && at[v] < key_at)) {
             mine_key = s[v];
-            at = i0 + v;
+            key_at = at[v];
           }
+        }
       });
   }
   if (a.m == 1) {
-    unsigned long long best = mine_key > -INFINITY ? composite(ordered(mine_key), at) : 0;
+    unsigned long long best = mine_key > -INFINITY ? composite(ordered(mine_key), key_at) : 0;
     best = block_max(best, sh);
     if (t.size > 1) {
       if (threadIdx.x == 0) t.g->best[t.rank] = best;
@@ -834,12 +976,13 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
   // Gumbel noise puts the largest keys within a few units of the best score, and ln n above it.
   const float last = static_cast<float>(t.bins - 1);
   const Bins by_key = {x.top + 24.0f, last / 48.0f, last};
+  const unsigned kept = static_cast<unsigned>(block_sum(entries, sh));
   // More than m threads: the m-th of their maxima bounds the m-th draw from below, and few
   // entries beside the draws lie above it.
   bool done = false;
   if (a.m <= t.size * static_cast<int>(blockDim.x) / 2) {
     int bin;
-    if (!bin_of_maxima(t, sh, by_key, a.m, mine_key, &bin)) return false;
+    if (!bin_of_maxima(t, sh, by_key, a.m, mine_key, kept, &bin)) return false;
     if (bin >= 0) {
       unsigned long long* list = t.size > 1 ? t.g->list[1] : sh.list;  // top-p's is read by now
       unsigned* listed = t.size > 1 ? &t.g->listed[3] : &sh.listed;
@@ -856,7 +999,7 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
       __syncthreads();
     }
   }
-  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.top, 0.0f, mine_key, draws, &found))
+  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.top, mine_key, draws, &found))
     return false;
   if (t.rank != 0) return true;
   const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
@@ -886,17 +1029,14 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
   const bool uncut = x.r.k == 0 && x.r.p >= 1.0f && x.r.log_min == -INFINITY;
   const bool direct = uncut && (a.m == 1 || x.r.greedy);
 
-  // Pass 1: maximum, minimum and sum of exponentials, each lane's own, then joined in a fixed order.
-  float top = -INFINITY, z = 0.0f, low = INFINITY;
+  // Pass 1: maximum and sum of exponentials, each lane's own, then joined in a fixed order.
+  float top = -INFINITY, z = 0.0f;
   float best_key = -INFINITY;
   int best_at = 0;
-  auto first = [&](int i0, float(&s)[V]) {
+  auto first = [&](const int(&at)[V], float(&s)[V]) {
     float b = top;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      b = fmaxf(b, s[v]);
-      low = fminf(low, s[v] > -INFINITY ? s[v] : INFINITY);
-    }
+    for (int v = 0; v < V; ++v) b = fmaxf(b, s[v]);
     if (b == -INFINITY) return;
     if (b > top) {
       z *= __expf(top - b);
@@ -905,20 +1045,27 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
 #pragma unroll
     for (int v = 0; v < V; ++v) z += __expf(s[v] - top);
     if (uncut) {
+      float g[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (s[v] > -INFINITY) {
-          const float k = x.r.greedy ? s[v] : draw_value(s[v], x.noise[i0 + v]);
-          if (k > best_key) {  // indices grow: the first of equal ones stays
-            best_key = k;
-            best_at = i0 + v;
-          }
+      for (int v = 0; v < V; ++v) {
+        g[v] = 0.0f;
+        if (s[v] > -INFINITY && !x.r.greedy) g[v] = __ldg(x.noise + at[v]);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!(s[v] > -INFINITY)) continue;
+        const float k = x.r.greedy ? s[v] : draw_value(s[v], g[v]);
+        if (k > best_key) {  // indices grow: the first of equal ones stays
+          best_key = k;
+          best_at = at[v];
         }
+      }
     }
   };
-  if (uncut) row.template walk<2>(t, first);
-  else row.template walk<sizeof(T) == 4 ? 4 : 2>(t, first);
+  if (uncut) row.template walk<1>(t, first);
+  else row.template walk<2>(t, first);
   const float mine = top;
+  float low = mine > -INFINITY ? mine : INFINITY;  // least of the lanes' maxima
   unsigned long long best = best_key > -INFINITY ? composite(ordered(best_key), best_at) : 0;
   auto join_lanes = [&]() {
 #pragma unroll
@@ -994,13 +1141,9 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
     return true;
   }
-  int log_n = 0;
-  while ((1ll << log_n) < a.n) ++log_n;
-  x.unit = static_cast<float>(1ull << (62 - log_n));
-
-  // Scores more than 40 below the best share the last bin: their mass is nothing, and only
-  // a top-k of a very peaked row looks there.
-  const float range = fminf(__fsub_rn(x.top, sh.low), 40.0f), last = static_cast<float>(t.bins - 1);
+  // Bins reach four times as far down as the least of the threads' maxima, which covers a row of
+  // any usual shape; what lies below shares the last bin.  Further than 40 there is no mass.
+  const float range = fminf(4.0f * __fsub_rn(x.top, sh.low), 40.0f), last = static_cast<float>(t.bins - 1);
   const Bins by_score = {x.top, range > 0.0f ? fminf(last / range, 1e30f) : 0.0f, last};
 
   // A top-k of less than half as many entries as threads: the k-th of the threads' maxima bounds the
@@ -1009,14 +1152,14 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
   const long long threads = static_cast<long long>(t.size) * blockDim.x;
   if (x.r.k != 0 && 2ll * x.r.k <= threads) {
     int bin;
-    if (!bin_of_maxima(t, sh, by_score, x.r.k, mine, &bin)) return false;
+    if (!bin_of_maxima(t, sh, by_score, x.r.k, mine, kList + 1, &bin)) return false;
     if (bin >= 0) {
       unsigned long long* list = t.size > 1 ? t.g->large : sh.list;
       unsigned* listed = t.size > 1 ? &t.g->listed[0] : &sh.listed;
       const unsigned capacity = t.size > 1 ? kLarge : kList;
       if (threadIdx.x == 0) sh.listed = 0;
       __syncthreads();
-      collect<true>(row, t, by_score, bin, mine, kIndexBits + 32, 0, [](int, float(&)[V]) {}, list, listed, capacity);
+      collect<true>(row, t, by_score, bin, mine, kIndexBits + 32, 0, All(), list, listed, capacity);
       if (!team_sync(t, sh)) return false;
       const unsigned have = t.size > 1 ? __ldcg(listed) : sh.listed;
       if (have <= capacity) {
@@ -1030,7 +1173,10 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
         // more than can be sorted: the same selections, from the candidates and by this CTA alone
         const Candidates src = {list, static_cast<int>(have)};
         float own = -INFINITY;
-        src.walk<1>(t, [&](int, float(&s)[1]) { own = fmaxf(own, s[0]); });
+        src.walk<1>(t, [&](const int(&)[Candidates::V], float(&s)[Candidates::V]) {
+#pragma unroll
+          for (int v = 0; v < Candidates::V; ++v) own = fmaxf(own, s[v]);
+        });
         Team alone = t;
         alone.size = 1;
         return finish_select(a, alone, sh, x, row, src, by_score, own, __int_as_float(0x7FFFFFFF));
@@ -1047,7 +1193,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
 }
 
 template <typename T>
-__global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size, int bins) {
+__global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size, int bins, int cluster) {
   extern __shared__ __align__(16) unsigned char smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
   Team t;
@@ -1055,6 +1201,7 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
   t.rank = blockIdx.x % team_size;
   t.g = team_size > 1 ? static_cast<TeamMem*>(a.ws) + blockIdx.x / team_size : nullptr;
   t.err = a.err;
+  t.cluster = cluster != 0;
   t.barriers = 0;
   t.stage = 0;
   t.bins = bins;
@@ -1063,21 +1210,68 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
 
 bool by_warp(long long n, int m) { return n <= kWarpMaxN && m <= kWarpMaxM; }
 
-// CTAs per row: all SMs divided over the rows, but no CTA with less than 4,096 entries (one row of
-// 50,021 with top-p: 35 us by 13 CTAs, 55 by two).
-int team_of(long long rows, long long n, int sms) {
-  if (rows * 2 > sms) return 1;
+constexpr int kMaxCluster = 16;
+
+size_t row_smem() { return sizeof(Shared); }
+
+// Clusters of `size` CTAs that the device holds at once (0: none, or no device).
+int resident_clusters(int size) {
+  static std::atomic<int> known[kMaxCluster + 1];  // 0: not asked yet, else one more than the number
+  int v = known[size].load(std::memory_order_relaxed);
+  if (v == 0) {
+    auto kernel = k_sample_row<float>;
+    int n = 0;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = size;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(size);
+    cfg.blockDim = dim3(1024);
+    cfg.dynamicSmemBytes = row_smem();
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (allow_smem(reinterpret_cast<const void*>(kernel), row_smem()) != cudaSuccess ||
+        cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+            cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      cudaGetLastError();  // no device: nothing sticks
+      n = 0;
+    }
+    v = n + 1;
+    known[size].store(v, std::memory_order_relaxed);
+  }
+  return v - 1;
+}
+
+// CTAs of a team: all SMs divided over the rows, but no CTA with less than 4,096 entries (one row of
+// 50,021 with top-p: 35 us by 13 CTAs, 55 by two).  Teams are clusters, whose barrier takes a
+// tenth of one in global memory (0.3 us against 3), of the largest size of which the device
+// holds one for every row; where these would use less than two thirds of the SMs that a
+// barrier in global memory could, it is that.  (8 rows of 1,048,576 scores: eight clusters of 16
+// are not resident at once and take two turns, 157 us with top-p against 81.)
+struct TeamPlan {
+  int size;
+  bool cluster;
+};
+TeamPlan team_of(long long rows, long long n, int sms) {
+  if (rows * 2 > sms) return {1, false};
   long long t = sms / rows;
   t = t < (n + 4095) / 4096 ? t : (n + 4095) / 4096;
   t = t < kMaxTeam ? t : kMaxTeam;
-  return static_cast<int>(t < 1 ? 1 : t);
+  if (t < 2) return {1, false};
+  int c = t < kMaxCluster ? static_cast<int>(t) : kMaxCluster;
+  while (c > 1 && resident_clusters(c) < rows) --c;
+  if (c > 1 && 3 * c >= 2 * t) return {c, true};
+  return {static_cast<int>(t), false};
 }
 
 }  // namespace
 
 size_t sample_workspace(int, long long rows, long long n, int m, int sms) {
   if (rows == 0 || by_warp(n, m)) return 0;
-  return team_of(rows, n, sms) > 1 ? up256(sizeof(TeamMem) * static_cast<size_t>(rows)) : 0;
+  return team_of(rows, n, sms).size > 1 ? up256(sizeof(TeamMem) * static_cast<size_t>(rows)) : 0;
 }
 
 cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cudaStream_t st) {
@@ -1093,13 +1287,17 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
       if (per <= 8) return launch_pdl(k_sample_warp<T, 8>, grid, dim3(128), 0, st, a);
       return launch_pdl(k_sample_warp<T, 16>, grid, dim3(128), 0, st, a);
     }
-    const int team = team_of(a.rows, a.n, sms);
-    const size_t smem = sizeof(Shared);
+    const TeamPlan plan = team_of(a.rows, a.n, sms);
+    const int team = plan.size;
+    const size_t smem = row_smem();
     cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_sample_row<T>), smem);
     if (e != cudaSuccess) return e;
     // small CTAs for short rows: several share an SM, and barriers take fewer warps
-    const int threads = a.n <= 4096 ? 128 : a.n <= 16384 ? 256 : a.n <= 32768 ? 512 : 1024;
-    const int bins = a.n <= 16384 ? 512 : kBins;
+    // (many draws want threads to sort them)
+    int threads = a.n <= 4096 ? 128 : a.n <= 16384 ? 256 : a.n <= 32768 ? 512 : 1024;
+    while (threads < 1024 && threads * 4 < a.m) threads *= 2;
+    if (team > 1) threads = 1024;
+    const int bins = a.n <= 16384 && threads <= 512 ? 512 : kBins;  // a multiple of the threads
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
@@ -1107,19 +1305,29 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
     if (team == 1) {
       cfg.gridDim = dim3(static_cast<unsigned>(a.rows));
       ++*launches;
-      return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, 1, bins);
+      return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, 1, bins, 0);
+    }
+    cfg.gridDim = dim3(static_cast<unsigned>(team * a.rows));
+    cudaLaunchAttribute attr[1];
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    ++*launches;
+    if (plan.cluster) {
+      e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k_sample_row<T>),
+                               cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = team;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, team, bins, 1);
     }
     // the barriers' counters start from zero
     e = cudaMemset2DAsync(a.ws, sizeof(TeamMem), 0, 16, static_cast<size_t>(a.rows), st);
     if (e != cudaSuccess) return e;
-    cfg.gridDim = dim3(static_cast<unsigned>(team * a.rows));
-    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeCooperative;
     attr[0].val.cooperative = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    ++*launches;
-    return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, team, bins);
+    return cudaLaunchKernelEx(&cfg, k_sample_row<T>, a, team, bins, 0);
   });
 }
 

@@ -334,18 +334,37 @@ def merge_topk(scores, indices, k: int, out=None, stream=None):
 # Sequence-model operators
 # ---------------------------------------------------------------------------
 
-_DTYPES = {}
+# These calls are short: a small draw or lookup takes the GPU about 5 us, so the checks
+# here go by attributes that cost next to nothing.
+
+_torch = None
+_DTYPES: dict = {}
+_raw_stream = None
 
 
-def _dtype_code(t) -> int:
-    if not _DTYPES:
+def _setup():
+    """The library and, once, what the calls below need of torch."""
+    global _torch, _raw_stream
+    if _torch is None:
         import torch
 
         _DTYPES.update({torch.float32: MLT_F32, torch.bfloat16: MLT_BF16, torch.float16: MLT_F16})
-    try:
-        return _DTYPES[t.dtype]
-    except KeyError:
-        raise TypeError(f"float32, bfloat16 or float16 wanted, got {t.dtype}") from None
+        # the handle of the current stream without building a Stream object
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _torch = torch
+    return _lib or lib()
+
+
+def _stream_of(t, stream):
+    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _dtype_code(t) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"float32, bfloat16 or float16 wanted, got {t.dtype}")
+    return code
 
 
 def _need(ok: bool, what: str) -> None:
@@ -354,9 +373,7 @@ def _need(ok: bool, what: str) -> None:
 
 
 def _cuda(t, name: str, dtype=None):
-    import torch
-
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and (dtype is None or t.dtype == dtype)):
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and (dtype is None or t.dtype == dtype)):
         raise TypeError(f"{name} must be a CUDA tensor" + (f" of {dtype}" if dtype is not None else ""))
     return t
 
@@ -365,9 +382,10 @@ def _rows(t, name: str) -> int:
     """Elements between the rows of a matrix whose columns are adjacent."""
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    stride, column = t.stride()
+    if column != 1 and t.shape[1] > 1:
         raise ValueError(f"{name} must have adjacent columns")
-    return t.stride(0)
+    return stride
 
 
 _ws_bytes: dict = {}
@@ -386,9 +404,7 @@ def _workspace(key, query, device, stream):
         n = _ws_bytes[key] = out.value
     if n == 0:
         return None, 0
-    import torch
-
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws = _torch.empty(n, dtype=_torch.uint8, device=device)
     if stream is not None:
         ws.record_stream(stream)
     return ws, n
@@ -414,11 +430,11 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
     numbers -ln(-ln u)).  `rules` (sample_rules) gives every row its own
     cuts instead of the four numbers.  Returns (index [rows][m] int64, -1
     past the last kept entry, logprob [rows][m] fp32)."""
-    import torch
-
+    L = _setup()
+    torch = _torch
     _cuda(scores, "scores")
-    code = _dtype_code(scores)
     _cuda(noise, "noise", torch.float32)
+    code = _dtype_code(scores)
     one = scores.dim() == 1
     if one:
         scores, noise = scores[None], noise[None] if noise.dim() == 1 else noise
@@ -427,67 +443,70 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
     stride, noise_stride = _rows(scores, "scores"), _rows(noise, "noise")
     rows, n = scores.shape
     m = int(m)
-    rule = None
+    rule = each = None
     if rules is None:
         rule = C.byref(SampleRule(temperature, top_k, top_p, min_p))
     else:
         _cuda(rules, "rules", torch.int32)
         if rules.shape != (rows, 4) or not rules.is_contiguous():
             raise ValueError("rules must be a contiguous int32 tensor [rows][4]")
-    L = lib()
+        each = rules.data_ptr()
+    device = scores.device
     if out is None:
-        index = torch.empty((rows, m), dtype=torch.int64, device=scores.device)
-        logprob = torch.empty((rows, m), dtype=torch.float32, device=scores.device)
+        index = torch.empty((rows, m), dtype=torch.int64, device=device)
+        logprob = torch.empty((rows, m), dtype=torch.float32, device=device)
     else:
         index, logprob = out
         for t, dt in ((index, torch.int64), (logprob, torch.float32)):
             _cuda(t, "out", dt)
             _need(t.is_contiguous() and t.numel() == rows * m, "out must be contiguous [rows][m] tensors")
     ws, n_ws = _workspace(("sample", code, rows, n, m),
-                          lambda b: L.mlt_sample_workspace(code, rows, n, m, C.byref(b)), scores.device, stream)
-    _check(L.mlt_sample(_stream_ptr(stream), scores.data_ptr(), code, rows, n, stride, noise.data_ptr(), noise_stride,
-                        rule, None if rules is None else rules.data_ptr(), m, None if ws is None else ws.data_ptr(),
-                        n_ws, index.data_ptr(), logprob.data_ptr()))
+                          lambda b: L.mlt_sample_workspace(code, rows, n, m, C.byref(b)), device, stream)
+    rc = L.mlt_sample(_stream_of(scores, stream), scores.data_ptr(), code, rows, n, stride, noise.data_ptr(),
+                      noise_stride, rule, each, m, None if ws is None else ws.data_ptr(), n_ws, index.data_ptr(),
+                      logprob.data_ptr())
+    if rc:
+        _check(rc)
     return (index[0], logprob[0]) if one and out is None else (index, logprob)
 
 
 def _ids(ids):
-    import torch
-
     _cuda(ids, "ids")
-    if ids.dtype not in (torch.int64, torch.int32):
+    dtype = ids.dtype
+    if dtype != _torch.int64 and dtype != _torch.int32:
         raise TypeError("ids must be int32 or int64")
-    _need(ids.is_contiguous(), "ids must be contiguous")
-    return 1 if ids.dtype == torch.int64 else 0
+    if not ids.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return 1 if dtype == _torch.int64 else 0
 
 
 def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None):
     """mlt_embed: scale * table[ids], rounded once to `out_dtype` (default: the
     table's); ids of any shape, negative ones give zeros."""
-    import torch
-
+    L = _setup()
     ids_64 = _ids(ids)
     _cuda(table, "table")
     code, stride = _dtype_code(table), _rows(table, "table")
     vocab, dim = table.shape
     if out is None:
-        out = torch.empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
+        out = _torch.empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
         out_stride = dim
     else:
         _cuda(out, "out")
         _need(tuple(out.shape) == (*ids.shape, dim), "out must have the shape of ids and one more dimension, dim")
         flat = out if out.dim() == 2 else out.view(-1, dim)
         out_stride = _rows(flat, "out")
-    _check(lib().mlt_embed(_stream_ptr(stream), table.data_ptr(), code, vocab, dim, stride, ids.data_ptr(), ids_64,
-                           ids.numel(), scale, out.data_ptr(), _dtype_code(out), out_stride))
+    rc = L.mlt_embed(_stream_of(table, stream), table.data_ptr(), code, vocab, dim, stride, ids.data_ptr(), ids_64,
+                     ids.numel(), scale, out.data_ptr(), _dtype_code(out), out_stride)
+    if rc:
+        _check(rc)
     return out
 
 
 def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, out=None, stream=None):
     """mlt_embed_grad: the gradient [vocab][dim] of embed's table from that of
     its output; the same from call to call."""
-    import torch
-
+    L = _setup()
     ids_64 = _ids(ids)
     _cuda(grad_out, "grad_out")
     dim = grad_out.shape[-1]
@@ -496,24 +515,23 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
     code, stride = _dtype_code(flat), _rows(flat, "grad_out")
     vocab, tokens = int(vocab), ids.numel()
     if out is None:
-        out = torch.empty((vocab, dim), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
+        out = _torch.empty((vocab, dim), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
     else:
         _cuda(out, "out")
         _need(tuple(out.shape) == (vocab, dim), "out must be [vocab][dim]")
-    L = lib()
     ws, n_ws = _workspace(("embed_grad", tokens, vocab, dim),
                           lambda b: L.mlt_embed_grad_workspace(tokens, vocab, dim, C.byref(b)), out.device, stream)
-    _check(L.mlt_embed_grad(_stream_ptr(stream), flat.data_ptr(), code, stride, ids.data_ptr(), ids_64, tokens, vocab,
+    _check(L.mlt_embed_grad(_stream_of(out, stream), flat.data_ptr(), code, stride, ids.data_ptr(), ids_64, tokens, vocab,
                             dim, scale, None if ws is None else ws.data_ptr(), n_ws, out.data_ptr(), _dtype_code(out),
                             _rows(out, "out")))
     return out
 
 
 def _scan_args(x, dt, B, Cm, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state):
-    import torch
-
+    torch = _torch
     _cuda(x, "x")
     a = ScanArgs()
+    dtype = x.dtype
     a.dtype = _dtype_code(x)
     _need(x.dim() == 3, "x must be [batch][length][dim]")
     b, L, d = x.shape
@@ -529,25 +547,27 @@ def _scan_args(x, dt, B, Cm, A, z, skip, dt_bias, conv_w, conv_b, lengths, state
     for name, t, shape in (("x", x, wide), ("dt", dt, wide), ("z", z, wide), ("B", B, narrow), ("C", Cm, narrow)):
         if t is None:
             continue
-        if not (t.is_cuda and t.dtype == x.dtype):
+        if not t.is_cuda or t.dtype != dtype:
             raise TypeError(f"{name} must be a CUDA tensor of x's type")
-        _need(tuple(t.shape) == shape, f"{name} must have the shape {shape}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have the shape {shape}")
         s = t.stride()
-        _need(t.numel() == 0 or ((shape[-1] == 1 or s[-1] == 1) and (t.dim() == 3 or g == 1 or s[2] == n)),
-              f"the channels of {name} must be adjacent")
+        if (s[-1] != 1 and shape[-1] > 1 or len(s) == 4 and g > 1 and s[2] != n) and t.numel() > 0:
+            raise ValueError(f"the channels of {name} must be adjacent")
         setattr(a, name, t.data_ptr())
         setattr(a, name + "_batch", s[0])
         setattr(a, name + "_step", s[1])
     f32 = torch.float32
-    for name, t, shape, dtype in (("A", A, (d, n), f32), ("skip", skip, (d,), f32), ("dt_bias", dt_bias, (d,), f32),
-                                  ("conv_w", conv_w, (d, taps), f32), ("conv_b", conv_b, (d,), f32),
-                                  ("lengths", lengths, (b,), torch.int32), ("state", state, (b, d, n), f32),
-                                  ("conv_state", conv_state, (b, max(0, taps - 1), d), x.dtype)):
+    for name, t, shape, want in (("A", A, (d, n), f32), ("skip", skip, (d,), f32), ("dt_bias", dt_bias, (d,), f32),
+                                 ("conv_w", conv_w, (d, taps), f32), ("conv_b", conv_b, (d,), f32),
+                                 ("lengths", lengths, (b,), torch.int32), ("state", state, (b, d, n), f32),
+                                 ("conv_state", conv_state, (b, max(0, taps - 1), d), dtype)):
         if t is None:
             continue
-        if not (t.is_cuda and t.dtype == dtype):
-            raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
-        _need(tuple(t.shape) == shape and t.is_contiguous(), f"{name} must be contiguous, of the shape {shape}")
+        if not t.is_cuda or t.dtype != want:
+            raise TypeError(f"{name} must be a CUDA tensor of {want}")
+        if t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, of the shape {shape}")
         setattr(a, name, t.data_ptr())
     return a
 
@@ -560,8 +580,8 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     Returns (y, state, conv_state), the last None with fewer than two taps.
     For single tokens (length 1) pass state_out=state and
     conv_state_out=conv_state to update them in place."""
-    import torch
-
+    lb = _setup()
+    torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
     b, L, d = x.shape
     y = torch.empty((b, L, d), dtype=x.dtype, device=x.device) if out is None else out
@@ -585,10 +605,9 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     a.y, a.y_batch, a.y_step = y.data_ptr(), y.stride(0), y.stride(1)
     a.state_out = state_out.data_ptr()
     a.conv_state_out = None if conv_state_out is None else conv_state_out.data_ptr()
-    lb = lib()
     ws, n_ws = _workspace(("scan", a.dtype, b, L, d, a.states, a.groups, a.taps),
                           lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)), x.device, stream)
-    _check(lb.mlt_scan(_stream_ptr(stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws))
+    _check(lb.mlt_scan(_stream_of(x, stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws))
     return y, state_out, conv_state_out
 
 
@@ -597,8 +616,8 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
     """mlt_scan_grad: the gradients of scan's inputs from those of y (`gy`) and
     of the returned state (`g_state`, or None).  Returns a dict by the names of
     the arguments (C_'s as "C"); None for inputs that were not given."""
-    import torch
-
+    lb = _setup()
+    torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
     _cuda(gy, "gy", x.dtype)
     _need(gy.shape == x.shape, "gy must have x's shape")
@@ -620,10 +639,9 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
             continue
         g[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
         setattr(q, name, g[name].data_ptr())
-    lb = lib()
     ws, n_ws = _workspace(("scan_grad", a.dtype, *x.shape, a.states, a.groups, a.taps),
                           lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device, stream)
-    _check(lb.mlt_scan_grad(_stream_ptr(stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws))
+    _check(lb.mlt_scan_grad(_stream_of(x, stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws))
     return g
 
 

@@ -150,6 +150,7 @@ def test_refusals():
         call(t, gy.half(), gs)
     with pytest.raises(ValueError):
         call(t, gy, gs[..., :8])
+    mlt._setup()
     a = mlt._scan_args(t["x"], t["dt"], t["B"], t["C"], t["A"], None, None, None, t["conv_w"], None, None, None, None)
     q = mlt.ScanGrads()
     q.gy, q.gy_step, q.gy_batch = gy.data_ptr(), 64, 320
