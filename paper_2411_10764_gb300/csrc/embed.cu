@@ -90,6 +90,18 @@ cudaError_t with_width(int v, F f) {
 // ---------------------------------------------------------------------------
 // Stable radix sort of token positions by id
 // ---------------------------------------------------------------------------
+// The warp's lanes with the caller's digit, among those `in`: a ballot for each of eight bits.
+// (__match_any_sync gives it in one instruction, but takes the SM 190 cycles a warp.)
+__device__ __forceinline__ unsigned lanes_with(uint32_t digit, bool in) {
+  unsigned peers = __ballot_sync(~0u, in);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const unsigned set = __ballot_sync(~0u, digit >> b & 1u);
+    peers &= digit >> b & 1u ? set : ~set;
+  }
+  return peers;
+}
+
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256;
@@ -100,10 +112,8 @@ int sort_per_lane(long long tokens) { return tokens > (1 << 18) ? 8 : 2; }
 struct SortPass {
   const void* ids;  // first pass: the ids themselves, else null
   int ids_64;
-  const uint32_t* keys_in;
-  const uint32_t* pos_in;
-  uint32_t* keys_out;
-  uint32_t* pos_out;
+  const uint2* in;  // (key, position) records
+  uint2* out;
   uint32_t* counts;  // [kDigits][tiles], then prefixes over the tiles
   uint32_t* totals;  // [kDigits]
   long long tokens, vocab;
@@ -113,10 +123,10 @@ struct SortPass {
 };
 
 // Ids outside [0, vocab) sort behind all others.
-__device__ __forceinline__ uint32_t sort_key(const SortPass& s, long long i) {
-  if (s.ids == nullptr) return s.keys_in[i];
+__device__ __forceinline__ uint2 sort_record(const SortPass& s, long long i) {
+  if (s.ids == nullptr) return s.in[i];
   const long long id = id_of(s.ids, s.ids_64, i);
-  return static_cast<uint32_t>(id < 0 || id >= s.vocab ? s.vocab : id);
+  return make_uint2(static_cast<uint32_t>(id < 0 || id >= s.vocab ? s.vocab : id), static_cast<uint32_t>(i));
 }
 
 template <int kPerLane>
@@ -136,7 +146,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortPass s) {
     const long long i = base + k * kSortThreads + threadIdx.x;
     if (i >= s.tokens) break;
     if (s.ids != nullptr && id_of(s.ids, s.ids_64, i) >= s.vocab) atomicOr(s.err, kErrBadToken);
-    atomicAdd(&hist[(sort_key(s, i) >> s.shift) & (kDigits - 1)], 1u);
+    atomicAdd(&hist[(sort_record(s, i).x >> s.shift) & (kDigits - 1)], 1u);
   }
   __syncthreads();
   for (int d = threadIdx.x; d < kDigits; d += kSortThreads)
@@ -178,7 +188,11 @@ __global__ void __launch_bounds__(256) k_sort_scan(uint32_t* counts, uint32_t* t
 template <int kPerLane>
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
   __shared__ uint32_t cnt[kSortWarps][kDigits];
-  __shared__ uint32_t warp_sum[kDigits / 32];
+  __shared__ uint2 warp_sum[kDigits / 32];
+  __shared__ uint32_t start[kDigits], local[kDigits];
+  extern __shared__ __align__(16) unsigned char smem[];
+  uint2* tile = reinterpret_cast<uint2*>(smem);  // the tile's records in the order of their digits
+  static_assert(kSortThreads == 2 * kDigits, "two threads a digit");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int d = lane; d < kDigits; d += 32) cnt[warp][d] = 0;
   __syncwarp();
@@ -187,17 +201,18 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
   // a warp owns kPerLane * 32 consecutive positions; rank[k] counts the
   // equal digits before the lane's k-th one within the warp
   const long long base = static_cast<long long>(blockIdx.x) * (kSortThreads * kPerLane) + warp * (kPerLane * 32) + lane;
-  uint32_t key[kPerLane], rank[kPerLane];
+  uint2 rec[kPerLane];
+  uint32_t rank[kPerLane];
 #pragma unroll
   for (int k = 0; k < kPerLane; ++k) {
     const long long i = base + k * 32;
-    key[k] = i < s.tokens ? sort_key(s, i) : 0;
+    rec[k] = i < s.tokens ? sort_record(s, i) : make_uint2(0, 0);
   }
 #pragma unroll
   for (int k = 0; k < kPerLane; ++k) {
     const bool in = base + k * 32 < s.tokens;
-    const uint32_t d = in ? (key[k] >> s.shift) & (kDigits - 1) : kDigits;
-    const unsigned peers = __match_any_sync(~0u, d);
+    const uint32_t d = (rec[k].x >> s.shift) & (kDigits - 1);
+    const unsigned peers = lanes_with(d, in);
     const unsigned before = peers & ((1u << lane) - 1u);
     uint32_t seen = 0;
     if (in) seen = cnt[warp][d];
@@ -207,40 +222,234 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
     __syncwarp();
   }
   __syncthreads();
-  // digit d's first place: digits below it, tiles before this one, warps before
+  // counts of the warps before, two threads a digit
+  {
+    constexpr int kHalf = kSortWarps / 2;
+    const int d = threadIdx.x / 2, first = (threadIdx.x & 1) * kHalf;
+    uint32_t c[kHalf], sum = 0;
+#pragma unroll
+    for (int w = 0; w < kHalf; ++w) {
+      c[w] = cnt[first + w][d];
+      sum += c[w];
+    }
+    const uint32_t other = __shfl_xor_sync(~0u, sum, 1);
+    if (first == 0) local[d] = sum + other;  // of the tile
+    uint32_t at = first > 0 ? other : 0;
+#pragma unroll
+    for (int w = 0; w < kHalf; ++w) {
+      cnt[first + w][d] = at;
+      at += c[w];
+    }
+  }
+  __syncthreads();
+  // digit d's first place: digits below it, tiles before this one; and within the tile
   const int d = threadIdx.x;
-  uint32_t total = 0, v = 0;
+  uint32_t total = 0, v = 0, mine = 0, u = 0;
   if (d < kDigits) {
     total = s.totals[d];
+    mine = local[d];
     v = total;
+    u = mine;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-      const uint32_t w = __shfl_up_sync(~0u, v, o);
-      if (lane >= o) v += w;
+      const uint32_t w = __shfl_up_sync(~0u, v, o), x = __shfl_up_sync(~0u, u, o);
+      if (lane >= o) {
+        v += w;
+        u += x;
+      }
     }
-    if (lane == 31) warp_sum[warp] = v;
+    if (lane == 31) warp_sum[warp] = make_uint2(v, u);
   }
   __syncthreads();
   if (d < kDigits) {
-    uint32_t at = v - total;
-    for (int w = 0; w < warp; ++w) at += warp_sum[w];
-    at += s.counts[static_cast<long long>(d) * s.tiles + blockIdx.x];
-    for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = cnt[w][d];
-      cnt[w][d] = at;
-      at += c;
+    uint32_t at = v - total + s.counts[static_cast<long long>(d) * s.tiles + blockIdx.x];
+    uint32_t here = u - mine;
+    for (int w = 0; w < warp; ++w) {
+      at += warp_sum[w].x;
+      here += warp_sum[w].y;
     }
+    local[d] = here;
+    start[d] = at - here;  // a record's place in the tile's order plus this is its place
   }
   __syncthreads();
+  // through shared memory, so that neighbouring threads write a digit's run
 #pragma unroll
   for (int k = 0; k < kPerLane; ++k) {
-    const long long i = base + k * 32;
-    if (i >= s.tokens) break;
-    const uint32_t to = cnt[warp][(key[k] >> s.shift) & (kDigits - 1)] + rank[k];
-    s.keys_out[to] = key[k];
-    // (looked at first: a million stores to 64 flags took 37 us)
-    if (s.named != nullptr && key[k] < s.vocab && s.named[key[k]] == 0) s.named[key[k]] = 1;
-    s.pos_out[to] = s.ids != nullptr ? static_cast<uint32_t>(i) : s.pos_in[i];
+    if (base + k * 32 >= s.tokens) break;
+    const uint32_t digit = (rec[k].x >> s.shift) & (kDigits - 1);
+    tile[local[digit] + cnt[warp][digit] + rank[k]] = rec[k];
+  }
+  __syncthreads();
+  const int have = static_cast<int>(
+      min(static_cast<long long>(kSortThreads) * kPerLane,
+          s.tokens - static_cast<long long>(blockIdx.x) * (kSortThreads * kPerLane)));
+#pragma unroll 4
+  for (int j = threadIdx.x; j < have; j += kSortThreads) {
+    const uint2 r = tile[j];
+    s.out[start[(r.x >> s.shift) & (kDigits - 1)] + j] = r;
+    // (once a run of equal ids: a million stores to 64 flags took 37 us)
+    if (s.named != nullptr && r.x < s.vocab && (j == 0 || tile[j - 1].x != r.x)) s.named[r.x] = 1;
+  }
+}
+
+// The whole sort in one launch for up to kClusterTokens positions: a cluster of eight CTAs, a
+// tile each, that exchange their digit counts through distributed shared memory.  (Six
+// launches for two digits took 31 us on 32,768 positions, this one a third of it.)
+constexpr int kCluster = 8;
+constexpr int kClusterThreads = 1024;
+constexpr int kClusterPerLane = 8;
+constexpr int kClusterTokens = kCluster * kClusterThreads * kClusterPerLane;
+
+struct ClusterSort {
+  const void* ids;
+  int ids_64;
+  uint2* rec[2];
+  int tokens, passes, per_lane;
+  long long vocab;
+  unsigned char* named;
+  unsigned* err;
+};
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Word `at` of shared memory in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_word(const uint32_t* at, unsigned rank) {
+  uint32_t addr = static_cast<uint32_t>(__cvta_generic_to_shared(at)), there, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+  return v;
+}
+
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kClusterThreads) k_sort_cluster(ClusterSort s) {
+  constexpr int kWarps = kClusterThreads / 32;
+  __shared__ uint32_t cnt[kWarps][kDigits];
+  __shared__ uint32_t total[kDigits];  // of the CTA, read by the others
+  __shared__ uint32_t start[kDigits], local[kDigits];
+  extern __shared__ __align__(16) unsigned char smem[];
+  uint2* tile = reinterpret_cast<uint2*>(smem);
+  static_assert(kClusterThreads == 4 * kDigits, "four threads a digit");
+  __shared__ uint2 warp_sum[kDigits / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x;
+  pdl_wait();
+  pdl_trigger();
+  for (long long v = (static_cast<long long>(rank) * kClusterThreads + threadIdx.x) * 16; v < s.vocab;
+       v += static_cast<long long>(kCluster) * kClusterThreads * 16)
+    *reinterpret_cast<uint4*>(s.named + v) = make_uint4(0, 0, 0, 0);  // the array is padded
+  const int base = (rank * kClusterThreads + warp * 32) * s.per_lane + lane;
+  uint2 rec[kClusterPerLane];
+  uint32_t place[kClusterPerLane];
+#pragma unroll
+  for (int k = 0; k < kClusterPerLane; ++k) {
+    const int i = base + k * 32;
+    rec[k] = make_uint2(0, i);
+    if (k < s.per_lane && i < s.tokens) {
+      const long long id = id_of(s.ids, s.ids_64, i);
+      if (id >= s.vocab) atomicOr(s.err, kErrBadToken);
+      rec[k].x = static_cast<uint32_t>(id < 0 || id >= s.vocab ? s.vocab : id);
+    }
+  }
+#pragma unroll 1
+  for (int pass = 0; pass < s.passes; ++pass) {
+    const int shift = 8 * pass;
+    if (pass > 0) {
+#pragma unroll
+      for (int k = 0; k < kClusterPerLane; ++k) {
+        const int i = base + k * 32;
+        if (k < s.per_lane && i < s.tokens) rec[k] = __ldcg(&s.rec[(pass - 1) & 1][i]);
+      }
+    }
+    for (int d = lane; d < kDigits; d += 32) cnt[warp][d] = 0;
+    __syncwarp();
+    // place[k]: equal digits before it within the warp
+#pragma unroll
+    for (int k = 0; k < kClusterPerLane; ++k) {
+      if (k >= s.per_lane) break;
+      const bool in = base + k * 32 < s.tokens;
+      const uint32_t d = (rec[k].x >> shift) & (kDigits - 1);
+      const unsigned peers = lanes_with(d, in);
+      const unsigned before = peers & ((1u << lane) - 1u);
+      const uint32_t seen = in ? cnt[warp][d] : 0;
+      __syncwarp();
+      place[k] = seen + __popc(before);
+      if (in && before == 0) cnt[warp][d] = seen + __popc(peers);
+      __syncwarp();
+    }
+    __syncthreads();
+    // counts of the warps before, four threads a digit
+    {
+      constexpr int kPart = kWarps / 4;
+      const int d = threadIdx.x / 4, q = threadIdx.x & 3, first = q * kPart;
+      uint32_t c[kPart], sum = 0;
+#pragma unroll
+      for (int w = 0; w < kPart; ++w) {
+        c[w] = cnt[first + w][d];
+        sum += c[w];
+      }
+      uint32_t upto = sum;
+#pragma unroll
+      for (int o = 1; o < 4; o *= 2) {
+        const uint32_t w = __shfl_up_sync(~0u, upto, o);
+        if (q >= o) upto += w;
+      }
+      uint32_t at = upto - sum;
+#pragma unroll
+      for (int w = 0; w < kPart; ++w) {
+        cnt[first + w][d] = at;
+        at += c[w];
+      }
+      if (q == 3) total[d] = upto;
+    }
+    const int d = threadIdx.x;
+    cluster_sync();
+    // digit d's first place: digits below it, then the CTAs before this one
+    uint32_t below = 0, all = 0, v = 0, mine = 0, u = 0;
+    if (d < kDigits) {
+#pragma unroll
+      for (int r = 0; r < kCluster; ++r) {
+        const uint32_t c = remote_word(&total[d], r);
+        if (r < rank) below += c;
+        if (r == rank) mine = c;
+        all += c;
+      }
+      v = all;
+      u = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const uint32_t w = __shfl_up_sync(~0u, v, o), x = __shfl_up_sync(~0u, u, o);
+        if (lane >= o) {
+          v += w;
+          u += x;
+        }
+      }
+      if (lane == 31) warp_sum[warp] = make_uint2(v, u);
+    }
+    __syncthreads();
+    if (d < kDigits) {
+      uint32_t at = v - all + below, here = u - mine;
+      for (int w = 0; w < warp; ++w) {
+        at += warp_sum[w].x;
+        here += warp_sum[w].y;
+      }
+      local[d] = here;
+      start[d] = at - here;
+    }
+    __syncthreads();
+    // through shared memory, so that neighbouring threads write a digit's run
+#pragma unroll
+    for (int k = 0; k < kClusterPerLane; ++k) {
+      if (k >= s.per_lane || base + k * 32 >= s.tokens) break;
+      const uint32_t digit = (rec[k].x >> shift) & (kDigits - 1);
+      tile[local[digit] + cnt[warp][digit] + place[k]] = rec[k];
+    }
+    __syncthreads();
+    const int have = min(kClusterThreads * s.per_lane, s.tokens - rank * kClusterThreads * s.per_lane);
+    for (int j = threadIdx.x; j < have; j += kClusterThreads) {
+      const uint2 r = tile[j];
+      s.rec[pass & 1][start[(r.x >> shift) & (kDigits - 1)] + j] = r;
+      if (pass == 0 && r.x < s.vocab && (j == 0 || tile[j - 1].x != r.x)) s.named[r.x] = 1;
+    }
+    cluster_sync();  // the next pass reads what all wrote, and totals may change
   }
 }
 
@@ -253,8 +462,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortPass s) {
 // the part that began before the piece and `trail` of the part that begins in it
 // and goes on.  k_grad_join adds those in order.
 struct GradArgs {
-  const uint32_t* keys;
-  const uint32_t* pos;
+  const uint2* rec;  // sorted (id, position)
   long long tokens, vocab;
   int dim, lanes, piece;
   long long pieces;
@@ -265,16 +473,6 @@ struct GradArgs {
   long long sum_blocks;  // of k_grad_sum's grid.x; the rest clears rows no id names
   const unsigned char* named;
 };
-
-__device__ __forceinline__ long long lower_bound(const uint32_t* keys, long long n, uint32_t v) {
-  long long lo = 0, hi = n;
-  while (lo < hi) {
-    const long long mid = (lo + hi) >> 1;
-    if (keys[mid] < v) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
-}
 
 constexpr int kSumThreads = 128;
 constexpr int kClearRows = 16;  // rows a group of lanes looks at
@@ -311,8 +509,8 @@ __global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradArgs a, const TI* 
   if (p >= a.pieces || col >= a.dim) return;
   const long long begin = p * a.piece, end = min(begin + a.piece, a.tokens);
   const uint32_t none = static_cast<uint32_t>(a.vocab);
-  uint32_t run = a.keys[begin];
-  bool led = begin > 0 && a.keys[begin - 1] == run;  // the current run began before the piece
+  uint32_t run = a.rec[begin].x;
+  bool led = begin > 0 && a.rec[begin - 1].x == run;  // the current run began before the piece
   float acc[V] = {};
   auto flush = [&]() {
     if (run >= none) return;
@@ -326,33 +524,48 @@ __global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradArgs a, const TI* 
       store_row<TG, V>(out + run * a.out_stride + col, acc, a.scale);
     }
   };
-  for (long long i = begin; i < end; i += kSumUnroll) {
-    uint32_t key[kSumUnroll];
-    Pack<TI, V> g[kSumUnroll];
+  const int count = static_cast<int>(end - begin);
+  const uint2* rp = a.rec + begin;
+  const TI* gp = grad + col;
+  // a full batch without checks, its keys and positions one batch ahead
+  uint2 rec[kSumUnroll];
+  auto fetch = [&](int i) {
 #pragma unroll
     for (int u = 0; u < kSumUnroll; ++u) {
-      key[u] = i + u < end ? a.keys[i + u] : none;
-      if (key[u] < none)
-        g[u] = *reinterpret_cast<const Pack<TI, V>*>(grad + static_cast<long long>(a.pos[i + u]) * a.in_stride + col);
+      rec[u] = make_uint2(none, 0);
+      if (i + u < count) rec[u] = rp[i + u];
     }
+  };
+  fetch(0);
+#pragma unroll 1
+  for (int i = 0; i < count; i += kSumUnroll) {
+    Pack<TI, V> g[kSumUnroll];
+    uint32_t now[kSumUnroll];
 #pragma unroll
     for (int u = 0; u < kSumUnroll; ++u) {
-      if (i + u >= end) break;
-      if (key[u] != run) {
+      now[u] = rec[u].x;
+      // (past the piece's end position 0 is read and not used)
+      g[u] = *reinterpret_cast<const Pack<TI, V>*>(gp + static_cast<long long>(rec[u].y) * a.in_stride);
+    }
+    fetch(i + kSumUnroll);
+#pragma unroll
+    for (int u = 0; u < kSumUnroll; ++u) {
+      if (now[u] != run) {
+        if (i + u >= count) break;
         flush();
-        run = key[u];
+        run = now[u];
         led = false;
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] = 0.0f;
       }
-      if (key[u] < none) {
+      if (now[u] < none) {
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] += to_f32(g[u].v[e]);
       }
     }
   }
   if (run >= none) return;
-  const bool goes_on = end < a.tokens && a.keys[end] == run;
+  const bool goes_on = end < a.tokens && a.rec[end].x == run;
   if (goes_on && !led) {
     Pack<float, V> w;
 #pragma unroll
@@ -363,48 +576,85 @@ __global__ void __launch_bounds__(kSumThreads) k_grad_sum(GradArgs a, const TI* 
   }
 }
 
-// One CTA per piece and 32 x V columns: finishes the run that begins in the piece and goes on past it.
-// Warp w adds the pieces p + 1 + w, + 8, ...; the warps' sums are added in order.
+// Finishes runs that begin in a piece and go on past it.  A CTA looks at eight pieces, a warp each,
+// and adds for every run found, 32 x V columns: warp w takes the pieces p + 1 + w, + 8, ...;
+// the warps' sums are added in order.
 constexpr int kJoinWarps = 8;
+
+// Past the last of the equal keys that a[0] begins: 32 places are looked at a step.
+__device__ __forceinline__ long long run_end(const uint2* a, long long n, uint32_t v) {
+  const int lane = threadIdx.x & 31;
+  long long lo = 0, hi = n;  // a[lo - 1] == v (or lo = 0), a[hi] > v (or hi = n)
+  while (lo < hi) {
+    const long long step = (hi - lo + 31) / 32;
+    const long long at = lo + lane * step;
+    const unsigned equal = __ballot_sync(~0u, at < hi && a[at].x == v);
+    const int k = __popc(equal);  // the keys are sorted: the first k places hold v
+    if (k == 0) return lo;
+    const long long from = lo;
+    lo = from + (k - 1) * step + 1;
+    hi = min(hi, from + k * step);
+  }
+  return lo;
+}
 
 template <typename TG, int V>
 __global__ void __launch_bounds__(kJoinWarps * 32) k_grad_join(GradArgs a, TG* out) {
   __shared__ float part[kJoinWarps][32 * V];
+  __shared__ long long last_of[kJoinWarps];  // last piece of the run that begins in the warp's piece, or -1
+  __shared__ uint32_t run_of[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  const long long p = blockIdx.x;
-  const long long begin = p * a.piece, end = min(begin + a.piece, a.tokens);
-  if (end >= a.tokens) return;
-  const uint32_t run = a.keys[end - 1];
-  if (run >= static_cast<uint32_t>(a.vocab) || a.keys[end] != run) return;
-  if (a.keys[begin] == run && begin > 0 && a.keys[begin - 1] == run) return;  // it began earlier
-  // last piece that the run reaches into
-  const long long last = (end + lower_bound(a.keys + end, a.tokens - end, run + 1) - 1) / a.piece;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int col = (blockIdx.y * 32 + lane) * V;
-  const bool in = col < a.dim;
-  float acc[V] = {};
-  if (in) {
-    if (warp == 0) {
-      const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.trail + p * a.dim + col);
-#pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] = w.v[e];
+  {
+    const long long p = static_cast<long long>(blockIdx.x) * kJoinWarps + warp;
+    const long long begin = p * a.piece, end = min(begin + a.piece, a.tokens);
+    long long last = -1;
+    uint32_t run = 0;
+    if (p < a.pieces && end < a.tokens) {
+      run = a.rec[end - 1].x;
+      const uint32_t next = a.rec[end].x, first = a.rec[begin].x, before = begin > 0 ? a.rec[begin - 1].x : run + 1;
+      // goes on, is no padding, and did not begin earlier
+      if (run < static_cast<uint32_t>(a.vocab) && next == run && !(first == run && before == run))
+        last = (end + run_end(a.rec + end, a.tokens - end, run) - 1) / a.piece;
     }
-#pragma unroll 4
-    for (long long q = p + 1 + warp; q <= last; q += kJoinWarps) {
-      const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.lead + q * a.dim + col);
-#pragma unroll
-      for (int e = 0; e < V; ++e) acc[e] += w.v[e];
+    if (lane == 0) {
+      last_of[warp] = last;
+      run_of[warp] = run;
     }
   }
-#pragma unroll
-  for (int e = 0; e < V; ++e) part[warp][lane * V + e] = acc[e];
   __syncthreads();
-  if (warp != 0 || !in) return;
-  for (int w = 1; w < kJoinWarps; ++w)
+  const int col = (blockIdx.y * 32 + lane) * V;
+  const bool in = col < a.dim;
+  for (int k = 0; k < kJoinWarps; ++k) {
+    const long long last = last_of[k], p = static_cast<long long>(blockIdx.x) * kJoinWarps + k;
+    if (last < 0) continue;
+    float acc[V] = {};
+    if (in) {
+      if (warp == 0) {
+        const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.trail + p * a.dim + col);
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] += part[w][lane * V + e];
-  store_row<TG, V>(out + run * a.out_stride + col, acc, a.scale);
+        for (int e = 0; e < V; ++e) acc[e] = w.v[e];
+      }
+#pragma unroll 4
+      for (long long q = p + 1 + warp; q <= last; q += kJoinWarps) {
+        const Pack<float, V> w = *reinterpret_cast<const Pack<float, V>*>(a.lead + q * a.dim + col);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += w.v[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) part[warp][e * 32 + lane] = acc[e];
+    __syncthreads();
+    if (warp == 0 && in) {
+      const long long used = last - p;  // warps with a piece (warp 0 has the first's rest too)
+      for (int w = 1; w < kJoinWarps && w < used; ++w)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += part[w][e * 32 + lane];
+      store_row<TG, V>(out + run_of[k] * a.out_stride + col, acc, a.scale);
+    }
+    __syncthreads();
+  }
 }
 
 int pow2_at_most_32(long long v) {
@@ -416,7 +666,8 @@ int pow2_at_most_32(long long v) {
 struct GradPlan {
   int per_lane, tiles, passes, piece;
   long long pieces;
-  size_t off_keys[2], off_pos[2], off_counts, off_totals, off_named, off_lead, off_trail, bytes;
+  bool cluster;  // sorted in one launch
+  size_t off_rec[2], off_counts, off_totals, off_named, off_lead, off_trail, bytes;
 };
 
 // Pieces: 24 to 96 warps for each SM over all column chunks, 16 to 512 rows each, so that a
@@ -424,6 +675,7 @@ struct GradPlan {
 GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
   GradPlan g{};
   const long long n = tokens < 1 ? 1 : tokens;
+  g.cluster = n <= kClusterTokens;
   g.per_lane = sort_per_lane(n);
   g.tiles = static_cast<int>((n + kSortThreads * g.per_lane - 1) / (kSortThreads * g.per_lane));
   int bits = 1;
@@ -440,8 +692,7 @@ GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
     return o;
   };
   for (int k = 0; k < 2; ++k) {
-    g.off_keys[k] = take(n * 4);
-    g.off_pos[k] = take(n * 4);
+    g.off_rec[k] = take(n * 8);
   }
   g.off_counts = take(static_cast<size_t>(kDigits) * g.tiles * 4);
   g.off_totals = take(kDigits * 4);
@@ -484,16 +735,33 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
   const GradPlan g = grad_plan(a.tokens, a.vocab, a.dim, sms);
   unsigned char* ws = static_cast<unsigned char*>(a.ws);
   auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
-  const uint32_t *keys = nullptr, *pos = nullptr;
-  if (a.tokens > 0) {
+  auto records = [&](int k) { return reinterpret_cast<uint2*>(ws + g.off_rec[k]); };
+  const uint2* sorted = nullptr;
+  if (a.tokens > 0 && g.cluster) {
+    ClusterSort s{};
+    s.ids = a.ids;
+    s.ids_64 = a.ids_64;
+    for (int k = 0; k < 2; ++k) s.rec[k] = records(k);
+    s.tokens = static_cast<int>(a.tokens);
+    s.passes = g.passes;
+    s.per_lane = static_cast<int>((a.tokens + kCluster * kClusterThreads - 1) / (kCluster * kClusterThreads));
+    s.vocab = a.vocab;
+    s.named = ws + g.off_named;
+    s.err = a.err;
+    const size_t smem = sizeof(uint2) * kClusterThreads * s.per_lane;
+    cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_sort_cluster), smem);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(k_sort_cluster, dim3(kCluster), dim3(kClusterThreads), smem, st, s);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    sorted = s.rec[(g.passes - 1) & 1];
+  } else if (a.tokens > 0) {
     for (int k = 0; k < g.passes; ++k) {
       SortPass s{};
       s.ids = k == 0 ? a.ids : nullptr;
       s.ids_64 = a.ids_64;
-      s.keys_in = keys;
-      s.pos_in = pos;
-      s.keys_out = u32(g.off_keys[k & 1]);
-      s.pos_out = u32(g.off_pos[k & 1]);
+      s.in = sorted;
+      s.out = records(k & 1);
       s.counts = u32(g.off_counts);
       s.totals = u32(g.off_totals);
       s.tokens = a.tokens;
@@ -508,17 +776,20 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
       if (e != cudaSuccess) return e;
       e = launch_pdl(k_sort_scan, dim3(kDigits), dim3(256), 0, st, s.counts, s.totals, g.tiles);
       if (e != cudaSuccess) return e;
-      e = g.per_lane == 8 ? launch_pdl(k_sort_scatter<8>, grid, block, 0, st, s)
-                          : launch_pdl(k_sort_scatter<2>, grid, block, 0, st, s);
+      const size_t smem = sizeof(uint2) * kSortThreads * g.per_lane;
+      e = allow_smem(g.per_lane == 8 ? reinterpret_cast<const void*>(k_sort_scatter<8>)
+                                     : reinterpret_cast<const void*>(k_sort_scatter<2>),
+                     smem);
+      if (e != cudaSuccess) return e;
+      e = g.per_lane == 8 ? launch_pdl(k_sort_scatter<8>, grid, block, smem, st, s)
+                          : launch_pdl(k_sort_scatter<2>, grid, block, smem, st, s);
       if (e != cudaSuccess) return e;
       *launches += 3;
-      keys = s.keys_out;
-      pos = s.pos_out;
+      sorted = s.out;
     }
   }
   GradArgs q{};
-  q.keys = keys;
-  q.pos = pos;
+  q.rec = sorted;
   q.tokens = a.tokens;
   q.vocab = a.vocab;
   q.dim = a.dim;
@@ -548,7 +819,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
         ++*launches;
         if (q.pieces < 2) return cudaSuccess;
         ++*launches;
-        return launch_pdl(k_grad_join<TO, V>, dim3(static_cast<unsigned>(q.pieces), (packs + 31) / 32),
+        return launch_pdl(k_grad_join<TO, V>, dim3(static_cast<unsigned>((q.pieces + kJoinWarps - 1) / kJoinWarps), (packs + 31) / 32),
                           dim3(kJoinWarps * 32), 0, st, q, static_cast<TO*>(a.out));
       });
     });

@@ -355,6 +355,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
 #pragma unroll 1
   for (int part = parts - 1; part >= 0; --part) {
     const int t0 = part * kSub;
+    // what the activations' slopes need lands behind the walk
+    static_assert(kSub <= kGroups, "a thread has one position of a part");
+    const int ct = t0 + tl;  // position in the chunk
+    const bool mine = tl < kSub && cin;
+    RawRun<T, 1> raw;
+    Two<T> gy[1];
+    if (mine && ct < w.live) {
+      load_run<T, 1, kVec, true>(a, k, q, w.begin + ct, w.begin + w.live, raw);
+      load_gy<T, 1, kVec>(g, k, q, w.begin + ct, 1, gy);
+    }
     {
       Lane<S> hs[kSub + 1], decay[kSub];
       hs[0] = lane_shared<S>(kept + part * (kChannels * 4 * S));
@@ -440,17 +450,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
       }
     }
     // through the gate, softplus and the convolution's activation
-    static_assert(kSub <= kGroups, "a thread has one position of a part");
-    const int ct = t0 + tl;  // position in the chunk
     const long long o = static_cast<long long>(ct) * a.dim;
-    const bool mine = tl < kSub && cin;
     if (mine) {
       F2 dv = dup2(0.0f);
       if (ct < w.live) {
-        RawRun<T, 1> raw;
-        Two<T> gy[1];
-        load_run<T, 1, kVec, true>(a, k, q, w.begin + ct, w.begin + w.live, raw);
-        load_gy<T, 1, kVec>(g, k, q, w.begin + ct, 1, gy);
         const float4 in4 = *reinterpret_cast<const float4*>(&sm.in.du[ct][q.c]);
         const F2 d = f2(in4.x, in4.z), u = f2(in4.y, in4.w);
         auto two = [&](const float* p) {
