@@ -306,9 +306,32 @@ struct ClusterSort {
   uint2* rec[2];
   int tokens, passes, per_lane;
   long long vocab;
-  unsigned char* named;
+  unsigned char* named;  // null: the other CTAs of the grid clear the table
   unsigned* err;
+  unsigned char* table;
+  long long rows, row_bytes, stride_bytes;
 };
+
+// Rows of the table to zero by the CTAs after the cluster that sorts: W bytes an access.
+template <int W>
+__device__ __forceinline__ void clear_rows(const ClusterSort& s) {
+  const long long threads = static_cast<long long>(gridDim.x - kCluster) * kClusterThreads;
+  const long long per = s.row_bytes / W, all = s.rows * per;
+  long long i = static_cast<long long>(blockIdx.x - kCluster) * kClusterThreads + threadIdx.x;
+  long long row = i / per, at = i - row * per;
+  const long long step_row = threads / per, step_at = threads - step_row * per;
+  for (; i < all; i += threads) {
+    unsigned char* p = s.table + row * s.stride_bytes + at * W;
+    if constexpr (W == 16) *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
+    else *reinterpret_cast<unsigned short*>(p) = 0;
+    row += step_row;
+    at += step_at;
+    if (at >= per) {
+      at -= per;
+      ++row;
+    }
+  }
+}
 
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -333,8 +356,16 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kClusterThrea
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x;
   pdl_wait();
   pdl_trigger();
-  for (long long v = (static_cast<long long>(rank) * kClusterThreads + threadIdx.x) * 16; v < s.vocab;
-       v += static_cast<long long>(kCluster) * kClusterThreads * 16)
+  if (rank >= kCluster) {
+    if (s.row_bytes % 16 == 0 && s.stride_bytes % 16 == 0 && reinterpret_cast<uintptr_t>(s.table) % 16 == 0)
+      clear_rows<16>(s);
+    else
+      clear_rows<2>(s);
+    return;
+  }
+  if (s.named != nullptr)
+    for (long long v = (static_cast<long long>(rank) * kClusterThreads + threadIdx.x) * 16; v < s.vocab;
+         v += static_cast<long long>(kCluster) * kClusterThreads * 16)
     *reinterpret_cast<uint4*>(s.named + v) = make_uint4(0, 0, 0, 0);  // the array is padded
   const int base = (rank * kClusterThreads + warp * 32) * s.per_lane + lane;
   uint2 rec[kClusterPerLane];
@@ -447,7 +478,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kClusterThrea
     for (int j = threadIdx.x; j < have; j += kClusterThreads) {
       const uint2 r = tile[j];
       s.rec[pass & 1][start[(r.x >> shift) & (kDigits - 1)] + j] = r;
-      if (pass == 0 && r.x < s.vocab && (j == 0 || tile[j - 1].x != r.x)) s.named[r.x] = 1;
+      if (pass == 0 && s.named != nullptr && r.x < s.vocab && (j == 0 || tile[j - 1].x != r.x)) s.named[r.x] = 1;
     }
     cluster_sync();  // the next pass reads what all wrote, and totals may change
   }
@@ -472,6 +503,7 @@ struct GradArgs {
   float* trail;  // [pieces][dim]
   long long sum_blocks;  // of k_grad_sum's grid.x; the rest clears rows no id names
   const unsigned char* named;
+  bool cleared;  // the table is zero already
 };
 
 constexpr int kSumThreads = 128;
@@ -667,6 +699,7 @@ struct GradPlan {
   int per_lane, tiles, passes, piece;
   long long pieces;
   bool cluster;  // sorted in one launch
+  bool clear;    // the table is cleared meanwhile
   size_t off_rec[2], off_counts, off_totals, off_named, off_lead, off_trail, bytes;
 };
 
@@ -732,7 +765,7 @@ size_t embed_grad_workspace(long long tokens, long long vocab, int dim, int sms)
 }
 
 cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st) {
-  const GradPlan g = grad_plan(a.tokens, a.vocab, a.dim, sms);
+  GradPlan g = grad_plan(a.tokens, a.vocab, a.dim, sms);
   unsigned char* ws = static_cast<unsigned char*>(a.ws);
   auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
   auto records = [&](int k) { return reinterpret_cast<uint2*>(ws + g.off_rec[k]); };
@@ -746,12 +779,21 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
     s.passes = g.passes;
     s.per_lane = static_cast<int>((a.tokens + kCluster * kClusterThreads - 1) / (kCluster * kClusterThreads));
     s.vocab = a.vocab;
-    s.named = ws + g.off_named;
+    // A table of up to 160 MB is zeroed by the SMs that the sort leaves idle, in about its time;
+    // rows that are named are then written twice.  Of a larger one only rows not named are cleared.
+    const size_t elem = dtype_size(a.out_dtype);
+    g.clear = static_cast<size_t>(a.vocab) * a.dim * elem <= (size_t(160) << 20);
+    s.named = g.clear ? nullptr : ws + g.off_named;
+    s.table = static_cast<unsigned char*>(a.out);
+    s.rows = a.vocab;
+    s.row_bytes = static_cast<long long>(a.dim) * elem;
+    s.stride_bytes = a.out_stride * elem;
     s.err = a.err;
+    const unsigned extra = g.clear ? static_cast<unsigned>(2 * (sms - kCluster) / kCluster * kCluster) : 0;
     const size_t smem = sizeof(uint2) * kClusterThreads * s.per_lane;
     cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_sort_cluster), smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(k_sort_cluster, dim3(kCluster), dim3(kClusterThreads), smem, st, s);
+    e = launch_pdl(k_sort_cluster, dim3(kCluster + extra), dim3(kClusterThreads), smem, st, s);
     if (e != cudaSuccess) return e;
     ++*launches;
     sorted = s.rec[(g.passes - 1) & 1];
@@ -795,7 +837,8 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
   q.dim = a.dim;
   q.piece = g.piece;
   q.pieces = a.tokens > 0 ? g.pieces : 0;
-  q.named = a.tokens > 0 ? ws + g.off_named : nullptr;
+  q.cleared = g.clear;
+  q.named = a.tokens > 0 && !g.clear ? ws + g.off_named : nullptr;
   q.scale = a.scale;
   q.in_stride = a.in_stride;
   q.out_stride = a.out_stride;
@@ -812,7 +855,7 @@ cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, 
         const long long groups = kSumThreads / q.lanes;
         q.sum_blocks = (q.pieces + groups - 1) / groups;
         const unsigned chunks = static_cast<unsigned>((packs + q.lanes - 1) / q.lanes);
-        const dim3 grid(static_cast<unsigned>(q.sum_blocks + (a.vocab + groups * kClearRows - 1) / (groups * kClearRows)), chunks);
+        const dim3 grid(static_cast<unsigned>(q.sum_blocks + (q.cleared ? 0 : (a.vocab + groups * kClearRows - 1) / (groups * kClearRows))), chunks);
         cudaError_t e = launch_pdl(k_grad_sum<TI, TO, V>, grid, dim3(kSumThreads), 0, st, q,
                                    static_cast<const TI*>(a.table), static_cast<TO*>(a.out));
         if (e != cudaSuccess) return e;
