@@ -88,6 +88,30 @@ __device__ __forceinline__ uint32_t fixed_weight(float s, float top) {
   return __float2uint_rn(__expf(__fsub_rn(s, top)) * 2147483648.0f);
 }
 
+// Loads and shared-memory adds under a predicate, so that those of a group of entries issue one
+// after another (behind branches each waits for the one before).
+__device__ __forceinline__ float load_if(const float* p, bool on) {
+  float v;
+  asm volatile("{.reg .pred q; setp.ne.u32 q, %2, 0; mov.f32 %0, 0f00000000; @q ld.global.nc.f32 %0, [%1];}"
+               : "=f"(v)
+               : "l"(p), "r"(static_cast<unsigned>(on)));
+  return v;
+}
+__device__ __forceinline__ void add_if(unsigned* p, unsigned v, bool on) {
+  asm volatile("{.reg .pred q; setp.ne.u32 q, %2, 0; @q red.shared.add.u32 [%0], %1;}" ::"r"(
+                   static_cast<unsigned>(__cvta_generic_to_shared(p))),
+               "r"(v), "r"(static_cast<unsigned>(on))
+               : "memory");
+}
+__device__ __forceinline__ unsigned fetch_add_if(unsigned* p, unsigned v, bool on) {
+  unsigned old;
+  asm volatile("{.reg .pred q; setp.ne.u32 q, %3, 0; mov.u32 %0, 0; @q atom.shared.add.u32 %0, [%1], %2;}"
+               : "=r"(old)
+               : "r"(static_cast<unsigned>(__cvta_generic_to_shared(p))), "r"(v), "r"(static_cast<unsigned>(on))
+               : "memory");
+  return old;
+}
+
 // ---------------------------------------------------------------------------
 // A warp per row
 // ---------------------------------------------------------------------------
@@ -344,19 +368,27 @@ struct Row {
   float inv;
 
   __device__ __forceinline__ float score(int i) const { return scaled(to_f32(row[i]), inv); }
+  __device__ __forceinline__ void load(const T* base, int q, int skew, Pack<T, V>& p) const {
+    const int i0 = q * V - skew;
+    if (i0 >= 0 && i0 <= n - V) p = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
+  }
   template <int U, typename F>
   __device__ __forceinline__ void walk(const Team& t, F f) const {
     const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
     const int groups = (skew + n + V - 1) / V;
     const int stride = t.size * static_cast<int>(blockDim.x), last = n - V;
     const T* base = row - skew;  // aligned to the group; entries before `row` are not read
+    int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x;
+    Pack<T, V> p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(base, min(q0 + u * stride, groups), skew, p[u]);
 #pragma unroll 1
-    for (int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x; q0 < groups; q0 += stride * U) {
-      Pack<T, V> p[U];
+    for (; q0 < groups; q0 += stride * U) {
+      Pack<T, V> now[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int q = q0 + u * stride, i0 = q * V - skew;
-        if (i0 >= 0 && i0 <= last) p[u] = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
+        now[u] = p[u];
+        load(base, min(q0 + (U + u) * stride, groups), skew, p[u]);  // the next ones land meanwhile
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -365,7 +397,7 @@ struct Row {
         float s[V];
         if (i0 >= 0 && i0 <= last) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) s[v] = scaled(to_f32(p[u].v[v]), inv);
+          for (int v = 0; v < V; ++v) s[v] = scaled(to_f32(now[u].v[v]), inv);
         } else {
           // a row's ends
 #pragma unroll
@@ -565,7 +597,87 @@ __device__ void sort_registers(Shared& sh, unsigned n) {
   __syncthreads();
 }
 
-__device__ void sort_list(Shared& sh, unsigned n) {
+// Bins of a selection: linear from `from` down, `scale` a unit; what lies outside goes to
+// the first or last one.  Rounded steps of it are monotone, so a bin is an interval.
+struct Bins {
+  float from, scale, last;
+  __device__ __forceinline__ int of(float v) const {
+    return static_cast<int>(fminf(fmaxf(__fmul_rn(__fsub_rn(from, v), scale), 0.0f), last));
+  }
+};
+
+// By buckets, linear in the value between the list's extremes: an entry's place is its
+// bucket's plus the number of larger ones in it.  False, and the list as it was, where
+// a bucket is crowded.  (Entries are held in registers meanwhile, E a thread.)
+constexpr unsigned kCrowd = 48;
+
+template <int E>
+__device__ bool sort_buckets(const Team& t, Shared& sh, unsigned n) {
+  const unsigned threads = blockDim.x;
+  unsigned long long v[E];
+  unsigned long long high = 0, low = 0;  // largest entry, largest complement
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const unsigned i = e * threads + threadIdx.x;
+    v[e] = i < n ? sh.list[i] : 0;
+    if (i < n) {
+      high = max(high, v[e]);
+      low = max(low, ~v[e]);
+    }
+  }
+  high = block_max(high, sh);
+  low = ~block_max(low, sh);
+  const float range = __fsub_rn(score_of(high), score_of(low)), last = static_cast<float>(t.bins - 1);
+  if (!(range > 0.0f)) return false;
+  const Bins bins = {score_of(high), fminf(last / range, 1e30f), last};
+  for (int b = threadIdx.x; b < t.bins; b += threads) sh.count[b] = 0;
+  __syncthreads();
+  int bin[E];
+  unsigned slot[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (v[e] != 0) {
+      bin[e] = bins.of(score_of(v[e]));
+      slot[e] = atomicAdd(&sh.count[bin[e]], 1u);
+    }
+  __syncthreads();
+  // count -> place of the bucket's first entry
+  const int span = t.bins / threads, first = threadIdx.x * span;
+  unsigned mine = 0, most = 0;
+  for (int j = 0; j < span; ++j) {
+    mine += sh.count[first + j];
+    most = max(most, sh.count[first + j]);
+  }
+  unsigned at = static_cast<unsigned>(block_below(mine, sh));
+  if (__syncthreads_or(most > kCrowd)) return false;
+  for (int j = 0; j < span; ++j) {
+    const unsigned c = sh.count[first + j];
+    sh.count[first + j] = at;
+    at += c;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (v[e] != 0) sh.list[sh.count[bin[e]] + slot[e]] = v[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (v[e] != 0) {
+      const unsigned begin = sh.count[bin[e]];
+      const unsigned end = bin[e] + 1 < t.bins ? sh.count[bin[e] + 1] : n;
+      unsigned rank = begin;
+      for (unsigned j = begin; j < end; ++j) rank += sh.list[j] > v[e];
+      slot[e] = rank;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (v[e] != 0) sh.list[slot[e]] = v[e];
+  __syncthreads();
+  return true;
+}
+
+__device__ void sort_list(const Team& t, Shared& sh, unsigned n) {
   const unsigned threads = blockDim.x;
   if (n <= kRanked && n <= threads) {
     // an entry's place is the number of larger ones
@@ -578,6 +690,7 @@ __device__ void sort_list(Shared& sh, unsigned n) {
     __syncthreads();
     return;
   }
+  if (n <= 4 * threads && sort_buckets<4>(t, sh, n)) return;
   if (n <= threads) return sort_registers<1>(sh, n);
   if (n <= 2 * threads) return sort_registers<2>(sh, n);
   if (n <= 4 * threads) return sort_registers<4>(sh, n);
@@ -643,15 +756,6 @@ __device__ __forceinline__ unsigned long long share_of(float share, unsigned lon
              ? max(1ull, static_cast<unsigned long long>(static_cast<double>(share) * static_cast<double>(sum)))
              : 1ull;
 }
-
-// Bins of a selection: linear from `from` down, `scale` a unit; what lies outside goes to
-// the first or last one.  Rounded steps of it are monotone, so a bin is an interval.
-struct Bins {
-  float from, scale, last;
-  __device__ __forceinline__ int of(float v) const {
-    return static_cast<int>(fminf(fmaxf(__fmul_rn(__fsub_rn(from, v), scale), 0.0f), last));
-  }
-};
 
 // The bin that holds the `need`-th largest of the threads' own maxima (-infinity: none), one a
 // thread; all entries in bins up to it are at least `need`.  -1 where there are not so many.
@@ -745,17 +849,15 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      old[v] = 0;
-      if (s[v] > -INFINITY) {
-        atomicAdd(&sh.count[b[v]], 1u);
-        if (kMass) old[v] = atomicAdd(&sh.lo[b[v]], w[v]);
-      }
+      const bool on = s[v] > -INFINITY;
+      add_if(&sh.count[b[v]], 1u, on);
+      if (kMass) old[v] = fetch_add_if(&sh.lo[b[v]], w[v], on);
     }
     if (kMass) {
       // shared memory adds 32 bits at a time: carries go to the upper half
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (s[v] > -INFINITY && old[v] + w[v] < old[v]) atomicAdd(&sh.hi[b[v]], 1u);
+        add_if(&sh.hi[b[v]], 1u, s[v] > -INFINITY && old[v] + w[v] < old[v]);
     }
   });
   if (!merge_bins<kMass>(t, sh)) return false;
@@ -811,7 +913,7 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   if (kAbove && t.rank != 0) return true;
   take_list(t, sh, list, listed);
   const unsigned have = sh.listed;
-  sort_list(sh, have);
+  sort_list(t, sh, have);
   if (kAbove) return true;
   *edge = kMass ? sh.list[mass_reaches(sh, have, need, top)] : sh.list[need - 1];
   __syncthreads();
@@ -878,8 +980,7 @@ struct Draws {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!(edge.keeps(s[v], at[v]) && __fsub_rn(s[v], top) >= log_min)) s[v] = -INFINITY;
-      g[v] = 0.0f;
-      if (s[v] > -INFINITY) g[v] = __ldg(noise + at[v]);
+      g[v] = load_if(noise + at[v], s[v] > -INFINITY);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -894,7 +995,7 @@ __device__ __forceinline__ void put(const SampleArgs& a, const Ctx& x, int j, in
 
 // Cuts and draws from sh.list, sorted, which holds the row's best entries: at least the top k.
 template <typename T>
-__device__ void finish_list(const SampleArgs& a, Shared& sh, const Ctx& x, const Row<T>& src) {
+__device__ void finish_list(const SampleArgs& a, const Team& t, Shared& sh, const Ctx& x, const Row<T>& src) {
   unsigned keep = min(sh.listed, x.r.k);
   if (x.r.p < 1.0f)
     keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.top)), x.top) + 1;
@@ -917,7 +1018,7 @@ __device__ void finish_list(const SampleArgs& a, Shared& sh, const Ctx& x, const
     return;
   }
   __syncthreads();
-  sort_list(sh, keep);
+  sort_list(t, sh, keep);
   const int drawn = static_cast<int>(min(keep, static_cast<unsigned>(a.m)));
   for (int j = threadIdx.x; j < drawn; j += blockDim.x)
     put(a, x, j, index_of(sh.list[j]), src.score(index_of(sh.list[j])));
@@ -994,7 +1095,7 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
       if (done) {
         if (t.rank != 0) return true;
         take_list(t, sh, list, listed);
-        sort_list(sh, sh.listed);
+        sort_list(t, sh, sh.listed);
       }
       __syncthreads();
     }
@@ -1048,8 +1149,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
       float g[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        g[v] = 0.0f;
-        if (s[v] > -INFINITY && !x.r.greedy) g[v] = __ldg(x.noise + at[v]);
+        g[v] = load_if(x.noise + at[v], s[v] > -INFINITY && !x.r.greedy);
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -1063,7 +1163,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     }
   };
   if (uncut) row.template walk<1>(t, first);
-  else row.template walk<2>(t, first);
+  else row.template walk<1>(t, first);
   const float mine = top;
   float low = mine > -INFINITY ? mine : INFINITY;  // least of the lanes' maxima
   unsigned long long best = best_key > -INFINITY ? composite(ordered(best_key), best_at) : 0;
@@ -1166,8 +1266,8 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
         if (t.rank != 0) return true;
         if (have <= kList) {
           take_list(t, sh, list, listed);
-          sort_list(sh, have);
-          finish_list(a, sh, x, row);
+          sort_list(t, sh, have);
+          finish_list(a, t, sh, x, row);
           return true;
         }
         // more than can be sorted: the same selections, from the candidates and by this CTA alone
