@@ -518,6 +518,9 @@ int mlt_tune_head_levels(int levels);
  * allocates the error word that mlt_sync_status reads; issue it outside a
  * capture.
  *
+ * Strides of inputs may be 0 or make rows overlap; outputs' rows lie apart and
+ * overlap no input unless a call says so.
+ *
  * Element types of the buffers that may be narrow.  Sums and states are held in
  * fp32 and rounded once. */
 enum { MLT_F32 = 0, MLT_BF16 = 1, MLT_F16 = 2 };

@@ -44,7 +44,8 @@ int check_embed(int dtype, int out_dtype, int64_t tokens, int64_t vocab, int dim
   return MLT_OK;
 }
 
-// A row stride that keeps rows apart (one row needs none).
+// A stride of an output that keeps rows apart (one row needs none).  Inputs may repeat rows or
+// overlap: theirs only must not be negative.
 bool stride_ok(int64_t stride, int64_t width, int64_t rows) { return rows <= 1 || stride >= width; }
 
 int check_scan(const mlt_scan_args* a) {
@@ -63,7 +64,7 @@ int check_scan(const mlt_scan_args* a) {
 }
 
 int check_scan_inputs(const mlt_scan_args* a) {
-  const int64_t L = a->length, bs = static_cast<int64_t>(a->groups) * a->states;
+  const int64_t L = a->length;
   if (a->A == nullptr) return api_fail(MLT_EINVAL, "A must be non-NULL");
   if (a->taps > 0 && a->conv_w == nullptr) return api_fail(MLT_EINVAL, "conv_w must be non-NULL with %d taps", a->taps);
   if (L > 0 && (a->x == nullptr || a->dt == nullptr || a->B == nullptr || a->C == nullptr))
@@ -71,17 +72,15 @@ int check_scan_inputs(const mlt_scan_args* a) {
   struct {
     const char* name;
     const void* p;
-    int64_t step, batch, width;
-  } in[] = {{"x", a->x, a->x_step, a->x_batch, a->dim},
-            {"dt", a->dt, a->dt_step, a->dt_batch, a->dim},
-            {"z", a->z, a->z_step, a->z_batch, a->dim},
-            {"B", a->B, a->B_step, a->B_batch, bs},
-            {"C", a->C, a->C_step, a->C_batch, bs}};
+    int64_t step, batch;
+  } in[] = {{"x", a->x, a->x_step, a->x_batch},
+            {"dt", a->dt, a->dt_step, a->dt_batch},
+            {"z", a->z, a->z_step, a->z_batch},
+            {"B", a->B, a->B_step, a->B_batch},
+            {"C", a->C, a->C_step, a->C_batch}};
   for (const auto& t : in) {
     if (t.p == nullptr) continue;
-    if (!stride_ok(t.step, t.width, L) || t.batch < 0)
-      return api_fail(MLT_EINVAL, "%s: positions must be at least %lld elements apart", t.name,
-                      static_cast<long long>(t.width));
+    if (t.step < 0 || t.batch < 0) return api_fail(MLT_EINVAL, "%s: strides must not be negative", t.name);
     if (!aligned_to(t.p, dtype_size(a->dtype))) return api_fail(MLT_EINVAL, "%s is not aligned to its elements", t.name);
   }
   return MLT_OK;
@@ -112,8 +111,7 @@ int mlt_sample(void* stream, const void* scores, int dtype, int64_t rows, int64_
   if (rows == 0) return MLT_OK;
   if (out_index == nullptr || out_logprob == nullptr || (n > 0 && (scores == nullptr || noise == nullptr)))
     return api_fail(MLT_EINVAL, "device buffers must be non-NULL");
-  if (!stride_ok(row_stride, n, rows) || !stride_ok(noise_stride, n, rows))
-    return api_fail(MLT_EINVAL, "rows must be at least n elements apart");
+  if (row_stride < 0 || noise_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
   if (!aligned_to(scores, dtype_size(dtype)) || !aligned_to(noise, 4) || !aligned_to(rules, 16))
     return api_fail(MLT_EINVAL, "scores and noise must be aligned to their elements, rules to 16 bytes");
   const int sms = api_sm_count();
@@ -148,8 +146,8 @@ int mlt_embed(void* stream, const void* table, int dtype, int64_t vocab, int dim
   if (rc != MLT_OK) return rc;
   if (tokens == 0) return MLT_OK;
   if (table == nullptr || ids == nullptr || out == nullptr) return api_fail(MLT_EINVAL, "device buffers must be non-NULL");
-  if (!stride_ok(table_stride, dim, vocab) || !stride_ok(out_stride, dim, tokens))
-    return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
+  if (table_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
+  if (!stride_ok(out_stride, dim, tokens)) return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
   if (!aligned_to(table, dtype_size(dtype)) || !aligned_to(out, dtype_size(out_dtype)) ||
       !aligned_to(ids, ids_64 ? 8 : 4))
     return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
@@ -189,8 +187,8 @@ int mlt_embed_grad(void* stream, const void* grad_out, int dtype, int64_t grad_s
   if (rc != MLT_OK) return rc;
   if (grad_table == nullptr || (tokens > 0 && (grad_out == nullptr || ids == nullptr)))
     return api_fail(MLT_EINVAL, "device buffers must be non-NULL");
-  if (!stride_ok(grad_stride, dim, tokens) || !stride_ok(out_stride, dim, vocab))
-    return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
+  if (grad_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
+  if (!stride_ok(out_stride, dim, vocab)) return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
   if (!aligned_to(grad_out, dtype_size(dtype)) || !aligned_to(grad_table, dtype_size(out_dtype)) ||
       !aligned_to(ids, ids_64 ? 8 : 4))
     return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
@@ -261,8 +259,9 @@ int mlt_scan_grad(void* stream, const mlt_scan_args* args, const mlt_scan_grads*
   rc = check_scan_inputs(args);
   if (rc != MLT_OK) return rc;
   if (args->length > 0 && args->batch > 0 && grads->gy == nullptr) return api_fail(MLT_EINVAL, "gy must be non-NULL");
-  if (!stride_ok(grads->gy_step, args->dim, args->length) || grads->gy_batch < 0)
-    return api_fail(MLT_EINVAL, "gy: positions must be at least dim elements apart");
+  if (grads->gy_step < 0 || grads->gy_batch < 0) return api_fail(MLT_EINVAL, "gy: strides must not be negative");
+  if ((args->length + 31) / 32 * args->groups * ((args->dim / args->groups + 63) / 64) > kMaxCount)
+    return api_fail(MLT_EINVAL, "length x dim is too large for one gradient call");
   if (!aligned_to(grads->gy, dtype_size(args->dtype))) return api_fail(MLT_EINVAL, "gy is not aligned to its elements");
   if ((grads->z != nullptr && args->z == nullptr) || (grads->skip != nullptr && args->skip == nullptr) ||
       (grads->dt_bias != nullptr && args->dt_bias == nullptr) || (grads->conv_b != nullptr && args->conv_b == nullptr) ||

@@ -527,49 +527,59 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
     return out
 
 
+def _wide(t, name, dtype, shape):
+    """(address, batch stride, step stride) of a [batch][length]... input."""
+    if t is None:
+        return None, 0, 0
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name} must be a CUDA tensor of x's type")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {shape}")
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] > 1 and t.numel() > 0:
+        raise ValueError(f"the channels of {name} must be adjacent")
+    return t.data_ptr(), s[0], s[1]
+
+
+def _plain(t, name, dtype, shape):
+    """Address of a contiguous input, or None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of the shape {shape}")
+    return t.data_ptr()
+
+
 def _scan_args(x, dt, B, Cm, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state):
-    torch = _torch
     _cuda(x, "x")
-    a = ScanArgs()
-    dtype = x.dtype
-    a.dtype = _dtype_code(x)
-    _need(x.dim() == 3, "x must be [batch][length][dim]")
+    dtype, f32 = x.dtype, _torch.float32
+    if x.dim() != 3:
+        raise ValueError("x must be [batch][length][dim]")
     b, L, d = x.shape
     if B.dim() == 3:
         B = B.unsqueeze(2)
     if Cm.dim() == 3:
         Cm = Cm.unsqueeze(2)
-    _need(B.dim() == 4, "B must be [batch][length][groups][states]")
+    if B.dim() != 4:
+        raise ValueError("B must be [batch][length][groups][states]")
     g, n = B.shape[2:]
     taps = 0 if conv_w is None else conv_w.shape[1]
-    a.batch, a.length, a.dim, a.states, a.groups, a.taps = b, L, d, n, g, taps
     wide, narrow = (b, L, d), (b, L, g, n)
-    for name, t, shape in (("x", x, wide), ("dt", dt, wide), ("z", z, wide), ("B", B, narrow), ("C", Cm, narrow)):
-        if t is None:
-            continue
-        if not t.is_cuda or t.dtype != dtype:
-            raise TypeError(f"{name} must be a CUDA tensor of x's type")
-        if t.shape != shape:
-            raise ValueError(f"{name} must have the shape {shape}")
-        s = t.stride()
-        if (s[-1] != 1 and shape[-1] > 1 or len(s) == 4 and g > 1 and s[2] != n) and t.numel() > 0:
-            raise ValueError(f"the channels of {name} must be adjacent")
-        setattr(a, name, t.data_ptr())
-        setattr(a, name + "_batch", s[0])
-        setattr(a, name + "_step", s[1])
-    f32 = torch.float32
-    for name, t, shape, want in (("A", A, (d, n), f32), ("skip", skip, (d,), f32), ("dt_bias", dt_bias, (d,), f32),
-                                 ("conv_w", conv_w, (d, taps), f32), ("conv_b", conv_b, (d,), f32),
-                                 ("lengths", lengths, (b,), torch.int32), ("state", state, (b, d, n), f32),
-                                 ("conv_state", conv_state, (b, max(0, taps - 1), d), dtype)):
-        if t is None:
-            continue
-        if not t.is_cuda or t.dtype != want:
-            raise TypeError(f"{name} must be a CUDA tensor of {want}")
-        if t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous, of the shape {shape}")
-        setattr(a, name, t.data_ptr())
-    return a
+    xp, xb, xs = _wide(x, "x", dtype, wide)
+    dp, db, ds = _wide(dt, "dt", dtype, wide)
+    zp, zb, zs = _wide(z, "z", dtype, wide)
+    Bp, Bb, Bs = _wide(B, "B", dtype, narrow)
+    Cp, Cb, Cs = _wide(Cm, "C", dtype, narrow)
+    if g > 1 and B.numel() > 0 and (B.stride(2) != n or Cm.stride(2) != n):
+        raise ValueError("the groups of B and C must be adjacent")
+    return ScanArgs(_dtype_code(x), b, d, n, g, taps, L, xp, dp, zp, Bp, Cp, xb, xs, db, ds, zb, zs, Bb, Bs, Cb, Cs,
+                    _plain(A, "A", f32, (d, n)), _plain(skip, "skip", f32, (d,)),
+                    _plain(dt_bias, "dt_bias", f32, (d,)), _plain(conv_w, "conv_w", f32, (d, taps)),
+                    _plain(conv_b, "conv_b", f32, (d,)), _plain(lengths, "lengths", _torch.int32, (b,)),
+                    _plain(state, "state", f32, (b, d, n)),
+                    _plain(conv_state, "conv_state", dtype, (b, max(0, taps - 1), d)))
 
 
 def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=None, lengths=None, state=None,
@@ -588,26 +598,23 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     if out is not None:
         _need(tuple(y.shape) == (b, L, d) and y.dtype == x.dtype and y.is_cuda and (d == 1 or y.stride(2) == 1),
               "out must be like x, its channels adjacent")
+    n, taps = a.states, a.taps
     if state_out is None:
-        state_out = torch.empty((b, d, a.states), dtype=torch.float32, device=x.device)
-    else:
-        _cuda(state_out, "state_out", torch.float32)
-        _need(state_out.is_contiguous() and tuple(state_out.shape) == (b, d, a.states),
-              "state_out must be contiguous [batch][dim][states]")
-    if a.taps < 2:
+        state_out = torch.empty((b, d, n), dtype=torch.float32, device=x.device)
+    a.state_out = _plain(state_out, "state_out", torch.float32, (b, d, n))
+    if taps < 2:
         conv_state_out = None
-    elif conv_state_out is None:
-        conv_state_out = torch.empty((b, a.taps - 1, d), dtype=x.dtype, device=x.device)
     else:
-        _cuda(conv_state_out, "conv_state_out", x.dtype)
-        _need(conv_state_out.is_contiguous() and tuple(conv_state_out.shape) == (b, a.taps - 1, d),
-              "conv_state_out must be contiguous [batch][taps - 1][dim]")
-    a.y, a.y_batch, a.y_step = y.data_ptr(), y.stride(0), y.stride(1)
-    a.state_out = state_out.data_ptr()
-    a.conv_state_out = None if conv_state_out is None else conv_state_out.data_ptr()
-    ws, n_ws = _workspace(("scan", a.dtype, b, L, d, a.states, a.groups, a.taps),
-                          lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)), x.device, stream)
-    _check(lb.mlt_scan(_stream_of(x, stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws))
+        if conv_state_out is None:
+            conv_state_out = torch.empty((b, taps - 1, d), dtype=x.dtype, device=x.device)
+        a.conv_state_out = _plain(conv_state_out, "conv_state_out", x.dtype, (b, taps - 1, d))
+    a.y = y.data_ptr()
+    a.y_batch, a.y_step, _ = y.stride()
+    ws, n_ws = _workspace(("scan", b, L, d, n, a.groups), lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)),
+                          x.device, stream)
+    rc = lb.mlt_scan(_stream_of(x, stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
+    if rc:
+        _check(rc)
     return y, state_out, conv_state_out
 
 
@@ -619,29 +626,24 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
     lb = _setup()
     torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
-    _cuda(gy, "gy", x.dtype)
-    _need(gy.shape == x.shape, "gy must have x's shape")
-    s = gy.stride()
-    _need(gy.numel() == 0 or x.shape[2] == 1 or s[2] == 1, "the channels of gy must be adjacent")
     q = ScanGrads()
-    q.gy, q.gy_batch, q.gy_step = gy.data_ptr(), s[0], s[1]
-    if g_state is not None:
-        _cuda(g_state, "g_state", torch.float32)
-        _need(g_state.is_contiguous() and tuple(g_state.shape) == (a.batch, a.dim, a.states),
-              "g_state must be contiguous [batch][dim][states]")
-        q.g_state_out = g_state.data_ptr()
+    q.gy, q.gy_batch, q.gy_step = _wide(gy, "gy", x.dtype, x.shape)
+    q.g_state_out = _plain(g_state, "g_state", torch.float32, (a.batch, a.dim, a.states))
     g = {}
     for name, t in (("x", x), ("dt", dt), ("z", z), ("B", B), ("C", C_), ("A", A), ("skip", skip),
                     ("dt_bias", dt_bias), ("conv_w", conv_w), ("conv_b", conv_b), ("state", state),
                     ("conv_state", conv_state)):
-        if t is None or t.numel() == 0:
-            g[name] = None if t is None else torch.empty_like(t)
+        if t is None:
+            g[name] = None
             continue
-        g[name] = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        setattr(q, name, g[name].data_ptr())
-    ws, n_ws = _workspace(("scan_grad", a.dtype, *x.shape, a.states, a.groups, a.taps),
+        g[name] = t.new_empty(t.shape)
+        if t.numel() > 0:
+            setattr(q, name, g[name].data_ptr())
+    ws, n_ws = _workspace(("scan_grad", *x.shape, a.states, a.groups),
                           lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device, stream)
-    _check(lb.mlt_scan_grad(_stream_of(x, stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws))
+    rc = lb.mlt_scan_grad(_stream_of(x, stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
+    if rc:
+        _check(rc)
     return g
 
 

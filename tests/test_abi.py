@@ -214,3 +214,58 @@ def test_decode_jit_tuning_and_queries():
 def test_walk_shape_rejects(args):
     with pytest.raises(mlt.MltError):
         mlt.walk_shape(*args)
+
+
+def test_sequence_operators_reject_bad_arguments(L):
+    """Rejected on the host, before any CUDA call."""
+    buf, size = C.c_void_p(256), C.c_size_t()
+    rule = mlt.SampleRule(1.0, 0, 1.0, 0.0)
+
+    def sample(dtype=0, rows=2, n=8, stride=8, noise_stride=8, rule=C.byref(rule), rules=None, m=1, scores=buf,
+               noise=buf, index=buf, logp=buf):
+        return L.mlt_sample(None, scores, dtype, rows, n, stride, noise, noise_stride, rule, rules, m, None, 0, index, logp)
+
+    for bad in (dict(dtype=3), dict(rows=-1), dict(n=-1), dict(n=(1 << 27) + 1), dict(m=0), dict(m=2049),
+                dict(rule=None), dict(rules=buf), dict(stride=-8), dict(noise_stride=-1), dict(scores=None),
+                dict(noise=None), dict(index=None), dict(logp=None), dict(scores=C.c_void_p(258)),
+                dict(rule=C.byref(mlt.SampleRule(-1.0, 0, 1.0, 0.0))),
+                dict(rule=C.byref(mlt.SampleRule(float("inf"), 0, 1.0, 0.0))),
+                dict(rule=C.byref(mlt.SampleRule(1.0, 0, float("nan"), 0.0))),
+                dict(rule=None, rules=C.c_void_p(260))):
+        assert sample(**bad) == -1, bad
+    assert sample(rows=0) == 0
+    assert L.mlt_sample_workspace(0, 2, 8, 1, None) == -1
+    assert L.mlt_sample_workspace(0, 2, 8, 0, C.byref(size)) == -1
+    assert L.mlt_sample_workspace(0, 2, 8, 1, C.byref(size)) == 0 and size.value == 0
+
+    def embed(dtype=0, vocab=4, dim=8, stride=8, tokens=3, out_dtype=0, out_stride=8, table=buf, ids=buf, out=buf):
+        return L.mlt_embed(None, table, dtype, vocab, dim, stride, ids, 1, tokens, C.c_float(1), out, out_dtype, out_stride)
+
+    for bad in (dict(dtype=-1), dict(out_dtype=5), dict(vocab=0), dict(dim=0), dict(dim=(1 << 20) + 1),
+                dict(stride=-8), dict(out_stride=7), dict(tokens=-1), dict(table=None), dict(ids=None), dict(out=None),
+                dict(ids=C.c_void_p(260)), dict(table=C.c_void_p(258))):
+        assert embed(**bad) == -1, bad
+    assert embed(tokens=0) == 0
+    assert L.mlt_embed_grad_workspace(10, 0, 8, C.byref(size)) == -1
+    assert L.mlt_embed_grad_workspace(10, 4, 8, C.byref(size)) == 0 and size.value > 0
+    grad = lambda ws, n: L.mlt_embed_grad(None, buf, 0, 8, buf, 1, 10, 4, 8, C.c_float(1), ws, n, buf, 0, 8)  # noqa: E731
+    assert grad(None, 0) == -1 and grad(buf, size.value - 1) == -1 and grad(C.c_void_p(264), size.value) == -1
+    assert b"workspace" in L.mlt_last_error()
+
+    def scan(**kw):
+        a = mlt.ScanArgs(0, 2, 8, 16, 1, 4, 5, *[256] * 5, *[40, 8] * 3, *[80, 16] * 2, 256, None, None, 256, None, None,
+                         None, None, 256, 40, 8, None, None)
+        for k, v in kw.items():
+            setattr(a, k, v)
+        return L.mlt_scan(None, C.byref(a), buf, 1 << 30), L.mlt_scan_workspace(C.byref(a), C.byref(size))
+
+    for bad in (dict(dtype=9), dict(batch=-1), dict(batch=65536), dict(length=-1), dict(dim=0), dict(groups=3),
+                dict(groups=0), dict(states=0), dict(states=33), dict(taps=5), dict(taps=-1)):
+        assert scan(**bad) == (-1, -1), bad
+    for bad in (dict(x=None), dict(dt=None), dict(B=None), dict(C=None), dict(A=None), dict(conv_w=None), dict(y=None),
+                dict(x_step=-8), dict(dt_batch=-8), dict(z_step=-8), dict(B_step=-16), dict(y_step=7), dict(y_batch=7),
+                dict(x=258), dict(y=258)):
+        assert scan(**bad)[0] == -1, bad
+    assert scan(batch=0) == (0, 0)
+    assert L.mlt_scan(None, None, None, 0) == -1 and L.mlt_scan_grad(None, None, None, None, 0) == -1
+    assert L.mlt_scan_workspace(None, C.byref(size)) == -1 and L.mlt_scan_grad_workspace(None, C.byref(size)) == -1
