@@ -1397,7 +1397,7 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
     int threads = a.n <= 4096 ? 128 : a.n <= 16384 ? 256 : a.n <= 32768 ? 512 : 1024;
     while (threads < 1024 && threads * 4 < a.m) threads *= 2;
     if (team > 1) threads = 1024;
-    const int bins = a.n <= 16384 && threads <= 512 ? 512 : kBins;  // a multiple of the threads
+    const int bins = threads <= 512 && a.n <= 16384 ? 512 : a.n <= 262144 ? 1024 : kBins;  // a multiple of the threads
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;

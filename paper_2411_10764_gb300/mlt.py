@@ -453,8 +453,8 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
         each = rules.data_ptr()
     device = scores.device
     if out is None:
-        index = torch.empty((rows, m), dtype=torch.int64, device=device)
-        logprob = torch.empty((rows, m), dtype=torch.float32, device=device)
+        index = torch.empty(rows, m, dtype=torch.int64, device=device)
+        logprob = torch.empty(rows, m, dtype=torch.float32, device=device)
     else:
         index, logprob = out
         for t, dt in ((index, torch.int64), (logprob, torch.float32)):
@@ -489,7 +489,7 @@ def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None)
     code, stride = _dtype_code(table), _rows(table, "table")
     vocab, dim = table.shape
     if out is None:
-        out = _torch.empty((*ids.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
+        out = _torch.empty(*ids.shape, dim, dtype=out_dtype or table.dtype, device=table.device)
         out_stride = dim
     else:
         _cuda(out, "out")
@@ -515,7 +515,7 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
     code, stride = _dtype_code(flat), _rows(flat, "grad_out")
     vocab, tokens = int(vocab), ids.numel()
     if out is None:
-        out = _torch.empty((vocab, dim), dtype=out_dtype or grad_out.dtype, device=grad_out.device)
+        out = _torch.empty(vocab, dim, dtype=out_dtype or grad_out.dtype, device=grad_out.device)
     else:
         _cuda(out, "out")
         _need(tuple(out.shape) == (vocab, dim), "out must be [vocab][dim]")
@@ -594,19 +594,19 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
     b, L, d = x.shape
-    y = torch.empty((b, L, d), dtype=x.dtype, device=x.device) if out is None else out
+    y = torch.empty(b, L, d, dtype=x.dtype, device=x.device) if out is None else out
     if out is not None:
         _need(tuple(y.shape) == (b, L, d) and y.dtype == x.dtype and y.is_cuda and (d == 1 or y.stride(2) == 1),
               "out must be like x, its channels adjacent")
     n, taps = a.states, a.taps
     if state_out is None:
-        state_out = torch.empty((b, d, n), dtype=torch.float32, device=x.device)
+        state_out = torch.empty(b, d, n, dtype=torch.float32, device=x.device)
     a.state_out = _plain(state_out, "state_out", torch.float32, (b, d, n))
     if taps < 2:
         conv_state_out = None
     else:
         if conv_state_out is None:
-            conv_state_out = torch.empty((b, taps - 1, d), dtype=x.dtype, device=x.device)
+            conv_state_out = torch.empty(b, taps - 1, d, dtype=x.dtype, device=x.device)
         a.conv_state_out = _plain(conv_state_out, "conv_state_out", x.dtype, (b, taps - 1, d))
     a.y = y.data_ptr()
     a.y_batch, a.y_step, _ = y.stride()
