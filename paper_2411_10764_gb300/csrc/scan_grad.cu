@@ -19,7 +19,11 @@
 // a chunk every kSub-th state is kept in shared memory and the others, with their decays,
 // in registers while their kSub positions are walked backwards.
 //
-// Bound: issue.  A position and channel takes about 60 instructions in each of its four lanes.
+// Bound: issue.  Eight channels' position costs a warp about 190 instructions with 16 states: 18 to
+// find the kept states, 22 to recompute, 56 backwards, 40 for the sums over lanes and
+// channels, the rest for the activations' slopes and stores; 49 % of the issue slots are
+// used at the 16 warps an SM that the registers allow.  Halves of the chunk (24 warps at 80
+// registers) took 143 us where this takes 128.
 #include "scan.cuh"
 
 namespace mlt {
@@ -68,6 +72,7 @@ struct alignas(16) Walk {
   float ga[Shape<S>::kSub][kChannels + 4];         // e . A, times log2 e
   float bc[kThreads / 32][Shape<S>::kSub][2 * 4 * S];  // each warp's share of dB, dC
   float dv[kRing][kChannels];
+  float params[kScanMaxTaps + 3][kChannels];  // convolution weights and bias, dt_bias, skip
 };
 
 // Two channels of gy at `count` positions from t on.
@@ -308,6 +313,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     return;
   }
   stage_chunk<T, S, kVec>(a, g, k, q, w.begin, w.live, sm.in);
+  if (tl == 0) {
+    auto keep = [&](int row, F2 v) {
+      float2 f;
+      un2(v, f.x, f.y);
+      *reinterpret_cast<float2*>(&sm.params[row][q.c]) = f;
+    };
+#pragma unroll
+    for (int j = 0; j < kScanMaxTaps; ++j) keep(j, q.w[j]);
+    keep(kScanMaxTaps, q.conv_b);
+    keep(kScanMaxTaps + 1, q.bias);
+    F2 skip = dup2(0.0f);
+    if (cin && a.skip != nullptr) skip = f2(a.skip[cc], q.n > 1 ? a.skip[cc + 1] : 0.0f);
+    keep(kScanMaxTaps + 2, skip);
+  }
   for (int i = threadIdx.x; i < kRing * kChannels; i += kThreads) sm.dv[i / kChannels][i % kChannels] = 0.0f;
   Lane<S> A = lane_zero<S>(), h = A, r = A, dA = A;
   if (in) {
@@ -341,8 +360,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     }
   }
 
-  F2 skip = dup2(0.0f);
-  if (cin && a.skip != nullptr) skip = f2(a.skip[cc], q.n > 1 ? a.skip[cc + 1] : 0.0f);
+  // the parameters come from shared memory after each walk, which needs the registers
+  auto kept_params = [&](F2& skip) {
+    auto two = [&](int row) {
+      const volatile float* v = &sm.params[row][q.c];  // volatile: not kept in registers
+      return f2(v[0], v[1]);
+    };
+    PairParams r;
+    r.c = q.c;
+    r.n = q.n;
+#pragma unroll
+    for (int j = 0; j < kScanMaxTaps; ++j) r.w[j] = two(j);
+    r.conv_b = two(kScanMaxTaps);
+    r.bias = two(kScanMaxTaps + 1);
+    skip = two(kScanMaxTaps + 2);
+    return r;
+  };
   const bool next_live = w.begin + Sh::kChunk < w.len;  // its convolution reads this chunk's last inputs
   const int halo = a.taps > 1 ? a.taps - 1 : 0;
   F2 vec[kVecs];
@@ -451,6 +484,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
     }
     // through the gate, softplus and the convolution's activation
     const long long o = static_cast<long long>(ct) * a.dim;
+    F2 skip;
+    const PairParams par = kept_params(skip);
     if (mine) {
       F2 dv = dup2(0.0f);
       if (ct < w.live) {
@@ -467,13 +502,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
           store_two<T, kVec>(gz + o, q.n, mul2(mul2(two_f32(gy[0]), fma2(skip, u, two(&sm.y[tl][q.c]))), slope));
         }
         const F2 graw = mul2(fma2(gp, u, mul2(two(&sm.ga[tl][q.c]), dup2(1.0f / kLog2E))),
-                             sigmoid2(add2(two_f32(raw.dt[0]), q.bias)));
+                             sigmoid2(add2(two_f32(raw.dt[0]), par.bias)));
         if (g.dt != nullptr) store_two<T, kVec>(gdt + o, q.n, graw);
         vec[kScanMaxTaps + 1] = fma2(gc, u, vec[kScanMaxTaps + 1]);
         vec[kScanMaxTaps + 2] = add2(graw, vec[kScanMaxTaps + 2]);
         dv = fma2(gp, d, mul2(gc, skip));
         if (a.taps > 0) {
-          const F2 v = conv_run(a, q, raw, 0), sv = sigmoid2(v);
+          const F2 v = conv_run(a, par, raw, 0), sv = sigmoid2(v);
           dv = mul2(dv, mul2(sv, fma2(v, fma2(sv, dup2(-1.0f), dup2(1.0f)), dup2(1.0f))));
 #pragma unroll
           for (int j = 0; j < kScanMaxTaps; ++j)
@@ -502,10 +537,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
       };
       F2 d = dv(0);
       if (a.taps > 0) {
-        d = mul2(d, q.w[0]);
+        d = mul2(d, par.w[0]);
 #pragma unroll
         for (int j = 1; j < kScanMaxTaps; ++j)
-          if (j < a.taps && ct + j < Sh::kChunk) d = fma2(q.w[j], dv(j), d);
+          if (j < a.taps && ct + j < Sh::kChunk) d = fma2(par.w[j], dv(j), d);
       }
       if (next_live && ct >= Sh::kChunk - halo) {
         float v0, v1;
