@@ -1397,7 +1397,8 @@ cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cud
     int threads = a.n <= 4096 ? 128 : a.n <= 16384 ? 256 : a.n <= 32768 ? 512 : 1024;
     while (threads < 1024 && threads * 4 < a.m) threads *= 2;
     if (team > 1) threads = 1024;
-    const int bins = threads <= 512 && a.n <= 16384 ? 512 : a.n <= 262144 ? 1024 : kBins;  // a multiple of the threads
+    // a multiple of the threads; fewer are more crowded (64 x 50,021: 49 us with 1,024, 43 with 2,048)
+    const int bins = threads <= 512 && a.n <= 16384 ? 512 : kBins;
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
