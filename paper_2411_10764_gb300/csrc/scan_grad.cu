@@ -21,9 +21,10 @@
 //
 // Bound: issue.  Eight channels' position costs a warp about 190 instructions with 16 states: 18 to
 // find the kept states, 22 to recompute, 56 backwards, 40 for the sums over lanes and
-// channels, the rest for the activations' slopes and stores; 49 % of the issue slots are
+// channels, the rest for the activations' slopes and stores; about half of the issue slots are
 // used at the 16 warps an SM that the registers allow.  Halves of the chunk (24 warps at 80
-// registers) took 143 us where this takes 128.
+// registers) took 143 us where this takes 128.  The whole gradient of 4 x 1,021 x 1,024 with ragged
+// lengths takes 127 to 166 us by the lengths drawn.
 #include "scan.cuh"
 
 namespace mlt {
