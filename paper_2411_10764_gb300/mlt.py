@@ -356,8 +356,20 @@ def _setup():
     return _lib or lib()
 
 
-def _stream_of(t, stream):
-    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
+def _stream_of(t):
+    return _raw_stream(t.get_device())
+
+
+def _on(stream, call, *args):
+    """call(*args) with `stream` as the current one.  Workspace, copies and new outputs are then
+    of that stream's memory, which no work still queued elsewhere uses; and the
+    tensors given are kept until its work is done."""
+    with _torch.cuda.stream(stream):
+        for t in args:
+            for one in t if isinstance(t, tuple) else (t,):
+                if isinstance(one, _torch.Tensor) and one.is_cuda:
+                    one.record_stream(stream)
+        return call(*args)
 
 
 def _dtype_code(t) -> int:
@@ -391,9 +403,9 @@ def _rows(t, name: str) -> int:
 _ws_bytes: dict = {}
 
 
-def _workspace(key, query, device, stream):
-    """Device memory for one call (torch's allocator keeps it until the work
-    queued on the stream is done); the sizes that the library asks for are
+def _workspace(key, query, device):
+    """Device memory for one call (torch's allocator reuses it in the order of
+    the current stream); the sizes that the library asks for are
     remembered by the call's sizes."""
     n = _ws_bytes.get(key)
     if n is None:
@@ -404,10 +416,7 @@ def _workspace(key, query, device, stream):
         n = _ws_bytes[key] = out.value
     if n == 0:
         return None, 0
-    ws = _torch.empty(n, dtype=_torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws, n
+    return _torch.empty(n, dtype=_torch.uint8, device=device), n
 
 
 def sample_rules(temperature, top_k=0, top_p=1.0, min_p=0.0, rows: int | None = None, device="cuda"):
@@ -431,6 +440,8 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
     cuts instead of the four numbers.  Returns (index [rows][m] int64, -1
     past the last kept entry, logprob [rows][m] fp32)."""
     L = _setup()
+    if stream is not None:
+        return _on(stream, sample, scores, noise, temperature, top_k, top_p, min_p, m, rules, out)
     torch = _torch
     _cuda(scores, "scores")
     _cuda(noise, "noise", torch.float32)
@@ -461,8 +472,8 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
             _cuda(t, "out", dt)
             _need(t.is_contiguous() and t.numel() == rows * m, "out must be contiguous [rows][m] tensors")
     ws, n_ws = _workspace(("sample", code, rows, n, m),
-                          lambda b: L.mlt_sample_workspace(code, rows, n, m, C.byref(b)), device, stream)
-    rc = L.mlt_sample(_stream_of(scores, stream), scores.data_ptr(), code, rows, n, stride, noise.data_ptr(),
+                          lambda b: L.mlt_sample_workspace(code, rows, n, m, C.byref(b)), device)
+    rc = L.mlt_sample(_stream_of(scores), scores.data_ptr(), code, rows, n, stride, noise.data_ptr(),
                       noise_stride, rule, each, m, None if ws is None else ws.data_ptr(), n_ws, index.data_ptr(),
                       logprob.data_ptr())
     if rc:
@@ -484,6 +495,8 @@ def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None)
     """mlt_embed: scale * table[ids], rounded once to `out_dtype` (default: the
     table's); ids of any shape, negative ones give zeros."""
     L = _setup()
+    if stream is not None:
+        return _on(stream, embed, ids, table, scale, out_dtype, out)
     ids_64 = _ids(ids)
     _cuda(table, "table")
     code, stride = _dtype_code(table), _rows(table, "table")
@@ -496,7 +509,7 @@ def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None)
         _need(tuple(out.shape) == (*ids.shape, dim), "out must have the shape of ids and one more dimension, dim")
         flat = out if out.dim() == 2 else out.view(-1, dim)
         out_stride = _rows(flat, "out")
-    rc = L.mlt_embed(_stream_of(table, stream), table.data_ptr(), code, vocab, dim, stride, ids.data_ptr(), ids_64,
+    rc = L.mlt_embed(_stream_of(table), table.data_ptr(), code, vocab, dim, stride, ids.data_ptr(), ids_64,
                      ids.numel(), scale, out.data_ptr(), _dtype_code(out), out_stride)
     if rc:
         _check(rc)
@@ -507,6 +520,8 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
     """mlt_embed_grad: the gradient [vocab][dim] of embed's table from that of
     its output; the same from call to call."""
     L = _setup()
+    if stream is not None:
+        return _on(stream, embed_grad, ids, grad_out, vocab, scale, out_dtype, out)
     ids_64 = _ids(ids)
     _cuda(grad_out, "grad_out")
     dim = grad_out.shape[-1]
@@ -520,8 +535,8 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
         _cuda(out, "out")
         _need(tuple(out.shape) == (vocab, dim), "out must be [vocab][dim]")
     ws, n_ws = _workspace(("embed_grad", tokens, vocab, dim),
-                          lambda b: L.mlt_embed_grad_workspace(tokens, vocab, dim, C.byref(b)), out.device, stream)
-    _check(L.mlt_embed_grad(_stream_of(out, stream), flat.data_ptr(), code, stride, ids.data_ptr(), ids_64, tokens, vocab,
+                          lambda b: L.mlt_embed_grad_workspace(tokens, vocab, dim, C.byref(b)), out.device)
+    _check(L.mlt_embed_grad(_stream_of(out), flat.data_ptr(), code, stride, ids.data_ptr(), ids_64, tokens, vocab,
                             dim, scale, None if ws is None else ws.data_ptr(), n_ws, out.data_ptr(), _dtype_code(out),
                             _rows(out, "out")))
     return out
@@ -591,6 +606,9 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     For single tokens (length 1) pass state_out=state and
     conv_state_out=conv_state to update them in place."""
     lb = _setup()
+    if stream is not None:
+        return _on(stream, scan, x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state, out,
+                   state_out, conv_state_out)
     torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
     b, L, d = x.shape
@@ -611,8 +629,8 @@ def scan(x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None, conv_b=N
     a.y = y.data_ptr()
     a.y_batch, a.y_step, _ = y.stride()
     ws, n_ws = _workspace(("scan", b, L, d, n, a.groups), lambda q: lb.mlt_scan_workspace(C.byref(a), C.byref(q)),
-                          x.device, stream)
-    rc = lb.mlt_scan(_stream_of(x, stream), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
+                          x.device)
+    rc = lb.mlt_scan(_stream_of(x), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
     if rc:
         _check(rc)
     return y, state_out, conv_state_out
@@ -624,6 +642,9 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
     of the returned state (`g_state`, or None).  Returns a dict by the names of
     the arguments (C_'s as "C"); None for inputs that were not given."""
     lb = _setup()
+    if stream is not None:
+        return _on(stream, scan_grad, gy, x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state,
+                   g_state)
     torch = _torch
     a = _scan_args(x, dt, B, C_, A, z, skip, dt_bias, conv_w, conv_b, lengths, state, conv_state)
     q = ScanGrads()
@@ -640,8 +661,8 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
         if t.numel() > 0:
             setattr(q, name, g[name].data_ptr())
     ws, n_ws = _workspace(("scan_grad", *x.shape, a.states, a.groups),
-                          lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device, stream)
-    rc = lb.mlt_scan_grad(_stream_of(x, stream), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
+                          lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device)
+    rc = lb.mlt_scan_grad(_stream_of(x), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
     if rc:
         _check(rc)
     return g
