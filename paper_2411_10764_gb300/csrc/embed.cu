@@ -65,6 +65,53 @@ __global__ void __launch_bounds__(256) k_embed(const TI* table, long long in_str
   }
 }
 
+// The same with `rows` whole rows a warp, one after the other: for rows of more than 64 narrow packs, where
+// k_embed's warps are short and what each does before its first load counts.  200,000 rows: of 269
+// 16-bit values (packs of one) 33 us for 101, 269 fp32 values 42 for 102, 402 16-bit values 33 for
+// 69; with 35 packs 24 for 20, and with packs of 16 bytes no gain.
+constexpr int kRowsUnroll = 8;
+
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(256) k_embed_rows(const TI* table, long long in_stride, const void* ids, int ids_64,
+                                                    long long tokens, long long vocab, int dim, float scale, TO* out,
+                                                    long long out_stride, int rows, unsigned* err) {
+  const int lane = threadIdx.x & 31;
+  const long long first = (static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5)) * rows;
+  pdl_wait();
+  pdl_trigger();
+  if (first >= tokens) return;
+  const int have = static_cast<int>(min(static_cast<long long>(rows), tokens - first)), packs = dim / V;
+  int mine = -1;
+  if (lane < have) {
+    const long long id = id_of(ids, ids_64, first + lane);
+    if (id >= vocab) atomicOr(err, kErrBadToken);
+    if (id >= 0 && id < vocab) mine = static_cast<int>(id);
+  }
+  TO* dst = out + first * out_stride;
+  for (int r = 0; r < have; ++r, dst += out_stride) {
+    const int id = __shfl_sync(0xffffffffu, mine, r);
+    const bool live = id >= 0;
+    const TI* row = table + (live ? id : 0) * in_stride;
+    for (int c0 = 0; c0 < packs; c0 += 32 * kRowsUnroll) {
+      const int c1 = c0 + lane, left = packs - c1;
+      const TI* from = row + static_cast<long long>(c1) * V;
+      TO* to = dst + static_cast<long long>(c1) * V;
+      Pack<TI, V> p[kRowsUnroll];
+#pragma unroll
+      for (int u = 0; u < kRowsUnroll; ++u)
+        if (live && u * 32 < left) p[u] = *reinterpret_cast<const Pack<TI, V>*>(from + u * 32 * V);
+#pragma unroll
+      for (int u = 0; u < kRowsUnroll; ++u) {
+        if (u * 32 >= left) break;
+        Pack<TO, V> q;
+#pragma unroll
+        for (int e = 0; e < V; ++e) q.v[e] = from_f32<TO>(live ? __fmul_rn(to_f32(p[u].v[e]), scale) : 0.0f);
+        *reinterpret_cast<Pack<TO, V>*>(to + u * 32 * V) = q;
+      }
+    }
+  }
+}
+
 // Widest pack (elements) that divides the row length, both strides and both
 // addresses; at most 16 bytes of the narrower type.
 int pack_width(const EmbedArgs& a) {
@@ -743,7 +790,7 @@ GradPlan grad_plan(long long tokens, long long vocab, int dim, int sms) {
 
 }  // namespace
 
-cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t st) {
+cudaError_t launch_embed(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st) {
   if (a.tokens == 0) return cudaSuccess;
   ++*launches;
   return with_width(pack_width(a), [&](auto width) {
@@ -754,6 +801,15 @@ cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t s
         using TO = decltype(to);
         const int packs = a.dim / V;
         const int lanes = pow2_at_most_32((packs + kUnroll - 1) / kUnroll);
+        if (packs > 64 && V * (sizeof(TI) < sizeof(TO) ? sizeof(TI) : sizeof(TO)) < 16) {
+          // 16 CTAs for each SM before a warp takes a second row, four rows at most
+          const long long full = a.tokens / (16LL * 8 * sms);
+          const int rows = full < 1 ? 1 : full > 4 ? 4 : static_cast<int>(full);
+          const dim3 ctas(static_cast<unsigned>((a.tokens + 8LL * rows - 1) / (8LL * rows)));
+          return launch_pdl(k_embed_rows<TI, TO, V>, ctas, dim3(256), 0, st, static_cast<const TI*>(a.table), a.in_stride,
+                            a.ids, a.ids_64, a.tokens, a.vocab, a.dim, a.scale, static_cast<TO*>(a.out), a.out_stride,
+                            rows, a.err);
+        }
         const long long per = 256 / lanes;
         const dim3 grid(static_cast<unsigned>((a.tokens + per - 1) / per),
                         static_cast<unsigned>((packs + lanes * kUnroll - 1) / (lanes * kUnroll)));

@@ -89,7 +89,7 @@ struct EmbedArgs {
   unsigned* err;
   void* ws;
 };
-cudaError_t launch_embed(const EmbedArgs& a, long long* launches, cudaStream_t st);
+cudaError_t launch_embed(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st);
 size_t embed_grad_workspace(long long tokens, long long vocab, int dim, int sms);
 cudaError_t launch_embed_grad(const EmbedArgs& a, int sms, long long* launches, cudaStream_t st);
 

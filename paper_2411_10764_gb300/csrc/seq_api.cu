@@ -168,7 +168,7 @@ int mlt_embed(void* stream, const void* table, int dtype, int64_t vocab, int dim
   a.out_stride = tokens > 1 ? out_stride : dim;
   a.err = err;
   long long launches = 0;
-  const cudaError_t e = launch_embed(a, &launches, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_embed(a, api_sm_count(), &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "embed launch");
 }
 

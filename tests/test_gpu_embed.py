@@ -181,3 +181,22 @@ def test_binding_refuses():
         mlt.embed_grad(ids, t, 4)
     with pytest.raises(mlt.MltError):
         mlt.embed_grad(ids, t[:3], 0)
+
+
+@pytest.mark.parametrize("kinds", ["f32 f32", "bf16 bf16", "f16 f32", "f32 bf16"])
+@pytest.mark.parametrize("tokens,dim,stride", [(5, 269, 269), (20011, 131, 140), (39001, 174, 174), (80003, 269, 273),
+                                               (100003, 140, 140)])
+def test_many_rows_of_narrow_packs(tokens, dim, stride, kinds):
+    """Rows that only narrow accesses fit, by one to four rows a warp."""
+    import torch
+
+    ti, to = ({"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[k] for k in kinds.split())
+    rng = np.random.default_rng(tokens + dim)
+    ids = torch.from_numpy(rng.integers(-3, 301, tokens)).cuda()
+    table = torch.from_numpy(rng.standard_normal((301, stride)).astype(np.float32)).cuda().to(ti)[:, :dim]
+    buf = torch.full((tokens, stride), 7.0, device="cuda", dtype=to)
+    mlt.embed(ids, table, scale=1.7, out=buf[:, :dim])
+    want = (table.float() * np.float32(1.7).item())[ids.clamp(min=0)] * (ids >= 0)[:, None]
+    assert torch.equal(buf[:, :dim], want.to(to))
+    assert (buf[:, dim:] == 7.0).all()
+    mlt.sync_status()
