@@ -271,14 +271,16 @@ __global__ void __launch_bounds__(kThreads, 5) k_scan(mlt_scan_args a, Plan p, u
   T* yp = kOut ? y0 + run * a.y_step : nullptr;
   auto write = [&](int i) {
     const Staged<S>& st = sm.staged[i & 1];
-    const int rows = n > 0 ? written - i * kTile - run : 0;
+    const int rows = n > 0 ? written - i * kTile - run : 0, live = positions - i * kTile - run;
     T* to = yp;
     yp += kTile * a.y_step;
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
       const float4 o = st.out[run + j][c / 2];
       const float2 y = st.y[run + j][c / 2];
-      if (j < rows) store_two<T, (W >= 2 * sizeof(T))>(to, n, f2((y.x + o.x) * o.z, (y.y + o.y) * o.w));
+      // (past the sequence's end 0, whatever the state: a factor of 0 would leave NaN)
+      const F2 v = j < live ? f2((y.x + o.x) * o.z, (y.y + o.y) * o.w) : dup2(0.0f);
+      if (j < rows) store_two<T, (W >= 2 * sizeof(T))>(to, n, v);
       to += a.y_step;
     }
   };
@@ -540,7 +542,7 @@ __global__ void __launch_bounds__(256) k_scan_step(mlt_scan_args a) {
       }
     }
   }
-  if (in) static_cast<T*>(a.y)[b * a.y_batch + c] = from_f32<T>((y + add) * gate);
+  if (in) static_cast<T*>(a.y)[b * a.y_batch + c] = from_f32<T>(live ? (y + add) * gate : 0.0f);
 }
 
 // Length 0: the states as they were.
