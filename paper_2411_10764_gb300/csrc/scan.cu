@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_scan(mlt_scan_args a, Plan p, u
                                        : (a.state != nullptr ? a.state + k.b * of_seq : nullptr);
       if (from != nullptr) h[c] = lane_load<S>(from + o, lane * S, a.states);
 #pragma unroll
-      for (int s = 0; s < Lane<S>::H; ++s) A[c].v[s] = mul2(A[c].v[s], dup2(kLog2E));
+      for (int s = 0; s < Lane<S>::H; ++s) A[c].v[s] = rate2(A[c].v[s]);
     }
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll 1
@@ -404,9 +404,10 @@ __global__ void __launch_bounds__(256) k_scan_carry(mlt_scan_args a, Plan p, uns
   float* e = reinterpret_cast<float*>(ws + p.off_e) + static_cast<long long>(b) * p.chunks * of_seq + i;
   const float* sum = reinterpret_cast<const float*>(ws + p.off_sum) + static_cast<long long>(b) * p.chunks * a.dim +
                      i / a.states;
-  const float A = a.A[i] * kLog2E;
+  const float A = rate(a.A[i]);
   float h = a.state != nullptr ? a.state[b * of_seq + i] : 0.0f;
   const int last = p.chunks - 1;
+  const int live = static_cast<int>((length_of(a, b) + p.chunk - 1) / p.chunk);  // later chunks leave the state
   // loads of eight chunks first: the stores go to the same memory
   for (int c0 = 0; c0 < last; c0 += 8) {
     float end[8], d[8];
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(256) k_scan_carry(mlt_scan_args a, Plan p, uns
     for (int k = 0; k < 8; ++k)
       if (c0 + k < last) {
         e[(c0 + k) * of_seq] = h;
-        h = fmaf(ex2(A * d[k]), h, end[k]);
+        if (c0 + k < live) h = fmaf(ex2(A * d[k]), h, end[k]);
       }
   }
   e[last * of_seq] = h;
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(256) k_scan_step(mlt_scan_args a) {
 #pragma unroll
     for (int s = 0; s < Lane<S>::H; ++s) {
       const F2 decay = ex2_2(mul2(f2(dk * kLog2E, dk * kLog2E), A.v[s]));
-      h[k].v[s] = fma2(decay, h[k].v[s], mul2(f2(pk, pk), f2(Bs[2 * s], Bs[2 * s + 1])));
+      if (live) h[k].v[s] = fma2(decay, h[k].v[s], mul2(f2(pk, pk), f2(Bs[2 * s], Bs[2 * s + 1])));
       r.v[s] = mul2(h[k].v[s], f2(Cs[2 * s], Cs[2 * s + 1]));
     }
     o = lane_sum(r);

@@ -12,6 +12,7 @@
 // They take no immediate operands, so formulas full of constants stay scalar.
 #pragma once
 
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -113,6 +114,18 @@ __device__ __forceinline__ F2 ex2_2(F2 a) {
   float x, y;
   un2(a, x, y);
   return f2(ex2(x), ex2(y));
+}
+
+// A log2 e, for powers of two.  Kept finite: the staged positions past a sequence's end have a step of
+// 0, and 0 times an infinite rate would be NaN where the state is to stay as it is.  (NaN stays NaN.)
+__device__ __forceinline__ float rate(float a) {
+  const float r = a * kLog2E;
+  return isinf(r) ? copysignf(FLT_MAX, r) : r;
+}
+__device__ __forceinline__ F2 rate2(F2 a) {
+  float x, y;
+  un2(a, x, y);
+  return f2(rate(x), rate(y));
 }
 
 // States of a lane, as pairs (S = 1: the second half stays zero).
