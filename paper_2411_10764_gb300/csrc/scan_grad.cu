@@ -585,17 +585,39 @@ struct Finish {
   long long bc_blocks, sum_blocks, edge_blocks;
 };
 
-// Sum over the sequences' live chunks of p[(b chunks + chunk) stride], by 8 threads of a column.
+// Sum over the sequences' live chunks of at[(b chunks + chunk) stride]: `part`'s share of them, every
+// eighth (sequence, chunk) pair, so that sequences of one chunk each are shared too.  Loads of eight
+// pairs come before their sum, which is compensated: there may be 65,535 sequences, and a
+// plain sum of as many equal terms in 32 bits is off by a thousandth.
 __device__ __forceinline__ float sum_chunks(const mlt_scan_args& a, const GradPlan& p, const float* at, long long stride,
                                             int part) {
-  float sum = 0.0f;
-  for (int b = 0; b < a.batch; ++b) {
-    const long long live = (length_of(a, b) + p.chunk - 1) / p.chunk;
-    const float* q = at + b * p.chunks * stride;
-#pragma unroll 4
-    for (long long k = part; k < live; k += 8) sum += q[k * stride];
+  constexpr int kAhead = 8;
+  float sum = 0.0f, lost = 0.0f;
+  int b = 0;
+  long long k = part;  // the next pair's chunk
+  auto wrap = [&]() {
+    if (p.chunks == 1) {
+      b += static_cast<int>(k);
+      k = 0;
+    }
+    for (; k >= p.chunks && b < a.batch; ++b) k -= p.chunks;
+  };
+  wrap();
+  while (b < a.batch) {
+    float v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      v[i] = 0.0f;
+      if (b < a.batch && k * p.chunk < length_of(a, b)) v[i] = at[(b * p.chunks + k) * stride];
+      k += 8;
+      wrap();
+    }
+    const float now = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    const float y = __fsub_rn(now, lost), t = __fadd_rn(sum, y);
+    lost = isfinite(t) ? __fsub_rn(__fsub_rn(t, sum), y) : 0.0f;  // an infinite sum stays one
+    sum = t;
   }
-  return sum;
+  return __fsub_rn(sum, lost);
 }
 
 template <typename T>
