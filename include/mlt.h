@@ -552,8 +552,10 @@ typedef struct {
  *            temperature 0; -infinity where out_index is -1
  * With Gumbel noise, -ln(-ln u) of uniform u, these are m draws without
  * replacement, the first one exactly a draw from the kept entries' softmax.
- * Probability masses are summed as 64-bit integers in units of 2^-31 of the
- * best entry's weight, so results do not depend on the order of summation.
+ * Probability masses are summed as 64-bit integers, so results do not depend
+ * on the order of summation; rounding to them moves the mass of the best
+ * entries by at most 2^-23 of it, however many there are and however
+ * improbable.
  *   scores   device [rows][n] of `dtype`, row_stride elements apart
  *   noise    device [rows][n] fp32, noise_stride elements apart
  *   rule     host, for every row; or `rules`, device [rows], instead of it

@@ -85,10 +85,41 @@ __device__ __forceinline__ Rule read_rule(const mlt_sample_rule& q, long long n)
   return r;
 }
 
-// Weight of an entry in fixed point, units of 2^-31 of the best one's.
+// Weight of an entry of a short row in fixed point, units of 2^-31 of the best one's: rounding moves
+// the mass of 512 by at most 2^-23 of the best one's.
 __device__ __forceinline__ uint32_t fixed_weight(float s, float top) {
   return __float2uint_rn(__expf(__fsub_rn(s, top)) * 2147483648.0f);
 }
+
+// Weights of a long row, whose tail may be a hundred million entries far below the best: the unit is
+// 2^-25 of the mean weight, so rounding moves the mass of any entries that are the best ones by at
+// most 2^-26 of it, and the row's mass stays below 2^53.
+struct Weights {
+  float top, one;  // the best score, units in its weight
+
+  Weights() = default;
+  // z: the sum of all n weights, to a few digits
+  __device__ __forceinline__ Weights(float top_, float z, int n) : top(top_) {
+    const int bits = 25 + (32 - __clz(n - 1)) - ((__float_as_int(z) >> 23) - 127);
+    one = __int_as_float((bits + 127) << 23);
+  }
+  // As halves, upper 2^32 + lower modulo 2^64: the upper one by adding 2^23, which leaves the nearest
+  // whole number in a float's low bits (it is below 2^21), the lower one from the exact rest,
+  // which may be negative.  (64 rows x 50,021 with top-p 43.9 us; converted to 64 bits 46.1.)
+  struct Halves {
+    uint32_t upper, lower;
+  };
+  __device__ __forceinline__ Halves halves(float s) const {
+    const float x = __expf(__fsub_rn(s, top)) * one;
+    const float shifted = __fmaf_rn(x, 0x1p-32f, 0x1p23f);
+    const int rest = __float2int_rn(__fmaf_rn(__fsub_rn(shifted, 0x1p23f), -0x1p32f, x));
+    return {static_cast<uint32_t>((__float_as_int(shifted) & 0x7FFFFF) + (rest >> 31)), static_cast<uint32_t>(rest)};
+  }
+  __device__ __forceinline__ unsigned long long of(float s) const {
+    const Halves h = halves(s);
+    return (static_cast<unsigned long long>(h.upper) << 32) + h.lower;
+  }
+};
 
 // Loads and shared-memory adds under a predicate, so that those of a group of entries issue one
 // after another (behind branches each waits for the one before).
@@ -728,23 +759,23 @@ __device__ __forceinline__ void take_list(const Team& t, Shared& sh, const unsig
   __syncthreads();
 }
 // Mass of the first `n` entries of sh.list.
-__device__ __forceinline__ unsigned long long list_mass(Shared& sh, unsigned n, float top) {
+__device__ __forceinline__ unsigned long long list_mass(Shared& sh, unsigned n, Weights weight) {
   unsigned long long sum = 0;
-  for (unsigned j = threadIdx.x; j < n; j += blockDim.x) sum += fixed_weight(score_of(sh.list[j]), top);
+  for (unsigned j = threadIdx.x; j < n; j += blockDim.x) sum += weight.of(score_of(sh.list[j]));
   return block_sum(sum, sh);
 }
 // The entry of the sorted list (of n >= 1) at which the running mass reaches `need`; the last one
 // where rounding leaves less.
-__device__ __forceinline__ unsigned mass_reaches(Shared& sh, unsigned n, unsigned long long need, float top) {
+__device__ __forceinline__ unsigned mass_reaches(Shared& sh, unsigned n, unsigned long long need, Weights weight) {
   const unsigned span = (n + blockDim.x - 1) / blockDim.x, first = threadIdx.x * span;
   unsigned long long mine = 0;
-  for (unsigned j = first; j < min(first + span, n); ++j) mine += fixed_weight(score_of(sh.list[j]), top);
+  for (unsigned j = first; j < min(first + span, n); ++j) mine += weight.of(score_of(sh.list[j]));
   unsigned long long at = block_below(mine, sh);
   if (threadIdx.x == 0) sh.found = n - 1;
   __syncthreads();
   if (at < need && at + mine >= need)
     for (unsigned j = first; j < min(first + span, n); ++j) {
-      at += fixed_weight(score_of(sh.list[j]), top);
+      at += weight.of(score_of(sh.list[j]));
       if (at >= need) {
         sh.found = j;
         break;
@@ -832,7 +863,7 @@ __device__ __forceinline__ void collect(const Src& src, const Team& t, Bins bins
 // reach that far, all are kept).  kAbove: sh.listed entries, on rank 0 only, and no edge.
 template <bool kMass, bool kAbove, typename Src, typename Get>
 __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use, Bins bins, unsigned long long need,
-                                    float share, float top, float mine, Get get,
+                                    float share, Weights weight, float mine, Get get,
                                     unsigned long long* edge) {
   constexpr int V = Src::V;
   *edge = 0;
@@ -842,24 +873,32 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   clear_bins(t, sh, kMass);
   src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
     get(at, s);
-    int b[V];
-    uint32_t w[V], old[V];
+    // (masses in halves of the group: 64 bits of eight entries would not fit the registers)
+    constexpr int kPart = kMass ? V / 2 : V;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      b[v] = bins.of(s[v]);
-      if (kMass) w[v] = fixed_weight(s[v], top);
-    }
+    for (int f = 0; f < V; f += kPart) {
+      int b[kPart];
+      Weights::Halves w[kPart];
+      uint32_t old[kPart];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const bool on = s[v] > -INFINITY;
-      add_if(&sh.count[b[v]], 1u, on);
-      if (kMass) old[v] = fetch_add_if(&sh.lo[b[v]], w[v], on);
-    }
-    if (kMass) {
-      // shared memory adds 32 bits at a time: carries go to the upper half
+      for (int v = 0; v < kPart; ++v) {
+        b[v] = bins.of(s[f + v]);
+        if (kMass) w[v] = weight.halves(s[f + v]);
+      }
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        add_if(&sh.hi[b[v]], 1u, s[v] > -INFINITY && old[v] + w[v] < old[v]);
+      for (int v = 0; v < kPart; ++v) {
+        const bool on = s[f + v] > -INFINITY;
+        add_if(&sh.count[b[v]], 1u, on);
+        if (kMass) old[v] = fetch_add_if(&sh.lo[b[v]], w[v].lower, on);
+      }
+      if (kMass) {
+        // shared memory adds 32 bits at a time: carries go to the upper half (as a rule nothing does)
+#pragma unroll
+        for (int v = 0; v < kPart; ++v) {
+          const uint32_t hi = w[v].upper + (old[v] + w[v].lower < old[v] ? 1u : 0u);
+          add_if(&sh.hi[b[v]], hi, s[f + v] > -INFINITY && hi != 0);
+        }
+      }
     }
   });
   if (!merge_bins<kMass>(t, sh)) return false;
@@ -898,8 +937,9 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
         const int b = t.bins - 1 - static_cast<int>((c >> shift) & ((1u << bits) - 1u));
         atomicAdd(&sh.count[b], 1u);
         if (kMass) {
-          const uint32_t w = fixed_weight(s[v], top), old = atomicAdd(&sh.lo[b], w);
-          if (old + w < old) atomicAdd(&sh.hi[b], 1u);
+          const Weights::Halves w = weight.halves(s[v]);
+          const uint32_t old = atomicAdd(&sh.lo[b], w.lower), hi = w.upper + (old + w.lower < old ? 1u : 0u);
+          if (hi != 0) atomicAdd(&sh.hi[b], hi);
         }
       }
     });
@@ -917,7 +957,7 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   const unsigned have = sh.listed;
   sort_list(t, sh, have);
   if (kAbove) return true;
-  *edge = kMass ? sh.list[mass_reaches(sh, have, need, top)] : sh.list[need - 1];
+  *edge = kMass ? sh.list[mass_reaches(sh, have, need, weight)] : sh.list[need - 1];
   __syncthreads();
   return true;
 }
@@ -941,6 +981,7 @@ struct Ctx {
   const float* noise;
   Rule r;
   float top, logz;
+  Weights weight;
   long long row;
 };
 
@@ -1000,7 +1041,7 @@ template <typename T>
 __device__ void finish_list(const SampleArgs& a, const Team& t, Shared& sh, const Ctx& x, const Row<T>& src) {
   unsigned keep = min(sh.listed, x.r.k);
   if (x.r.p < 1.0f)
-    keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.top)), x.top) + 1;
+    keep = mass_reaches(sh, keep, share_of(x.r.p, list_mass(sh, keep, x.weight)), x.weight) + 1;
   if (x.r.log_min > -INFINITY) {
     unsigned long long mine = 0;
     for (unsigned j = threadIdx.x; j < keep; j += blockDim.x)
@@ -1036,12 +1077,12 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
   Edge edge;
   unsigned long long found;
   if (x.r.k != 0) {
-    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.top, mine, All(), &found))
+    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.weight, mine, All(), &found))
       return false;
     edge.raise(found);
   }
   if (x.r.p < 1.0f) {
-    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.top, mine, Kept{edge}, &found)) return false;
+    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.weight, mine, Kept{edge}, &found)) return false;
     edge.raise(found);
   }
   const Draws draws = {edge, x.noise, x.top, x.r.log_min};
@@ -1102,7 +1143,7 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
       __syncthreads();
     }
   }
-  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.top, mine_key, draws, &found))
+  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.weight, mine_key, draws, &found))
     return false;
   if (t.rank != 0) return true;
   const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
@@ -1116,7 +1157,7 @@ template <typename T>
 __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long row_at) {
   constexpr int V = Row<T>::V;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  Ctx x;
+  Ctx x = {};
   x.r = read_rule(a.rules != nullptr ? a.rules[row_at] : a.rule, a.n);
   x.noise = a.noise + row_at * a.noise_stride;
   x.row = row_at;
@@ -1250,6 +1291,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     return true;
   }
   x.logz = logf(sh.z);
+  x.weight = Weights(x.top, sh.z, static_cast<int>(a.n));
   if (direct) {
     if (t.rank == 0) {
       if (threadIdx.x == 0) put(a, x, 0, index_of(best), row.score(index_of(best)));
