@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_scan(mlt_scan_args a, Plan p, u
             F2 o = dup2(0.0f);
 #pragma unroll
             for (int s = 0; s < Lane<S>::H; ++s) {
-              h[c].v[s] = fma2(ex2_2(mul2(dup2(d[c]), A[c].v[s])), h[c].v[s], mul2(dup2(du[c]), B.v[s]));
+              h[c].v[s] = fma2(decay2(dup2(d[c]), A[c].v[s]), h[c].v[s], mul2(dup2(du[c]), B.v[s]));
               if (kOut) o = s == 0 ? mul2(C.v[0], h[c].v[0]) : fma2(C.v[s], h[c].v[s], o);
             }
             if (kOut) {
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(256) k_scan_step(mlt_scan_args a) {
     Lane<S> r;
 #pragma unroll
     for (int s = 0; s < Lane<S>::H; ++s) {
-      const F2 decay = ex2_2(mul2(f2(dk * kLog2E, dk * kLog2E), A.v[s]));
+      const F2 decay = decay2(f2(dk * kLog2E, dk * kLog2E), A.v[s]);
       if (live) h[k].v[s] = fma2(decay, h[k].v[s], mul2(f2(pk, pk), f2(Bs[2 * s], Bs[2 * s + 1])));
       r.v[s] = mul2(h[k].v[s], f2(Cs[2 * s], Cs[2 * s + 1]));
     }

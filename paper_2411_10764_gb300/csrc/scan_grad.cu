@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_local(mlt_scan_args a, mlt_sc
     const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y), gg = f2(gc, gc);
 #pragma unroll
     for (int s = 0; s < Lane<S>::H; ++s) {
-      const F2 decay = ex2_2(mul2(d, A.v[s]));
+      const F2 decay = decay2(d, A.v[s]);
       h.v[s] = fma2(decay, h.v[s], mul2(push, B.v[s]));
       prod.v[s] = mul2(prod.v[s], decay);
       acc.v[s] = fma2(prod.v[s], mul2(gg, C.v[s]), acc.v[s]);
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
       const Lane<S> B = lane_shared<S>(sm.in.B + ((part * kSub + t) * 4 + lane) * S);
       const F2 d = f2(du.x, du.x), push = f2(du.x * du.y, du.x * du.y);
 #pragma unroll
-      for (int s = 0; s < Lane<S>::H; ++s) h.v[s] = fma2(ex2_2(mul2(d, A.v[s])), h.v[s], mul2(push, B.v[s]));
+      for (int s = 0; s < Lane<S>::H; ++s) h.v[s] = fma2(decay2(d, A.v[s]), h.v[s], mul2(push, B.v[s]));
     }
   }
 
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_grad_chunk(mlt_scan_args a, mlt
         Lane<S> o;
 #pragma unroll
         for (int s = 0; s < Lane<S>::H; ++s) {
-          decay[t].v[s] = ex2_2(mul2(d, A.v[s]));
+          decay[t].v[s] = decay2(d, A.v[s]);
           hs[t + 1].v[s] = fma2(decay[t].v[s], hs[t].v[s], mul2(push, B.v[s]));
           o.v[s] = mul2(C.v[s], hs[t + 1].v[s]);
         }
