@@ -384,6 +384,10 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+# ctypes passes the low 32 bits of larger numbers; the library refuses those it does see
+_INT_MAX = 0x7FFFFFFF
+
+
 def _cuda(t, name: str, dtype=None):
     if not (isinstance(t, _torch.Tensor) and t.is_cuda and (dtype is None or t.dtype == dtype)):
         raise TypeError(f"{name} must be a CUDA tensor" + (f" of {dtype}" if dtype is not None else ""))
@@ -429,6 +433,7 @@ def sample_rules(temperature, top_k=0, top_p=1.0, min_p=0.0, rows: int | None = 
     [rows][4].  Each argument is a number or one value a row."""
     import torch
 
+    top_k = torch.as_tensor(top_k, dtype=torch.int64, device=device).clamp(-1, _INT_MAX)
     cols = [torch.as_tensor(v, dtype=dt, device=device) for v, dt in
             ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32))]
     if rows is None:
@@ -459,8 +464,11 @@ def sample(scores, noise, temperature: float = 1.0, top_k: int = 0, top_p: float
     stride, noise_stride = _rows(scores, "scores"), _rows(noise, "noise")
     rows, n = scores.shape
     m = int(m)
+    _need(m <= _INT_MAX, "m must lie in [1, 2048]")
     rule = each = None
     if rules is None:
+        if not 0 <= top_k <= _INT_MAX:
+            top_k = 0  # all
         rule = C.byref(SampleRule(temperature, top_k, top_p, min_p))
     else:
         _cuda(rules, "rules", torch.int32)
@@ -506,6 +514,7 @@ def embed(ids, table, scale: float = 1.0, out_dtype=None, out=None, stream=None)
     _cuda(table, "table")
     code, stride = _dtype_code(table), _rows(table, "table")
     vocab, dim = table.shape
+    _need(dim <= _INT_MAX, "dim must lie in [1, 2^20]")
     if out is None:
         out = _torch.empty(*ids.shape, dim, dtype=out_dtype or table.dtype, device=table.device)
         out_stride = dim
@@ -534,6 +543,7 @@ def embed_grad(ids, grad_out, vocab: int, scale: float = 1.0, out_dtype=None, ou
     flat = grad_out if grad_out.dim() == 2 else grad_out.reshape(-1, dim)
     code, stride = _dtype_code(flat), _rows(flat, "grad_out")
     vocab, tokens = int(vocab), ids.numel()
+    _need(dim <= _INT_MAX, "dim must lie in [1, 2^20]")
     if out is None:
         out = _torch.empty(vocab, dim, dtype=out_dtype or grad_out.dtype, device=grad_out.device)
     else:
@@ -586,6 +596,7 @@ def _scan_args(x, dt, B, Cm, A, z, skip, dt_bias, conv_w, conv_b, lengths, state
         raise ValueError("B must be [batch][length][groups][states]")
     g, n = B.shape[2:]
     taps = 0 if conv_w is None else conv_w.shape[1]
+    _need(b <= _INT_MAX and d <= _INT_MAX, "batch must lie in [0, 65535], dim in [1, 2^20]")
     wide, narrow = (b, L, d), (b, L, g, n)
     xp, xb, xs = _wide(x, "x", dtype, wide)
     dp, db, ds = _wide(dt, "dt", dtype, wide)
