@@ -388,6 +388,14 @@ int mlt_selftest_walk_timeout(int cta, int64_t limit_ns);
  * MLT_ETIMEOUT and the next call is unaffected.  Host-only bookkeeping. */
 int mlt_selftest_ordinal_timeout(int64_t limit_ns);
 
+/* The same inside mlt_sample: arms a one-shot so that in the next call whose
+ * rows are shared by CTAs that meet in global memory (few rows of more than
+ * some 100,000 entries; any next call uses it up) the last CTA of each row does
+ * not arrive and the others' waits give up after limit_ns (1e6 .. 2e9 ns).
+ * Nothing is drawn then (-1 and -infinity); mlt_sync_status reports
+ * MLT_ETIMEOUT and the next call is unaffected.  Host-only bookkeeping. */
+int mlt_selftest_sample_timeout(int64_t limit_ns);
+
 /* Test support: writes `value` into the four counters (survivor count,
  * collected keys, two CTA tickets) of the selection state that the
  * allocating entry points (static_scratch = 0) or mlt_screen_noalloc
@@ -550,6 +558,8 @@ typedef struct {
  *   out_logprob[r][j] = its s - ln(sum over the row's drawable entries of
  *            exp s): the log-probability before the rule's cuts; 0 at
  *            temperature 0; -infinity where out_index is -1
+ * A row whose rule is out of range or whose CTAs' wait for each other gave up
+ * (the next mlt_sync_status reports either) draws nothing: -1 and -infinity.
  * With Gumbel noise, -ln(-ln u) of uniform u, these are m draws without
  * replacement, the first one exactly a draw from the kept entries' softmax.
  * Probability masses are summed as 64-bit integers, so results do not depend

@@ -219,6 +219,8 @@ int g_stall_cta = -1;
 unsigned long long g_stall_ns = 0;
 // the same for the next kernel that writes ordinals (mlt_selftest_ordinal_timeout)
 unsigned long long g_ord_stall_ns = 0;
+// the same for the next draw (mlt_selftest_sample_timeout)
+unsigned long long g_sample_stall_ns = 0;
 
 size_t align16(size_t v) { return (v + 15) & ~static_cast<size_t>(15); }
 
@@ -1355,6 +1357,13 @@ void api_count_launches(long long n) {
   g_launches += n;
 }
 
+unsigned long long api_take_sample_stall() {
+  std::lock_guard<std::mutex> lk(g_mu);
+  const unsigned long long ns = g_sample_stall_ns;
+  g_sample_stall_ns = 0;
+  return ns;
+}
+
 int api_sm_count() {
   std::lock_guard<std::mutex> lk(g_mu);
   return sm_count();
@@ -1870,6 +1879,14 @@ int mlt_selftest_ordinal_timeout(int64_t limit_ns) {
     return fail(MLT_EINVAL, "limit_ns must lie in [1e6, %llu]", kWaitLimitNs);
   std::lock_guard<std::mutex> lk(g_mu);
   g_ord_stall_ns = static_cast<unsigned long long>(limit_ns);
+  return MLT_OK;
+}
+
+int mlt_selftest_sample_timeout(int64_t limit_ns) {
+  if (limit_ns < 1000000LL || limit_ns > static_cast<int64_t>(kWaitLimitNs))
+    return fail(MLT_EINVAL, "limit_ns must lie in [1e6, %llu]", kWaitLimitNs);
+  std::lock_guard<std::mutex> lk(g_mu);
+  g_sample_stall_ns = static_cast<unsigned long long>(limit_ns);
   return MLT_OK;
 }
 

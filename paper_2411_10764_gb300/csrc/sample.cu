@@ -336,6 +336,7 @@ struct Team {
   bool cluster;  // the team is a thread-block cluster
   TeamMem* g;
   unsigned* err;
+  unsigned long long wait_ns;
   int size, rank;
   unsigned barriers;
   int stage;  // histograms used so far
@@ -363,7 +364,7 @@ __device__ bool team_sync(Team& t, Shared& sh) {
       asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(&t.g->arrivals) : "memory");
       if (v >= want) break;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-      if (now - start > kWaitLimitNs) {
+      if (now - start > t.wait_ns) {
         atomicOr(t.err, kErrWaitTimeout);
         dead = 1;
         break;
@@ -1363,7 +1364,11 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
   t.barriers = 0;
   t.stage = 0;
   t.bins = bins;
-  sample_row<T>(a, t, sh, blockIdx.x / team_size);
+  t.wait_ns = a.wait_ns;
+  if (a.stall && team_size > 1 && !t.cluster && t.rank == team_size - 1) return;
+  const long long row = blockIdx.x / team_size;
+  // Rank 0 alone writes the row, and only after its last wait: where one gave up nothing is drawn.
+  if (!sample_row<T>(a, t, sh, row) && t.rank == 0) none_drawn(a, row, 0);
 }
 
 bool by_warp(long long n, int m) { return n <= kWarpMaxN && m <= kWarpMaxM; }

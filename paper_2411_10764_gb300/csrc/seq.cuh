@@ -21,6 +21,7 @@ int api_fail(int code, const char* fmt, ...);
 unsigned* api_error_word(int* rc);
 void api_count_launches(long long n);
 int api_sm_count();
+unsigned long long api_take_sample_stall();  // nanoseconds, 0: not armed
 
 inline size_t dtype_size(int dtype) { return dtype == MLT_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == MLT_F32 || dtype == MLT_BF16 || dtype == MLT_F16; }
@@ -69,6 +70,8 @@ struct SampleArgs {
   float* out_logprob;
   unsigned* err;
   void* ws;
+  unsigned long long wait_ns;  // limit of a wait in global memory
+  bool stall;  // self-test: the last CTA of each such team does not arrive
 };
 size_t sample_workspace(int dtype, long long rows, long long n, int m, int sms);
 cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cudaStream_t st);

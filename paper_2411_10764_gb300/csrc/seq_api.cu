@@ -134,6 +134,9 @@ int mlt_sample(void* stream, const void* scores, int dtype, int64_t rows, int64_
   a.out_logprob = out_logprob;
   a.err = err;
   a.ws = workspace;
+  const unsigned long long stall_ns = api_take_sample_stall();
+  a.wait_ns = stall_ns != 0 ? stall_ns : kWaitLimitNs;
+  a.stall = stall_ns != 0;
   long long launches = 0;
   const cudaError_t e = launch_sample(a, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "sample launch");

@@ -88,6 +88,7 @@ def lib(build_if_missing: bool = True):
             "mlt_selftest_wait_timeout": [P, i64],
             "mlt_selftest_walk_timeout": [i32, i64],
             "mlt_selftest_ordinal_timeout": [i64],
+            "mlt_selftest_sample_timeout": [i64],
             "mlt_selftest_poison_state": [i32, C.c_uint32],
             "mlt_free_ensemble": [i32],
             "mlt_validity_cut": [f32, P],
@@ -779,6 +780,12 @@ def selftest_ordinal_timeout(limit_ns: int) -> None:
     """Arm a one-shot: CTA 0 of the next kernel that writes ordinals waits
     limit_ns on a barrier nothing completes."""
     _check(lib().mlt_selftest_ordinal_timeout(int(limit_ns)))
+
+
+def selftest_sample_timeout(limit_ns: int) -> None:
+    """Arm a one-shot: in the next draw from long rows one CTA of each row stays away and the
+    others' waits give up after limit_ns; the row draws nothing."""
+    _check(lib().mlt_selftest_sample_timeout(int(limit_ns)))
 
 
 def selftest_poison_state(value: int, static_scratch: bool = False) -> None:
