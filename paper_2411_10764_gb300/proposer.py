@@ -186,10 +186,12 @@ def main() -> None:
     w = W.make_workload(4, seed=1, n=65536)
     mlt.load_workload_models(w)
     out = explore(w.decoder, w.thr, 0, 65536)
-    ok = out["accepted"].bool()
-    print(f"screened 65536, drew {out['drawn'].numel()}, loss {out['losses'][0]:.3f} -> {out['losses'][-1]:.3f}, "
-          f"{int(ok.sum())} of {ok.numel()} annealed proposals valid, best score {float(out['score'][ok].max()):.4f} "
-          f"(screened: {float(out['perf'].max()):.4f})")
+    ok, losses, screened = out["accepted"].bool(), out["losses"], float(out["perf"].max())
+    print(f"screened 65536, drew {out['drawn'].numel()}"
+          + (f", loss {losses[0]:.3f} -> {losses[-1]:.3f}" if losses else "")
+          + f", {int(ok.sum())} of {ok.numel()} annealed proposals valid"
+          + (f", best score {float(out['score'][ok].max()):.4f}" if bool(ok.any()) else "")
+          + (f" (screened: {screened:.4f})" if math.isfinite(screened) else " (screened: none valid)"))
 
 
 if __name__ == "__main__":
