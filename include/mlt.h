@@ -522,9 +522,10 @@ int mlt_tune_head_levels(int levels);
  * needs a workspace takes it from the caller (device memory of at least the
  * bytes its ..._workspace call gives, 256-byte aligned), so calls with
  * workspaces of their own may run on different streams at once and be captured
- * in graphs.  All are asynchronous on `stream`.  The first call on a device
- * allocates the error word that mlt_sync_status reads; issue it outside a
- * capture.
+ * in graphs.  All are asynchronous on `stream`.  Where no other call has, the
+ * first draw or lookup on a device allocates what the library keeps there (some
+ * 200 KB: the error word that mlt_sync_status reads, and screening's smallest
+ * scratch); issue it outside a capture.
  *
  * Strides of inputs may be 0 or make rows overlap; outputs' rows lie apart and
  * overlap no input unless a call says so.

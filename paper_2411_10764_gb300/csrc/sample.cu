@@ -299,19 +299,21 @@ __global__ void __launch_bounds__(128) k_sample_warp(SampleArgs a) {
 // A team of CTAs per row
 // ---------------------------------------------------------------------------
 constexpr int kMaxTeam = 160;
-constexpr int kUses = 4;  // selections of a row: top-k, top-p, draws; candidates for the top-k
 constexpr int kLarge = 16384;  // candidates that one CTA finishes without the team
+// Lists of a row, by what they are for.  Candidates for the top-k are in `large` and counted as its list;
+// those for the draws are in top-p's list, read by then, with a counter of their own.
+enum { kTopK, kTopP, kDraws, kLists, kDrawCandidates = kLists, kCounters };
 
 // Global memory of a team; teams of one CTA use none of it.
 struct TeamMem {
   unsigned arrivals;      // barrier: CTAs arrived, over all barriers of the call (zeroed before the launch)
-  unsigned listed[kUses]; // entries in list (the last: in large)
+  unsigned listed[kCounters];
   float4 stats[kMaxTeam]; // each CTA's (max, sum of exp, min)
   unsigned long long best[kMaxTeam];
   unsigned entries[kMaxTeam];
   unsigned long long mass[3][kBins];
   unsigned count[3][kBins];
-  unsigned long long list[kUses][kList];
+  unsigned long long list[kLists][kList];
   unsigned long long large[kLarge];
 };
 
@@ -329,6 +331,7 @@ struct Shared {
   unsigned long long above;
   unsigned in, bin, listed, found;
   float top, z, low;
+  unsigned long long wait_ns;  // limit of a wait in global memory
   int dead;
 };
 
@@ -336,7 +339,6 @@ struct Team {
   bool cluster;  // the team is a thread-block cluster
   TeamMem* g;
   unsigned* err;
-  unsigned long long wait_ns;
   int size, rank;
   unsigned barriers;
   int stage;  // histograms used so far
@@ -364,7 +366,7 @@ __device__ bool team_sync(Team& t, Shared& sh) {
       asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(&t.g->arrivals) : "memory");
       if (v >= want) break;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-      if (now - start > t.wait_ns) {
+      if (now - start > sh.wait_ns) {
         atomicOr(t.err, kErrWaitTimeout);
         dead = 1;
         break;
@@ -391,7 +393,7 @@ __device__ __forceinline__ float score_of(unsigned long long c) {
 
 // A row of scores.  walk: f(at, s) for every group of eight that the thread owns, the same ones
 // at each walk: s[v] is the scaled score of entry at[v], -infinity where it cannot be
-// drawn or is outside the row.  U groups are loaded at once.  What f loads or adds by
+// drawn or is outside the row.  The next group is loaded before f.  What f loads or adds by
 // atomics it does for all of a group before it uses any of it: one after another, each
 // would wait for memory (64 rows x 50,021 with min-p: 10 us a pass).
 template <typename T>
@@ -406,43 +408,34 @@ struct Row {
     const int i0 = q * V - skew;
     if (i0 >= 0 && i0 <= n - V) p = *reinterpret_cast<const Pack<T, V>*>(base + static_cast<long long>(q) * V);
   }
-  template <int U, typename F>
+  template <typename F>
   __device__ __forceinline__ void walk(const Team& t, F f) const {
     const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(row) / sizeof(T)) % V);
     const int groups = (skew + n + V - 1) / V;
     const int stride = t.size * static_cast<int>(blockDim.x), last = n - V;
     const T* base = row - skew;  // aligned to the group; entries before `row` are not read
-    int q0 = t.rank * static_cast<int>(blockDim.x) + threadIdx.x;
-    Pack<T, V> p[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) load(base, min(q0 + u * stride, groups), skew, p[u]);
+    int q = t.rank * static_cast<int>(blockDim.x) + threadIdx.x;
+    Pack<T, V> p;
+    load(base, min(q, groups), skew, p);
 #pragma unroll 1
-    for (; q0 < groups; q0 += stride * U) {
-      Pack<T, V> now[U];
+    for (; q < groups; q += stride) {
+      const Pack<T, V> now = p;
+      load(base, min(q + stride, groups), skew, p);  // the next one lands meanwhile
+      const int i0 = q * V - skew;
+      float s[V];
+      if (i0 >= 0 && i0 <= last) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        now[u] = p[u];
-        load(base, min(q0 + (U + u) * stride, groups), skew, p[u]);  // the next ones land meanwhile
+        for (int v = 0; v < V; ++v) s[v] = scaled(to_f32(now.v[v]), inv);
+      } else {
+        // a row's ends
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          s[v] = i0 + v >= 0 && i0 + v < n ? scaled(to_f32(row[i0 + v]), inv) : -INFINITY;
       }
+      int at[V];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int q = q0 + u * stride, i0 = q * V - skew;
-        if (q >= groups) break;
-        float s[V];
-        if (i0 >= 0 && i0 <= last) {
-#pragma unroll
-          for (int v = 0; v < V; ++v) s[v] = scaled(to_f32(now[u].v[v]), inv);
-        } else {
-          // a row's ends
-#pragma unroll
-          for (int v = 0; v < V; ++v)
-            s[v] = i0 + v >= 0 && i0 + v < n ? scaled(to_f32(row[i0 + v]), inv) : -INFINITY;
-        }
-        int at[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) at[v] = i0 + v;
-        f(at, s);
-      }
+      for (int v = 0; v < V; ++v) at[v] = i0 + v;
+      f(at, s);
     }
   }
 };
@@ -452,7 +445,7 @@ struct Candidates {
   const unsigned long long* list;
   int n;
 
-  template <int U, typename F>
+  template <typename F>
   __device__ __forceinline__ void walk(const Team&, F f) const {
 #pragma unroll 1
     for (int j = threadIdx.x; j < n; j += V * blockDim.x) {
@@ -831,7 +824,7 @@ __device__ __forceinline__ void collect(const Src& src, const Team& t, Bins bins
   const float to = static_cast<float>(bin) == bins.last || bins.scale == 0.0f
                        ? -FLT_MAX
                        : bins.from - (static_cast<float>(bin) + 1.5f) / bins.scale;
-  src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+  src.walk(t, [&](const int(&at)[V], float(&s)[V]) {
     get(at, s);
     unsigned hit = 0;
 #pragma unroll
@@ -872,7 +865,7 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
   unsigned* listed = t.size > 1 ? &t.g->listed[use] : &sh.listed;
   if (threadIdx.x == 0) sh.listed = 0;
   clear_bins(t, sh, kMass);
-  src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+  src.walk(t, [&](const int(&at)[V], float(&s)[V]) {
     get(at, s);
     // (masses in halves of the group: 64 bits of eight entries would not fit the registers)
     constexpr int kPart = kMass ? V / 2 : V;
@@ -928,7 +921,7 @@ __device__ __noinline__ bool select(const Src& src, Team& t, Shared& sh, int use
     const int bits = min(31 - __clz(t.bins), shift);
     shift -= bits;
     clear_bins(t, sh, kMass);
-    src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+    src.walk(t, [&](const int(&at)[V], float(&s)[V]) {
       get(at, s);
 #pragma unroll 1
       for (int v = 0; v < V; ++v) {
@@ -1078,12 +1071,12 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
   Edge edge;
   unsigned long long found;
   if (x.r.k != 0) {
-    if (!select<false, false>(src, t, sh, 0, by_score, x.r.k, 0.0f, x.weight, mine, All(), &found))
+    if (!select<false, false>(src, t, sh, kTopK, by_score, x.r.k, 0.0f, x.weight, mine, All(), &found))
       return false;
     edge.raise(found);
   }
   if (x.r.p < 1.0f) {
-    if (!select<true, false>(src, t, sh, 1, by_score, 0, x.r.p, x.weight, mine, Kept{edge}, &found)) return false;
+    if (!select<true, false>(src, t, sh, kTopP, by_score, 0, x.r.p, x.weight, mine, Kept{edge}, &found)) return false;
     edge.raise(found);
   }
   const Draws draws = {edge, x.noise, x.top, x.r.log_min};
@@ -1094,7 +1087,7 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
     entries = 0;
     mine_key = -INFINITY;
     if (mine >= edge.s && __fsub_rn(mine, x.top) >= x.r.log_min)
-      src.template walk<1>(t, [&](const int(&at)[V], float(&s)[V]) {
+      src.walk(t, [&](const int(&at)[V], float(&s)[V]) {
         draws(at, s);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -1129,8 +1122,8 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
     int bin;
     if (!bin_of_maxima(t, sh, by_key, a.m, mine_key, kept, &bin)) return false;
     if (bin >= 0) {
-      unsigned long long* list = t.size > 1 ? t.g->list[1] : sh.list;  // top-p's is read by now
-      unsigned* listed = t.size > 1 ? &t.g->listed[3] : &sh.listed;
+      unsigned long long* list = t.size > 1 ? t.g->list[kTopP] : sh.list;
+      unsigned* listed = t.size > 1 ? &t.g->listed[kDrawCandidates] : &sh.listed;
       if (threadIdx.x == 0) sh.listed = 0;
       __syncthreads();
       collect<true>(src, t, by_key, bin, mine_key, kIndexBits + 32, 0, draws, list, listed, kList);
@@ -1144,7 +1137,7 @@ __device__ bool finish_select(const SampleArgs& a, Team& t, Shared& sh, const Ct
       __syncthreads();
     }
   }
-  if (!done && !select<false, true>(src, t, sh, 2, by_key, a.m, 0.0f, x.weight, mine_key, draws, &found))
+  if (!done && !select<false, true>(src, t, sh, kDraws, by_key, a.m, 0.0f, x.weight, mine_key, draws, &found))
     return false;
   if (t.rank != 0) return true;
   const int drawn = static_cast<int>(min(sh.listed, static_cast<unsigned>(a.m)));
@@ -1219,8 +1212,10 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
       }
     }
   };
-  if (uncut) row.template walk<1>(t, first);
-  else row.template walk<1>(t, first);
+  // (two copies, each compiled for its case: one for both took 45.5 us for 43.9 on 64 rows x 50,021 with
+  // top-p, and 237 for 217 on 80 uncut ones of 1,048,576)
+  if (uncut) row.walk(t, first);
+  else row.walk(t, first);
   z = __fsub_rn(z, lost);
   const float mine = top;
   float low = mine > -INFINITY ? mine : INFINITY;  // least of the lanes' maxima
@@ -1261,7 +1256,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
         t.g->count[t.stage % 3][b] = 0;
         t.g->mass[t.stage % 3][b] = 0;
       }
-      if (threadIdx.x < kUses) t.g->listed[threadIdx.x] = 0;
+      if (threadIdx.x < kCounters) t.g->listed[threadIdx.x] = 0;
     }
     if (!team_sync(t, sh)) return false;
     if (warp == 0) {
@@ -1314,7 +1309,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
     if (!bin_of_maxima(t, sh, by_score, x.r.k, mine, kList + 1, &bin)) return false;
     if (bin >= 0) {
       unsigned long long* list = t.size > 1 ? t.g->large : sh.list;
-      unsigned* listed = t.size > 1 ? &t.g->listed[0] : &sh.listed;
+      unsigned* listed = t.size > 1 ? &t.g->listed[kTopK] : &sh.listed;
       const unsigned capacity = t.size > 1 ? kLarge : kList;
       if (threadIdx.x == 0) sh.listed = 0;
       __syncthreads();
@@ -1332,7 +1327,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
         // more than can be sorted: the same selections, from the candidates and by this CTA alone
         const Candidates src = {list, static_cast<int>(have)};
         float own = -INFINITY;
-        src.walk<1>(t, [&](const int(&)[Candidates::V], float(&s)[Candidates::V]) {
+        src.walk(t, [&](const int(&)[Candidates::V], float(&s)[Candidates::V]) {
 #pragma unroll
           for (int v = 0; v < Candidates::V; ++v) own = fmaxf(own, s[v]);
         });
@@ -1343,7 +1338,7 @@ __device__ bool sample_row(const SampleArgs& a, Team& t, Shared& sh, long long r
       if (t.size > 1) {
         // a crowded bin: the list's counter starts anew
         if (!team_sync(t, sh)) return false;
-        if (t.rank == 0 && threadIdx.x == 0) t.g->listed[0] = 0;
+        if (t.rank == 0 && threadIdx.x == 0) t.g->listed[kTopK] = 0;
         if (!team_sync(t, sh)) return false;
       }
     }
@@ -1364,11 +1359,14 @@ __global__ void __launch_bounds__(1024) k_sample_row(SampleArgs a, int team_size
   t.barriers = 0;
   t.stage = 0;
   t.bins = bins;
-  t.wait_ns = a.wait_ns;
-  if (a.stall && team_size > 1 && !t.cluster && t.rank == team_size - 1) return;
-  const long long row = blockIdx.x / team_size;
-  // Rank 0 alone writes the row, and only after its last wait: where one gave up nothing is drawn.
-  if (!sample_row<T>(a, t, sh, row) && t.rank == 0) none_drawn(a, row, 0);
+  if (team_size > 1 && !t.cluster) {
+    if (a.stall_us != 0 && t.rank == team_size - 1) return;
+    // thread 0 alone reads it
+    if (threadIdx.x == 0) sh.wait_ns = a.stall_us != 0 ? a.stall_us * 1000ull : kWaitLimitNs;
+    // rank 0 writes the row's draws after its last wait; where a wait gives up this is what remains
+    if (t.rank == 0) none_drawn(a, blockIdx.x / team_size, 0);
+  }
+  sample_row<T>(a, t, sh, blockIdx.x / team_size);
 }
 
 bool by_warp(long long n, int m) { return n <= kWarpMaxN && m <= kWarpMaxM; }

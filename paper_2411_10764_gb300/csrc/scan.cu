@@ -562,8 +562,8 @@ __global__ void __launch_bounds__(256) k_scan_nothing(mlt_scan_args a, int elem)
   for (long long i = first; i < m; i += stride) to[i] = from != nullptr ? from[i] : 0;
 }
 
-// One chunk where sequences x channel blocks give every SM three CTAs or more; else chunks of
-// at least 64 positions, for about ten CTAs an SM.
+// One chunk where sequences x channel blocks give every SM three CTAs or more; else chunks for about ten
+// CTAs an SM, no more of them than lengths of 64 (two of 48 for 65 positions).
 Plan plan_of(const mlt_scan_args& a, int sms) {
   Plan p{};
   const long long ctas = static_cast<long long>(a.batch) * a.groups * blocks_per_group<kCh>(a);

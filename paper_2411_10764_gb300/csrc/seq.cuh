@@ -60,6 +60,7 @@ struct alignas(sizeof(T) * V > 16 ? 16 : sizeof(T) * V) Pack {
 struct SampleArgs {
   const void* scores;
   int dtype;
+  unsigned stall_us;  // not 0: in teams that meet in global memory the last CTA stays away, waits last as long
   long long rows, n, row_stride;
   const float* noise;
   long long noise_stride;
@@ -70,8 +71,6 @@ struct SampleArgs {
   float* out_logprob;
   unsigned* err;
   void* ws;
-  unsigned long long wait_ns;  // limit of a wait in global memory
-  bool stall;  // self-test: the last CTA of each such team does not arrive
 };
 size_t sample_workspace(int dtype, long long rows, long long n, int m, int sms);
 cudaError_t launch_sample(const SampleArgs& a, int sms, long long* launches, cudaStream_t st);

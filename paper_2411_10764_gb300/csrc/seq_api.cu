@@ -1,6 +1,7 @@
 // C entry points of the sequence-model operators: argument checks, then the
 // launches of sample.cu, embed.cu, scan.cu and scan_grad.cu.  Nothing here
-// allocates device memory but the error word at the first call.
+// allocates device memory, but that the first draw or lookup on a device makes the library's own state
+// (the error word is part of it) where no other call has.
 #include <cmath>
 
 #include "seq.cuh"
@@ -134,9 +135,7 @@ int mlt_sample(void* stream, const void* scores, int dtype, int64_t rows, int64_
   a.out_logprob = out_logprob;
   a.err = err;
   a.ws = workspace;
-  const unsigned long long stall_ns = api_take_sample_stall();
-  a.wait_ns = stall_ns != 0 ? stall_ns : kWaitLimitNs;
-  a.stall = stall_ns != 0;
+  a.stall_us = static_cast<unsigned>(api_take_sample_stall() / 1000);
   long long launches = 0;
   const cudaError_t e = launch_sample(a, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "sample launch");
