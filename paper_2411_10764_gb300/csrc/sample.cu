@@ -19,8 +19,8 @@
 // Bound: the scores are read from HBM once and from L1 or L2 by the later passes;
 // noise is read for kept entries only.  What is left beside the first read is latency: two
 // to five passes over a CTA's share and a barrier for each.  Measured, whole calls: 64 rows x
-// 50,021 with a rule each 43 us; 8 x 1,048,576, top-k 8,192 and 512 draws, 72 us; one row of
-// 16,777,216 with min-p and 1,024 draws 62 us (its first pass 10.4 us, 6.4 TB/s).
+// 50,021 with a rule each 44 us; 8 x 1,048,576, top-k 8,192 and 512 draws, 72 us; one row of
+// 16,777,216 with min-p and 1,024 draws 53 to 66 us (its first pass 10.4 us, 6.4 TB/s).
 //
 // Two kernels:
 //   k_sample_warp  rows of up to 512 entries and m <= 32: a warp per row, the row in

@@ -20,11 +20,11 @@
 // would take a third of the time.  History: registers for inputs of the next
 // tile, unpacked after the load, waited for memory (466 us on 8 x 2048 x 2048 ragged; packed
 // until used 329); two lanes of eight states a channel 310; staging by warps of their
-// own behind the walk 270; two channels a lane 232.  Now 201 to 241 us by the lengths drawn;
-// one sequence of 16,381 x 1,024 in fp32 168 us in chunks, 40 % of it the chunks' end states.
+// own behind the walk 270; two channels a lane 232.  Now 216 to 237 us by the lengths drawn;
+// one sequence of 16,381 x 1,024 in fp32 169 us in chunks, 40 % of it the chunks' end states.
 //
 // Single tokens (length 1).  Bound by reading and writing the states: k_scan_step, 512 x 2,048
-// channels of 16 states in 37 to 39 us (4.2 TB/s).
+// channels of 16 states in 39 us (4.0 TB/s).
 #include "scan.cuh"
 
 namespace mlt {

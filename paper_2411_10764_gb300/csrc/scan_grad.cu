@@ -24,7 +24,7 @@
 // channels, the rest for the activations' slopes and stores; about half of the issue slots are
 // used at the 16 warps an SM that the registers allow.  Halves of the chunk (24 warps at 80
 // registers) took 143 us where this takes 128.  The whole gradient of 4 x 1,021 x 1,024 with ragged
-// lengths takes 127 to 166 us by the lengths drawn.
+// lengths takes 126 to 156 us by the lengths drawn; 256 sequences of 8 x 128 in fp32 52 us.
 #include "scan.cuh"
 
 namespace mlt {
