@@ -515,8 +515,9 @@ int mlt_tune_head_levels(int levels);
  * what a proposer over knob digits and tuning histories needs next to
  * screening: draws from scores instead of the top-k (mlt_sample), digits or
  * tokens to vectors with the gradient of the table (mlt_embed,
- * mlt_embed_grad), and a recurrent state over a sequence (mlt_scan,
- * mlt_scan_grad).  The paper has no counterpart.
+ * mlt_embed_grad), a recurrent state over a sequence (mlt_scan,
+ * mlt_scan_grad), and the norm of a block (mlt_layer_norm, mlt_layer_norm_grad).
+ * The paper has no counterpart.
  *
  * They keep no state between calls and use no library scratch: a call that
  * needs a workspace takes it from the caller (device memory of at least the
@@ -663,6 +664,55 @@ typedef struct {
 int mlt_scan_grad(void *stream, const mlt_scan_args *args, const mlt_scan_grads *grads, void *workspace,
                   size_t workspace_bytes);
 int mlt_scan_grad_workspace(const mlt_scan_args *args, size_t *bytes_out);
+
+/* Layer norm of rows, after an optional residual addition:
+ *   t    = round(x + residual) to x's type   (no residual: t = x)
+ *   mean = sum t / dim;  rstd = 1 / sqrt(sum (t - mean)^2 / dim + eps)
+ *   y    = round((t - mean) rstd weight + bias)
+ *   x, residual, total  device [rows][dim] of `dtype`, each with its distance
+ *             between rows in elements; total receives t
+ *   y         device [rows][dim] of `y_dtype`: x's type, or a narrower one where
+ *             x is fp32
+ *   weight, bias  device [dim] of `w_dtype`
+ *   stats     device [rows][2] fp32: mean and rstd, for the gradient
+ * residual, weight, bias, total and stats may be NULL.  y and total may each be
+ * x or residual themselves (same address and stride), not both the same one.
+ *   rows 0 .. 2^31-1;  dim 1 .. 2^20;  eps >= 0 */
+typedef struct {
+    int32_t dtype, y_dtype, w_dtype, dim;
+    int64_t rows;
+    const void *x, *residual, *weight, *bias;
+    int64_t x_stride, residual_stride;
+    void *y, *total;
+    int64_t y_stride, total_stride;
+    float *stats;
+    float eps;
+} mlt_norm_args;
+
+int mlt_layer_norm(void *stream, const mlt_norm_args *args);
+
+/* Its gradients from those of y (gy, of `y_dtype`) and, where the residual
+ * stream goes on, of total (g_total, of `dtype`, or NULL: 0).  `args` as for the
+ * forward call with t as its x; stats is read, bias, residual, y, total and eps
+ * are not used.
+ *   h  = (t - mean) rstd;  gw = gy weight
+ *   gx = round(rstd (gw - mean(gw) - h mean(gw h)) + g_total), the gradient of x
+ *        and of residual alike;  gx may be gy or g_total themselves where the
+ *        types are the same
+ *   gweight = round(sum over rows of gy h), gbias = round(sum over rows of gy), of
+ *        `w_dtype`, summed in a fixed order; 0 without rows
+ * Each output may be NULL. */
+typedef struct {
+    const void *gy, *g_total;
+    int64_t gy_stride, g_total_stride;
+    void *gx;
+    int64_t gx_stride;
+    void *gweight, *gbias;
+} mlt_norm_grads;
+
+int mlt_layer_norm_grad(void *stream, const mlt_norm_args *args, const mlt_norm_grads *grads, void *workspace,
+                        size_t workspace_bytes);
+int mlt_layer_norm_grad_workspace(int64_t rows, int dim, size_t *bytes_out);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

@@ -104,4 +104,10 @@ size_t scan_grad_workspace(const mlt_scan_args& a, int sms);
 cudaError_t launch_scan_grad(const mlt_scan_args& a, const mlt_scan_grads& g, void* ws, int sms, long long* launches,
                              cudaStream_t st);
 
+// --- norm.cu, norm_grad.cu -------------------------------------------------
+cudaError_t launch_norm(const mlt_norm_args& a, int sms, long long* launches, cudaStream_t st);
+size_t norm_grad_workspace(long long rows, int dim, int sms);
+cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, void* ws, int sms, long long* launches,
+                             cudaStream_t st);
+
 }  // namespace mlt

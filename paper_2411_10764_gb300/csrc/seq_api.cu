@@ -87,6 +87,22 @@ int check_scan_inputs(const mlt_scan_args* a) {
   return MLT_OK;
 }
 
+int check_norm(const mlt_norm_args* a) {
+  if (a == nullptr) return api_fail(MLT_EINVAL, "args must be non-NULL");
+  if (!dtype_ok(a->dtype) || !dtype_ok(a->y_dtype) || !dtype_ok(a->w_dtype))
+    return api_fail(MLT_EINVAL, "unknown element type");
+  if (a->y_dtype != a->dtype && a->dtype != MLT_F32)
+    return api_fail(MLT_EINVAL, "y must be of x's type, or a narrower one where x is fp32");
+  if (a->rows < 0 || a->rows > kMaxCount) return api_fail(MLT_EINVAL, "rows must lie in [0, 2^31-1]");
+  if (a->dim < 1 || a->dim > kMaxDim) return api_fail(MLT_EINVAL, "dim must lie in [1, %d], got %d", kMaxDim, a->dim);
+  if (a->x_stride < 0 || a->residual_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
+  if (a->rows > 0 && a->x == nullptr) return api_fail(MLT_EINVAL, "x must be non-NULL");
+  if (!aligned_to(a->x, dtype_size(a->dtype)) || !aligned_to(a->weight, dtype_size(a->w_dtype)) ||
+      !aligned_to(a->bias, dtype_size(a->w_dtype)) || !aligned_to(a->stats, 8))
+    return api_fail(MLT_EINVAL, "buffers must be aligned to their elements, stats to 8 bytes");
+  return MLT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -275,6 +291,66 @@ int mlt_scan_grad(void* stream, const mlt_scan_args* args, const mlt_scan_grads*
   long long launches = 0;
   const cudaError_t e = launch_scan_grad(*args, *grads, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "scan gradient launch");
+}
+
+int mlt_layer_norm(void* stream, const mlt_norm_args* args) {
+  int rc = check_norm(args);
+  if (rc != MLT_OK) return rc;
+  if (!(args->eps >= 0.0f && std::isfinite(args->eps))) return api_fail(MLT_EINVAL, "eps must be finite and not negative");
+  if (args->rows == 0) return MLT_OK;
+  if (args->y == nullptr) return api_fail(MLT_EINVAL, "y must be non-NULL");
+  if (!stride_ok(args->y_stride, args->dim, args->rows) ||
+      (args->total != nullptr && !stride_ok(args->total_stride, args->dim, args->rows)))
+    return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
+  if (args->total != nullptr && args->total == args->y) return api_fail(MLT_EINVAL, "y and total must differ");
+  if (!aligned_to(args->residual, dtype_size(args->dtype)) || !aligned_to(args->total, dtype_size(args->dtype)) ||
+      !aligned_to(args->y, dtype_size(args->y_dtype)))
+    return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
+  mlt_norm_args a = *args;
+  if (a.rows == 1) a.x_stride = a.residual_stride = a.y_stride = a.total_stride = 0;
+  long long launches = 0;
+  const cudaError_t e = launch_norm(a, api_sm_count(), &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "layer norm launch");
+}
+
+int mlt_layer_norm_grad_workspace(int64_t rows, int dim, size_t* bytes_out) {
+  if (bytes_out == nullptr) return api_fail(MLT_EINVAL, "bytes_out must be non-NULL");
+  mlt_norm_args a{};
+  a.rows = rows;
+  a.dim = dim;
+  a.x = bytes_out;
+  const int rc = check_norm(&a);
+  if (rc != MLT_OK) return rc;
+  *bytes_out = norm_grad_workspace(rows, dim, api_sm_count());
+  return MLT_OK;
+}
+
+int mlt_layer_norm_grad(void* stream, const mlt_norm_args* args, const mlt_norm_grads* grads, void* workspace,
+                        size_t workspace_bytes) {
+  int rc = check_norm(args);
+  if (rc != MLT_OK) return rc;
+  if (grads == nullptr) return api_fail(MLT_EINVAL, "grads must be non-NULL");
+  if (args->residual != nullptr) return api_fail(MLT_EINVAL, "the gradient takes the sum as x and no residual");
+  if (args->rows > 0 && (grads->gy == nullptr || args->stats == nullptr))
+    return api_fail(MLT_EINVAL, "gy and stats must be non-NULL");
+  if (grads->gy_stride < 0 || grads->g_total_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
+  if (grads->gx != nullptr && !stride_ok(grads->gx_stride, args->dim, args->rows))
+    return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
+  if (!aligned_to(grads->gy, dtype_size(args->y_dtype)) || !aligned_to(grads->g_total, dtype_size(args->dtype)) ||
+      !aligned_to(grads->gx, dtype_size(args->dtype)) || !aligned_to(grads->gweight, dtype_size(args->w_dtype)) ||
+      !aligned_to(grads->gbias, dtype_size(args->w_dtype)))
+    return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
+  const bool sums = grads->gweight != nullptr || grads->gbias != nullptr;
+  const int sms = api_sm_count();
+  rc = check_ws(workspace, workspace_bytes, sums ? norm_grad_workspace(args->rows, args->dim, sms) : 0);
+  if (rc != MLT_OK) return rc;
+  if (!sums && (grads->gx == nullptr || args->rows == 0)) return MLT_OK;
+  mlt_norm_args a = *args;
+  mlt_norm_grads g = *grads;
+  if (a.rows == 1) a.x_stride = g.gy_stride = g.g_total_stride = g.gx_stride = 0;
+  long long launches = 0;
+  const cudaError_t e = launch_norm_grad(a, g, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "layer norm gradient launch");
 }
 
 }  // extern "C"

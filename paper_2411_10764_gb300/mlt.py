@@ -51,6 +51,22 @@ class ScanGrads(C.Structure):
                 + [(k, C.c_void_p) for k in ("g_state_out", "x", "dt", "z", "B", "C", "A", "skip", "dt_bias", "conv_w",
                                              "conv_b", "state", "conv_state")])
 
+
+
+class NormArgs(C.Structure):
+    """mlt_norm_args"""
+    _fields_ = ([(k, C.c_int32) for k in ("dtype", "y_dtype", "w_dtype", "dim")] + [("rows", C.c_int64)]
+                + [(k, C.c_void_p) for k in ("x", "residual", "weight", "bias")]
+                + [("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("y", C.c_void_p), ("total", C.c_void_p),
+                   ("y_stride", C.c_int64), ("total_stride", C.c_int64), ("stats", C.c_void_p), ("eps", C.c_float)])
+
+
+class NormGrads(C.Structure):
+    """mlt_norm_grads"""
+    _fields_ = [("gy", C.c_void_p), ("g_total", C.c_void_p), ("gy_stride", C.c_int64), ("g_total_stride", C.c_int64),
+                ("gx", C.c_void_p), ("gx_stride", C.c_int64), ("gweight", C.c_void_p), ("gbias", C.c_void_p)]
+
+
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
 
 
@@ -123,6 +139,9 @@ def lib(build_if_missing: bool = True):
             "mlt_scan_workspace": [P, P],
             "mlt_scan_grad": [P, P, P, P, C.c_size_t],
             "mlt_scan_grad_workspace": [P, P],
+            "mlt_layer_norm": [P, P],
+            "mlt_layer_norm_grad": [P, P, P, P, C.c_size_t],
+            "mlt_layer_norm_grad_workspace": [i64, i32, P],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -683,6 +702,133 @@ def scan_grad(gy, x, dt, B, C_, A, z=None, skip=None, dt_bias=None, conv_w=None,
     ws, n_ws = _workspace(("scan_grad", *x.shape, a.states, a.groups),
                           lambda w: lb.mlt_scan_grad_workspace(C.byref(a), C.byref(w)), x.device)
     rc = lb.mlt_scan_grad(_stream_of(x), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
+    if rc:
+        _check(rc)
+    return g
+
+
+def _flat(t, name: str, dim: int, dtype=None):
+    """(tensor [rows][dim], elements between its rows); a copy where t's rows lie at no one distance."""
+    _cuda(t, name, dtype)
+    if t.dim() != 2:
+        t = t.reshape(-1, dim)
+    stride, column = t.stride()
+    if column != 1 and dim > 1 and t.numel() > 0:
+        raise ValueError(f"{name} must have adjacent columns")
+    return t, stride
+
+
+def _flat_out(t, name: str, like, dtype):
+    """The same for an output of like's shape, which may not be copied."""
+    _cuda(t, name, dtype)
+    _need(t.shape == like.shape, f"{name} must have x's shape")
+    dim = t.shape[-1]
+    flat = t if t.dim() == 2 else t.view(-1, dim)
+    return flat.data_ptr(), _rows(flat, name)
+
+
+def _one_device(first, *others):
+    """That all tensors lie on first's device, and it is the current one."""
+    d = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError("all tensors must lie on one device")
+    if _torch.cuda.current_device() != d:
+        raise ValueError(f"the tensors lie on device {d}, which is not the current one (torch.cuda.set_device)")
+
+
+def _norm_weights(weight, bias, dim):
+    """(type code, address, address)"""
+    code, at = MLT_F32, [None, None]
+    for k, (t, name) in enumerate(((weight, "weight"), (bias, "bias"))):
+        if t is None:
+            continue
+        _cuda(t, name)
+        code = _dtype_code(t)
+        _need(t.shape == (dim,) and t.is_contiguous(), f"{name} must be contiguous, of the shape ({dim},)")
+        at[k] = t.data_ptr()
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias must be of one type")
+    return code, at[0], at[1]
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, out_dtype=None, out=None, total_out=None,
+               stream=None):
+    """mlt_layer_norm over the last dimension of x, after adding `residual` (x's
+    shape and type) where one is given.  Returns (y, total, stats): y in
+    `out_dtype` (x's type, or a narrower one where x is fp32), the sum (x itself without a residual)
+    and fp32 [...][2] of mean and 1 / deviation, which layer_norm_grad takes.  `out` and
+    `total_out` receive y and total and may be x or residual themselves."""
+    L = _setup()
+    if stream is not None:
+        return _on(stream, layer_norm, x, weight, bias, eps, residual, out_dtype, out, total_out)
+    _cuda(x, "x")
+    _need(x.dim() > 0, "x must have a last dimension")
+    code, dim = _dtype_code(x), x.shape[-1]
+    _need(1 <= dim <= _INT_MAX, "dim must lie in [1, 2^20]")
+    flat, stride = _flat(x, "x", dim)
+    w_code, w, b = _norm_weights(weight, bias, dim)
+    r, r_stride = None, 0
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError("residual must have x's shape")
+        r, r_stride = _flat(residual, "residual", dim, x.dtype)
+    if out is None:
+        y = _torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        at, y_stride = y.data_ptr(), dim
+    else:
+        y = out
+        at, y_stride = _flat_out(out, "out", x, out_dtype)
+    total, t_at, t_stride = x, None, 0
+    if residual is not None:
+        total = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if total_out is None else total_out
+        t_at, t_stride = _flat_out(total, "total_out", x, x.dtype)
+    else:
+        _need(total_out is None, "total_out needs a residual")
+    stats = _torch.empty((*x.shape[:-1], 2), dtype=_torch.float32, device=x.device)
+    _one_device(x, weight, bias, residual, y, total)
+    a = NormArgs(code, _dtype_code(y), w_code, dim, flat.shape[0], flat.data_ptr(), None if r is None else r.data_ptr(), w, b,
+                 stride, r_stride, at, t_at, y_stride, t_stride, stats.data_ptr(), eps)
+    rc = L.mlt_layer_norm(_stream_of(x), C.byref(a))
+    if rc:
+        _check(rc)
+    return y, total, stats
+
+
+def layer_norm_grad(gy, x, stats, weight=None, bias=None, g_total=None, out=None, stream=None):
+    """mlt_layer_norm_grad: the gradients of layer_norm's inputs from those of y (`gy`) and of
+    total (`g_total`, or None).  `x` is what was normed: the total where a residual was added.
+    Returns a dict: "x" (x's type, also the residual's gradient), "weight" and
+    "bias" (their types; None where they were not given).  `out` receives "x" and may be g_total, or
+    gy where the types are the same."""
+    L = _setup()
+    if stream is not None:
+        return _on(stream, layer_norm_grad, gy, x, stats, weight, bias, g_total, out)
+    _cuda(x, "x")
+    _need(x.dim() > 0, "x must have a last dimension")
+    code, dim = _dtype_code(x), x.shape[-1]
+    _need(1 <= dim <= _INT_MAX, "dim must lie in [1, 2^20]")
+    flat, stride = _flat(x, "x", dim)
+    rows = flat.shape[0]
+    for t, name in ((gy, "gy"), (g_total, "g_total")):
+        _need(t is None or t.shape == x.shape, f"{name} must have x's shape")
+    gy, gy_stride = _flat(gy, "gy", dim)
+    t, t_stride = (None, 0) if g_total is None else _flat(g_total, "g_total", dim, x.dtype)
+    w_code, w, b = _norm_weights(weight, bias, dim)
+    s = _plain(stats, "stats", _torch.float32, (*x.shape[:-1], 2))
+    g = {"x": _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out, "weight": None, "bias": None}
+    at, x_stride = _flat_out(g["x"], "out", x, x.dtype)
+    if weight is not None:
+        g["weight"] = _like(weight)
+    if bias is not None:
+        g["bias"] = _like(bias)
+    _one_device(x, gy, stats, weight, bias, g_total, out)
+    a = NormArgs(code, _dtype_code(gy), w_code, dim, rows, flat.data_ptr(), None, w, b, stride, 0, None, None, 0, 0, s, 0.0)
+    q = NormGrads(gy.data_ptr(), None if t is None else t.data_ptr(), gy_stride, t_stride, at, x_stride,
+                  None if weight is None else g["weight"].data_ptr(), None if bias is None else g["bias"].data_ptr())
+    ws, n_ws = (None, 0) if weight is None and bias is None else _workspace(
+        ("layer_norm_grad", rows, dim), lambda o: L.mlt_layer_norm_grad_workspace(rows, dim, C.byref(o)), x.device)
+    rc = L.mlt_layer_norm_grad(_stream_of(x), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
     if rc:
         _check(rc)
     return g
