@@ -516,8 +516,8 @@ int mlt_tune_head_levels(int levels);
  * screening: draws from scores instead of the top-k (mlt_sample), digits or
  * tokens to vectors with the gradient of the table (mlt_embed,
  * mlt_embed_grad), a recurrent state over a sequence (mlt_scan,
- * mlt_scan_grad), and the norm of a block (mlt_layer_norm, mlt_layer_norm_grad).
- * The paper has no counterpart.
+ * mlt_scan_grad), the norm of a block (mlt_layer_norm, mlt_layer_norm_grad) and a
+ * training step (mlt_adamw).  The paper has no counterpart.
  *
  * They keep no state between calls and use no library scratch: a call that
  * needs a workspace takes it from the caller (device memory of at least the
@@ -713,6 +713,69 @@ typedef struct {
 int mlt_layer_norm_grad(void *stream, const mlt_norm_args *args, const mlt_norm_grads *grads, void *workspace,
                         size_t workspace_bytes);
 int mlt_layer_norm_grad_workspace(int64_t rows, int dim, size_t *bytes_out);
+
+/* One AdamW step over many tensors, in few launches (one for each 500 tensors).
+ * For each element, all in fp32:
+ *   g = grad * grad_scale
+ *   m = m beta1 + g (1 - beta1);  v = v beta2 + g g (1 - beta2)
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) *
+ *       m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * The lines of m and v are single 32-bit operations in this order, so moments are the
+ * same on every machine; p is off by a few roundings of its change, and
+ * rounded once to the parameter's type.  `copy` receives p in another type
+ * (parameters in fp32, copies that the model computes with in 16 bits).
+ *
+ * Moments of all tensors lie one after the other, each tensor's from a multiple of
+ * 256 elements on (mlt_adamw_blocks gives the number of such blocks).
+ *   bits 32: m, v fp32 [blocks * 256];
+ *   bits 8:  m e4m3, v e5m2, one byte each, and m_scale, v_scale fp32
+ *            [blocks]: a moment is its byte's value times its block's
+ *            scale, a power of two that puts the block's largest |m| into [128, 256),
+ *            its largest v into [2^14, 2^15) (the largest one counted as at
+ *            least 2^-111).  The update uses the moments before
+ *            they are rounded.  A value between two codes becomes the
+ *            upper one with the probability of its place between them, from a
+ *            hash of seed, step and place: rounding to the nearest would leave v
+ *            where it is, for 1 - beta2 is less than half a step.  v > 0 becomes
+ *            at least the smallest code.  A block with an infinite or NaN moment
+ *            becomes NaN as a whole.
+ * The hash, in 32-bit whole numbers, of element i of block b:
+ *   mix(h): h ^= h >> 16; h *= 0x9E3779B1; h ^= h >> 15; h *= 0xB504F333;
+ *           h ^= h >> 16
+ *   mix(mix(mix(mix(seed) + step) + b) + i 0x9E3779B9)
+ * its low 16 bits place m, its high ones v: x + bits / 2^16 of a step, rounded down.
+ *
+ * Tensors of length 0 are passed over.  Parameters, copies and moments must not
+ * overlap (compared and refused).  A non-finite gradient makes its element (with 8 bits: its block)
+ * non-finite. */
+typedef struct {
+    void *param;          /* device [n] of `dtype`, updated in place         */
+    const void *grad;     /* device [n] of `grad_dtype`; NULL: the tensor and
+                             its moments stay as they are                    */
+    void *copy;           /* device [n] of `copy_dtype`, or NULL             */
+    int64_t n;            /* 0 .. 2^40                                       */
+    int16_t dtype, grad_dtype, copy_dtype, reserved;
+    float lr;             /* used where the rule has no lr on the device;
+                             a factor on it where it has                     */
+    float weight_decay;
+} mlt_adamw_tensor;
+
+typedef struct {
+    double beta1, beta2, eps;
+    int64_t step;              /* 1 for the first one                        */
+    const int64_t *step_device; /* read instead of `step` if not NULL, so
+                                  that a captured step may be replayed       */
+    const float *lr;           /* device, one value, or NULL                 */
+    const float *grad_scale;   /* device, one value, or NULL: 1              */
+    int32_t bits;              /* 32 or 8                                    */
+    uint32_t seed;             /* of the rounding to 8 bits                  */
+} mlt_adamw_rule;
+
+/* tensors: host, [count], 0 .. 2^20 of them; read before the call returns.  m, v: device, 16-byte
+ * aligned. */
+int mlt_adamw(void *stream, const mlt_adamw_tensor *tensors, int count, const mlt_adamw_rule *rule, void *m, void *v,
+              float *m_scale, float *v_scale);
+int mlt_adamw_blocks(const mlt_adamw_tensor *tensors, int count, int64_t *blocks_out);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

@@ -110,4 +110,8 @@ size_t norm_grad_workspace(long long rows, int dim, int sms);
 cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, void* ws, int sms, long long* launches,
                              cudaStream_t st);
 
+// --- adamw.cu --------------------------------------------------------------
+cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_adamw_rule& rule, void* m, void* v,
+                         float* m_scale, float* v_scale, long long* launches, cudaStream_t st);
+
 }  // namespace mlt

@@ -2,7 +2,11 @@
 // launches of sample.cu, embed.cu, scan.cu and scan_grad.cu.  Nothing here
 // allocates device memory, but that the first draw or lookup on a device makes the library's own state
 // (the error word is part of it) where no other call has.
+#include <algorithm>
 #include <cmath>
+#include <new>
+#include <utility>
+#include <vector>
 
 #include "seq.cuh"
 
@@ -101,6 +105,34 @@ int check_norm(const mlt_norm_args* a) {
       !aligned_to(a->bias, dtype_size(a->w_dtype)) || !aligned_to(a->stats, 8))
     return api_fail(MLT_EINVAL, "buffers must be aligned to their elements, stats to 8 bytes");
   return MLT_OK;
+}
+
+int check_tensors(const mlt_adamw_tensor* tensors, int count) {
+  if (count < 0 || count > (1 << 20)) return api_fail(MLT_EINVAL, "count must lie in [0, 2^20], got %d", count);
+  if (count > 0 && tensors == nullptr) return api_fail(MLT_EINVAL, "tensors must be non-NULL");
+  int64_t all = 0;
+  for (int i = 0; i < count; ++i) {
+    const mlt_adamw_tensor& t = tensors[i];
+    if (!dtype_ok(t.dtype) || !dtype_ok(t.grad_dtype) || !dtype_ok(t.copy_dtype))
+      return api_fail(MLT_EINVAL, "tensor %d: unknown element type", i);
+    if (t.n < 0 || t.n > (1LL << 40)) return api_fail(MLT_EINVAL, "tensor %d: n must lie in [0, 2^40]", i);
+    all += (t.n + 255) / 256;
+    if (all > (1LL << 40)) return api_fail(MLT_EINVAL, "the tensors have more than 2^40 blocks");
+  }
+  return MLT_OK;
+}
+
+// Whether two of the ranges [first, second) of addresses overlap; orders them.
+bool overlap(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges) {
+  std::sort(ranges.begin(), ranges.end());
+  for (size_t i = 1; i < ranges.size(); ++i)
+    if (ranges[i].first < ranges[i - 1].second) return true;
+  return false;
+}
+
+void add_range(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges, const void* p, int64_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  if (p != nullptr && bytes > 0) ranges.emplace_back(at, at + static_cast<uintptr_t>(bytes));
 }
 
 }  // namespace
@@ -351,6 +383,66 @@ int mlt_layer_norm_grad(void* stream, const mlt_norm_args* args, const mlt_norm_
   long long launches = 0;
   const cudaError_t e = launch_norm_grad(a, g, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "layer norm gradient launch");
+}
+
+int mlt_adamw_blocks(const mlt_adamw_tensor* tensors, int count, int64_t* blocks_out) {
+  if (blocks_out == nullptr) return api_fail(MLT_EINVAL, "blocks_out must be non-NULL");
+  const int rc = check_tensors(tensors, count);
+  if (rc != MLT_OK) return rc;
+  *blocks_out = 0;
+  for (int i = 0; i < count; ++i) *blocks_out += (tensors[i].n + 255) / 256;
+  return MLT_OK;
+}
+
+int mlt_adamw(void* stream, const mlt_adamw_tensor* tensors, int count, const mlt_adamw_rule* rule, void* m, void* v,
+              float* m_scale, float* v_scale) try {
+  const int rc = check_tensors(tensors, count);
+  if (rc != MLT_OK) return rc;
+  if (rule == nullptr) return api_fail(MLT_EINVAL, "rule must be non-NULL");
+  if (!(rule->beta1 >= 0 && rule->beta1 < 1 && rule->beta2 >= 0 && rule->beta2 < 1))
+    return api_fail(MLT_EINVAL, "beta1 and beta2 must lie in [0, 1)");
+  if (!(rule->eps >= 0 && std::isfinite(rule->eps))) return api_fail(MLT_EINVAL, "eps must be finite and not negative");
+  if (rule->bits != 8 && rule->bits != 32) return api_fail(MLT_EINVAL, "bits must be 8 or 32, got %d", rule->bits);
+  if (rule->step_device == nullptr && rule->step < 1) return api_fail(MLT_EINVAL, "step must be at least 1");
+  if (!aligned_to(rule->step_device, 8) || !aligned_to(rule->lr, 4) || !aligned_to(rule->grad_scale, 4))
+    return api_fail(MLT_EINVAL, "values on the device must be aligned to their types");
+  std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+  ranges.reserve(2 * static_cast<size_t>(count) + 4);
+  int64_t blocks = 0;
+  bool any = false;
+  for (int i = 0; i < count; ++i) {
+    const mlt_adamw_tensor& t = tensors[i];
+    blocks += (t.n + 255) / 256;
+    if (t.n == 0 || t.grad == nullptr) continue;
+    any = true;
+    if (t.param == nullptr) return api_fail(MLT_EINVAL, "tensor %d: param must be non-NULL", i);
+    if (!std::isfinite(t.lr) || !std::isfinite(t.weight_decay))
+      return api_fail(MLT_EINVAL, "tensor %d: lr and weight_decay must be finite", i);
+    if (!aligned_to(t.param, dtype_size(t.dtype)) || !aligned_to(t.grad, dtype_size(t.grad_dtype)) ||
+        !aligned_to(t.copy, dtype_size(t.copy_dtype)))
+      return api_fail(MLT_EINVAL, "tensor %d: buffers must be aligned to their elements", i);
+    add_range(ranges, t.param, t.n * static_cast<int64_t>(dtype_size(t.dtype)));
+    add_range(ranges, t.copy, t.n * static_cast<int64_t>(dtype_size(t.copy_dtype)));
+  }
+  if (!any) return MLT_OK;
+  if (m == nullptr || v == nullptr || !aligned_to(m, 16) || !aligned_to(v, 16))
+    return api_fail(MLT_EINVAL, "m and v must be non-NULL, aligned to 16 bytes");
+  const int64_t each = 256 * (rule->bits / 8);
+  add_range(ranges, m, blocks * each);
+  add_range(ranges, v, blocks * each);
+  if (rule->bits == 8) {
+    if (m_scale == nullptr || v_scale == nullptr || !aligned_to(m_scale, 4) || !aligned_to(v_scale, 4))
+      return api_fail(MLT_EINVAL, "moments of 8 bits need m_scale and v_scale");
+    add_range(ranges, m_scale, blocks * 4);
+    add_range(ranges, v_scale, blocks * 4);
+  }
+  if (overlap(ranges)) return api_fail(MLT_EINVAL, "parameters, copies and moments must not overlap");
+  long long launches = 0;
+  const cudaError_t e =
+      launch_adamw(tensors, count, *rule, m, v, m_scale, v_scale, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "AdamW launch");
+} catch (const std::bad_alloc&) {
+  return api_fail(MLT_ENOMEM, "out of host memory for %d tensors", count);
 }
 
 }  // extern "C"

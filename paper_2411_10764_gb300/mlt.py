@@ -10,7 +10,9 @@ from __future__ import annotations
 import ctypes as C
 import os
 import re
+import struct
 import threading
+from array import array
 
 import numpy as np
 
@@ -65,6 +67,13 @@ class NormGrads(C.Structure):
     """mlt_norm_grads"""
     _fields_ = [("gy", C.c_void_p), ("g_total", C.c_void_p), ("gy_stride", C.c_int64), ("g_total_stride", C.c_int64),
                 ("gx", C.c_void_p), ("gx_stride", C.c_int64), ("gweight", C.c_void_p), ("gbias", C.c_void_p)]
+
+
+class AdamWRule(C.Structure):
+    """mlt_adamw_rule"""
+    _fields_ = ([(k, C.c_double) for k in ("beta1", "beta2", "eps")] + [("step", C.c_int64)]
+                + [(k, C.c_void_p) for k in ("step_device", "lr", "grad_scale")]
+                + [("bits", C.c_int32), ("seed", C.c_uint32)])
 
 
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
@@ -142,6 +151,8 @@ def lib(build_if_missing: bool = True):
             "mlt_layer_norm": [P, P],
             "mlt_layer_norm_grad": [P, P, P, P, C.c_size_t],
             "mlt_layer_norm_grad_workspace": [i64, i32, P],
+            "mlt_adamw": [P, P, i32, P, P, P, P, P],
+            "mlt_adamw_blocks": [P, i32, P],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -386,7 +397,7 @@ def _on(stream, call, *args):
     tensors given are kept until its work is done."""
     with _torch.cuda.stream(stream):
         for t in args:
-            for one in t if isinstance(t, tuple) else (t,):
+            for one in t if isinstance(t, (tuple, list)) else (t,):
                 if isinstance(one, _torch.Tensor) and one.is_cuda:
                     one.record_stream(stream)
         return call(*args)
@@ -832,6 +843,138 @@ def layer_norm_grad(gy, x, stats, weight=None, bias=None, g_total=None, out=None
     if rc:
         _check(rc)
     return g
+
+
+ADAMW_BLOCK = 256
+
+
+class AdamWState(tuple):
+    """The moments of adamw's tensors: flat tensors m, v, m_scale and v_scale (the scales None with
+    moments in 32 bits); each parameter's part begins at a multiple of ADAMW_BLOCK
+    elements.  32 bits: m and v fp32; 8 bits: m float8_e4m3fn, v float8_e5m2, and a moment
+    is its value times its block's scale."""
+
+    def __new__(cls, m, v, m_scale=None, v_scale=None):
+        return super().__new__(cls, (m, v, m_scale, v_scale))
+
+    m, v, m_scale, v_scale = (property(lambda self, k=k: self[k]) for k in range(4))
+
+    @property
+    def bits(self) -> int:
+        return 32 if self[2] is None else 8
+
+
+def adamw_state(params, bits: int = 32) -> AdamWState:
+    """Moments of zero for adamw over `params` (a list of tensors), in 32 or 8 bits."""
+    import torch
+
+    _need(bits in (8, 32), "bits must be 8 or 32")
+    blocks = sum(-(-p.numel() // ADAMW_BLOCK) for p in params)
+    device = params[0].device if len(params) else "cuda"
+    new = lambda n, dt: torch.zeros(n, dtype=dt, device=device)  # noqa: E731
+    if bits == 32:
+        return AdamWState(*(new(blocks * ADAMW_BLOCK, torch.float32) for _ in range(2)))
+    return AdamWState(*(new(blocks * ADAMW_BLOCK, torch.uint8).view(dt) for dt in (torch.float8_e4m3fn, torch.float8_e5m2)),
+                      *(new(blocks, torch.float32) for _ in range(2)))
+
+
+_rate_words: dict = {}
+
+
+def _rate_word(lr: float, decay: float) -> int:
+    """lr and weight_decay of an mlt_adamw_tensor as one 64-bit word."""
+    word = _rate_words.get((lr, decay))
+    if word is None:
+        if len(_rate_words) > 4096:
+            _rate_words.clear()
+        word = _rate_words[lr, decay] = struct.unpack("<q", struct.pack("<ff", lr, decay))[0]
+    return word
+
+
+def _per_tensor(value, count: int, name: str):
+    if isinstance(value, (list, tuple)):
+        _need(len(value) == count, f"{name} must have a value for each tensor")
+        return value
+    return [value] * count
+
+
+def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
+          copies=None, grad_scale=None, seed: int = 0, lr_scale=1.0, stream=None) -> None:
+    """mlt_adamw: one AdamW step over the tensors of `params`, in place, with `state` (adamw_state
+    of the same list).  `grads`: a tensor of the parameter's shape for each, any of the three types, or
+    None: that one is left as it is.  `step` counts from 1: a number or an int64 CUDA
+    tensor of one value; `lr`: a number, a list of one for each tensor or an fp32 CUDA tensor of one
+    value (tensors are read when the step runs, so a captured one may be replayed with others).
+    `lr_scale` multiplies it; `weight_decay`, `lr_scale`: a number or a list.  `copies`: a list of tensors
+    (or None) of the parameters' shapes that receive them in their types.  `grad_scale`: an
+    fp32 CUDA tensor of one value that multiplies the gradients.  `seed`: of the rounding of moments in
+    8 bits, 32 bits of it."""
+    L = _setup()
+    if stream is not None:
+        return _on(stream, adamw, params, grads, state, step, lr, betas, eps, weight_decay, copies, grad_scale, seed,
+                   lr_scale)
+    torch = _torch
+    count = len(params)
+    _need(len(grads) == count and (copies is None or len(copies) == count),
+          "grads and copies must have an entry for each parameter")
+    m, v, ms, vs = state
+    bits = 32 if ms is None else 8
+    _need((ms is None) == (vs is None), "state must have both scales or none")
+    f32 = torch.float32
+    for t, dt in ((m, f32 if bits == 32 else torch.float8_e4m3fn), (v, f32 if bits == 32 else torch.float8_e5m2), (ms, f32),
+                  (vs, f32)):
+        if t is not None:
+            _cuda(t, "moments", dt)
+            _need(t.is_contiguous(), "moments must be contiguous")
+    scalars = []
+    for t, dt, name in ((step, torch.int64, "step"), (lr, f32, "lr"), (grad_scale, f32, "grad_scale")):
+        if t is not None and (isinstance(t, torch.Tensor) or name == "grad_scale"):
+            _cuda(t, name, dt)
+            _need(t.numel() == 1, f"{name} must have one value")
+            scalars.append(t.data_ptr())
+        else:
+            scalars.append(None)
+    rates = _per_tensor(1.0 if scalars[1] is not None else lr, count, "lr")
+    decays = _per_tensor(weight_decay, count, "weight_decay")
+    if isinstance(lr_scale, (list, tuple)) or lr_scale != 1.0:
+        rates = [a * b for a, b in zip(rates, _per_tensor(lr_scale, count, "lr_scale"))]
+    device, codes, kept = m.get_device(), _DTYPES, []
+    words, blocks = [], 0
+    for p, g, rate, decay, copy in zip(params, grads, rates, decays, copies or [None] * count):
+        n = p.numel()
+        blocks += -(-n // ADAMW_BLOCK)
+        if g is None:
+            words += (0, 0, 0, n, 0, 0)
+            continue
+        if p.get_device() != device or g.get_device() != device:
+            raise ValueError("parameters, gradients and moments must lie on one CUDA device")
+        if not p.is_contiguous():
+            raise ValueError("parameters must be contiguous")
+        if g.shape != p.shape:
+            raise ValueError("a gradient must have its parameter's shape")
+        if not g.is_contiguous():
+            g = g.contiguous()
+            kept.append(g)
+        try:
+            kinds = codes[p.dtype] | codes[g.dtype] << 16
+            to = 0
+            if copy is not None:
+                kinds |= codes[copy.dtype] << 32
+                if copy.shape != p.shape or not copy.is_contiguous() or copy.get_device() != device:
+                    raise ValueError("a copy must be contiguous, of its parameter's shape and device")
+                to = copy.data_ptr()
+        except KeyError as e:
+            raise TypeError(f"float32, bfloat16 or float16 wanted, got {e.args[0]}") from None
+        words += (p.data_ptr(), g.data_ptr(), to, n, kinds, _rate_words.get((rate, decay)) or _rate_word(rate, decay))
+    _need(m.numel() == v.numel() == blocks * ADAMW_BLOCK and (ms is None or ms.numel() == vs.numel() == blocks),
+          "the moments are of other parameters")
+    _one_device(m, v, ms, vs, *(t for t in (step, lr, grad_scale) if isinstance(t, torch.Tensor)))
+    table = array("q", words)
+    rule = AdamWRule(betas[0], betas[1], eps, 0 if scalars[0] is not None else int(step), *scalars, bits, seed & 0xFFFFFFFF)
+    rc = L.mlt_adamw(_stream_of(m), table.buffer_info()[0], count, C.byref(rule), m.data_ptr(), v.data_ptr(),
+                     None if ms is None else ms.data_ptr(), None if vs is None else vs.data_ptr())
+    if rc:
+        _check(rc)
 
 
 def screen_host(feats: np.ndarray, thr: float, k: int, out=None, stream=None):
