@@ -516,15 +516,16 @@ int mlt_tune_head_levels(int levels);
  * screening: draws from scores instead of the top-k (mlt_sample), digits or
  * tokens to vectors with the gradient of the table (mlt_embed,
  * mlt_embed_grad), a recurrent state over a sequence (mlt_scan,
- * mlt_scan_grad), the norm of a block (mlt_layer_norm, mlt_layer_norm_grad) and a
- * training step (mlt_adamw).  The paper has no counterpart.
+ * mlt_scan_grad), the norm of a block (mlt_layer_norm, mlt_layer_norm_grad), a
+ * training step (mlt_adamw), and the most probable sequences instead of drawn ones
+ * (mlt_beam_step, mlt_beam_reorder).  The paper has no counterpart.
  *
  * They keep no state between calls and use no library scratch: a call that
  * needs a workspace takes it from the caller (device memory of at least the
  * bytes its ..._workspace call gives, 256-byte aligned), so calls with
  * workspaces of their own may run on different streams at once and be captured
  * in graphs.  All are asynchronous on `stream`.  Where no other call has, the
- * first draw or lookup on a device allocates what the library keeps there (some
+ * first draw, lookup or reordering on a device allocates what the library keeps there (some
  * 200 KB: the error word that mlt_sync_status reads, and screening's smallest
  * scratch); issue it outside a capture.
  *
@@ -776,6 +777,63 @@ typedef struct {
 int mlt_adamw(void *stream, const mlt_adamw_tensor *tensors, int count, const mlt_adamw_rule *rule, void *m, void *v,
               float *m_scale, float *v_scale);
 int mlt_adamw_blocks(const mlt_adamw_tensor *tensors, int count, int64_t *blocks_out);
+
+/* One step of beam search for each of `batch` items: of all continuations of its
+ * beams, the m best by their total log-probability.
+ *   s       = score clamped to the finite floats; a NaN or -infinity score is no
+ *             continuation
+ *   lse[w]  = ln(sum over the continuations of beam w of exp s), or 0 with
+ *             normalised != 0 (scores are log-probabilities)
+ *   total   = logp[w] + (s - lse[w]), compared in more than 32 bits
+ * Order: the larger total; then the lower beam, of one beam the higher score, then
+ * the lower token.  A beam whose logp is NaN or -infinity has no continuations (a
+ * search starts from logp 0 and -infinity for the other beams); a finished one
+ * (`done`) has one, token `eos` with its own logp as the total, and its scores are
+ * not read.
+ *   scores  device [batch][beams][n] of `dtype`, beam_stride elements
+ *           between beams and batch_stride between items
+ *   logp    device [batch][beams] fp32;  done  device [batch][beams] bytes, not
+ *           0: finished, or NULL
+ *   eos     the token that finishes a beam, below n; < 0: none (then `done` must be NULL)
+ *   out_parent, out_token  device [batch][m] int64;  out_logp  device [batch][m]
+ *           fp32, the total rounded (below the lowest
+ *           float: -infinity);  out_done  device [batch][m] bytes, 0 or
+ *           1: the parent was finished or the token is eos
+ * With fewer than m continuations the rest is -1, -1, -infinity and 0.  Outputs
+ * must not overlap logp or done.
+ *   batch 0 .. 65535;  beams 1 .. 1024;  n 1 .. 2^22;  m 1 .. 1024;
+ *   beams x min(m, n) <= 8192 */
+typedef struct {
+    int32_t dtype, batch, beams, n, m, normalised;
+    int64_t eos;
+    const void *scores;
+    int64_t batch_stride, beam_stride;
+    const float *logp;
+    const uint8_t *done;
+    int64_t *out_parent, *out_token;
+    float *out_logp;
+    uint8_t *out_done;
+} mlt_beam_args;
+
+int mlt_beam_step(void *stream, const mlt_beam_args *args, void *workspace, size_t workspace_bytes);
+int mlt_beam_step_workspace(const mlt_beam_args *args, size_t *bytes_out);
+
+/* Beams' states in place: row [b][w] of every tensor becomes what row
+ * [b][parent[b][w]] was.  A negative parent leaves the row as it is; one >= beams
+ * does too and is reported by the next mlt_sync_status (MLT_EINVAL).  Rows that are
+ * their own parents are not touched.
+ *   tensors  host, [count], 0 .. 64 of them, read before the call returns:
+ *            [batch * beams] rows of row_bytes bytes, row_stride bytes apart;
+ *            they must not overlap each other or parent (compared and refused)
+ *   parent   device [batch][beams] int64
+ *   batch 0 .. 65535;  beams 1 .. 1024 */
+typedef struct {
+    void *data;
+    int64_t row_bytes, row_stride;
+} mlt_beam_state;
+
+int mlt_beam_reorder(void *stream, const int64_t *parent, int batch, int beams, const mlt_beam_state *tensors,
+                     int count);
 
 /* Cumulative number of GPU kernels this library has launched. */
 int64_t mlt_kernel_launches(void);

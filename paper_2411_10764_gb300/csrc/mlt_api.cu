@@ -1847,6 +1847,7 @@ int mlt_sync_status(void* stream) {
   if (word & kErrWaitTimeout) return fail(MLT_ETIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
   if (word & kErrBadRule) return fail(MLT_EINVAL, "a sampling rule was out of range (error word 0x%x)", word);
   if (word & kErrBadToken) return fail(MLT_EINVAL, "an embedding id was not below vocab (error word 0x%x)", word);
+  if (word & kErrBadParent) return fail(MLT_EINVAL, "a beam's parent was not below beams (error word 0x%x)", word);
   if (word & kErrBadIndex) return fail(MLT_EINVAL, "a rerank candidate index was outside [0, n) (error word 0x%x)", word);
   return fail(MLT_ECUDA, "device-side bookkeeping error (error word 0x%x)", word);
 }

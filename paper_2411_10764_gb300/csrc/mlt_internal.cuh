@@ -24,6 +24,7 @@ constexpr unsigned kErrSelect = 2u;       // top-k bookkeeping out of range
 constexpr unsigned kErrBadIndex = 4u;     // a rerank candidate index outside [0, n)
 constexpr unsigned kErrBadRule = 8u;      // a sampling rule out of range
 constexpr unsigned kErrBadToken = 16u;    // an embedding id not below vocab
+constexpr unsigned kErrBadParent = 32u;   // a beam's parent not below the number of beams
 
 // A bounded device wait gives up after this many nanoseconds.
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;

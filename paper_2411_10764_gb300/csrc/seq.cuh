@@ -114,4 +114,12 @@ cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, vo
 cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_adamw_rule& rule, void* m, void* v,
                          float* m_scale, float* v_scale, long long* launches, cudaStream_t st);
 
+// --- beam.cu ---------------------------------------------------------------
+constexpr int kBeamMostBeams = 1024;
+constexpr int kBeamMostStates = 64;
+size_t beam_workspace(const mlt_beam_args& a, int sms);
+cudaError_t launch_beam(const mlt_beam_args& a, void* ws, int sms, long long* launches, cudaStream_t st);
+cudaError_t launch_reorder(const int64_t* parent, int batch, int beams, const mlt_beam_state* tensors, int count,
+                           unsigned* err, long long* launches, cudaStream_t st);
+
 }  // namespace mlt

@@ -1,6 +1,6 @@
 // C entry points of the sequence-model operators: argument checks, then the
-// launches of sample.cu, embed.cu, scan.cu and scan_grad.cu.  Nothing here
-// allocates device memory, but that the first draw or lookup on a device makes the library's own state
+// launches of sample.cu, embed.cu, scan.cu, scan_grad.cu, norm.cu, norm_grad.cu, adamw.cu and
+// beam.cu.  Nothing here allocates device memory, but that the first draw, lookup or reordering on a device makes the library's own state
 // (the error word is part of it) where no other call has.
 #include <algorithm>
 #include <cmath>
@@ -133,6 +133,19 @@ bool overlap(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges) {
 void add_range(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges, const void* p, int64_t bytes) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
   if (p != nullptr && bytes > 0) ranges.emplace_back(at, at + static_cast<uintptr_t>(bytes));
+}
+
+int check_beam(const mlt_beam_args* a) {
+  if (a == nullptr) return api_fail(MLT_EINVAL, "args must be non-NULL");
+  if (!dtype_ok(a->dtype)) return api_fail(MLT_EINVAL, "unknown element type %d", a->dtype);
+  if (a->batch < 0 || a->batch > 65535) return api_fail(MLT_EINVAL, "batch must lie in [0, 65535], got %d", a->batch);
+  if (a->beams < 1 || a->beams > kBeamMostBeams)
+    return api_fail(MLT_EINVAL, "beams must lie in [1, %d], got %d", kBeamMostBeams, a->beams);
+  if (a->n < 1 || a->n > (1 << 22)) return api_fail(MLT_EINVAL, "n must lie in [1, 2^22], got %d", a->n);
+  if (a->m < 1 || a->m > 1024) return api_fail(MLT_EINVAL, "m must lie in [1, 1024], got %d", a->m);
+  if (static_cast<int64_t>(a->beams) * std::min(a->m, a->n) > 8192)
+    return api_fail(MLT_EINVAL, "beams x min(m, n) must be at most 8192, got %d x %d", a->beams, std::min(a->m, a->n));
+  return MLT_OK;
 }
 
 }  // namespace
@@ -441,6 +454,72 @@ int mlt_adamw(void* stream, const mlt_adamw_tensor* tensors, int count, const ml
   const cudaError_t e =
       launch_adamw(tensors, count, *rule, m, v, m_scale, v_scale, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "AdamW launch");
+} catch (const std::bad_alloc&) {
+  return api_fail(MLT_ENOMEM, "out of host memory for %d tensors", count);
+}
+
+int mlt_beam_step_workspace(const mlt_beam_args* args, size_t* bytes_out) {
+  if (bytes_out == nullptr) return api_fail(MLT_EINVAL, "bytes_out must be non-NULL");
+  const int rc = check_beam(args);
+  if (rc != MLT_OK) return rc;
+  *bytes_out = beam_workspace(*args, api_sm_count());
+  return MLT_OK;
+}
+
+int mlt_beam_step(void* stream, const mlt_beam_args* args, void* workspace, size_t workspace_bytes) {
+  int rc = check_beam(args);
+  if (rc != MLT_OK) return rc;
+  if (args->batch == 0) return MLT_OK;
+  if (args->scores == nullptr || args->logp == nullptr || args->out_parent == nullptr || args->out_token == nullptr ||
+      args->out_logp == nullptr || args->out_done == nullptr)
+    return api_fail(MLT_EINVAL, "device buffers must be non-NULL");
+  if (args->batch_stride < 0 || args->beam_stride < 0) return api_fail(MLT_EINVAL, "strides must not be negative");
+  if (args->eos >= args->n) return api_fail(MLT_EINVAL, "eos must be below n");
+  if (args->eos < 0 && args->done != nullptr) return api_fail(MLT_EINVAL, "finished beams need an eos");
+  if (!aligned_to(args->scores, dtype_size(args->dtype)) || !aligned_to(args->logp, 4) || !aligned_to(args->out_parent, 8) ||
+      !aligned_to(args->out_token, 8) || !aligned_to(args->out_logp, 4))
+    return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
+  const int sms = api_sm_count();
+  rc = check_ws(workspace, workspace_bytes, beam_workspace(*args, sms));
+  if (rc != MLT_OK) return rc;
+  mlt_beam_args a = *args;
+  if (a.eos < 0) a.eos = -1;
+  long long launches = 0;
+  const cudaError_t e = launch_beam(a, workspace, sms, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "beam step launch");
+}
+
+int mlt_beam_reorder(void* stream, const int64_t* parent, int batch, int beams, const mlt_beam_state* tensors,
+                     int count) try {
+  if (batch < 0 || batch > 65535) return api_fail(MLT_EINVAL, "batch must lie in [0, 65535], got %d", batch);
+  if (beams < 1 || beams > kBeamMostBeams)
+    return api_fail(MLT_EINVAL, "beams must lie in [1, %d], got %d", kBeamMostBeams, beams);
+  if (count < 0 || count > kBeamMostStates)
+    return api_fail(MLT_EINVAL, "count must lie in [0, %d], got %d", kBeamMostStates, count);
+  if (count > 0 && tensors == nullptr) return api_fail(MLT_EINVAL, "tensors must be non-NULL");
+  const int64_t rows = static_cast<int64_t>(batch) * beams;
+  std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+  for (int i = 0; i < count; ++i) {
+    const mlt_beam_state& t = tensors[i];
+    if (t.row_bytes < 0 || t.row_bytes > (1LL << 40) || t.row_stride > (1LL << 40))
+      return api_fail(MLT_EINVAL, "tensor %d: row_bytes must lie in [0, 2^40], row_stride below it", i);
+    if (rows == 0 || t.row_bytes == 0) continue;
+    if (t.data == nullptr) return api_fail(MLT_EINVAL, "tensor %d: data must be non-NULL", i);
+    if (!stride_ok(t.row_stride, t.row_bytes, rows))
+      return api_fail(MLT_EINVAL, "tensor %d: rows must be at least row_bytes apart", i);
+    add_range(ranges, t.data, (rows - 1) * t.row_stride + t.row_bytes);
+  }
+  if (ranges.empty()) return MLT_OK;
+  if (parent == nullptr || !aligned_to(parent, 8)) return api_fail(MLT_EINVAL, "parent must be non-NULL, aligned to 8 bytes");
+  add_range(ranges, parent, rows * 8);
+  if (overlap(ranges)) return api_fail(MLT_EINVAL, "tensors must not overlap each other or parent");
+  int rc = MLT_OK;
+  unsigned* err = api_error_word(&rc);
+  if (err == nullptr) return rc;
+  long long launches = 0;
+  const cudaError_t e =
+      launch_reorder(parent, batch, beams, tensors, count, err, &launches, static_cast<cudaStream_t>(stream));
+  return launched(e, launches, "beam reorder launch");
 } catch (const std::bad_alloc&) {
   return api_fail(MLT_ENOMEM, "out of host memory for %d tensors", count);
 }

@@ -76,6 +76,18 @@ class AdamWRule(C.Structure):
                 + [("bits", C.c_int32), ("seed", C.c_uint32)])
 
 
+class BeamArgs(C.Structure):
+    """mlt_beam_args"""
+    _fields_ = ([(k, C.c_int32) for k in ("dtype", "batch", "beams", "n", "m", "normalised")]
+                + [("eos", C.c_int64), ("scores", C.c_void_p), ("batch_stride", C.c_int64), ("beam_stride", C.c_int64)]
+                + [(k, C.c_void_p) for k in ("logp", "done", "out_parent", "out_token", "out_logp", "out_done")])
+
+
+class BeamState(C.Structure):
+    """mlt_beam_state"""
+    _fields_ = [("data", C.c_void_p), ("row_bytes", C.c_int64), ("row_stride", C.c_int64)]
+
+
 HEADER = os.path.join(_build.ROOT, "include", "mlt.h")
 
 
@@ -153,6 +165,9 @@ def lib(build_if_missing: bool = True):
             "mlt_layer_norm_grad_workspace": [i64, i32, P],
             "mlt_adamw": [P, P, i32, P, P, P, P, P],
             "mlt_adamw_blocks": [P, i32, P],
+            "mlt_beam_step": [P, P, P, C.c_size_t],
+            "mlt_beam_step_workspace": [P, P],
+            "mlt_beam_reorder": [P, P, i32, i32, P, i32],
             "mlt_sa_step": [P, P, P, i32, P, P, P, P, P, P, i64, f32, f32, P, P, P],
         }
         for name, args in sig.items():
@@ -973,6 +988,80 @@ def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), e
     rule = AdamWRule(betas[0], betas[1], eps, 0 if scalars[0] is not None else int(step), *scalars, bits, seed & 0xFFFFFFFF)
     rc = L.mlt_adamw(_stream_of(m), table.buffer_info()[0], count, C.byref(rule), m.data_ptr(), v.data_ptr(),
                      None if ms is None else ms.data_ptr(), None if vs is None else vs.data_ptr())
+    if rc:
+        _check(rc)
+
+
+def beam_step(scores, logp, m: int, done=None, eos: int = -1, normalised: bool = False, stream=None):
+    """mlt_beam_step: the m best continuations of every item's beams.  `scores` [batch][beams][n]
+    (or [beams][n] for one item), `logp` fp32 [batch][beams], `done` bool or uint8 of the same
+    shape.  Returns (parent, token, logp, done): int64, int64, fp32 and bool
+    [batch][m]; -1, -1, -infinity and False past the last continuation."""
+    L = _setup()
+    if stream is not None:
+        return _on(stream, beam_step, scores, logp, m, done, eos, normalised)
+    torch = _torch
+    _cuda(scores, "scores")
+    code = _dtype_code(scores)
+    one = scores.dim() == 2
+    if one:
+        scores, logp = scores[None], logp[None]
+        done = None if done is None else done[None]
+    _need(scores.dim() == 3, "scores must be [batch][beams][n]")
+    batch, beams, n = scores.shape
+    m, eos = int(m), int(eos)
+    _need(max(batch, beams, n, m) <= _INT_MAX, "batch, beams, n or m too large")
+    strides = scores.stride()
+    if strides[2] != 1 and n > 1 and scores.numel() > 0:
+        raise ValueError("the scores of a beam must be adjacent")
+    lp = _plain(logp, "logp", torch.float32, (batch, beams))
+    d = None if done is None else _plain(done, "done", torch.uint8 if done.dtype == torch.uint8 else torch.bool, (batch, beams))
+    device = scores.device
+    parent, token = torch.empty((2, batch, m), dtype=torch.int64, device=device)
+    out = torch.empty(batch, m, dtype=torch.float32, device=device)
+    ended = torch.empty(batch, m, dtype=torch.bool, device=device)
+    _one_device(scores, logp, done)
+    a = BeamArgs(code, batch, beams, n, m, 1 if normalised else 0, eos, scores.data_ptr(), strides[0], strides[1], lp, d,
+                 parent.data_ptr(), token.data_ptr(), out.data_ptr(), ended.data_ptr())
+    ws, n_ws = _workspace(("beam", code, batch, beams, n, m), lambda q: L.mlt_beam_step_workspace(C.byref(a), C.byref(q)),
+                          device)
+    rc = L.mlt_beam_step(_stream_of(scores), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
+    if rc:
+        _check(rc)
+    return (parent[0], token[0], out[0], ended[0]) if one else (parent, token, out, ended)
+
+
+def beam_reorder(parent, *tensors, stream=None) -> None:
+    """mlt_beam_reorder: puts the rows of beams' states into the order that `parent` (int64
+    [batch][beams], or [beams] for one item) gives, in place: row w of an item becomes what row
+    parent[w] was; a negative parent leaves the row.  `tensors`: of any type,
+    [batch * beams][...] or [batch][beams][...], the elements of a row adjacent."""
+    L = _setup()
+    if stream is not None:
+        return _on(stream, beam_reorder, parent, *tensors)
+    _cuda(parent, "parent", _torch.int64)
+    _need(parent.dim() in (1, 2) and parent.is_contiguous(), "parent must be a contiguous int64 tensor [batch][beams]")
+    batch, beams = (1, *parent.shape) if parent.dim() == 1 else parent.shape
+    rows = batch * beams
+    _need(batch <= _INT_MAX and beams <= _INT_MAX, "batch must lie in [0, 65535], beams in [1, 1024]")
+    moves = (BeamState * len(tensors))()
+    for k, t in enumerate(tensors):
+        _cuda(t, "states")
+        shape = t.shape
+        _need(len(shape) > 0 and (shape[0] == rows or tuple(shape[:2]) == (batch, beams)),
+              "states must be [batch * beams][...] or [batch][beams][...]")
+        if t.numel() == 0:
+            continue
+        try:
+            flat = t.view(rows, -1)
+        except RuntimeError:
+            raise ValueError("the elements of a state's row must be adjacent, its rows at one distance") from None
+        stride, column = flat.stride()
+        _need(column == 1 or flat.shape[1] == 1, "the elements of a state's row must be adjacent")
+        size = t.element_size()
+        moves[k] = BeamState(t.data_ptr(), flat.shape[1] * size, stride * size)
+    _one_device(parent, *tensors)
+    rc = L.mlt_beam_reorder(_stream_of(parent), parent.data_ptr(), batch, beams, moves, len(tensors))
     if rc:
         _check(rc)
 
