@@ -10,9 +10,13 @@ together as a user would:
     draw from its scores, not only the best mlt.sample (rejected ones score -inf)
     train the proposer on the draws         mlt.embed, mlt.scan and their gradients
     propose, digit by digit                 mlt.embed, mlt.scan in place, mlt.sample
+    or the most probable ones at once       mlt.beam_step, mlt.beam_reorder
     anneal from the proposals               mlt.sa_step
 
-    python -m paper_2411_10764_gb300.proposer
+With `norm` the block ends in a layer norm (mlt.layer_norm and its gradient), with
+optimizer "adamw" it is trained by mlt.adamw.
+
+    python -m paper_2411_10764_gb300.proposer [--norm] [--adamw] [--beams N]
 
 Matrix products are torch's.  B, C and the step sizes are projected from the
 embedded tokens, so that the short convolution stays inside mlt.scan.
@@ -29,12 +33,13 @@ TAPS = 4
 
 
 class Proposer:
-    """Embedding -> selective scan with gate -> residual -> scores of digits, in fp32.
+    """Embedding -> selective scan with gate -> residual (-> layer norm) -> scores of digits, in fp32.
 
     radices: options of each knob (knob 0 least significant).  Token of digit d of knob
     j: offset_j + d; the last token starts a sequence."""
 
-    def __init__(self, radices, dim: int = 64, inner: int = 128, states: int = 16, seed: int = 0, device="cuda"):
+    def __init__(self, radices, dim: int = 64, inner: int = 128, states: int = 16, seed: int = 0, device="cuda",
+                 norm: bool = False):
         import torch
 
         self.radices = [int(r) for r in radices]
@@ -56,6 +61,8 @@ class Proposer:
             w_out=r(inner, dim) / math.sqrt(inner),
             head=r(dim, self.vocab - 1) / math.sqrt(dim),
         )
+        if norm:
+            p.update(norm_w=torch.ones(dim), norm_b=torch.zeros(dim))
         self.params = {k: v.to(device).contiguous() for k, v in p.items()}
 
     # -- candidates and tokens ------------------------------------------------
@@ -84,8 +91,11 @@ class Proposer:
                     conv_state=conv_state)
         outs = dict(state_out=state, conv_state_out=conv_state) if in_place else {}
         y, state, conv_state = mlt.scan(x, dt, B, C, P["A"], **args, **outs)
-        o = e + y @ P["w_out"]
-        return o @ P["head"], state, conv_state, (tokens, e, x, dt, B, C, args, y, o)
+        if "norm_w" not in P:
+            o = e + y @ P["w_out"]
+            return o @ P["head"], state, conv_state, (tokens, e, x, dt, B, C, args, y, o, None)
+        o, total, stats = mlt.layer_norm(y @ P["w_out"], P["norm_w"], P["norm_b"], residual=e)
+        return o @ P["head"], state, conv_state, (tokens, e, x, dt, B, C, args, y, o, (total, stats))
 
     def loss_and_grads(self, index, weight=None):
         """Mean negative log-likelihood of candidates' digits (weighted) and its gradients."""
@@ -93,7 +103,7 @@ class Proposer:
 
         P = self.params
         tokens = self.tokens_of(index)
-        scores, _, _, (_, e, x, dt, B, C, args, y, o) = self.forward(tokens[:, :-1].contiguous())
+        scores, _, _, (_, e, x, dt, B, C, args, y, o, normed) = self.forward(tokens[:, :-1].contiguous())
         # a position's digits are those of its knob
         at = torch.arange(self.vocab - 1, device=index.device)
         lo = torch.tensor(self.offsets[:-1], device=index.device)[:, None]
@@ -106,7 +116,12 @@ class Proposer:
         gs = (logp.exp() - want) * w
         flat = lambda t: t.reshape(-1, t.shape[-1])  # noqa: E731
         go = gs @ P["head"].t()
-        grads = {"head": flat(o).t() @ flat(gs), "w_out": flat(y).t() @ flat(go)}
+        grads = {"head": flat(o).t() @ flat(gs)}
+        if normed is not None:
+            total, stats = normed
+            g = mlt.layer_norm_grad(go, total, stats, P["norm_w"], P["norm_b"])
+            go, grads["norm_w"], grads["norm_b"] = g["x"], g["weight"], g["bias"]
+        grads["w_out"] = flat(y).t() @ flat(go)
         s = mlt.scan_grad(go @ P["w_out"].t(), x, dt, B, C, P["A"], **args)
         for k in ("A", "skip", "dt_bias", "conv_w", "conv_b"):
             grads[k] = s[k]
@@ -116,9 +131,25 @@ class Proposer:
         grads["table"] = mlt.embed_grad(tokens[:, :-1].contiguous(), ge, self.vocab, scale=math.sqrt(self.dim))
         return loss, grads
 
-    def train(self, index, weight=None, steps: int = 20, lr: float = 0.005):
-        """Gradient steps scaled by each parameter's own root mean square; returns the losses."""
+    def train(self, index, weight=None, steps: int = 20, lr: float = 0.005, optimizer: str = "rms",
+              weight_decay: float = 0.01, bits: int = 32):
+        """Gradient steps scaled by each parameter's own root mean square, or AdamW's with moments
+        in `bits` bits; returns the losses."""
         losses = []
+        if optimizer == "adamw":
+            names = list(self.params)
+            tensors = [self.params[k] for k in names]
+            state = mlt.adamw_state(tensors, bits)
+            rates = [lr * (0.1 if k in ("A", "dt_bias") else 1.0) for k in names]
+            decay = [weight_decay if k in ("table", "w_in", "w_out", "head") else 0.0 for k in names]
+            for t in range(steps):
+                loss, grads = self.loss_and_grads(index, weight)
+                losses.append(loss)
+                mlt.adamw(tensors, [grads[k] for k in names], state, t + 1, lr=rates, weight_decay=decay, seed=t)
+                self.params["A"].clamp_(max=-1e-3)
+            return [float(v) for v in losses]
+        if optimizer != "rms":
+            raise ValueError(f'optimizer must be "rms" or "adamw", got {optimizer!r}')
         mean = {k: v.new_zeros(v.shape) for k, v in self.params.items()}
         for t in range(steps):
             loss, grads = self.loss_and_grads(index, weight)
@@ -154,11 +185,37 @@ class Proposer:
         return index, logp
 
 
+    def search(self, m: int, beams: int | None = None):
+        """The m most probable candidates that a beam of `beams` (default: m) finds, best first:
+        (indices int64 [m], -1 where there are fewer; log-probabilities [m])."""
+        import torch
+
+        P = self.params
+        device = P["table"].device
+        w = max(m, beams or m)
+        state = torch.zeros((w, self.inner, self.states), device=device)
+        conv = torch.zeros((w, TAPS - 1, self.inner), device=device)
+        token = torch.full((w, 1), self.vocab - 1, dtype=torch.int64, device=device)
+        index = torch.zeros(w, dtype=torch.int64, device=device)
+        logp, place = torch.full((w,), -math.inf, device=device), 1
+        logp[0] = 0.0
+        for j, r in enumerate(self.radices):
+            scores, _, _, _ = self.forward(token, state, conv, in_place=True)
+            parent, digit, logp, _ = mlt.beam_step(scores[:, 0, self.offsets[j]:self.offsets[j + 1]], logp, w)
+            mlt.beam_reorder(parent, state, conv, index)
+            digit = digit.clamp(min=0)  # beams without a continuation stay out by their logp
+            index += digit * place
+            place *= r
+            token = digit[:, None] + self.offsets[j]
+        return index.masked_fill(logp == -math.inf, -1)[:m], logp[:m]
+
+
 def explore(decoder, thr: float, first: int, n: int, keep: int = 256, chains: int = 1024, temperature: float = 0.05,
-            seed: int = 0, steps: int = 20):
+            seed: int = 0, steps: int = 20, beams: int = 0, norm: bool = False, optimizer: str = "rms"):
     """One round over a knob space whose V and P models are loaded: screen candidates first ..
     first + n - 1, draw `keep` of the valid ones by their scores, train a proposer on them, and
-    anneal one step from its proposals.  Returns a dict of tensors and the losses."""
+    anneal one step from its proposals, the first up to `beams` of them its most probable
+    candidates, the others drawn.  Returns a dict of tensors and the losses."""
     import torch
 
     r, ov, prog = decoder.radices, decoder.option_values, decoder.program
@@ -168,9 +225,12 @@ def explore(decoder, thr: float, first: int, n: int, keep: int = 256, chains: in
     noise = -torch.empty(n, device="cuda").exponential_(generator=g).log()
     drawn, logp = mlt.sample(perf, noise, temperature=temperature, m=keep)
     drawn = drawn[drawn >= 0]
-    model = Proposer(r, seed=seed)
-    losses = model.train(drawn + first, steps=steps) if drawn.numel() else []
+    model = Proposer(r, seed=seed, norm=norm)
+    losses = model.train(drawn + first, steps=steps, optimizer=optimizer) if drawn.numel() else []
     parent, _ = model.propose(chains, g, temperature=0.8, top_p=0.95)
+    if beams:
+        best, _ = model.search(min(beams, chains))
+        parent[:best.numel()] = torch.where(best >= 0, best, parent[:best.numel()])
     draw = lambda: torch.randint(0, 1 << 30, (chains,), dtype=torch.int32, device="cuda", generator=g)  # noqa: E731
     log_u = torch.rand(chains, device="cuda", generator=g).log()
     nxt, score, accepted = mlt.sa_step(r, ov, prog, parent, torch.full((chains,), -1e30, device="cuda"), draw(), draw(),
@@ -180,12 +240,20 @@ def explore(decoder, thr: float, first: int, n: int, keep: int = 256, chains: in
                 losses=losses, perf=perf)
 
 
-def main() -> None:
+def main(argv=()) -> None:
+    import argparse
+
     from . import workloads as W
 
+    p = argparse.ArgumentParser(prog="python -m paper_2411_10764_gb300.proposer", description=__doc__.splitlines()[0])
+    p.add_argument("--norm", action="store_true", help="end the block in a layer norm")
+    p.add_argument("--adamw", action="store_true", help="train with AdamW")
+    p.add_argument("--beams", type=int, default=0, help="anneal from so many most probable candidates too")
+    args = p.parse_args(argv)
     w = W.make_workload(4, seed=1, n=65536)
     mlt.load_workload_models(w)
-    out = explore(w.decoder, w.thr, 0, 65536)
+    out = explore(w.decoder, w.thr, 0, 65536, beams=args.beams, norm=args.norm,
+                  optimizer="adamw" if args.adamw else "rms")
     ok, losses, screened = out["accepted"].bool(), out["losses"], float(out["perf"].max())
     print(f"screened 65536, drew {out['drawn'].numel()}"
           + (f", loss {losses[0]:.3f} -> {losses[-1]:.3f}" if losses else "")
@@ -195,4 +263,6 @@ def main() -> None:
 
 
 if __name__ == "__main__":
-    main()
+    import sys
+
+    main(sys.argv[1:])
