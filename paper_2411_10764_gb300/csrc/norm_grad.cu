@@ -4,8 +4,8 @@
 // input's gradient.  Each thread keeps its columns' sums of gy h and gy in registers over
 // all rows of its team; the teams' sums go to the workspace and a second
 // kernel adds them up in a fixed order.  Bound: memory (x and gy read, gx written, once).
-// Where a thread adds more than kPlainRows rows its sums are compensated (Kahan 1965): of n
-// equal terms in a plain sum the error grows with n.
+// Of n equal terms in a plain sum the error grows with n: where a thread has more than kPlainRows rows, its
+// sums move to pairs of numbers in shared memory every kFlushRows of them (Knuth's exact addition).
 #include <utility>
 
 #include "norm.cuh"
@@ -13,168 +13,209 @@
 namespace mlt {
 namespace {
 
-constexpr int kEach = 8;  // values of a row a thread (16: 300 to 1,400 bytes of spills)
-constexpr int kPlainRows = 64;
+constexpr int kPlainRows = 48;
+constexpr int kFlushRows = 16;
+constexpr int kMostThreads = 512;
+constexpr int kGroupThreads = 256;
 constexpr int kLongRows = 256;  // rows a partial sum of the columns of long rows
 
-enum { kNoSums, kPlainSums, kCompensated };
-
-template <int MODE>
-__device__ __forceinline__ void add_to(float& s, float& c, float v) {
-  if (MODE == kCompensated) {
-    const float y = __fsub_rn(v, c), t = __fadd_rn(s, y);
-    c = __fsub_rn(__fsub_rn(t, s), y);
-    s = t;
-  } else if (MODE == kPlainSums) {
-    s += v;
-  }
+// (s, c) + v, s + c being the sum
+__device__ __forceinline__ void add_exactly(float& s, float& c, float v) {
+  const float t = __fadd_rn(s, v), b = __fsub_rn(t, s);
+  c = __fadd_rn(c, __fadd_rn(__fsub_rn(s, __fsub_rn(t, b)), __fsub_rn(v, b)));
+  s = t;
 }
 
-// As k_norm in norm.cu.  partial: [teams][2][dim].
-template <typename TI, typename TO, int V, bool MULTI, int MODE>
-__global__ void __launch_bounds__(MULTI ? 512 : 256)
+constexpr int registers(bool cta, bool edge) { return cta ? 128 : 128; }
+
+// As k_norm in norm.cu.  SUMS: weight and bias have gradients; partial: [teams][2][dim]; flush: rows between
+// moves to shared memory, or 0.
+template <typename TI, typename TO, int V, int C, bool CTA, bool EDGE, bool SUMS>
+__global__ void __maxnreg__(registers(CTA, EDGE))
     k_norm_grad(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g, float* partial,
-                int lanes, int seg) {
-  constexpr int C = kEach / V;
+                int lanes, int seg, int skew0, int skew_step, int flush) {
+  extern __shared__ __align__(16) float mem[];
   __shared__ RowSums<2> sums;
-  __shared__ float by_warp[MULTI ? 1 : 8][2][MULTI ? 1 : kNormGroupDim];
+  constexpr int E = C * V;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
-  const int ranks = MULTI ? cluster_ranks() : 1, rank = MULTI ? cluster_rank() : 0;
-  if (MULTI && ranks > 1) cluster_barrier();
-  const int j = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1);
-  const int first = rank * seg, cols = min(seg, a.dim - first);
-  const long long at = first + static_cast<long long>(j) * V;
-  const int hop = lanes * V;
-  bool on[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) on[c] = j * V + c * hop < cols;
-  float w[C][V], sw[C][V], cw[C][V], sb[C][V], cb[C][V];
+  const int ranks = CTA ? cluster_ranks() : 1, rank = CTA ? cluster_rank() : 0;
+  const int j = CTA ? threadIdx.x : threadIdx.x & (lanes - 1);
+  const int in_warp = CTA ? 1 : 32 / lanes;
+  const long long step = CTA ? gridDim.x / ranks : static_cast<long long>(gridDim.x) * 8 * in_warp;
+  const int sub = CTA ? 0 : (threadIdx.x & 31) / lanes;
+  const long long base0 = CTA ? blockIdx.x / ranks : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
+  const int skew = EDGE ? static_cast<int>((skew0 + (base0 + sub) % V * skew_step) % V) : 0;
+  const Columns<V, C, EDGE> cols(rank * seg + j * V, lanes * V, (rank + 1) * seg, skew, a.dim);
+  const bool scaled = a.weight != nullptr;
+  const Kept<V, C> ws{mem};
+  float* moved = CTA && scaled ? mem + blockDim.x * E : mem;  // [2 sums][2][E][threads]
+  float w[C][V], sw[C][V], sb[C][V];
+  const bool more = g.g_total != nullptr;
+  const TI *x0 = static_cast<const TI*>(a.x), *t0 = static_cast<const TI*>(g.g_total);
+  const TO* g0 = static_cast<const TO*>(g.gy);
+  const TI *x1 = x0 + (a.rows - 1) * a.x_stride + a.dim, *t1 = t0 + (a.rows - 1) * g.g_total_stride + a.dim;
+  const TO* g1 = g0 + (a.rows - 1) * g.gy_stride + a.dim;
+  Vec<TI, V> px[C], pt[C];
+  Vec<TO, V> pg[C];
+  float2 next = make_float2(0.0f, 0.0f);
+  auto fetch = [&](long long row) {
+    if (row >= a.rows) return;
+    cols.load(px, x0 + row * a.x_stride, x0, x1);
+    cols.load(pg, g0 + row * g.gy_stride, g0, g1);
+    next = *reinterpret_cast<const float2*>(a.stats + 2 * row);
+  };
+  fetch(base0 + sub);
+  if (!CTA || scaled) {
+    load_columns(w, cols, a.weight, a.w_dtype, 1.0f);
+    if (CTA) ws.put(w);
+  }
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      w[c][v] = a.weight != nullptr && on[c] ? load_as_f32(a.weight, a.w_dtype, at + c * hop + v) : 1.0f;
-      sw[c][v] = cw[c][v] = sb[c][v] = cb[c][v] = 0.0f;
-    }
-  const int in_warp = MULTI ? 1 : 32 / lanes;
-  const long long step = MULTI ? gridDim.x / ranks : static_cast<long long>(gridDim.x) * 8 * in_warp;
-  long long base = MULTI ? blockIdx.x / ranks : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
-  const int sub = MULTI ? 0 : (threadIdx.x & 31) / lanes;
-  const bool more = g.g_total != nullptr;
-  Pack<TI, V> px[C], pt[C];
-  Pack<TO, V> pg[C];
-  float next_mean = 0.0f, next_rstd = 0.0f;
-  auto fetch = [&](long long row) {
-    const TI* x = static_cast<const TI*>(a.x) + row * a.x_stride + at;
-    const TO* gy = static_cast<const TO*>(g.gy) + row * g.gy_stride + at;
-    if (row >= a.rows) return;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (on[c]) {
-        px[c] = *reinterpret_cast<const Pack<TI, V>*>(x + c * hop);
-        pg[c] = *reinterpret_cast<const Pack<TO, V>*>(gy + c * hop);
-      }
-    const float2 s = *reinterpret_cast<const float2*>(a.stats + 2 * row);
-    next_mean = s.x;
-    next_rstd = s.y;
-  };
-  fetch(base + sub);
-  for (; base < a.rows; base += step) {
-    const long long row = base + sub;
-    const bool live = row < a.rows;
-    const float mean = next_mean, rstd = next_rstd;
-    if (more && live) {
-      const TI* gt = static_cast<const TI*>(g.g_total) + row * g.g_total_stride + at;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (on[c]) pt[c] = *reinterpret_cast<const Pack<TI, V>*>(gt + c * hop);
-    }
-    float h[C][V], gy[C][V], total[2] = {0.0f, 0.0f};
+    for (int v = 0; v < V; ++v) sw[c][v] = sb[c][v] = 0.0f;
+  if (SUMS && flush > 0)
+    for (int i = threadIdx.x; i < 4 * E * static_cast<int>(blockDim.x); i += blockDim.x) moved[i] = 0.0f;
+  if (CTA) sums.clear();
+  __syncthreads();
+  if (CTA && ranks > 1) cluster_barrier();
+  auto move = [&]() {
+    if (!SUMS) return;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        h[c][v] = gy[c][v] = 0.0f;
-        if (on[c] && live) {
-          h[c][v] = (to_f32(px[c].v[v]) - mean) * rstd;
-          gy[c][v] = to_f32(pg[c].v[v]);
-        }
-        add_to<MODE>(sw[c][v], cw[c][v], gy[c][v] * h[c][v]);
-        add_to<MODE>(sb[c][v], cb[c][v], gy[c][v]);
-        gy[c][v] *= w[c][v];
-        total[0] += gy[c][v];
-        total[1] = fmaf(gy[c][v], h[c][v], total[1]);
+        float* at = moved + (c * V + v) * blockDim.x + threadIdx.x;
+        const int hop = E * blockDim.x;
+        add_exactly(at[0], at[hop], sw[c][v]);
+        add_exactly(at[2 * hop], at[3 * hop], sb[c][v]);
+        sw[c][v] = sb[c][v] = 0.0f;
       }
+  };
+  int since = 0;
+  for (long long base = base0; base < a.rows; base += step) {
+    const long long row = base + sub;
+    const bool live = row < a.rows;
+    const float mean = next.x, rstd = next.y;
+    if (more && live) cols.load(pt, t0 + row * g.g_total_stride, t0, t1);
+    float h[C][V], gw[C][V], total[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (CTA && scaled) ws.get(w[c], c);
+      float s0 = 0.0f, s1 = 0.0f;
+      cols.each(
+          c,
+          [&](int c, int v) {
+            h[c][v] = live ? (px[c].get(v) - mean) * rstd : 0.0f;
+            const float gy = live ? pg[c].get(v) : 0.0f;
+            if (SUMS) {
+              sw[c][v] = fmaf(gy, h[c][v], sw[c][v]);
+              sb[c][v] += gy;
+            }
+            gw[c][v] = !CTA || scaled ? gy * w[c][v] : gy;
+            s0 += gw[c][v];
+            s1 = fmaf(gw[c][v], h[c][v], s1);
+          },
+          [&](int c, int v) { h[c][v] = gw[c][v] = 0.0f; });
+      total[0] += s0;
+      total[1] += s1;
+    }
     if (base + step < a.rows) fetch(row + step);
-    if (MULTI)
+    if (CTA)
       row_sums(total, sums, slot, ranks, rank);
     else
       group_sums(total, lanes);
+    if (flush > 0 && ++since == flush) {
+      move();
+      since = 0;
+    }
     if (g.gx == nullptr || !live) continue;
     const float m0 = total[0] / a.dim, m1 = total[1] / a.dim;
-    TI* to = static_cast<TI*>(g.gx) + row * g.gx_stride + at;
+    TI* to = static_cast<TI*>(g.gx) + row * g.gx_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (!on[c]) continue;
-      Pack<TI, V> q;
+      float f[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float d = fmaf(-h[c][v], m1, gy[c][v] - m0) * rstd;
-        if (more) d += to_f32(pt[c].v[v]);
-        q.v[v] = from_f32<TI>(d);
+        const float d = fmaf(-h[c][v], m1, gw[c][v] - m0) * rstd;
+        f[v] = more ? d + pt[c].get(v) : d;
       }
-      *reinterpret_cast<Pack<TI, V>*>(to + c * hop) = q;
+      Vec<TI, V> q;
+      q.put(f);
+      cols.store(q, to, c);
     }
   }
-  if (MODE == kNoSums) return;
-  if (MULTI) {
+  if (!SUMS) return;
+  if (flush > 0) {
+    move();
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float* at = moved + (c * V + v) * blockDim.x + threadIdx.x;
+        const int hop = E * blockDim.x;
+        sw[c][v] = at[0] + at[hop];
+        sb[c][v] = at[2 * hop] + at[3 * hop];
+      }
+  }
+  if (CTA) {
     float* out = partial + static_cast<long long>(blockIdx.x / ranks) * 2 * a.dim;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (on[c]) {
-          out[at + c * hop + v] = sw[c][v] - cw[c][v];
-          out[a.dim + at + c * hop + v] = sb[c][v] - cb[c][v];
+        if (cols.on(c, v)) {
+          const int col = cols.first + c * cols.hop + v;
+          out[col] = sw[c][v];
+          out[a.dim + col] = sb[c][v];
         }
     return;
   }
-  // the rows of a warp, then the warps of the CTA
+  // the CTA's groups: their sums by place, then some threads a column, each over every so many groups in turn
+  const int places = lanes * E, groups = kGroupThreads / lanes, group = threadIdx.x / lanes;
+  int wide = 1;
+  while (wide < a.dim) wide *= 2;
+  const int teams = wide < kGroupThreads ? kGroupThreads / wide : 1;
+  for (int k = 0; k < 2; ++k) {
+    __syncthreads();
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float s = sw[c][v] - cw[c][v], b = sb[c][v] - cb[c][v];
-      for (int o = lanes; o < 32; o *= 2) {
-        s += __shfl_xor_sync(0xffffffffu, s, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
+      for (int v = 0; v < V; ++v) mem[group * places + c * cols.hop + j * V + v] = k == 0 ? sw[c][v] : sb[c][v];
+    __syncthreads();
+    float s = 0.0f, rest = 0.0f;
+    for (int col = threadIdx.x % wide; col < a.dim; col += kGroupThreads) {
+      s = rest = 0.0f;
+      for (int q = threadIdx.x / wide; q < groups; q += teams) {
+        int at = col;
+        if (EDGE) at += static_cast<int>((skew0 + (blockIdx.x * static_cast<long long>(groups) + q) % V * skew_step) % V);
+        add_exactly(s, rest, mem[q * places + at]);
       }
-      if (sub == 0 && on[c]) {
-        by_warp[threadIdx.x >> 5][0][j * V + c * hop + v] = s;
-        by_warp[threadIdx.x >> 5][1][j * V + c * hop + v] = b;
+      if (teams == 1) partial[(blockIdx.x * 2LL + k) * a.dim + col] = s + rest;
+    }
+    if (teams > 1) {
+      __syncthreads();
+      mem[threadIdx.x] = s + rest;
+      for (int half = teams / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (static_cast<int>(threadIdx.x) < half * wide) mem[threadIdx.x] += mem[threadIdx.x + half * wide];
       }
+      if (static_cast<int>(threadIdx.x) < a.dim) partial[(blockIdx.x * 2LL + k) * a.dim + threadIdx.x] = mem[threadIdx.x];
     }
-  __syncthreads();
-  if (threadIdx.x < a.dim)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float s = 0.0f;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) s += by_warp[q][k][threadIdx.x];
-      partial[(blockIdx.x * 2LL + k) * a.dim + threadIdx.x] = s;
-    }
+  }
 }
 
 // Rows that no cluster holds: the input's gradient, a CTA a row.
 template <typename TI, typename TO>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(kMostThreads)
     k_norm_grad_long(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g) {
   __shared__ RowSums<2> sums;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
+  sums.clear();
+  __syncthreads();
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const TI* x = static_cast<const TI*>(a.x) + row * a.x_stride;
     const TO* gy = static_cast<const TO*>(g.gy) + row * g.gy_stride;
@@ -184,14 +225,14 @@ __global__ void __launch_bounds__(1024)
       return a.weight != nullptr ? v * load_as_f32(a.weight, a.w_dtype, i) : v;
     };
     float total[2] = {0.0f, 0.0f};
-    for (int i = threadIdx.x; i < a.dim; i += 1024) {
+    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
       const float v = weighted(i);
       total[0] += v;
       total[1] = fmaf(v, (to_f32(x[i]) - mean) * rstd, total[1]);
     }
     row_sums(total, sums, slot, 1, 0);
     const float m0 = total[0] / a.dim, m1 = total[1] / a.dim;
-    for (int i = threadIdx.x; i < a.dim; i += 1024) {
+    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
       const float h = (to_f32(x[i]) - mean) * rstd;
       float d = fmaf(-h, m1, weighted(i) - m0) * rstd;
       if (g.g_total != nullptr) d += to_f32(static_cast<const TI*>(g.g_total)[row * g.g_total_stride + i]);
@@ -215,12 +256,12 @@ __global__ void __launch_bounds__(256)
   for (long long row = from; row < to; ++row) {
     const float gy = to_f32(static_cast<const TO*>(g.gy)[row * g.gy_stride + col]);
     const float x = to_f32(static_cast<const TI*>(a.x)[row * a.x_stride + col]);
-    add_to<kCompensated>(sw, cw, gy * ((x - a.stats[2 * row]) * a.stats[2 * row + 1]));
-    add_to<kCompensated>(sb, cb, gy);
+    add_exactly(sw, cw, gy * ((x - a.stats[2 * row]) * a.stats[2 * row + 1]));
+    add_exactly(sb, cb, gy);
   }
   float* out = partial + blockIdx.y * 2LL * a.dim;
-  out[col] = sw - cw;
-  out[a.dim + col] = sb - cb;
+  out[col] = sw + cw;
+  out[a.dim + col] = sb + cb;
 }
 
 // The teams' sums of 32 columns: 32 threads a column take every 32nd team, then a tree.
@@ -235,89 +276,114 @@ __global__ void __launch_bounds__(1024)
   float sum = 0.0f, c = 0.0f;
   if (col < dim)
 #pragma unroll 8
-    for (int t = y; t < teams; t += 32) add_to<kCompensated>(sum, c, partial[(t * 2LL + blockIdx.y) * dim + col]);
-  s[y][x] = sum - c;
+    for (int t = y; t < teams; t += 32) add_exactly(sum, c, partial[(t * 2LL + blockIdx.y) * dim + col]);
+  s[y][x] = sum + c;
   __syncthreads();
   float v[1] = {s[x][y]};
-  group_sums(v, 32);
+  warp_sums(v);
   if (x == 0 && blockIdx.x * 32 + y < dim) store_from_f32(to, dtype, blockIdx.x * 32 + y, v[0]);
 }
 
 struct Plan {
-  bool group, far;  // groups of lanes; rows that no cluster holds
-  int lanes, threads, ranks, seg;
+  bool far;  // rows that no cluster holds
+  bool group;
+  int lanes, threads, ranks, seg, flush;
   long long teams;  // of rows, and of partial sums
-  bool compensated;
+  size_t smem;
 };
 
-// 24 warps an SM; the number of teams sets the order of the sums and follows from sizes alone.
-Plan plan_of(long long rows, int dim, int sms) {
+// Values of a row a thread: two packs where rows are read in packs of eight 16-bit values, else eight.
+constexpr int each_of(int pack) { return pack == 8 ? 16 : 8; }
+
+// By sizes and how the rows lie; the number of teams sets the order of the sums.
+Plan plan_of(long long rows, int dim, int pack, bool edges, int period, bool scaled, int sms) {
   Plan p{};
-  if (dim <= kNormGroupDim) {
-    p.group = true;
-    p.lanes = 1;
-    while (p.lanes * kEach < dim) p.lanes *= 2;
-    p.threads = 256;
-    p.ranks = 1;
-    p.seg = dim;
-    const long long need = (rows + 8 * (32 / p.lanes) - 1) / (8 * (32 / p.lanes)), most = 3LL * sms;
-    p.teams = need < most ? need : most;
-    p.compensated = rows > p.teams * 8 * (32 / p.lanes) * kPlainRows;
-    return p;
-  }
-  if (dim > kNormMaxCluster * 512 * kEach) {
+  const int each = each_of(pack), places = (dim + (edges ? pack - 1 : 0) + pack - 1) / pack * pack;
+  long long in_turn = 0;  // rows of a thread
+  if (dim + pack > kNormMaxCluster * kMostThreads * each) {
     p.far = true;
     p.teams = (rows + kLongRows - 1) / kLongRows;
     if (p.teams > 256) p.teams = 256;
     return p;
   }
-  p.ranks = (dim + 512 * kEach - 1) / (512 * kEach);
-  p.seg = ((dim + p.ranks - 1) / p.ranks + kEach - 1) / kEach * kEach;
-  p.ranks = (dim + p.seg - 1) / p.seg;
-  p.threads = p.lanes = ((p.seg + kEach - 1) / kEach + 31) / 32 * 32;
-  if (p.ranks == 1) p.seg = dim;
-  long long most = static_cast<long long>(sms) * (768 / p.threads) / p.ranks;
-  if (most < 1) most = 1;
-  p.teams = rows < most ? rows : most;
-  p.compensated = rows > p.teams * kPlainRows;
+  if (places <= 32 * each) {
+    p.group = true;
+    p.lanes = 1;
+    while (p.lanes * each < places) p.lanes *= 2;
+    p.threads = kGroupThreads;
+    p.ranks = 1;
+    p.seg = places;
+    const long long per = kGroupThreads / p.lanes, need = (rows + per - 1) / per, most = 2LL * sms;
+    p.teams = need < most ? need : most;
+    in_turn = (need + p.teams - 1) / p.teams;
+  } else {
+    p.ranks = (places + kMostThreads * each - 1) / (kMostThreads * each);
+    p.seg = ((places + p.ranks - 1) / p.ranks + pack - 1) / pack * pack;
+    p.ranks = (places + p.seg - 1) / p.seg;
+    p.threads = p.lanes = ((p.seg + each - 1) / each + 31) / 32 * 32;
+    int per_sm = 512 / p.threads;  // by registers
+    if (per_sm > 16) per_sm = 16;
+    long long most = static_cast<long long>(sms) * per_sm / p.ranks;
+    most = most < period ? period : most / period * period;
+    p.teams = rows < most ? rows : most;
+    in_turn = (rows + p.teams - 1) / p.teams;
+  }
+  p.flush = in_turn > kPlainRows ? kFlushRows : 0;
+  const size_t own = sizeof(float) * p.threads * each;
+  p.smem = (p.group || !scaled ? 0 : own) + (p.flush > 0 ? 4 * own : 0);
+  if (p.group && p.smem < own) p.smem = own;
   return p;
 }
 
-template <typename TI, typename TO, int V, bool MULTI>
-cudaError_t launch_rows(const mlt_norm_args& a, const mlt_norm_grads& g, const Plan& p, float* partial, bool sums,
-                        cudaStream_t st) {
+template <typename TI, typename TO, int V, bool EDGE>
+cudaError_t launch_as(const mlt_norm_args& a, const mlt_norm_grads& g, const Plan& p, const Skew& skew, float* partial,
+                      bool sums, cudaStream_t st) {
+  constexpr int C = each_of(V) / V;
   const unsigned grid = static_cast<unsigned>(p.teams * p.ranks);
   auto go = [&](auto kernel) {
-    return launch_cluster(kernel, grid, p.threads, p.ranks, st, a, g, partial, p.lanes, p.seg);
+    return launch_cluster(kernel, grid, p.threads, p.ranks, p.smem, st, a, g, partial, p.lanes, p.seg, skew.first,
+                          skew.step, p.flush);
   };
-  if (!sums) return go(k_norm_grad<TI, TO, V, MULTI, kNoSums>);
-  return p.compensated ? go(k_norm_grad<TI, TO, V, MULTI, kCompensated>)
-                       : go(k_norm_grad<TI, TO, V, MULTI, kPlainSums>);
-}
-
-template <typename TI, typename TO, int V>
-cudaError_t launch_as(const mlt_norm_args& a, const mlt_norm_grads& g, const Plan& p, float* partial, bool sums,
-                      cudaStream_t st) {
-  return p.group ? launch_rows<TI, TO, V, false>(a, g, p, partial, sums, st)
-                 : launch_rows<TI, TO, V, true>(a, g, p, partial, sums, st);
+  if (p.group)
+    return sums ? go(k_norm_grad<TI, TO, V, C, false, EDGE, true>) : go(k_norm_grad<TI, TO, V, C, false, EDGE, false>);
+  return sums ? go(k_norm_grad<TI, TO, V, C, true, EDGE, true>) : go(k_norm_grad<TI, TO, V, C, true, EDGE, false>);
 }
 
 }  // namespace
 
 size_t norm_grad_workspace(long long rows, int dim, int sms) {
-  return rows == 0 ? 0 : up256(static_cast<size_t>(plan_of(rows, dim, sms).teams) * 2 * dim * sizeof(float));
+  if (rows == 0) return 0;
+  // whichever way the rows will lie
+  long long most = 0;
+  for (int pack : {1, 4, 8})
+    for (int edges = 0; edges < 2; ++edges)
+      for (int period = 1; period <= pack; period *= 2) {
+        const long long teams = plan_of(rows, dim, pack, edges != 0, period, true, sms).teams;
+        if (teams > most) most = teams;
+      }
+  return up256(static_cast<size_t>(most) * 2 * dim * sizeof(float));
 }
 
 cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, void* ws, int sms, long long* launches,
                              cudaStream_t st) {
-  const Plan p = a.rows > 0 ? plan_of(a.rows, a.dim, sms) : Plan{};
   float* partial = static_cast<float*>(ws);
   const bool sums = g.gweight != nullptr || g.gbias != nullptr;
   cudaError_t e = cudaSuccess;
+  long long teams = 0;
   if (a.rows > 0)
     e = with_norm_types(a.dtype, a.y_dtype, [&](auto ti, auto to) -> cudaError_t {
       using TI = decltype(ti);
       using TO = decltype(to);
+      constexpr int V = 16 / sizeof(TI);
+      Skew skew;
+      skew.add(a.x, a.x_stride, sizeof(TI), V);
+      skew.add(g.gy, g.gy_stride, sizeof(TO), V);
+      skew.add(g.g_total, g.g_total_stride, sizeof(TI), V);
+      skew.add(g.gx, g.gx_stride, sizeof(TI), V);
+      const bool edges = skew.same && skew.edges(a.dim, V);
+      const Plan p = plan_of(a.rows, a.dim, skew.same ? V : 1, edges, skew.same ? skew.period(V) : 1,
+                             a.weight != nullptr, sms);
+      teams = p.teams;
       if (p.far) {
         // the sums first: gx may be written over gy
         if (sums) {
@@ -328,24 +394,20 @@ cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, vo
           if (r != cudaSuccess) return r;
         }
         if (g.gx == nullptr) return cudaSuccess;
-        const long long most = 2LL * sms;
+        const long long most = 4LL * sms;
         ++*launches;
-        return launch_cluster(k_norm_grad_long<TI, TO>, static_cast<unsigned>(a.rows < most ? a.rows : most), 1024, 1,
-                              st, a, g);
+        return launch_cluster(k_norm_grad_long<TI, TO>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMostThreads,
+                              1, 0, st, a, g);
       }
-      constexpr int V = 16 / sizeof(TI);
-      auto fits = [&](const void* q, int64_t stride, size_t bytes) {
-        return q == nullptr || (aligned_to(q, bytes * V) && stride % V == 0);
-      };
-      const bool wide = a.dim % V == 0 && fits(a.x, a.x_stride, sizeof(TI)) && fits(g.gy, g.gy_stride, sizeof(TO)) &&
-                        fits(g.g_total, g.g_total_stride, sizeof(TI)) && fits(g.gx, g.gx_stride, sizeof(TI));
       ++*launches;
-      return wide ? launch_as<TI, TO, V>(a, g, p, partial, sums, st) : launch_as<TI, TO, 1>(a, g, p, partial, sums, st);
+      if (!skew.same) return launch_as<TI, TO, 1, false>(a, g, p, Skew{true, 0, 0}, partial, sums, st);
+      return edges ? launch_as<TI, TO, V, true>(a, g, p, skew, partial, sums, st)
+                   : launch_as<TI, TO, V, false>(a, g, p, skew, partial, sums, st);
     });
   if (e != cudaSuccess || !sums) return e;
   ++*launches;
   return launch_pdl(k_norm_cols, dim3((a.dim + 31) / 32, 2), dim3(1024), 0, st, static_cast<const float*>(partial),
-                    a.rows > 0 ? static_cast<int>(p.teams) : 0, a.dim, g.gweight, g.gbias, a.w_dtype);
+                    static_cast<int>(teams), a.dim, g.gweight, g.gbias, a.w_dtype);
 }
 
 }  // namespace mlt
