@@ -3,7 +3,7 @@
 //
 // The tensors' addresses travel in the launch's parameters (up to kMost of them, in
 // three sizes of table), so nothing is copied to the device and a captured
-// graph holds them by value.  Each CTA takes a span of kSpan blocks of 256 elements; it finds its
+// graph holds them by value.  Each CTA takes a span of 8 to 32 blocks of 256 elements; it finds its
 // tensor by bisection over the table.  A warp takes a block at a time, each lane 2 x 4
 // elements 128 apart, so every access of a warp is one contiguous run.
 //
@@ -28,7 +28,7 @@ namespace mlt {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kSpan = 16;  // blocks a CTA: two for each of its eight warps
+constexpr int kMostSpan = 32;  // blocks a CTA
 constexpr int kMost = 500;
 
 struct Tensor {
@@ -50,7 +50,7 @@ struct Common {
   const float* grad_scale;
   long long step;
   unsigned seed;
-  int count;
+  int count, span;
   void *m, *v;
   float *m_scale, *v_scale;
 };
@@ -77,31 +77,28 @@ __device__ __forceinline__ unsigned mix(unsigned h) {
   return h ^ (h >> 16);
 }
 
-// Four values of any type as they lie in memory, loaded before any of them is looked at.  Where the
-// addresses allow no packs, or fewer than four are left, as fp32.
+// Four values of any type as they lie in memory, loaded before any of them is looked at.
 struct Four {
   unsigned r[4];
 };
-
-__device__ __forceinline__ Four load4(const void* p, int dtype, long long i, int left, bool wide) {
+__device__ __forceinline__ Four wide4(const char* p) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  return {{w.x, w.y, w.z, w.w}};
+}
+__device__ __forceinline__ Four narrow4(const char* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return {{w.x, w.y, 0u, 0u}};
+}
+// As fp32, where addresses allow no packs or fewer than four are left.
+__device__ __forceinline__ Four some4(const void* p, int dtype, long long i, int left) {
   Four q;
-  if (wide && left == 4) {
-    if (dtype == MLT_F32) {
-      const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
-      q = {{w.x, w.y, w.z, w.w}};
-    } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-      q = {{w.x, w.y, 0u, 0u}};
-    }
-    return q;
-  }
 #pragma unroll
   for (int k = 0; k < 4; ++k) q.r[k] = k < left ? __float_as_uint(load_as_f32(p, dtype, i + k)) : 0u;
   return q;
 }
 
-__device__ __forceinline__ void values4(float (&v)[4], const Four& q, int dtype, int left, bool wide) {
-  if (dtype == MLT_F32 || !wide || left < 4) {
+__device__ __forceinline__ void values4(float (&v)[4], const Four& q, int dtype) {
+  if (dtype == MLT_F32) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(q.r[k]);
   } else if (dtype == MLT_BF16) {
@@ -109,31 +106,30 @@ __device__ __forceinline__ void values4(float (&v)[4], const Four& q, int dtype,
     for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(k & 1 ? q.r[k / 2] & 0xFFFF0000u : q.r[k / 2] << 16);
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      v[k] = __half2float(__ushort_as_half(static_cast<unsigned short>(k & 1 ? q.r[k / 2] >> 16 : q.r[k / 2])));
+    for (int k = 0; k < 2; ++k) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&q.r[k]));
+      v[2 * k] = f.x;
+      v[2 * k + 1] = f.y;
+    }
   }
 }
 
-__device__ __forceinline__ void store4(const float (&v)[4], void* p, int dtype, long long i, int left, bool wide) {
-  if (wide && left == 4) {
+// A lane's eight values of a whole block.
+__device__ __forceinline__ void store8(char* p, const float (&v)[2][4], int dtype) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
     if (dtype == MLT_F32) {
-      *reinterpret_cast<Pack<float, 4>*>(static_cast<float*>(p) + i) = {{v[0], v[1], v[2], v[3]}};
+      *reinterpret_cast<float4*>(p + 512 * h) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
     } else if (dtype == MLT_BF16) {
-      Pack<__nv_bfloat16, 4> q;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) q.v[k] = from_f32<__nv_bfloat16>(v[k]);
-      *reinterpret_cast<Pack<__nv_bfloat16, 4>*>(static_cast<__nv_bfloat16*>(p) + i) = q;
+      const __nv_bfloat162 a = __floats2bfloat162_rn(v[h][0], v[h][1]), b = __floats2bfloat162_rn(v[h][2], v[h][3]);
+      *reinterpret_cast<uint2*>(p + 256 * h) =
+          make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
     } else {
-      Pack<__half, 4> q;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) q.v[k] = from_f32<__half>(v[k]);
-      *reinterpret_cast<Pack<__half, 4>*>(static_cast<__half*>(p) + i) = q;
+      const __half2 a = __floats2half2_rn(v[h][0], v[h][1]), b = __floats2half2_rn(v[h][2], v[h][3]);
+      *reinterpret_cast<uint2*>(p + 256 * h) =
+          make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
     }
-    return;
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < left) store_from_f32(p, dtype, i + k, v[k]);
 }
 
 // Four codes of m (e4m3) or v (e5m2, the upper byte of a half) as numbers.
@@ -148,31 +144,44 @@ __device__ __forceinline__ void decode_e4m3(float (&v)[4], unsigned word, float 
 }
 __device__ __forceinline__ void decode_e5m2(float (&v)[4], unsigned word, float scale) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    v[k] = __half2float(__ushort_as_half(static_cast<unsigned short>((word >> (8 * k)) << 8))) * scale;
+  for (int k = 0; k < 2; ++k) {
+    const unsigned h = __byte_perm(word, 0, k == 0 ? 0x1404 : 0x3424);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    v[2 * k] = f.x * scale;
+    v[2 * k + 1] = f.y * scale;
+  }
 }
 
-// The word of four values' codes; e: the block's exponent (16 .. 255), u: numbers below 2^16.
-template <int MANTISSA>
-__device__ __forceinline__ unsigned encode4(const float (&v)[4], unsigned e, const unsigned (&u)[4]) {
-  constexpr int kBias = MANTISSA == 3 ? 134 : 141, kDrop = 23 - MANTISSA;
-  const float up = __uint_as_float((127 + kBias - e) << 23);
-  unsigned word = 0;
+// The words of four values' codes; em, ev: the block's exponents (16 .. 255), r: the values' hashes.  A code
+// is shifted into the upper byte of a word, the sign with it, and the four upper bytes are gathered.
+__device__ __forceinline__ unsigned gather(const unsigned (&x)[4]) {
+  return __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410);
+}
+__device__ __forceinline__ unsigned encode_e4m3(const float (&m)[4], unsigned e, const unsigned (&r)[4]) {
+  const float up = __uint_as_float((127 + 134 - e) << 23);
+  unsigned x[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float s = fabsf(v[k]) * up * (MANTISSA == 3 ? 0x1p-120f : 0x1p-112f);
-    unsigned code = (__float_as_uint(s) + (u[k] << (kDrop - 16))) >> kDrop;
-    if (MANTISSA == 3)
-      code |= (__float_as_uint(v[k]) >> 24) & 0x80u;
-    else if (v[k] > 0.0f && code == 0)
-      code = 1;
-    word |= code << (8 * k);
+    const float s = fabsf(m[k]) * up * 0x1p-120f;
+    const unsigned c = (__float_as_uint(s) + ((r[k] << 4) & 0xFFFF0u)) << 4;
+    x[k] = (c & 0x7F000000u) | (__float_as_uint(m[k]) & 0x80000000u);
   }
-  return e == 255 ? 0x7F7F7F7Fu : word;
+  return e == 255 ? 0x7F7F7F7Fu : gather(x);
+}
+__device__ __forceinline__ unsigned encode_e5m2(const float (&v)[4], unsigned e, const unsigned (&r)[4]) {
+  const float up = __uint_as_float((127 + 141 - e) << 23);
+  unsigned x[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float s = v[k] * up * 0x1p-112f;
+    const unsigned c = __float_as_uint(s) + ((r[k] >> 16) << 5);
+    x[k] = (v[k] > 0.0f ? max(c, 1u << 21) : c) << 3;
+  }
+  return e == 255 ? 0x7F7F7F7Fu : gather(x);
 }
 
 template <int N, int BITS>
-__global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ Table<N> q) {
+__global__ void __launch_bounds__(256, 4) k_adamw(const __grid_constant__ Table<N> q) {
   pdl_wait();
   pdl_trigger();
   const Common& c = q.c;
@@ -201,37 +210,69 @@ __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ Table<N> 
   const float scale = c.grad_scale != nullptr ? *c.grad_scale : 1.0f;
   const unsigned key = mix(mix(c.seed) + static_cast<unsigned>(step));
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long from = static_cast<long long>(blockIdx.x - t.first_cta) * kSpan;
+  const long long from = static_cast<long long>(blockIdx.x - t.first_cta) * c.span + warp;
   const long long blocks = (t.n + kBlock - 1) / kBlock;
+  const int turns = static_cast<int>(min(static_cast<long long>(c.span) - warp, blocks - from) + 7) / 8;
+  const bool f32 = t.dtype == MLT_F32, g32 = t.grad_dtype == MLT_F32, c32 = t.copy_dtype == MLT_F32;
+  // a tensor's whole blocks with aligned addresses, then what is left
+  const long long whole = t.wide ? t.n / kBlock : 0;
 #pragma unroll 1
-  for (int k = warp; k < kSpan; k += 8) {
-    if (from + k >= blocks) break;
-    const long long i0 = (from + k) * kBlock + lane * 4, b = t.block + from + k, s0 = b * kBlock + lane * 4;
+  for (int k = 0; k < turns; ++k) {
+    const long long at = from + 8 * k, b = t.block + at;
+    const long long i0 = at * kBlock + lane * 4, s0 = b * kBlock + lane * 4;
+    const bool full = at < whole;
     float p[2][4], g[2][4], m[2][4], v[2][4];
-    int left[2];
+    int left[2] = {4, 4};
     Four rp[2], rg[2], rm[2], rv[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const long long rest = t.n - (i0 + 128 * h);
-      left[h] = rest < 0 ? 0 : rest > 4 ? 4 : static_cast<int>(rest);
-      rp[h] = load4(t.param, t.dtype, i0 + 128 * h, left[h], t.wide);
-      rg[h] = load4(t.grad, t.grad_dtype, i0 + 128 * h, left[h], t.wide);
-      if (BITS == 32) {
-        rm[h] = load4(c.m, MLT_F32, s0 + 128 * h, 4, true);
-        rv[h] = load4(c.v, MLT_F32, s0 + 128 * h, 4, true);
+    if (full) {
+      const char* pp = static_cast<const char*>(t.param) + (i0 << (f32 ? 2 : 1));
+      const char* gg = static_cast<const char*>(t.grad) + (i0 << (g32 ? 2 : 1));
+      if (f32) {
+        rp[0] = wide4(pp);
+        rp[1] = wide4(pp + 512);
       } else {
-        rm[h].r[0] = *reinterpret_cast<const unsigned*>(static_cast<const uint8_t*>(c.m) + s0 + 128 * h);
-        rv[h].r[0] = *reinterpret_cast<const unsigned*>(static_cast<const uint8_t*>(c.v) + s0 + 128 * h);
+        rp[0] = narrow4(pp);
+        rp[1] = narrow4(pp + 256);
+      }
+      if (g32) {
+        rg[0] = wide4(gg);
+        rg[1] = wide4(gg + 512);
+      } else {
+        rg[0] = narrow4(gg);
+        rg[1] = narrow4(gg + 256);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long rest = t.n - (i0 + 128 * h);
+        left[h] = rest < 0 ? 0 : rest > 4 ? 4 : static_cast<int>(rest);
+        rp[h] = some4(t.param, t.dtype, i0 + 128 * h, left[h]);
+        rg[h] = some4(t.grad, t.grad_dtype, i0 + 128 * h, left[h]);
       }
     }
-    const float ms = BITS == 8 ? c.m_scale[b] : 0.0f, vs = BITS == 8 ? c.v_scale[b] : 0.0f;
+    const char *mm = static_cast<const char*>(c.m) + s0 * (BITS / 8), *vv = static_cast<const char*>(c.v) + s0 * (BITS / 8);
+    float ms = 0.0f, vs = 0.0f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      values4(p[h], rp[h], t.dtype, left[h], t.wide);
-      values4(g[h], rg[h], t.grad_dtype, left[h], t.wide);
       if (BITS == 32) {
-        values4(m[h], rm[h], MLT_F32, 4, true);
-        values4(v[h], rv[h], MLT_F32, 4, true);
+        rm[h] = wide4(mm + 512 * h);
+        rv[h] = wide4(vv + 512 * h);
+      } else {
+        rm[h].r[0] = *reinterpret_cast<const unsigned*>(mm + 128 * h);
+        rv[h].r[0] = *reinterpret_cast<const unsigned*>(vv + 128 * h);
+      }
+    }
+    if (BITS == 8) {
+      ms = c.m_scale[b];
+      vs = c.v_scale[b];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      values4(p[h], rp[h], full ? t.dtype : MLT_F32);
+      values4(g[h], rg[h], full ? t.grad_dtype : MLT_F32);
+      if (BITS == 32) {
+        values4(m[h], rm[h], MLT_F32);
+        values4(v[h], rv[h], MLT_F32);
       } else {
         decode_e4m3(m[h], rm[h].r[0], ms);
         decode_e5m2(v[h], rv[h].r[0], vs);
@@ -245,54 +286,83 @@ __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ Table<N> 
         const float x = __fmul_rn(g[h][e], scale);
         m[h][e] = __fadd_rn(__fmul_rn(m[h][e], c.beta1), __fmul_rn(x, c.one_beta1));
         v[h][e] = __fadd_rn(__fmul_rn(v[h][e], c.beta2), __fmul_rn(__fmul_rn(x, x), c.one_beta2));
-        if (e < left[h]) {
-          most_m = max(most_m, __float_as_uint(m[h][e]) & 0x7FFFFFFFu);
-          most_v = max(most_v, __float_as_uint(v[h][e]) & 0x7FFFFFFFu);
-        }
         const float d = __fdividef(m[h][e], fmaf(root_of(v[h][e]), root, c.eps));
         p[h][e] = fmaf(-rate, d, __fmul_rn(p[h][e], keep));
       }
+    if (full) {
+      char* pp = static_cast<char*>(t.param) + (i0 << (f32 ? 2 : 1));
+      store8(pp, p, t.dtype);
+      if (t.copy != nullptr) store8(static_cast<char*>(t.copy) + (i0 << (c32 ? 2 : 1)), p, t.copy_dtype);
+    } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      store4(p[h], t.param, t.dtype, i0 + 128 * h, left[h], t.wide);
-      if (t.copy != nullptr) store4(p[h], t.copy, t.copy_dtype, i0 + 128 * h, left[h], t.wide);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (e >= left[h]) continue;
+          store_from_f32(t.param, t.dtype, i0 + 128 * h + e, p[h][e]);
+          if (t.copy != nullptr) store_from_f32(t.copy, t.copy_dtype, i0 + 128 * h + e, p[h][e]);
+        }
     }
     if (BITS == 32) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        store4(m[h], c.m, MLT_F32, s0 + 128 * h, left[h], true);
-        store4(v[h], c.v, MLT_F32, s0 + 128 * h, left[h], true);
-      }
-    } else {
-      const unsigned em = max(__reduce_max_sync(0xffffffffu, most_m) >> 23, 16u);
-      const unsigned ev = max(__reduce_max_sync(0xffffffffu, most_v) >> 23, 16u);
-      const unsigned kb = mix(static_cast<unsigned>(b) + key);
+        char *to_m = const_cast<char*>(mm) + 512 * h, *to_v = const_cast<char*>(vv) + 512 * h;
+        if (left[h] == 4) {
+          *reinterpret_cast<float4*>(to_m) = make_float4(m[h][0], m[h][1], m[h][2], m[h][3]);
+          *reinterpret_cast<float4*>(to_v) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+        } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        unsigned um[4], uv[4];
+          for (int e = 0; e < 4; ++e)
+            if (e < left[h]) {
+              reinterpret_cast<float*>(to_m)[e] = m[h][e];
+              reinterpret_cast<float*>(to_v)[e] = v[h][e];
+            }
+        }
+      }
+      continue;
+    }
+    if (full) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const unsigned r = mix(kb + (lane * 4 + 128 * h + e) * 0x9E3779B9u);
-          um[e] = r & 0xFFFFu;
-          uv[e] = r >> 16;
+          most_m = max(most_m, __float_as_uint(m[h][e]) & 0x7FFFFFFFu);
+          most_v = max(most_v, __float_as_uint(v[h][e]) & 0x7FFFFFFFu);
         }
-        const unsigned wm = encode4<3>(m[h], em, um), wv = encode4<2>(v[h], ev, uv);
-        uint8_t* to_m = static_cast<uint8_t*>(c.m) + s0 + 128 * h;
-        uint8_t* to_v = static_cast<uint8_t*>(c.v) + s0 + 128 * h;
-        if (left[h] == 4) {
-          *reinterpret_cast<unsigned*>(to_m) = wm;
-          *reinterpret_cast<unsigned*>(to_v) = wv;
-        } else {
-          for (int e = 0; e < left[h]; ++e) {
-            to_m[e] = static_cast<uint8_t>(wm >> (8 * e));
-            to_v[e] = static_cast<uint8_t>(wv >> (8 * e));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < left[h]) {
+            most_m = max(most_m, __float_as_uint(m[h][e]) & 0x7FFFFFFFu);
+            most_v = max(most_v, __float_as_uint(v[h][e]) & 0x7FFFFFFFu);
           }
+    }
+    const unsigned em = max(__reduce_max_sync(0xffffffffu, most_m) >> 23, 16u);
+    const unsigned ev = max(__reduce_max_sync(0xffffffffu, most_v) >> 23, 16u);
+    const unsigned kb = mix(static_cast<unsigned>(b) + key) + lane * 4 * 0x9E3779B9u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      unsigned r[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = mix(kb + (128u * h + e) * 0x9E3779B9u);
+      const unsigned wm = encode_e4m3(m[h], em, r), wv = encode_e5m2(v[h], ev, r);
+      uint8_t* to_m = reinterpret_cast<uint8_t*>(const_cast<char*>(mm)) + 128 * h;
+      uint8_t* to_v = reinterpret_cast<uint8_t*>(const_cast<char*>(vv)) + 128 * h;
+      if (left[h] == 4) {
+        *reinterpret_cast<unsigned*>(to_m) = wm;
+        *reinterpret_cast<unsigned*>(to_v) = wv;
+      } else {
+        for (int e = 0; e < left[h]; ++e) {
+          to_m[e] = static_cast<uint8_t>(wm >> (8 * e));
+          to_v[e] = static_cast<uint8_t>(wv >> (8 * e));
         }
       }
-      if (lane == 0) {
-        c.m_scale[b] = __uint_as_float((em - 7) << 23);
-        c.v_scale[b] = __uint_as_float((ev - 14) << 23);
-      }
+    }
+    if (lane == 0) {
+      c.m_scale[b] = __uint_as_float((em - 7) << 23);
+      c.v_scale[b] = __uint_as_float((ev - 14) << 23);
     }
   }
 }
@@ -318,7 +388,7 @@ cudaError_t launch_part(const Common& c, const std::vector<Tensor>& list, size_t
 }  // namespace
 
 cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_adamw_rule& r, void* m, void* v,
-                         float* m_scale, float* v_scale, long long* launches, cudaStream_t st) {
+                         float* m_scale, float* v_scale, int sms, long long* launches, cudaStream_t st) {
   const bool on_device = r.step_device != nullptr;
   const double t = static_cast<double>(r.step);
   // 1 - beta^step without cancellation
@@ -342,6 +412,11 @@ cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_a
   c.v = v;
   c.m_scale = m_scale;
   c.v_scale = v_scale;
+  // four blocks a warp where they fill the GPU several times over, else one
+  long long all = 0;
+  for (int i = 0; i < count; ++i) all += tensors[i].grad == nullptr ? 0 : (tensors[i].n + kBlock - 1) / kBlock;
+  c.span = 8;
+  while (c.span < kMostSpan && all > 16LL * sms * c.span) c.span *= 2;
   std::vector<Tensor> list;
   list.reserve(count);
   long long block = 0, ctas = 0;
@@ -365,8 +440,8 @@ cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_a
     }
     // a launch has at most 2^31 - 1 CTAs: a longer tensor is taken in parts
     const long long most = 1LL << 30;
-    for (long long at = 0; at < blocks; at += most * kSpan) {
-      const long long part = std::min(blocks - at, most * kSpan), need = (part + kSpan - 1) / kSpan;
+    for (long long at = 0; at < blocks; at += most * c.span) {
+      const long long part = std::min(blocks - at, most * c.span), need = (part + c.span - 1) / c.span;
       if (list.size() - from == kMost || ctas + need > most) {
         const cudaError_t e = flush();
         if (e != cudaSuccess) return e;

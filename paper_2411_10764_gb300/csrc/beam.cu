@@ -7,12 +7,14 @@
 // where its terms are exact; fp32 exponentials are what is left, some 2^-26 of it on average).
 // GB300 adds two fp64 numbers a cycle and SM, so only candidates that may win get that far.
 //
-//   k_beam_rows   long rows: one pass over the scores, CTAs of 512 threads, as many a row as fill
-//                 the GPU.  Each thread keeps the running sum of exponentials and the largest score of each of
-//                 eight slots of its packs.  The k-th largest of these maxima is at most the k-th largest
-//                 score, so scores from it on are collected, from the few slots that reach
-//                 it, and the k best of them are kept for the item.
-//   k_beam_items  a CTA an item: the normalisers, then all candidates (the rows' lists, or all
+//   k_beam_rows   long rows: one pass over the scores, CTAs of 256 threads, as many a row as fill
+//                 the GPU.  Each thread keeps the running sum of exponentials, in units of a power of two, and
+//                 the largest score of each of four slots of its packs.  The k-th largest of these
+//                 maxima is at most the k-th largest score, so scores from it on are collected, from the few
+//                 slots that reach it, and the k best of them are kept for the item.  Sums that are not
+//                 finite (NaN, infinite or huge scores) are formed again score by score.
+//   k_beam_few    up to 128 candidates an item: a thread each, which finds its beam's normaliser by itself;
+//   k_beam_items  more: a CTA an item, the normalisers, then all candidates (the rows' lists, or all
 //                 scores where there are at most 8,192).  Each candidate's total is bounded from both
 //                 sides in fp32; m lower bounds reach some threshold, and those whose upper bound does
 //                 are formed in 64 bits and sorted.
@@ -20,6 +22,7 @@
 // Bound: memory for the scores, else the latency of two launches and some twenty barriers.
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 #include <utility>
 
 #include "norm.cuh"
@@ -27,8 +30,9 @@
 namespace mlt {
 namespace {
 
-constexpr int kRowThreads = 512;
-constexpr int kSlots = 8;
+constexpr int kRowThreads = 256;
+constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kSlots = 4;
 constexpr int kRowList = 2048;   // collected scores of a CTA's share of a row
 constexpr int kMostCands = 8192;
 constexpr int kItemThreads = 1024;
@@ -56,10 +60,24 @@ __device__ __forceinline__ double double_from_ordered(u64 k) {
 // A score as it counts: finite, or -infinity where it is no continuation.
 __device__ __forceinline__ float clean(float x) { return x > -INFINITY ? fminf(fmaxf(x, -FLT_MAX), FLT_MAX) : -INFINITY; }
 
-__device__ __forceinline__ float exp_of(float d) {
+// exp(x) / 2^unit: the product by log2 e is exact inside the sum, so all there is are the sum's rounding and
+// that of log2 e itself, a factor 1 + kLogE on x that the normaliser takes back for its largest terms.
+constexpr float kLog2E = 1.44269504f;
+constexpr double kLogE = 1.44269502162933349609375 / 1.44269504088896340736 - 1;
+__device__ __forceinline__ float power(float x) {
   float r;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(d * 1.44269504f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+__device__ __forceinline__ float exp_in(float x, float unit) { return power(fmaf(x, kLog2E, -unit)); }
+// Scores of 1e37 and more: next to such a one only its equals count, and the unit is exp of it.
+__device__ __forceinline__ bool is_huge(float top) { return !(fabsf(top) < 1e37f); }
+// The unit for terms up to exp(top); 0 where there are none.
+__device__ __forceinline__ float unit_of(float top) { return is_huge(top) ? 0.0f : rintf(top * kLog2E); }
+// exp(x) for x <= top, both finite or -infinity, in these units.
+__device__ __forceinline__ float term(float x, float top, float unit) {
+  if (is_huge(top)) return x == top ? 1.0f : 0.0f;
+  return exp_in(x, unit);
 }
 
 // A sum in two numbers (Knuth's exact addition).
@@ -74,18 +92,20 @@ struct Two {
     add(o.hi);
     lo = __fadd_rn(lo, o.lo);
   }
+  // to another unit; an empty sum's may lie at any distance
   __device__ __forceinline__ void scale(float f) {
-    hi *= f;
-    lo *= f;
+    const float g = hi > 0.0f ? f : 0.0f;
+    hi *= g;
+    lo *= g;
   }
   __device__ __forceinline__ Two shuffled(int o, int width = 32) const {
     return {__shfl_xor_sync(0xffffffffu, hi, o, width), __shfl_xor_sync(0xffffffffu, lo, o, width)};
   }
 };
 
-// top + ln(sum), by ln f = 2 atanh((f - 1) / (f + 1)) of the sum's fraction f in [0.7, 1.42): the leading
-// term in two numbers, the rest of the series (below 0.004) in fp32.  Off by some 2^-32.
-__device__ __forceinline__ double log_sum(float top, Two sum) {
+// ln(sum 2^unit) for terms up to exp(top), by ln f = 2 atanh((f - 1) / (f + 1)) of the sum's fraction f in
+// [0.7, 1.42): the leading term in two numbers, the rest of the series (below 0.004) in fp32.  Off by some 2^-32.
+__device__ __forceinline__ double log_sum(float top, float unit, Two sum) {
   float hi = __fadd_rn(sum.hi, sum.lo);
   float lo = __fadd_rn(__fsub_rn(sum.hi, hi), sum.lo);
   int e = (__float_as_int(hi) >> 23) - 127;
@@ -105,16 +125,44 @@ __device__ __forceinline__ double log_sum(float top, Two sum) {
   r = fmaf(q, r, 2.0f / 5);
   r = fmaf(q, r, 2.0f / 3);
   r = r * q * s + 2.0f * s_lo;
-  return fma(static_cast<double>(e), 0.693147180559945309417, static_cast<double>(top)) +
-         (static_cast<double>(2.0f * s) + static_cast<double>(r));
+  const float back = static_cast<float>(-kLogE) * top;
+  return fma(static_cast<double>(unit) + e, 0.693147180559945309417,
+             static_cast<double>(2.0f * s) + static_cast<double>(r + back));
+}
+
+// The normaliser: ln of a sum of terms up to exp(top), top finite.
+__device__ __forceinline__ double normaliser(float top, Two sum) {
+  if (is_huge(top)) return top + log_sum(0.0f, 0.0f, sum);
+  return log_sum(top, unit_of(top), sum);
 }
 
 // What a CTA found in its share of a row.
-struct RowPart {
+struct __align__(16) RowPart {
   float top;  // -infinity: no continuation
-  Two sum;
   int count;
+  Two sum;    // in units of 2^unit_of(top)
 };
+
+// The normaliser of a row from its parts, NaN where it has no continuation.
+__device__ __forceinline__ double join_parts(const RowPart* part, int parts, bool normalised) {
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) top = fmaxf(top, part[p].top);
+  if (top == -INFINITY) return NAN;
+  if (normalised) return 0.0;
+  const float unit = unit_of(top);
+  Two sum{0.0f, 0.0f};
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const RowPart q = part[p];
+    // beside a huge top only its equals count, and a huge negative one counts beside its equals alone
+    if (q.top == -INFINITY || ((is_huge(top) || is_huge(q.top)) && q.top != top)) continue;
+    Two s = q.sum;
+    s.scale(power(unit_of(q.top) - unit));
+    sum.add(s);
+  }
+  return normaliser(top, sum);
+}
 
 // Whether beam `row` has continuations to be read.
 __device__ __forceinline__ bool is_live(const mlt_beam_args& a, long long row) {
@@ -186,10 +234,30 @@ __device__ __forceinline__ u64 row_key(float s, int token) {
   return (static_cast<u64>(ordered(s)) << 32) | static_cast<unsigned>(~token);
 }
 
+// The largest of a pack's scores but NaN: -infinity or more.
+template <typename T, int V>
+__device__ __forceinline__ float pack_max(const Pack<T, V>& p) {
+  if constexpr (sizeof(T) == 4) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < V; ++e) m = fmaxf(m, p.v[e]);
+    return m;
+  } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    const __nv_bfloat162* q = reinterpret_cast<const __nv_bfloat162*>(&p);
+    const __nv_bfloat162 m = __hmax2(__hmax2(q[0], q[1]), __hmax2(q[2], q[3]));
+    return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+  } else {
+    const __half2* q = reinterpret_cast<const __half2*>(&p);
+    const __half2 m = __hmax2(__hmax2(q[0], q[1]), __hmax2(q[2], q[3]));
+    return fmaxf(fmaxf(__low2float(m), __high2float(m)), -INFINITY);
+  }
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 2)
+__global__ void __launch_bounds__(kRowThreads, 4)
     k_beam_rows(const __grid_constant__ mlt_beam_args a, int parts, int k, RowPart* found, u64* lists) {
-  __shared__ float warp_top[16], warp_hi[16], warp_lo[16];
+  __shared__ float warp_top[kRowWarps];
+  __shared__ Two warp_sum[kRowWarps];
   __shared__ int total[2], listed;
   __shared__ u64 list[kRowList];
   pdl_wait();
@@ -207,7 +275,7 @@ __global__ void __launch_bounds__(kRowThreads, 2)
   sh.first = static_cast<int>(static_cast<long long>(packs) * part / parts);
   sh.last = static_cast<int>(static_cast<long long>(packs) * (part + 1) / parts);
 
-  float slot[kSlots], top = -FLT_MAX;
+  float slot[kSlots], top = -INFINITY, unit = 0.0f;
   Two sum{0.0f, 0.0f};
 #pragma unroll
   for (int u = 0; u < kSlots; ++u) slot[u] = -INFINITY;
@@ -215,65 +283,100 @@ __global__ void __launch_bounds__(kRowThreads, 2)
   for (int q = sh.first + tid; q < sh.last; q += kSlots * kRowThreads) {
     Pack<T, V> p[kSlots];
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u)
-      if (q + u * kRowThreads < sh.last) sh.load(q + u * kRowThreads, p[u]);
+    for (int u = 0; u < kSlots; ++u) {
+      if (q + u * kRowThreads < sh.last) {
+        sh.load(q + u * kRowThreads, p[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) p[u].v[e] = from_f32<T>(-INFINITY);
+      }
+    }
     float best = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kSlots; ++u)
-      if (q + u * kRowThreads < sh.last) {
-        float high = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < V; ++e) high = fmaxf(high, clean(to_f32(p[u].v[e])));
-        slot[u] = fmaxf(slot[u], high);
-        best = fmaxf(best, high);
-      }
-    if (a.normalised == 0) {
-      if (best > top) {
-        sum.scale(exp_of(top - best));
-        top = best;
-      }
-#pragma unroll
-      for (int u = 0; u < kSlots; ++u)
-        if (q + u * kRowThreads < sh.last) {
-          float s = 0.0f;
-#pragma unroll
-          for (int e = 0; e < V; ++e) s += exp_of(clean(to_f32(p[u].v[e])) - top);
-          sum.add(s);
-        }
-    } else {
-      top = fmaxf(top, best);
+    for (int u = 0; u < kSlots; ++u) {
+      const float high = pack_max(p[u]);
+      slot[u] = fmaxf(slot[u], high);
+      best = fmaxf(best, high);
     }
+    if (best > top) {
+      top = best;
+      const float now = unit_of(top);
+      sum.scale(power(unit - now));
+      unit = now;
+    }
+    if (a.normalised == 0) {
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u) {
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e & 1] += exp_in(to_f32(p[u].v[e]), unit);
+        sum.add(s[0] + s[1]);
+      }
+    }
+  }
+
+  // the CTA's top, sum, and the least of the warps' tops
+  auto cta_top = [&](float mine) {
+    float high = mine;
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+    __syncthreads();
+    if (lane == 0) warp_top[warp] = high;
+    if (tid == 0) listed = total[0] = total[1] = 0;
+    __syncthreads();
+    high = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) high = fmaxf(high, warp_top[w]);
+    return high;
+  };
+  auto cta_sum = [&](float high) {
+    const float now = unit_of(high);
+    sum.scale(power(unit - now));
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) sum.add(sum.shuffled(o));
+    if (lane == 0) warp_sum[warp] = sum;
+    __syncthreads();
+    Two all{0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) all.add(warp_sum[w]);
+    return all;
+  };
+  float high = cta_top(top);
+  Two all = cta_sum(high);
+  // not finite: a NaN, an infinite or a huge score.  The same again, each score as it counts
+  if (high > -INFINITY && (is_huge(high) || !(all.hi + all.lo < INFINITY))) {
+    high = cta_top(clean(top));
+    unit = unit_of(high);
+    sum = Two{0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) slot[u] = fminf(slot[u], FLT_MAX);
+    if (a.normalised == 0)
+      for (int q = sh.first + tid; q < sh.last; q += kRowThreads) {
+        Pack<T, V> p;
+        sh.load(q, p);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum.add(term(clean(to_f32(p.v[e])), high, unit));
+      }
+    all = cta_sum(high);
   }
   float mine = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kSlots; ++u) mine = fmaxf(mine, slot[u]);
 
-  // the CTA's top and sum
-  float high = top;
-#pragma unroll
-  for (int o = 16; o > 0; o /= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-  if (lane == 0) warp_top[warp] = high;
-  if (tid == 0) listed = total[0] = total[1] = 0;
-  __syncthreads();
-  high = warp_top[lane & 15];
-#pragma unroll
-  for (int o = 8; o > 0; o /= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-  sum.scale(exp_of(top - high));
-#pragma unroll
-  for (int o = 16; o > 0; o /= 2) sum.add(sum.shuffled(o));
-  if (lane == 0) {
-    warp_hi[warp] = sum.hi;
-    warp_lo[warp] = sum.lo;
-  }
-
   // the largest threshold found that at least k maxima reach
   const unsigned key = ordered(mine);
   unsigned low = kNone, up = ordered(high) + 1;  // `low` always reached by k of them, or it is -infinity
   const bool by_slot = k > kRowThreads / 4;
-  const int enough = k + (k < 16 ? 8 : k / 2);
+  const int enough = k + (k < 48 ? 24 : k / 2);
   int flip = 0;
+  // with as many warps as wanted maxima the least of the warps' own is a good first try
+  float least = INFINITY;
+#pragma unroll
+  for (int w = 0; w < kRowWarps; ++w) least = fminf(least, warp_top[w]);
+  unsigned first = k <= kRowWarps ? ordered(fminf(least, high)) : 0u;
   while (up - low > 1) {
-    const unsigned mid = low + (up - low) / 2;
+    const unsigned mid = first > low && first < up ? first : low + (up - low) / 2;
+    first = 0;
     int c;
     if (!by_slot) {
       c = __syncthreads_count(key >= mid);
@@ -372,12 +475,7 @@ __global__ void __launch_bounds__(kRowThreads, 2)
     bitonic(list, size, [](u64 x, u64 y) { return x < y; });
     for (int i = tid; i < min(count, k); i += kRowThreads) to[i] = list[i];
   }
-  if (tid < 32) {
-    Two all = lane < 16 ? Two{warp_hi[lane], warp_lo[lane]} : Two{0.0f, 0.0f};
-#pragma unroll
-    for (int o = 8; o > 0; o /= 2) all.add(all.shuffled(o));
-    if (lane == 0) out = RowPart{count > 0 ? high : -INFINITY, all, min(count, k)};
-  }
+  if (tid == 0) out = RowPart{count > 0 ? high : -INFINITY, min(count, k), all};
 }
 
 // --- items -----------------------------------------------------------------------------------
@@ -387,6 +485,64 @@ struct Cand {
 };
 __device__ __forceinline__ bool less(const Cand& a, const Cand& b) {
   return a.total < b.total || (a.total == b.total && a.tie < b.tie);
+}
+
+__device__ __forceinline__ Cand candidate_of(int w, float s, int token, double total) {
+  return {ordered(total), (static_cast<u64>(1023 - w) << 54) | (static_cast<u64>(ordered(s)) << 22) |
+                              static_cast<u64>((1 << 22) - 1 - token)};
+}
+__device__ __forceinline__ int beam_of(const Cand& c) { return 1023 - static_cast<int>(c.tie >> 54); }
+
+__device__ __forceinline__ void write(const mlt_beam_args& a, int b, int at, const Cand& c, bool ended) {
+  const long long o = static_cast<long long>(b) * a.m + at;
+  const int token = (1 << 22) - 1 - static_cast<int>(c.tie & ((1 << 22) - 1));
+  a.out_parent[o] = beam_of(c);
+  a.out_token[o] = token;
+  a.out_logp[o] = static_cast<float>(double_from_ordered(c.total));
+  a.out_done[o] = ended || token == a.eos;
+}
+__device__ __forceinline__ void write_none(const mlt_beam_args& a, int b, int at) {
+  const long long o = static_cast<long long>(b) * a.m + at;
+  a.out_parent[o] = a.out_token[o] = -1;
+  a.out_logp[o] = -INFINITY;
+  a.out_done[o] = 0;
+}
+
+// Up to kCountSort candidates an item, out of the rows' lists.
+__global__ void __launch_bounds__(kCountSort)
+    k_beam_few(const __grid_constant__ mlt_beam_args a, int parts, int k, const RowPart* found, const u64* lists) {
+  __shared__ Cand list[kCountSort];
+  pdl_wait();
+  pdl_trigger();
+  const int b = blockIdx.x, tid = threadIdx.x, each = parts * k, cands = a.beams * each;
+  const int w = min(tid / each, a.beams - 1), at = tid - w * each;
+  const long long r = static_cast<long long>(b) * a.beams + w, o = r * parts + min(at / k, parts - 1);
+  const float lp = a.logp[r];
+  const bool ended = a.done != nullptr && a.done[r] != 0;
+  const u64 key = tid < cands ? lists[o * k + at % k] : 0;
+  bool valid = tid < cands && lp > -INFINITY;
+  Cand mine{0, 0};
+  if (valid) {
+    if (ended) {
+      valid = at == 0;
+      mine = candidate_of(w, 0.0f, static_cast<int>(a.eos), lp);
+    } else {
+      const double z = join_parts(found + r * parts, parts, a.normalised != 0);
+      valid = at % k < found[o].count;
+      const float s = from_ordered(static_cast<unsigned>(key >> 32));
+      mine = candidate_of(w, s, ~static_cast<int>(key), lp + (static_cast<double>(s) - z));
+    }
+    if (!valid) mine = Cand{0, 0};
+  }
+  list[tid] = mine;
+  const int count = __syncthreads_count(valid);
+  if (valid) {
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < cands; ++j) rank += less(mine, list[j]);
+    if (rank < a.m) write(a, b, rank, mine, ended);
+  }
+  for (int i = count + tid; i < a.m; i += blockDim.x) write_none(a, b, i);
 }
 
 // T: the scores' type where candidates are all scores; else the rows' lists are read (FROM_ROWS).
@@ -399,16 +555,17 @@ __global__ void __launch_bounds__(kItemThreads)
   double* lse = reinterpret_cast<double*>(list + cap);           // [beams]
   float* logp = reinterpret_cast<float*>(lse + a.beams);         // [beams]; NaN: no continuations
   uint8_t* ended = reinterpret_cast<uint8_t*>(logp + a.beams);   // [beams]
-  __shared__ int total[2], listed;
-  __shared__ unsigned most;
+  __shared__ int total[2], listed, all;
+  __shared__ unsigned most, fewest;
   pdl_wait();
   pdl_trigger();
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
   const int each = FROM_ROWS ? parts * k : a.n, cands = a.beams * each;
   const T* scores = static_cast<const T*>(a.scores) + b * a.batch_stride;
   if (tid == 0) {
-    listed = total[0] = total[1] = 0;
+    listed = total[0] = total[1] = all = 0;
     most = 0;
+    fewest = 0xFFFFFFFFu;
   }
   for (int w = tid; w < a.beams; w += threads) {
     const long long r = static_cast<long long>(b) * a.beams + w;
@@ -417,22 +574,8 @@ __global__ void __launch_bounds__(kItemThreads)
     if (!(lp > -INFINITY)) lp = NAN;
     ended[w] = over;
     if (FROM_ROWS && !over && lp == lp) {
-      double z = 0.0;
-      const RowPart* part = found + r * parts;
-      float top = -INFINITY;
-      for (int p = 0; p < parts; ++p) top = fmaxf(top, part[p].top);
-      if (top == -INFINITY) {
-        lp = NAN;
-      } else if (a.normalised == 0) {
-        Two sum{0.0f, 0.0f};
-        for (int p = 0; p < parts; ++p) {
-          if (part[p].top == -INFINITY) continue;
-          Two s = part[p].sum;
-          s.scale(exp_of(part[p].top - top));
-          sum.add(s);
-        }
-        z = log_sum(top, sum);
-      }
+      const double z = join_parts(found + r * parts, parts, a.normalised != 0);
+      if (z != z) lp = NAN;
       lse[w] = z;
     }
     logp[w] = lp;
@@ -452,12 +595,13 @@ __global__ void __launch_bounds__(kItemThreads)
         for (int i = j; i < a.n; i += lanes) top = fmaxf(top, clean(to_f32(row[i])));
       for (int o = lanes / 2; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       Two sum{0.0f, 0.0f};
+      const float unit = unit_of(top);
       if (on && top > -INFINITY && a.normalised == 0)
-        for (int i = j; i < a.n; i += lanes) sum.add(expf(clean(to_f32(row[i])) - top));
+        for (int i = j; i < a.n; i += lanes) sum.add(term(clean(to_f32(row[i])), top, unit));
       for (int o = lanes / 2; o > 0; o /= 2) sum.add(sum.shuffled(o));
       if (on && j == 0) {
         if (top == -INFINITY) logp[w] = NAN;
-        lse[w] = top == -INFINITY || a.normalised != 0 ? 0.0 : log_sum(top, sum);
+        lse[w] = top == -INFINITY || a.normalised != 0 ? 0.0 : normaliser(top, sum);
       }
     }
     __syncthreads();
@@ -487,11 +631,8 @@ __global__ void __launch_bounds__(kItemThreads)
   };
   auto put = [&](int w, float s, int token) {
     const double lp = logp[w];
-    Cand c;
-    c.total = ordered(ended[w] ? lp : lp + (static_cast<double>(s) - lse[w]));
-    c.tie = (static_cast<u64>(1023 - w) << 54) | (static_cast<u64>(ordered(s)) << 22) |
-            static_cast<u64>((1 << 22) - 1 - token);
-    list[atomicAdd(&listed, 1)] = c;
+    list[atomicAdd(&listed, 1)] =
+        candidate_of(w, s, token, ended[w] ? lp : lp + (static_cast<double>(s) - lse[w]));
   };
 
   if (cands <= kCountSort) {
@@ -502,14 +643,16 @@ __global__ void __launch_bounds__(kItemThreads)
     }
   } else {
     unsigned lower[kPerThread], upper[kPerThread];
-    unsigned best = 0;
+    unsigned best = 0, worst = 0xFFFFFFFFu;
+    int valid = 0;
+    const int per = (cands + threads - 1) / threads;
 #pragma unroll
     for (int c = 0; c < kPerThread; ++c) {
       lower[c] = upper[c] = 0;
       const int i = c * threads + tid;
       int w, token;
       float s;
-      if (i >= cands || !candidate(i, w, s, token)) continue;
+      if (c >= per || i >= cands || !candidate(i, w, s, token)) continue;
       const float z = ended[w] ? 0.0f : static_cast<float>(lse[w]), lp = logp[w];
       // three roundings, of the normaliser and two sums, each at most 2^-23 of these
       const float v = lp + (s - z), off = 0x1p-21f * (fabsf(lp) + fabsf(s) + fabsf(z));
@@ -517,18 +660,37 @@ __global__ void __launch_bounds__(kItemThreads)
       lower[c] = l == l ? ordered(l) : kNone;
       upper[c] = u == u ? ordered(u) : 0xFFFFFFFFu;
       best = max(best, lower[c]);
+      worst = min(worst, lower[c]);
+      ++valid;
     }
     best = __reduce_max_sync(0xffffffffu, best);
-    if (lane == 0) atomicMax(&most, best);
+    worst = __reduce_min_sync(0xffffffffu, worst);
+    valid = __reduce_add_sync(0xffffffffu, valid);
+    if (lane == 0) {
+      atomicMax(&most, best);
+      atomicMin(&fewest, worst);
+      atomicAdd(&all, valid);
+    }
     __syncthreads();
+    // the largest threshold found that m lower bounds reach: between two that are too low and too high, where
+    // the counts' logarithms would put it if they fell evenly, or halfway, in turn
     unsigned low = 0, up = most + 1;
     const int enough = a.m + (a.m < 64 ? 64 : a.m / 4);
     int flip = 0;
-    while (up - low > 1) {
-      const unsigned mid = low + (up - low) / 2;
+    float at_low = static_cast<float>(all), at_up = 0.5f;
+    if (all <= enough) up = 1;  // all of them
+    unsigned from = fewest;
+    for (int turn = 0; up - low > 1; ++turn) {
+      unsigned mid = low + (up - low) / 2;
+      if ((turn & 1) == 0) {
+        const float f = __fdividef(__log2f(__fdividef(at_low, a.m + 0.5f * (enough - a.m))), __log2f(__fdividef(at_low, at_up)));
+        const float lo = from_ordered(max(low, from)), v = lo + (from_ordered(up) - lo) * f;
+        if (v == v && ordered(v) > low && ordered(v) < up) mid = ordered(v);
+      }
       int have = 0;
 #pragma unroll
-      for (int c = 0; c < kPerThread; ++c) have += lower[c] >= mid;
+      for (int c = 0; c < kPerThread; ++c)
+        if (c < per) have += lower[c] >= mid;
       have = __reduce_add_sync(0xffffffffu, have);
       if (lane == 0 && have > 0) atomicAdd(&total[flip], have);
       __syncthreads();
@@ -536,49 +698,40 @@ __global__ void __launch_bounds__(kItemThreads)
       if (tid == 0) total[flip ^ 1] = 0;
       __syncthreads();
       flip ^= 1;
-      if (got >= a.m)
+      if (got >= a.m) {
         low = mid;
-      else
+        at_low = static_cast<float>(got);
+        if (got <= enough) break;
+      } else {
         up = mid;
-      if (got >= a.m && got <= enough) break;
+        at_up = fmaxf(static_cast<float>(got), 0.5f);
+      }
     }
 #pragma unroll
     for (int c = 0; c < kPerThread; ++c) {
       int w, token;
       float s;
-      if (upper[c] > 0 && upper[c] >= low && candidate(c * threads + tid, w, s, token)) put(w, s, token);
+      if (c < per && upper[c] > 0 && upper[c] >= low && candidate(c * threads + tid, w, s, token)) put(w, s, token);
     }
   }
   __syncthreads();
   const int count = listed;
-  auto write = [&](int at, const Cand& c) {
-    const long long o = static_cast<long long>(b) * a.m + at;
-    const int w = 1023 - static_cast<int>(c.tie >> 54), token = (1 << 22) - 1 - static_cast<int>(c.tie & ((1 << 22) - 1));
-    a.out_parent[o] = w;
-    a.out_token[o] = token;
-    a.out_logp[o] = static_cast<float>(double_from_ordered(c.total));
-    a.out_done[o] = ended[w] || token == a.eos;
-  };
   if (count <= kCountSort) {
     for (int i = tid; i < count; i += threads) {
       const Cand c = list[i];
       int rank = 0;
+#pragma unroll 4
       for (int j = 0; j < count; ++j) rank += less(c, list[j]);
-      if (rank < a.m) write(rank, c);
+      if (rank < a.m) write(a, b, rank, c, ended[beam_of(c)]);
     }
   } else {
     const int size = power_of_two(count);
     for (int i = count + tid; i < size; i += threads) list[i] = Cand{0, 0};
     __syncthreads();
     bitonic(list, size, [](const Cand& x, const Cand& y) { return less(x, y); });
-    for (int i = tid; i < min(count, a.m); i += threads) write(i, list[i]);
+    for (int i = tid; i < min(count, a.m); i += threads) write(a, b, i, list[i], ended[beam_of(list[i])]);
   }
-  for (int i = count + tid; i < a.m; i += threads) {
-    const long long o = static_cast<long long>(b) * a.m + i;
-    a.out_parent[o] = a.out_token[o] = -1;
-    a.out_logp[o] = -INFINITY;
-    a.out_done[o] = 0;
-  }
+  for (int i = count + tid; i < a.m; i += threads) write_none(a, b, i);
 }
 
 struct Plan {
@@ -595,9 +748,9 @@ Plan plan_of(const mlt_beam_args& a, int sms) {
   p.parts = 1;
   long long cands = static_cast<long long>(a.beams) * a.n;
   if (!p.direct) {
-    // parts of a row until the GPU is full, none shorter than eight packs a thread
+    // parts of a row until the GPU is full, none shorter than eight scores a thread
     const int least = kRowThreads * 8;
-    while (p.parts < 64 && rows * p.parts < 2LL * sms && a.n / (2 * p.parts) >= least &&
+    while (p.parts < 64 && rows * p.parts < 4LL * sms && a.n / (2 * p.parts) >= least &&
            static_cast<long long>(a.beams) * p.k * p.parts * 2 <= kMostCands)
       p.parts *= 2;
     cands = static_cast<long long>(a.beams) * p.k * p.parts;
@@ -605,7 +758,7 @@ Plan plan_of(const mlt_beam_args& a, int sms) {
     p.bytes = p.off_lists + up256(sizeof(u64) * rows * p.parts * p.k);
   }
   p.threads = 128;
-  while (p.threads < kItemThreads && p.threads * 2 < cands) p.threads *= 2;
+  while (p.threads < kItemThreads && p.threads * 4 < cands) p.threads *= 2;
   p.cap = 128;
   while (p.cap < cands) p.cap *= 2;
   p.smem = sizeof(Cand) * p.cap + a.beams * (sizeof(double) + sizeof(float) + 1);
@@ -718,6 +871,9 @@ cudaError_t launch_beam(const mlt_beam_args& a, void* ws, int sms, long long* la
                                      a, p.parts, p.k, found, lists);
     if (e != cudaSuccess) return e;
     ++*launches;
+    if (a.beams * p.parts * p.k <= kCountSort)
+      return launch_pdl(k_beam_few, dim3(a.batch), dim3(kCountSort), 0, st, a, p.parts, p.k,
+                        static_cast<const RowPart*>(found), static_cast<const u64*>(lists));
     return launch_items<float, true>(a, p, found, lists, st);
   });
 }

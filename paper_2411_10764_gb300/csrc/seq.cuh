@@ -112,7 +112,7 @@ cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, vo
 
 // --- adamw.cu --------------------------------------------------------------
 cudaError_t launch_adamw(const mlt_adamw_tensor* tensors, int count, const mlt_adamw_rule& rule, void* m, void* v,
-                         float* m_scale, float* v_scale, long long* launches, cudaStream_t st);
+                         float* m_scale, float* v_scale, int sms, long long* launches, cudaStream_t st);
 
 // --- beam.cu ---------------------------------------------------------------
 constexpr int kBeamMostBeams = 1024;

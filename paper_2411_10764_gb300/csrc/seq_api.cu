@@ -451,8 +451,8 @@ int mlt_adamw(void* stream, const mlt_adamw_tensor* tensors, int count, const ml
   }
   if (overlap(ranges)) return api_fail(MLT_EINVAL, "parameters, copies and moments must not overlap");
   long long launches = 0;
-  const cudaError_t e =
-      launch_adamw(tensors, count, *rule, m, v, m_scale, v_scale, &launches, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_adamw(tensors, count, *rule, m, v, m_scale, v_scale, api_sm_count(), &launches,
+                                     static_cast<cudaStream_t>(stream));
   return launched(e, launches, "AdamW launch");
 } catch (const std::bad_alloc&) {
   return api_fail(MLT_ENOMEM, "out of host memory for %d tensors", count);

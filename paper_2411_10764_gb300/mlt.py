@@ -386,11 +386,12 @@ def merge_topk(scores, indices, k: int, out=None, stream=None):
 _torch = None
 _DTYPES: dict = {}
 _raw_stream = None
+_current_device = None
 
 
 def _setup():
     """The library and, once, what the calls below need of torch."""
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _current_device
     if _torch is None:
         import torch
 
@@ -398,6 +399,7 @@ def _setup():
         # the handle of the current stream without building a Stream object
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _torch = torch
     return _lib or lib()
 
@@ -754,28 +756,32 @@ def _flat_out(t, name: str, like, dtype):
 
 
 def _one_device(first, *others):
-    """That all tensors lie on first's device, and it is the current one."""
+    """That all tensors lie on first's device, and it is the current one; its number."""
     d = first.get_device()
     for t in others:
         if t is not None and t.get_device() != d:
-            raise ValueError("all tensors must lie on one device")
-    if _torch.cuda.current_device() != d:
+            raise ValueError("all tensors must lie on one CUDA device")
+    if _current_device() != d:
         raise ValueError(f"the tensors lie on device {d}, which is not the current one (torch.cuda.set_device)")
+    return d
 
 
 def _norm_weights(weight, bias, dim):
-    """(type code, address, address)"""
-    code, at = MLT_F32, [None, None]
-    for k, (t, name) in enumerate(((weight, "weight"), (bias, "bias"))):
-        if t is None:
-            continue
-        _cuda(t, name)
-        code = _dtype_code(t)
-        _need(t.shape == (dim,) and t.is_contiguous(), f"{name} must be contiguous, of the shape ({dim},)")
-        at[k] = t.data_ptr()
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
-        raise TypeError("weight and bias must be of one type")
-    return code, at[0], at[1]
+    """(type code, address, address) of vectors of dim values; their device is looked at elsewhere."""
+    code, w, b = MLT_F32, None, None
+    if weight is not None:
+        code, w = _dtype_code(weight), weight.data_ptr()
+        if weight.shape != (dim,) or (dim > 1 and weight.stride(0) != 1):
+            raise ValueError(f"weight must be contiguous, of the shape ({dim},)")
+    if bias is not None:
+        b = bias.data_ptr()
+        if bias.shape != (dim,) or (dim > 1 and bias.stride(0) != 1):
+            raise ValueError(f"bias must be contiguous, of the shape ({dim},)")
+        if weight is None:
+            code = _dtype_code(bias)
+        elif bias.dtype != weight.dtype:
+            raise TypeError("weight and bias must be of one type")
+    return code, w, b
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, out_dtype=None, out=None, total_out=None,
@@ -800,22 +806,25 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, out_
             raise ValueError("residual must have x's shape")
         r, r_stride = _flat(residual, "residual", dim, x.dtype)
     if out is None:
-        y = _torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        y = _like(x) if out_dtype is None or out_dtype is x.dtype else _torch.empty(x.shape, dtype=out_dtype, device=x.device)
         at, y_stride = y.data_ptr(), dim
     else:
         y = out
         at, y_stride = _flat_out(out, "out", x, out_dtype)
     total, t_at, t_stride = x, None, 0
-    if residual is not None:
-        total = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if total_out is None else total_out
-        t_at, t_stride = _flat_out(total, "total_out", x, x.dtype)
-    else:
+    if residual is None:
         _need(total_out is None, "total_out needs a residual")
+    elif total_out is None:
+        total = _like(x)
+        t_at, t_stride = total.data_ptr(), dim
+    else:
+        total = total_out
+        t_at, t_stride = _flat_out(total, "total_out", x, x.dtype)
     stats = _torch.empty((*x.shape[:-1], 2), dtype=_torch.float32, device=x.device)
-    _one_device(x, weight, bias, residual, y, total)
+    d = _one_device(x, weight, bias, residual, y, total)
     a = NormArgs(code, _dtype_code(y), w_code, dim, flat.shape[0], flat.data_ptr(), None if r is None else r.data_ptr(), w, b,
                  stride, r_stride, at, t_at, y_stride, t_stride, stats.data_ptr(), eps)
-    rc = L.mlt_layer_norm(_stream_of(x), C.byref(a))
+    rc = L.mlt_layer_norm(_raw_stream(d), C.byref(a))
     if rc:
         _check(rc)
     return y, total, stats
@@ -842,19 +851,24 @@ def layer_norm_grad(gy, x, stats, weight=None, bias=None, g_total=None, out=None
     t, t_stride = (None, 0) if g_total is None else _flat(g_total, "g_total", dim, x.dtype)
     w_code, w, b = _norm_weights(weight, bias, dim)
     s = _plain(stats, "stats", _torch.float32, (*x.shape[:-1], 2))
-    g = {"x": _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out, "weight": None, "bias": None}
-    at, x_stride = _flat_out(g["x"], "out", x, x.dtype)
+    if out is None:
+        gx = _like(x)
+        at, x_stride = gx.data_ptr(), dim
+    else:
+        gx = out
+        at, x_stride = _flat_out(out, "out", x, x.dtype)
+    g = {"x": gx, "weight": None, "bias": None}
     if weight is not None:
         g["weight"] = _like(weight)
     if bias is not None:
         g["bias"] = _like(bias)
-    _one_device(x, gy, stats, weight, bias, g_total, out)
+    d = _one_device(x, gy, stats, weight, bias, g_total, out)
     a = NormArgs(code, _dtype_code(gy), w_code, dim, rows, flat.data_ptr(), None, w, b, stride, 0, None, None, 0, 0, s, 0.0)
     q = NormGrads(gy.data_ptr(), None if t is None else t.data_ptr(), gy_stride, t_stride, at, x_stride,
                   None if weight is None else g["weight"].data_ptr(), None if bias is None else g["bias"].data_ptr())
     ws, n_ws = (None, 0) if weight is None and bias is None else _workspace(
         ("layer_norm_grad", rows, dim), lambda o: L.mlt_layer_norm_grad_workspace(rows, dim, C.byref(o)), x.device)
-    rc = L.mlt_layer_norm_grad(_stream_of(x), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
+    rc = L.mlt_layer_norm_grad(_raw_stream(d), C.byref(a), C.byref(q), None if ws is None else ws.data_ptr(), n_ws)
     if rc:
         _check(rc)
     return g
@@ -953,40 +967,47 @@ def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), e
     decays = _per_tensor(weight_decay, count, "weight_decay")
     if isinstance(lr_scale, (list, tuple)) or lr_scale != 1.0:
         rates = [a * b for a, b in zip(rates, _per_tensor(lr_scale, count, "lr_scale"))]
-    device, codes, kept = m.get_device(), _DTYPES, []
-    words, blocks = [], 0
-    for p, g, rate, decay, copy in zip(params, grads, rates, decays, copies or [None] * count):
-        n = p.numel()
-        blocks += -(-n // ADAMW_BLOCK)
-        if g is None:
-            words += (0, 0, 0, n, 0, 0)
-            continue
-        if p.get_device() != device or g.get_device() != device:
-            raise ValueError("parameters, gradients and moments must lie on one CUDA device")
-        if not p.is_contiguous():
-            raise ValueError("parameters must be contiguous")
-        if g.shape != p.shape:
-            raise ValueError("a gradient must have its parameter's shape")
-        if not g.is_contiguous():
-            g = g.contiguous()
-            kept.append(g)
-        try:
-            kinds = codes[p.dtype] | codes[g.dtype] << 16
-            to = 0
-            if copy is not None:
-                kinds |= codes[copy.dtype] << 32
-                if copy.shape != p.shape or not copy.is_contiguous() or copy.get_device() != device:
-                    raise ValueError("a copy must be contiguous, of its parameter's shape and device")
-                to = copy.data_ptr()
-        except KeyError as e:
-            raise TypeError(f"float32, bfloat16 or float16 wanted, got {e.args[0]}") from None
-        words += (p.data_ptr(), g.data_ptr(), to, n, kinds, _rate_words.get((rate, decay)) or _rate_word(rate, decay))
+    device, Tensor = m.get_device(), torch.Tensor
+    missing = [k for k, g in enumerate(grads) if g is None]
+    if missing:  # their parameters stand in for them, and have no address below
+        grads = [p if g is None else g for p, g in zip(params, grads)]
+    given = [params, grads] if copies is None else [params, grads, copies]
+    for some in given:
+        if any(d != device for d in map(Tensor.get_device, some)):
+            raise ValueError("parameters, gradients, copies and moments must lie on one CUDA device")
+    if not all(map(Tensor.is_contiguous, params)) or not (copies is None or all(map(Tensor.is_contiguous, copies))):
+        raise ValueError("parameters and copies must be contiguous")
+    shapes = [p.shape for p in params]
+    if any([t.shape for t in some] != shapes for some in given[1:]):
+        raise ValueError("a gradient and a copy must have their parameter's shape")
+    if not all(map(Tensor.is_contiguous, grads)):
+        grads = given[1] = [g.contiguous() for g in grads]  # kept until the launch
+    kinds, mixed = 0, None
+    for k, some in enumerate(given):
+        types = {t.dtype for t in some}
+        if not types <= _DTYPES.keys():
+            raise TypeError(f"float32, bfloat16 or float16 wanted, got {(types - _DTYPES.keys()).pop()}")
+        if len(types) == 1:
+            kinds += _DTYPES[types.pop()] << 16 * k
+        elif types:
+            mixed = [x + (_DTYPES[t.dtype] << 16 * k) for x, t in zip(mixed or [0] * count, some)]
+    words = list(map(_rate_words.get, zip(rates, decays)))
+    if None in words:
+        words = [_rate_word(a, b) for a, b in zip(rates, decays)]
+    table = array("q", bytes(48 * count))
+    for k, some in enumerate(given):
+        table[k::6] = array("q", map(Tensor.data_ptr, some))
+    table[3::6] = sizes = array("q", map(Tensor.numel, params))
+    table[4::6] = array("q", [kinds] * count if mixed is None else [x + kinds for x in mixed])
+    table[5::6] = array("q", words)
+    blocks = int((-(-np.frombuffer(sizes, np.int64) // ADAMW_BLOCK)).sum()) if count else 0
+    for k in missing:
+        table[6 * k + 1] = 0
     _need(m.numel() == v.numel() == blocks * ADAMW_BLOCK and (ms is None or ms.numel() == vs.numel() == blocks),
           "the moments are of other parameters")
-    _one_device(m, v, ms, vs, *(t for t in (step, lr, grad_scale) if isinstance(t, torch.Tensor)))
-    table = array("q", words)
+    _one_device(m, v, ms, vs, *[t for t in (step, lr, grad_scale) if isinstance(t, Tensor)])
     rule = AdamWRule(betas[0], betas[1], eps, 0 if scalars[0] is not None else int(step), *scalars, bits, seed & 0xFFFFFFFF)
-    rc = L.mlt_adamw(_stream_of(m), table.buffer_info()[0], count, C.byref(rule), m.data_ptr(), v.data_ptr(),
+    rc = L.mlt_adamw(_raw_stream(device), table.buffer_info()[0], count, C.byref(rule), m.data_ptr(), v.data_ptr(),
                      None if ms is None else ms.data_ptr(), None if vs is None else vs.data_ptr())
     if rc:
         _check(rc)
@@ -1017,15 +1038,17 @@ def beam_step(scores, logp, m: int, done=None, eos: int = -1, normalised: bool =
     lp = _plain(logp, "logp", torch.float32, (batch, beams))
     d = None if done is None else _plain(done, "done", torch.uint8 if done.dtype == torch.uint8 else torch.bool, (batch, beams))
     device = scores.device
-    parent, token = torch.empty((2, batch, m), dtype=torch.int64, device=device)
-    out = torch.empty(batch, m, dtype=torch.float32, device=device)
-    ended = torch.empty(batch, m, dtype=torch.bool, device=device)
-    _one_device(scores, logp, done)
+    size = (batch, m)
+    parent = torch.empty(size, dtype=torch.int64, device=device)
+    token = torch.empty(size, dtype=torch.int64, device=device)
+    out = torch.empty(size, dtype=torch.float32, device=device)
+    ended = torch.empty(size, dtype=torch.bool, device=device)
+    on = _one_device(scores, logp, done)
     a = BeamArgs(code, batch, beams, n, m, 1 if normalised else 0, eos, scores.data_ptr(), strides[0], strides[1], lp, d,
                  parent.data_ptr(), token.data_ptr(), out.data_ptr(), ended.data_ptr())
     ws, n_ws = _workspace(("beam", code, batch, beams, n, m), lambda q: L.mlt_beam_step_workspace(C.byref(a), C.byref(q)),
                           device)
-    rc = L.mlt_beam_step(_stream_of(scores), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
+    rc = L.mlt_beam_step(_raw_stream(on), C.byref(a), None if ws is None else ws.data_ptr(), n_ws)
     if rc:
         _check(rc)
     return (parent[0], token[0], out[0], ended[0]) if one else (parent, token, out, ended)
@@ -1044,13 +1067,18 @@ def beam_reorder(parent, *tensors, stream=None) -> None:
     batch, beams = (1, *parent.shape) if parent.dim() == 1 else parent.shape
     rows = batch * beams
     _need(batch <= _INT_MAX and beams <= _INT_MAX, "batch must lie in [0, 65535], beams in [1, 1024]")
-    moves = (BeamState * len(tensors))()
-    for k, t in enumerate(tensors):
-        _cuda(t, "states")
+    words = []
+    on = _one_device(parent, *tensors)
+    for t in tensors:
         shape = t.shape
-        _need(len(shape) > 0 and (shape[0] == rows or tuple(shape[:2]) == (batch, beams)),
-              "states must be [batch * beams][...] or [batch][beams][...]")
-        if t.numel() == 0:
+        if len(shape) == 0 or (shape[0] != rows and tuple(shape[:2]) != (batch, beams)):
+            raise ValueError("states must be [batch * beams][...] or [batch][beams][...]")
+        n = t.numel()
+        if n == 0:
+            continue
+        size = t.element_size()
+        if t.is_contiguous():
+            words += (t.data_ptr(), n * size // rows, n * size // rows)
             continue
         try:
             flat = t.view(rows, -1)
@@ -1058,10 +1086,9 @@ def beam_reorder(parent, *tensors, stream=None) -> None:
             raise ValueError("the elements of a state's row must be adjacent, its rows at one distance") from None
         stride, column = flat.stride()
         _need(column == 1 or flat.shape[1] == 1, "the elements of a state's row must be adjacent")
-        size = t.element_size()
-        moves[k] = BeamState(t.data_ptr(), flat.shape[1] * size, stride * size)
-    _one_device(parent, *tensors)
-    rc = L.mlt_beam_reorder(_stream_of(parent), parent.data_ptr(), batch, beams, moves, len(tensors))
+        words += (t.data_ptr(), flat.shape[1] * size, stride * size)
+    moves = array("q", words)  # mlt_beam_state records
+    rc = L.mlt_beam_reorder(_raw_stream(on), parent.data_ptr(), batch, beams, moves.buffer_info()[0], len(words) // 3)
     if rc:
         _check(rc)
 
