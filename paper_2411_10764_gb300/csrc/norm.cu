@@ -15,25 +15,24 @@ namespace {
 constexpr int kMostThreads = 512;
 
 // The fewest without spills of consequence (edges in packs of 16-bit values: up to 84 bytes at eight less).
-constexpr int registers(bool cta, bool edge) { return cta ? (edge ? 80 : 72) : (edge ? 104 : 96); }
+constexpr int registers(bool cta, bool edge) { return cta ? 80 : edge ? 104 : 96; }
 
-// CTA: the CTA, or its cluster with `seg` places a CTA, takes a row; else groups of `lanes` lanes do.
+// CTA: the CTA takes a row; else groups of `lanes` lanes do.
 template <typename TI, typename TO, int V, int C, bool CTA, bool EDGE>
 __global__ void __maxnreg__(registers(CTA, EDGE))
-    k_norm(const __grid_constant__ mlt_norm_args a, int lanes, int seg, int skew, int skew_step) {
+    k_norm(const __grid_constant__ mlt_norm_args a, int lanes, int skew, int skew_step) {
   extern __shared__ __align__(16) float affine[];
   __shared__ RowSums<1> sums;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
-  const int ranks = CTA ? cluster_ranks() : 1, rank = CTA ? cluster_rank() : 0;
   const int j = CTA ? threadIdx.x : threadIdx.x & (lanes - 1);
   const int in_warp = CTA ? 1 : 32 / lanes;  // rows a warp
-  const long long step = CTA ? gridDim.x / ranks : static_cast<long long>(gridDim.x) * 8 * in_warp;
+  const long long step = CTA ? gridDim.x : static_cast<long long>(gridDim.x) * 8 * in_warp;
   const int sub = CTA ? 0 : (threadIdx.x & 31) / lanes;
-  long long base = CTA ? blockIdx.x / ranks : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
+  long long base = CTA ? blockIdx.x : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
   if (EDGE) skew = static_cast<int>((skew + (base + sub) % V * skew_step) % V);  // of all rows of this thread
-  const Columns<V, C, EDGE> cols(rank * seg + j * V, lanes * V, (rank + 1) * seg, skew, a.dim);
+  const Columns<V, C, EDGE> cols(j * V, lanes * V, skew, a.dim);
   const bool scaled = a.weight != nullptr || a.bias != nullptr;
   const Kept<V, C> ws{affine}, bs{affine + blockDim.x * C * V};
   const bool add = a.residual != nullptr;
@@ -58,7 +57,6 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
   if (CTA) {
     sums.clear();
     __syncthreads();
-    if (ranks > 1) cluster_barrier();  // every CTA runs before its memory is written to
   }
   for (; base < a.rows; base += step) {
     const long long row = base + sub;
@@ -80,18 +78,15 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float s = 0.0f;
-      cols.each(
-          c,
-          [&](int c, int v) {
-            t[c][v] = live ? px[c].get(v) : 0.0f;
-            s += t[c][v];
-          },
-          [&](int c, int v) { t[c][v] = 0.0f; });
+      cols.template each<CTA>(c, [&](int c, int v, bool on) {
+        t[c][v] = on && live ? px[c].get(v) : 0.0f;
+        s += t[c][v];
+      });
       total[0] += s;
     }
     if (base + step < a.rows) fetch(row + step);
     if (CTA)
-      row_sums(total, sums, slot, ranks, rank);
+      row_sums(total, sums, slot);
     else
       group_sums(total, lanes);
     const float mean = total[0] / a.dim;
@@ -99,22 +94,19 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float s = 0.0f;
-      cols.each(
-          c,
-          [&](int c, int v) {
-            t[c][v] -= mean;
-            s = fmaf(t[c][v], t[c][v], s);
-          },
-          [](int, int) {});
+      cols.template each<CTA>(c, [&](int c, int v, bool on) {
+        t[c][v] = on ? t[c][v] - mean : 0.0f;
+        s = fmaf(t[c][v], t[c][v], s);
+      });
       total[0] += s;
     }
     if (CTA)
-      row_sums(total, sums, slot, ranks, rank);
+      row_sums(total, sums, slot);
     else
       group_sums(total, lanes);
     const float rstd = 1.0f / sqrtf(total[0] / a.dim + a.eps);
     if (!live) continue;
-    if (a.stats != nullptr && j == 0 && rank == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
+    if (a.stats != nullptr && j == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
     TO* to = static_cast<TO*>(a.y) + row * a.y_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -135,50 +127,102 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
   }
 }
 
-// Rows that no cluster holds: a CTA reads the row three times.
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kMostThreads) k_norm_long(const __grid_constant__ mlt_norm_args a) {
+// Rows that a CTA's registers do not hold: in shared memory (`kept`), each thread's packs in places of its own, or
+// where that does not hold them either, read again for each pass.
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(kMostThreads, 2)
+    k_norm_long(const __grid_constant__ mlt_norm_args a, int kept, int skew0, int skew_step) {
+  extern __shared__ __align__(16) float affine[];
+  TI* held = reinterpret_cast<TI*>(affine);
   __shared__ RowSums<1> sums;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
   sums.clear();
   __syncthreads();
+  const float inv_dim = 1.0f / a.dim;
+  const bool add = a.residual != nullptr;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int skew = static_cast<int>((skew0 + row % V * skew_step) % V), first = static_cast<int>(threadIdx.x) * V - skew;
     const TI* x = static_cast<const TI*>(a.x) + row * a.x_stride;
     const TI* r = static_cast<const TI*>(a.residual) + row * a.residual_stride;
-    TI* to = a.total == nullptr ? nullptr : static_cast<TI*>(a.total) + row * a.total_stride;
+    TI* to = static_cast<TI*>(a.total) + row * a.total_stride;
     TO* y = static_cast<TO*>(a.y) + row * a.y_stride;
     // the first pass may write total over x or residual: later ones read what it wrote, each thread its own
-    const bool stored = to != nullptr;
-    auto value = [&](int i, bool again) {
-      if (again && stored) return to_f32(to[i]);
-      float t = to_f32(x[i]);
-      if (a.residual != nullptr) t = to_f32(from_f32<TI>(__fadd_rn(t, to_f32(r[i]))));
-      return t;
+    const bool stored = a.total != nullptr;
+    auto values = [&](float (&t)[V], int col, bool again) {
+      if (again && kept) {
+        Vec<TI, V> q;
+        q.load(held + (col + skew));
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] = q.get(v);
+        return;
+      }
+      if (again && stored) {
+        load_some<V>(t, to, col, a.dim);
+        return;
+      }
+      load_some<V>(t, x, col, a.dim);
+      if (!add) return;
+      float e[V];
+      load_some<V>(e, r, col, a.dim);
+#pragma unroll
+      for (int v = 0; v < V; ++v) t[v] = to_f32(from_f32<TI>(__fadd_rn(t[v], e[v])));
     };
     float total[1] = {0.0f};
-    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
-      const float t = value(i, false);
-      if (stored) to[i] = from_f32<TI>(t);
-      total[0] += t;
+#pragma unroll 4
+    for (int col = first; col < a.dim; col += kMostThreads * V) {
+      float t[V], s = 0.0f;
+      values(t, col, false);
+      if (stored) store_some<V>(t, to, col, a.dim);
+      if (kept) {
+        Vec<TI, V> q;
+        q.put(t);
+        q.store(held + (col + skew));
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) s += t[v];
+      total[0] += s;
     }
-    row_sums(total, sums, slot, 1, 0);
-    const float mean = total[0] / a.dim;
+    row_sums(total, sums, slot);
+    const float mean = total[0] * inv_dim;
     total[0] = 0.0f;
-    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
-      const float t = value(i, true) - mean;
-      total[0] = fmaf(t, t, total[0]);
+#pragma unroll 2
+    for (int col = first; col < a.dim; col += kMostThreads * V) {
+      float t[V], s = 0.0f;
+      values(t, col, true);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float d = V == 1 || (col + v >= 0 && col + v < a.dim) ? t[v] - mean : 0.0f;
+        s = fmaf(d, d, s);
+      }
+      total[0] += s;
     }
-    row_sums(total, sums, slot, 1, 0);
-    const float rstd = 1.0f / sqrtf(total[0] / a.dim + a.eps);
+    row_sums(total, sums, slot);
+    const float rstd = 1.0f / sqrtf(total[0] * inv_dim + a.eps);
     if (a.stats != nullptr && threadIdx.x == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
-    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
-      const float w = a.weight != nullptr ? load_as_f32(a.weight, a.w_dtype, i) : 1.0f;
-      const float b = a.bias != nullptr ? load_as_f32(a.bias, a.w_dtype, i) : 0.0f;
-      y[i] = from_f32<TO>(fmaf((value(i, true) - mean) * rstd, w, b));
+#pragma unroll 2
+    for (int col = first; col < a.dim; col += kMostThreads * V) {
+      float t[V], w[V], b[V];
+      values(t, col, true);
+      load_weights<V>(w, a.weight, a.w_dtype, col, a.dim, 1.0f);
+      load_weights<V>(b, a.bias, a.w_dtype, col, a.dim, 0.0f);
+#pragma unroll
+      for (int v = 0; v < V; ++v) t[v] = fmaf((t[v] - mean) * rstd, w[v], b[v]);
+      store_some<V>(t, y, col, a.dim);
     }
   }
+}
+
+template <typename TI, typename TO, int V>
+cudaError_t launch_long(const mlt_norm_args& a, const Skew& skew, int sms, cudaStream_t st) {
+  size_t smem = (static_cast<size_t>(a.dim) + 2 * V) / V * V * sizeof(TI);
+  const bool kept = smem <= 224 * 1024;
+  if (!kept) smem = 0;
+  const int per_sm = 2 * (smem + 2048) <= 227 * 1024 ? 2 : 1;
+  const long long most = static_cast<long long>(per_sm) * sms;
+  return launch_rows(k_norm_long<TI, TO, V>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMostThreads, smem, st, a,
+                     kept ? 1 : 0, skew.first, skew.step);
 }
 
 // E: values of a row a thread.
@@ -191,23 +235,18 @@ cudaError_t launch_as(const mlt_norm_args& a, const Skew& skew, int sms, cudaStr
     while (lanes * E < places) lanes *= 2;
     const long long per = 8 * (32 / lanes), need = (a.rows + per - 1) / per;
     const long long most = static_cast<long long>(sms) * resident_ctas<kernel>(256, 0);
-    return launch_cluster(kernel, static_cast<unsigned>(need < most ? need : most), 256, 1, 0, st, a, lanes, places,
-                          skew.first, skew.step);
+    return launch_rows(kernel, static_cast<unsigned>(need < most ? need : most), 256, 0, st, a, lanes, skew.first,
+                       skew.step);
   }
   constexpr auto kernel = k_norm<TI, TO, V, E / V, true, EDGE>;
-  // CTAs of 256 threads leave room for one another's barriers; longer rows take clusters, then larger CTAs
-  int ranks = (places + kMostThreads * E - 1) / (kMostThreads * E);
-  if (ranks > kNormMaxCluster) ranks = kNormMaxCluster;
-  const int seg = ((places + ranks - 1) / ranks + V - 1) / V * V;
-  ranks = (places + seg - 1) / seg;
-  const int threads = ((seg + E - 1) / E + 31) / 32 * 32;
+  if (places > kMostThreads * E) return launch_long<TI, TO, V>(a, skew, sms, st);
+  const int threads = ((places + E - 1) / E + 31) / 32 * 32;
   const size_t smem = a.weight != nullptr || a.bias != nullptr ? 2 * sizeof(float) * threads * E : 0;
-  long long most = static_cast<long long>(sms) * resident_ctas<kernel>(threads, smem) / ranks;
+  long long most = static_cast<long long>(sms) * resident_ctas<kernel>(threads, smem);
   const int period = skew.period(V);
   most = most < period ? period : most / period * period;
-  const long long teams = a.rows < most ? a.rows : most;
-  return launch_cluster(kernel, static_cast<unsigned>(teams * ranks), threads, ranks, smem, st, a, threads, seg, skew.first,
-                        skew.step);
+  return launch_rows(kernel, static_cast<unsigned>(a.rows < most ? a.rows : most), threads, smem, st, a, threads,
+                     skew.first, skew.step);
 }
 
 }  // namespace
@@ -223,11 +262,6 @@ cudaError_t launch_norm(const mlt_norm_args& a, int sms, long long* launches, cu
     skew.add(a.residual, a.residual_stride, sizeof(TI), V);
     skew.add(a.total, a.total_stride, sizeof(TI), V);
     skew.add(a.y, a.y_stride, sizeof(TO), V);
-    if (a.dim + V > kNormMaxCluster * kMostThreads * (skew.same ? E : 8)) {
-      const long long most = 4LL * sms;
-      return launch_cluster(k_norm_long<TI, TO>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMostThreads, 1, 0,
-                            st, a);
-    }
     if (!skew.same) return launch_as<TI, TO, 1, 8, false>(a, Skew{true, 0, 0}, sms, st);
     return skew.edges(a.dim, V) ? launch_as<TI, TO, V, E, true>(a, skew, sms, st)
                                 : launch_as<TI, TO, V, E, false>(a, skew, sms, st);

@@ -4,9 +4,9 @@
 // A row is held in registers, E values a thread, so it is read once:
 //   short rows      a power-of-two group of lanes a row, several rows a warp, sums by shuffles;
 //   longer ones     a CTA a row, sums by shuffles and one barrier each;
-//   longer still    a cluster of up to eight CTAs a row, which exchange their sums through
-//                   distributed shared memory;
-//   the rest        a CTA a row that reads it from memory once for each pass.
+//   the rest        a CTA a row that keeps it in shared memory or reads it again out of L2.  (Clusters of CTAs with
+//                   a row in their registers wait for all their stores at each of two barriers a row:
+//                   4,096 x 16,384 bf16 154 us by two CTAs a row, 216 by four.)
 // What costs beside memory is the work for each row and thread (shuffles, barrier, addresses: some 100
 // instructions), so threads take many values: 16,384 x 4,096 bf16 with eight a thread 136 us and 46
 // instructions a value, with 32 see norm.cu.
@@ -23,7 +23,6 @@
 
 namespace mlt {
 
-constexpr int kNormMaxCluster = 8;
 constexpr int kNormMostWarps = 16;
 
 // How the rows of some tensors lie towards 16-byte boundaries, in values: (skew + row * step) mod the values
@@ -74,27 +73,12 @@ __device__ __forceinline__ void store_from_f32(void* p, int dtype, long long i, 
     static_cast<float*>(p)[i] = v;
 }
 
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ unsigned cluster_ranks() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-
 // Sums of N values over the threads of a row, the same in each of them.  Slots are used in turn, so one
 // barrier a sum is enough: who writes a slot again has passed the barrier of the
 // sum in between, which no thread reaches before it has read the slot.
 template <int N>
 struct RowSums {
   float4 warps[2][N][kNormMostWarps / 4];
-  float peers[2][N][kNormMaxCluster];
   __device__ __forceinline__ void clear() {  // before the first sum, with a barrier in between
     float* w = reinterpret_cast<float*>(warps);
     for (int i = threadIdx.x; i < 2 * N * kNormMostWarps; i += blockDim.x) w[i] = 0.0f;
@@ -116,7 +100,7 @@ __device__ __forceinline__ void warp_sums(float (&v)[N]) {
 }
 
 template <int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], RowSums<N>& s, int& slot, int ranks, int rank) {
+__device__ __forceinline__ void row_sums(float (&v)[N], RowSums<N>& s, int& slot) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, fours = (blockDim.x + 127) / 128;
   warp_sums(v);
   if (blockDim.x > 32) {
@@ -131,24 +115,6 @@ __device__ __forceinline__ void row_sums(float (&v)[N], RowSums<N>& s, int& slot
         const float4 q = s.warps[slot][i][w];
         v[i] += (q.x + q.y) + (q.z + q.w);
       }
-    }
-  }
-  if (ranks > 1) {
-    if (threadIdx.x < ranks) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const unsigned mine = static_cast<unsigned>(__cvta_generic_to_shared(&s.peers[slot][i][rank]));
-        unsigned there;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(threadIdx.x));
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v[i]) : "memory");
-      }
-    }
-    cluster_barrier();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float all = 0.0f;
-      for (int r = 0; r < ranks; ++r) all += s.peers[slot][i][r];
-      v[i] = all;
     }
   }
   slot ^= 1;
@@ -232,13 +198,12 @@ struct Columns {
   int hop;
   int mask[C];   // by value of a pack; not EDGE: 0 or all
 
-  // pos: the thread's first place, counted from the boundary before the row; end: of the CTA's places
-  __device__ __forceinline__ Columns(int pos, int hop_, int end, int skew, int dim) : first(pos - skew), hop(hop_) {
+  // pos: the thread's first place, counted from the boundary before the row
+  __device__ __forceinline__ Columns(int pos, int hop_, int skew, int dim) : first(pos - skew), hop(hop_) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = first + c * hop;
       mask[c] = 0;
-      if (pos + c * hop >= end) continue;
       if (!EDGE) {
         if (col < dim) mask[c] = (1 << V) - 1;
       } else {
@@ -279,19 +244,15 @@ struct Columns {
       }
     }
   }
-  // f(c, v) for each of the thread's values, g(c, v) for the other places of its packs.
-  template <typename F, typename G>
-  __device__ __forceinline__ void each(int c, F f, G g) const {
-    if (whole(c)) {
+  // f(c, v, whether it is a value of the row) for each place.  BRANCH: whole packs apart, where few have edges.
+  template <bool BRANCH, typename F>
+  __device__ __forceinline__ void each(int c, F f) const {
+    if ((BRANCH || !EDGE) && whole(c)) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) f(c, v);
+      for (int v = 0; v < V; ++v) f(c, v, true);
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (EDGE && on(c, v))
-          f(c, v);
-        else
-          g(c, v);
+      for (int v = 0; v < V; ++v) f(c, v, EDGE && on(c, v));
     }
   }
   template <typename T>
@@ -305,6 +266,54 @@ struct Columns {
         if (on(c, v)) p.store_one(at + v, v);
     }
   }
+};
+
+// Packs on their way to shared memory, each thread's to places of its own, so that a thread's own wait is all
+// it takes.  kAhead rows of up to three tensors.
+constexpr int kAhead = 3;
+template <int V, int C>
+struct Ring {
+  static constexpr int kBytes = kAhead * (3 * C * 16 + 8);  // a thread
+  unsigned char* at;  // of the CTA
+
+  __device__ __forceinline__ unsigned char* pack(int stage, int tensor, int c) const {
+    return at + ((((stage * 3 + tensor) * C + c) * static_cast<int>(blockDim.x)) + threadIdx.x) * 16;
+  }
+  __device__ __forceinline__ float2* pair(int stage) const {
+    return reinterpret_cast<float2*>(at + kAhead * 3 * C * 16 * blockDim.x) + stage * blockDim.x + threadIdx.x;
+  }
+  template <int BYTES>
+  static __device__ __forceinline__ void copy(void* to, const void* from) {
+    const unsigned s = static_cast<unsigned>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+    else
+      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
+  }
+  // begin, end: as for Columns::load
+  template <typename T, bool EDGE>
+  __device__ __forceinline__ void fetch(const Columns<V, C, EDGE>& cols, int stage, int tensor, const T* row,
+                                        const T* begin, const T* end) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const T* from = row + cols.first + c * cols.hop;
+      if (cols.mask[c] == 0) continue;
+      if (!EDGE || cols.whole(c) || (from >= begin && from + V <= end))
+        copy<V * sizeof(T)>(pack(stage, tensor, c), from);
+      else
+#pragma unroll 1
+        for (int v = 0; v < V; ++v)
+          if (cols.on(c, v)) reinterpret_cast<T*>(pack(stage, tensor, c))[v] = from[v];
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ Vec<T, V> get(int stage, int tensor, int c) const {
+    Vec<T, V> q;
+    q.load(reinterpret_cast<const T*>(pack(stage, tensor, c)));
+    return q;
+  }
+  static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  static __device__ __forceinline__ void wait_oldest() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory"); }
 };
 
 // One value per column of a thread as fp32; all loads under way at once.
@@ -359,6 +368,63 @@ struct Kept {
   }
 };
 
+// A pack at a column that may lie before the row or reach past its end: 0 there.
+template <int V, typename T>
+__device__ __forceinline__ void load_some(float (&f)[V], const T* row, int col, int dim) {
+  if (col >= 0 && col + V <= dim) {
+    Vec<T, V> q;
+    q.load(row + col);
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = q.get(v);
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) f[v] = col + v >= 0 && col + v < dim ? to_f32(row[col + v]) : 0.0f;
+  }
+}
+template <int V, typename T>
+__device__ __forceinline__ void store_some(const float (&f)[V], T* row, int col, int dim) {
+  if (col >= 0 && col + V <= dim) {
+    Vec<T, V> q;
+    q.put(f);
+    q.store(row + col);
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (col + v >= 0 && col + v < dim) row[col + v] = from_f32<T>(f[v]);
+  }
+}
+template <int V>
+__device__ __forceinline__ void load_weights(float (&w)[V], const void* p, int dtype, int col, int dim, float none) {
+  if (p == nullptr) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) w[v] = none;
+    return;
+  }
+  auto with = [&](auto t) {
+    using T = decltype(t);
+    const T* from = static_cast<const T*>(p);
+    if (col >= 0 && col + V <= dim && reinterpret_cast<uintptr_t>(from + col) % 16 == 0 && V * sizeof(T) % 16 == 0) {
+      constexpr int P = 16 / sizeof(T) < V ? 16 / sizeof(T) : V;
+#pragma unroll
+      for (int k = 0; k < V / P; ++k) {
+        Vec<T, P> q;
+        q.load(from + col + k * P);
+#pragma unroll
+        for (int v = 0; v < P; ++v) w[k * P + v] = q.get(v);
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) w[v] = col + v >= 0 && col + v < dim ? to_f32(from[col + v]) : none;
+    }
+  };
+  if (dtype == MLT_BF16)
+    with(__nv_bfloat16());
+  else if (dtype == MLT_F16)
+    with(__half());
+  else
+    with(float());
+}
+
 // How many CTAs of `threads` threads and `smem` bytes an SM holds.
 template <auto kernel>
 int resident_ctas(int threads, size_t smem) {
@@ -374,30 +440,15 @@ int resident_ctas(int threads, size_t smem) {
   return n < 1 ? 1 : n > 32 ? 32 : n;
 }
 
-// A launch that may begin while the kernel before it ends (pdl_wait in the kernel), in clusters.
+// A launch that may begin while the kernel before it ends (pdl_wait in the kernel).
 template <typename... K, typename... A>
-cudaError_t launch_cluster(void (*kernel)(K...), unsigned grid, unsigned block, unsigned cluster, size_t smem,
-                           cudaStream_t st, A&&... args) {
+cudaError_t launch_rows(void (*kernel)(K...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, A&&... args) {
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster;
-  at[1].val.clusterDim.y = 1;
-  at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+  return launch_pdl(kernel, dim3(grid), dim3(block), smem, st, std::forward<A>(args)...);
 }
 #endif
 

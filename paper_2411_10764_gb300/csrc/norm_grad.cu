@@ -4,8 +4,10 @@
 // input's gradient.  Each thread keeps its columns' sums of gy h and gy in registers over
 // all rows of its team; the teams' sums go to the workspace and a second
 // kernel adds them up in a fixed order.  Bound: memory (x and gy read, gx written, once).
-// Of n equal terms in a plain sum the error grows with n: where a thread has more than kPlainRows rows, its
-// sums move to pairs of numbers in shared memory every kFlushRows of them (Knuth's exact addition).
+// Of n equal terms in a plain sum the error grows with n: where a thread has more than kPlainRows rows, every
+// so many its sums move on to pairs of numbers in the workspace (Knuth's exact addition), 32 bytes a
+// column that stay in L2.  (In shared memory they halved the warps that fit.)
+// Rows are on their way two ahead, in shared memory: in registers, one ahead, 32,768 x 2,048 took 145 us.
 #include <utility>
 
 #include "norm.cuh"
@@ -14,10 +16,8 @@ namespace mlt {
 namespace {
 
 constexpr int kPlainRows = 48;
-constexpr int kFlushRows = 16;
 constexpr int kMostThreads = 512;
 constexpr int kGroupThreads = 256;
-constexpr int kLongRows = 256;  // rows a partial sum of the columns of long rows
 
 // (s, c) + v, s + c being the sum
 __device__ __forceinline__ void add_exactly(float& s, float& c, float v) {
@@ -26,47 +26,66 @@ __device__ __forceinline__ void add_exactly(float& s, float& c, float v) {
   s = t;
 }
 
-constexpr int registers(bool cta, bool edge) { return cta ? 128 : 128; }
+// The fewest without spills of consequence.
+constexpr int registers(bool cta, int pack) {
+  if (!cta) return 128;
+  return pack == 8 ? 128 : 96;
+}
 
-// As k_norm in norm.cu.  SUMS: weight and bias have gradients; partial: [teams][2][dim]; flush: rows between
-// moves to shared memory, or 0.
+// As k_norm in norm.cu.  SUMS: weight and bias have gradients; partial: [teams][2][dim]; moved: for long sums
+// [CTAs][4][E][threads], else null.
 template <typename TI, typename TO, int V, int C, bool CTA, bool EDGE, bool SUMS>
-__global__ void __maxnreg__(registers(CTA, EDGE))
+__global__ void __maxnreg__(registers(CTA, V))
     k_norm_grad(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g, float* partial,
-                int lanes, int seg, int skew0, int skew_step, int flush) {
+                float* moved, int lanes, int skew0, int skew_step) {
   extern __shared__ __align__(16) float mem[];
   __shared__ RowSums<2> sums;
   constexpr int E = C * V;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
-  const int ranks = CTA ? cluster_ranks() : 1, rank = CTA ? cluster_rank() : 0;
   const int j = CTA ? threadIdx.x : threadIdx.x & (lanes - 1);
   const int in_warp = CTA ? 1 : 32 / lanes;
-  const long long step = CTA ? gridDim.x / ranks : static_cast<long long>(gridDim.x) * 8 * in_warp;
+  const long long step = CTA ? gridDim.x : static_cast<long long>(gridDim.x) * 8 * in_warp;
   const int sub = CTA ? 0 : (threadIdx.x & 31) / lanes;
-  const long long base0 = CTA ? blockIdx.x / ranks : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
+  const long long base0 = CTA ? blockIdx.x : (blockIdx.x * 8LL + (threadIdx.x >> 5)) * in_warp;
   const int skew = EDGE ? static_cast<int>((skew0 + (base0 + sub) % V * skew_step) % V) : 0;
-  const Columns<V, C, EDGE> cols(rank * seg + j * V, lanes * V, (rank + 1) * seg, skew, a.dim);
+  const Columns<V, C, EDGE> cols(j * V, lanes * V, skew, a.dim);
   const bool scaled = a.weight != nullptr;
   const Kept<V, C> ws{mem};
-  float* moved = CTA && scaled ? mem + blockDim.x * E : mem;  // [2 sums][2][E][threads]
   float w[C][V], sw[C][V], sb[C][V];
   const bool more = g.g_total != nullptr;
+  const float inv_dim = 1.0f / a.dim;
   const TI *x0 = static_cast<const TI*>(a.x), *t0 = static_cast<const TI*>(g.g_total);
   const TO* g0 = static_cast<const TO*>(g.gy);
   const TI *x1 = x0 + (a.rows - 1) * a.x_stride + a.dim, *t1 = t0 + (a.rows - 1) * g.g_total_stride + a.dim;
   const TO* g1 = g0 + (a.rows - 1) * g.gy_stride + a.dim;
+  // rows ahead: a CTA's packs in shared memory, two rows of them; else in registers, one (short rows of 61 fp32
+  // values 149 us so, 173 through shared memory)
+  constexpr bool kInRing = CTA && V > 1;
+  const Ring<V, C> ring{reinterpret_cast<unsigned char*>(scaled ? mem + blockDim.x * E : mem)};
   Vec<TI, V> px[C], pt[C];
   Vec<TO, V> pg[C];
   float2 next = make_float2(0.0f, 0.0f);
-  auto fetch = [&](long long row) {
-    if (row >= a.rows) return;
-    cols.load(px, x0 + row * a.x_stride, x0, x1);
-    cols.load(pg, g0 + row * g.gy_stride, g0, g1);
-    next = *reinterpret_cast<const float2*>(a.stats + 2 * row);
+  auto fetch = [&](long long row, int stage) {
+    if constexpr (kInRing) {
+      if (row < a.rows) {
+        ring.fetch(cols, stage, 0, x0 + row * a.x_stride, x0, x1);
+        ring.fetch(cols, stage, 1, g0 + row * g.gy_stride, g0, g1);
+        if (more) ring.fetch(cols, stage, 2, t0 + row * g.g_total_stride, t0, t1);
+        ring.template copy<8>(ring.pair(stage), a.stats + 2 * row);
+      }
+      ring.commit();
+    } else if (row < a.rows) {
+      cols.load(px, x0 + row * a.x_stride, x0, x1);
+      cols.load(pg, g0 + row * g.gy_stride, g0, g1);
+      next = *reinterpret_cast<const float2*>(a.stats + 2 * row);
+    }
   };
-  fetch(base0 + sub);
+  fetch(base0 + sub, 0);
+  if (kInRing)
+#pragma unroll
+    for (int d = 1; d < kAhead - 1; ++d) fetch(base0 + sub + d * step, d);
   if (!CTA || scaled) {
     load_columns(w, cols, a.weight, a.w_dtype, 1.0f);
     if (CTA) ws.put(w);
@@ -75,66 +94,86 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int v = 0; v < V; ++v) sw[c][v] = sb[c][v] = 0.0f;
-  if (SUMS && flush > 0)
-    for (int i = threadIdx.x; i < 4 * E * static_cast<int>(blockDim.x); i += blockDim.x) moved[i] = 0.0f;
   if (CTA) sums.clear();
   __syncthreads();
-  if (CTA && ranks > 1) cluster_barrier();
+  float* own = moved + blockIdx.x * 4LL * E * blockDim.x + threadIdx.x;
+  const int hop = E * blockDim.x;
+  bool first_move = true;
   auto move = [&]() {
-    if (!SUMS) return;
+    if constexpr (SUMS) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float* at = moved + (c * V + v) * blockDim.x + threadIdx.x;
-        const int hop = E * blockDim.x;
-        add_exactly(at[0], at[hop], sw[c][v]);
-        add_exactly(at[2 * hop], at[3 * hop], sb[c][v]);
+        float* at = own + (c * V + v) * blockDim.x;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!first_move)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[k] = at[k * hop];
+        add_exactly(s[0], s[1], sw[c][v]);
+        add_exactly(s[2], s[3], sb[c][v]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) at[k * hop] = s[k];
         sw[c][v] = sb[c][v] = 0.0f;
       }
+    }
+    first_move = false;
   };
-  int since = 0;
+  int since = 0, stage = 0;
   for (long long base = base0; base < a.rows; base += step) {
     const long long row = base + sub;
     const bool live = row < a.rows;
+    if constexpr (kInRing) {
+      fetch(row + (kAhead - 1) * step, stage == 0 ? kAhead - 1 : stage - 1);
+      ring.wait_oldest();
+      next = *ring.pair(stage);
+    } else if (more && live) {
+      cols.load(pt, t0 + row * g.g_total_stride, t0, t1);
+    }
     const float mean = next.x, rstd = next.y;
-    if (more && live) cols.load(pt, t0 + row * g.g_total_stride, t0, t1);
     float h[C][V], gw[C][V], total[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (CTA && scaled) ws.get(w[c], c);
+      if constexpr (kInRing) {
+        px[c] = ring.template get<TI>(stage, 0, c);
+        pg[c] = ring.template get<TO>(stage, 1, c);
+      }
       float s0 = 0.0f, s1 = 0.0f;
-      cols.each(
-          c,
-          [&](int c, int v) {
-            h[c][v] = live ? (px[c].get(v) - mean) * rstd : 0.0f;
-            const float gy = live ? pg[c].get(v) : 0.0f;
-            if (SUMS) {
-              sw[c][v] = fmaf(gy, h[c][v], sw[c][v]);
-              sb[c][v] += gy;
-            }
-            gw[c][v] = !CTA || scaled ? gy * w[c][v] : gy;
-            s0 += gw[c][v];
-            s1 = fmaf(gw[c][v], h[c][v], s1);
-          },
-          [&](int c, int v) { h[c][v] = gw[c][v] = 0.0f; });
+      cols.template each<CTA>(c, [&](int c, int v, bool on) {
+        on = on && live;
+        h[c][v] = on ? (px[c].get(v) - mean) * rstd : 0.0f;
+        const float gy = on ? pg[c].get(v) : 0.0f;
+        if (SUMS) {
+          sw[c][v] = fmaf(gy, h[c][v], sw[c][v]);
+          sb[c][v] += gy;
+        }
+        gw[c][v] = !CTA || scaled ? gy * w[c][v] : gy;
+        s0 += gw[c][v];
+        s1 = fmaf(gw[c][v], h[c][v], s1);
+      });
       total[0] += s0;
       total[1] += s1;
     }
-    if (base + step < a.rows) fetch(row + step);
+    if (!kInRing && base + step < a.rows) fetch(row + step, 0);
     if (CTA)
-      row_sums(total, sums, slot, ranks, rank);
+      row_sums(total, sums, slot);
     else
       group_sums(total, lanes);
-    if (flush > 0 && ++since == flush) {
+    if (SUMS && moved != nullptr && ++since == kPlainRows) {
       move();
       since = 0;
     }
+    const int now = stage;
+    stage = stage == kAhead - 1 ? 0 : stage + 1;
     if (g.gx == nullptr || !live) continue;
-    const float m0 = total[0] / a.dim, m1 = total[1] / a.dim;
+    const float m0 = total[0] * inv_dim, m1 = total[1] * inv_dim;
     TI* to = static_cast<TI*>(g.gx) + row * g.gx_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      if constexpr (kInRing) {
+        if (more) pt[c] = ring.template get<TI>(now, 2, c);
+      }
       float f[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -147,20 +186,19 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
     }
   }
   if (!SUMS) return;
-  if (flush > 0) {
+  if (moved != nullptr && !first_move) {
     move();
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const float* at = moved + (c * V + v) * blockDim.x + threadIdx.x;
-        const int hop = E * blockDim.x;
+        const float* at = own + (c * V + v) * blockDim.x;
         sw[c][v] = at[0] + at[hop];
         sb[c][v] = at[2 * hop] + at[3 * hop];
       }
   }
   if (CTA) {
-    float* out = partial + static_cast<long long>(blockIdx.x / ranks) * 2 * a.dim;
+    float* out = partial + blockIdx.x * 2LL * a.dim;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -206,62 +244,98 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
   }
 }
 
-// Rows that no cluster holds: the input's gradient, a CTA a row.
-template <typename TI, typename TO>
-__global__ void __launch_bounds__(kMostThreads)
-    k_norm_grad_long(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g) {
+// Rows that a CTA's registers do not hold: the input's gradient, a CTA a row, which it reads twice, the second time
+// out of L2.
+template <typename TI, typename TO, int V>
+__global__ void __launch_bounds__(kMostThreads, 2)
+    k_norm_grad_long(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g, int skew0,
+                     int skew_step) {
   __shared__ RowSums<2> sums;
   int slot = 0;
   pdl_wait();
   pdl_trigger();
   sums.clear();
   __syncthreads();
+  const TI *x0 = static_cast<const TI*>(a.x), *t0 = static_cast<const TI*>(g.g_total);
+  const TO* g0 = static_cast<const TO*>(g.gy);
+  const float inv_dim = 1.0f / a.dim;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const TI* x = static_cast<const TI*>(a.x) + row * a.x_stride;
-    const TO* gy = static_cast<const TO*>(g.gy) + row * g.gy_stride;
-    const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
-    auto weighted = [&](int i) {
-      const float v = to_f32(gy[i]);
-      return a.weight != nullptr ? v * load_as_f32(a.weight, a.w_dtype, i) : v;
-    };
+    const int skew = static_cast<int>((skew0 + row % V * skew_step) % V);
+    const TI *x = x0 + row * a.x_stride, *t = t0 + row * g.g_total_stride;
+    const TO* gy = g0 + row * g.gy_stride;
+    TI* to = static_cast<TI*>(g.gx) + row * g.gx_stride;
+    const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * row);
+    const float mean = st.x, rstd = st.y;
     float total[2] = {0.0f, 0.0f};
-    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
-      const float v = weighted(i);
-      total[0] += v;
-      total[1] = fmaf(v, (to_f32(x[i]) - mean) * rstd, total[1]);
+#pragma unroll 4
+    for (int col = static_cast<int>(threadIdx.x) * V - skew; col < a.dim; col += kMostThreads * V) {
+      float h[V], gw[V], w[V];
+      load_some<V>(h, x, col, a.dim);
+      load_some<V>(gw, gy, col, a.dim);
+      load_weights<V>(w, a.weight, a.w_dtype, col, a.dim, 1.0f);
+      float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float p = gw[v] * w[v];
+        s0 += p;
+        s1 = fmaf(p, (h[v] - mean) * rstd, s1);
+      }
+      total[0] += s0;
+      total[1] += s1;
     }
-    row_sums(total, sums, slot, 1, 0);
-    const float m0 = total[0] / a.dim, m1 = total[1] / a.dim;
-    for (int i = threadIdx.x; i < a.dim; i += kMostThreads) {
-      const float h = (to_f32(x[i]) - mean) * rstd;
-      float d = fmaf(-h, m1, weighted(i) - m0) * rstd;
-      if (g.g_total != nullptr) d += to_f32(static_cast<const TI*>(g.g_total)[row * g.g_total_stride + i]);
-      static_cast<TI*>(g.gx)[row * g.gx_stride + i] = from_f32<TI>(d);
+    row_sums(total, sums, slot);
+    const float m0 = total[0] * inv_dim, m1 = total[1] * inv_dim;
+#pragma unroll 2
+    for (int col = static_cast<int>(threadIdx.x) * V - skew; col < a.dim; col += kMostThreads * V) {
+      float h[V], gw[V], w[V], f[V];
+      load_some<V>(h, x, col, a.dim);
+      load_some<V>(gw, gy, col, a.dim);
+      load_weights<V>(w, a.weight, a.w_dtype, col, a.dim, 1.0f);
+      if (g.g_total != nullptr)
+        load_some<V>(f, t, col, a.dim);
+      else
+#pragma unroll
+        for (int v = 0; v < V; ++v) f[v] = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        f[v] = fmaf(-(h[v] - mean) * rstd, m1, gw[v] * w[v] - m0) * rstd + f[v];
+      store_some<V>(f, to, col, a.dim);
     }
   }
 }
 
-// Their columns' sums: a thread a column, `per` rows.
-template <typename TI, typename TO>
+// Their columns' sums: a thread a pack of columns, `per` rows.
+template <typename TI, typename TO, int V>
 __global__ void __launch_bounds__(256)
     k_norm_cols_long(const __grid_constant__ mlt_norm_args a, const __grid_constant__ mlt_norm_grads g, float* partial,
                      long long per) {
   pdl_wait();
   pdl_trigger();
-  const int col = blockIdx.x * 256 + threadIdx.x;
+  const int col = (blockIdx.x * 256 + threadIdx.x) * V;
   if (col >= a.dim) return;
   const long long from = blockIdx.y * per, to = min(static_cast<long long>(a.rows), from + per);
-  float sw = 0.0f, cw = 0.0f, sb = 0.0f, cb = 0.0f;
+  float sw[V], cw[V], sb[V], cb[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) sw[v] = cw[v] = sb[v] = cb[v] = 0.0f;
 #pragma unroll 4
   for (long long row = from; row < to; ++row) {
-    const float gy = to_f32(static_cast<const TO*>(g.gy)[row * g.gy_stride + col]);
-    const float x = to_f32(static_cast<const TI*>(a.x)[row * a.x_stride + col]);
-    add_exactly(sw, cw, gy * ((x - a.stats[2 * row]) * a.stats[2 * row + 1]));
-    add_exactly(sb, cb, gy);
+    float gy[V], x[V];
+    load_some<V>(gy, static_cast<const TO*>(g.gy) + row * g.gy_stride, col, a.dim);
+    load_some<V>(x, static_cast<const TI*>(a.x) + row * a.x_stride, col, a.dim);
+    const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * row);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      add_exactly(sw[v], cw[v], gy[v] * ((x[v] - st.x) * st.y));
+      add_exactly(sb[v], cb[v], gy[v]);
+    }
   }
   float* out = partial + blockIdx.y * 2LL * a.dim;
-  out[col] = sw + cw;
-  out[a.dim + col] = sb + cb;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (col + v < a.dim) {
+      out[col + v] = sw[v] + cw[v];
+      out[a.dim + col + v] = sb[v] + cb[v];
+    }
 }
 
 // The teams' sums of 32 columns: 32 threads a column take every 32nd team, then a tree.
@@ -287,66 +361,71 @@ __global__ void __launch_bounds__(1024)
 struct Plan {
   bool far;  // rows that no cluster holds
   bool group;
-  int lanes, threads, ranks, seg, flush;
+  int lanes, threads;
   long long teams;  // of rows, and of partial sums
-  size_t smem;
+  size_t smem, off_moved, bytes;
 };
 
-// Values of a row a thread: two packs where rows are read in packs of eight 16-bit values, else eight.
-constexpr int each_of(int pack) { return pack == 8 ? 16 : 8; }
+// Values of a row a thread: two packs, or eight single ones; of 16-bit rows that groups of lanes take one pack,
+// beside whose sums and weights registers have no room for another.
+constexpr int each_of(int pack, bool group) { return pack == 8 && !group ? 16 : 8; }
 
 // By sizes and how the rows lie; the number of teams sets the order of the sums.
 Plan plan_of(long long rows, int dim, int pack, bool edges, int period, bool scaled, int sms) {
   Plan p{};
-  const int each = each_of(pack), places = (dim + (edges ? pack - 1 : 0) + pack - 1) / pack * pack;
-  long long in_turn = 0;  // rows of a thread
-  if (dim + pack > kNormMaxCluster * kMostThreads * each) {
-    p.far = true;
-    p.teams = (rows + kLongRows - 1) / kLongRows;
-    if (p.teams > 256) p.teams = 256;
+  const int places = (dim + (edges ? pack - 1 : 0) + pack - 1) / pack * pack;
+  auto finish = [&](long long moved_floats) {
+    p.off_moved = up256(sizeof(float) * p.teams * 2 * dim);
+    p.bytes = p.off_moved + up256(sizeof(float) * moved_floats);
+    if (moved_floats == 0) p.off_moved = 0;
     return p;
+  };
+  const bool group = places <= 32 * each_of(pack, true);
+  const int each = each_of(pack, group);
+  if (places > kMostThreads * each) {
+    p.far = true;
+    // six CTAs an SM over the columns' sums
+    const long long wide = (dim + 256 * pack - 1) / (256 * pack), fill = (6LL * sms + wide - 1) / wide;
+    p.teams = rows < fill ? rows : fill;
+    return finish(0);
   }
-  if (places <= 32 * each) {
+  if (group) {
     p.group = true;
     p.lanes = 1;
     while (p.lanes * each < places) p.lanes *= 2;
     p.threads = kGroupThreads;
-    p.ranks = 1;
-    p.seg = places;
-    const long long per = kGroupThreads / p.lanes, need = (rows + per - 1) / per, most = 2LL * sms;
-    p.teams = need < most ? need : most;
-    in_turn = (need + p.teams - 1) / p.teams;
   } else {
-    p.ranks = (places + kMostThreads * each - 1) / (kMostThreads * each);
-    p.seg = ((places + p.ranks - 1) / p.ranks + pack - 1) / pack * pack;
-    p.ranks = (places + p.seg - 1) / p.seg;
-    p.threads = p.lanes = ((p.seg + each - 1) / each + 31) / 32 * 32;
-    int per_sm = 512 / p.threads;  // by registers
-    if (per_sm > 16) per_sm = 16;
-    long long most = static_cast<long long>(sms) * per_sm / p.ranks;
-    most = most < period ? period : most / period * period;
-    p.teams = rows < most ? rows : most;
-    in_turn = (rows + p.teams - 1) / p.teams;
+    p.threads = p.lanes = ((places + each - 1) / each + 31) / 32 * 32;
   }
-  p.flush = in_turn > kPlainRows ? kFlushRows : 0;
+  // weights and rows ahead; at the end of short rows the sums by place
   const size_t own = sizeof(float) * p.threads * each;
-  p.smem = (p.group || !scaled ? 0 : own) + (p.flush > 0 ? 4 * own : 0);
+  p.smem = (p.group || !scaled ? 0 : own) + (p.group || pack == 1 ? 0 : p.threads * static_cast<size_t>(Ring<8, 2>::kBytes));
   if (p.group && p.smem < own) p.smem = own;
-  return p;
+  int per_sm = 65536 / registers(!p.group, pack) / p.threads;
+  const int by_smem = static_cast<int>(227 * 1024 / (p.smem + 2048));
+  if (per_sm > by_smem) per_sm = by_smem;
+  per_sm = per_sm < 1 ? 1 : per_sm > 16 ? 16 : per_sm;
+  const long long most_ctas = static_cast<long long>(sms) * per_sm;
+  const long long in_turn_rows = p.group ? kGroupThreads / p.lanes : 1, need = (rows + in_turn_rows - 1) / in_turn_rows;
+  long long most = most_ctas;
+  if (!p.group) most = most < period ? period : most / period * period;
+  p.teams = need < most ? need : most;
+  const bool move = (need + p.teams - 1) / p.teams > kPlainRows;
+  return finish(move ? p.teams * 4LL * each * p.threads : 0);
 }
 
 template <typename TI, typename TO, int V, bool EDGE>
 cudaError_t launch_as(const mlt_norm_args& a, const mlt_norm_grads& g, const Plan& p, const Skew& skew, float* partial,
                       bool sums, cudaStream_t st) {
-  constexpr int C = each_of(V) / V;
-  const unsigned grid = static_cast<unsigned>(p.teams * p.ranks);
+  float* moved = sums && p.off_moved > 0 ? partial + p.off_moved / sizeof(float) : nullptr;
+  constexpr int GC = each_of(V, true) / V, CC = each_of(V, false) / V;
+  const unsigned grid = static_cast<unsigned>(p.teams);
   auto go = [&](auto kernel) {
-    return launch_cluster(kernel, grid, p.threads, p.ranks, p.smem, st, a, g, partial, p.lanes, p.seg, skew.first,
-                          skew.step, p.flush);
+    return launch_rows(kernel, grid, p.threads, p.smem, st, a, g, partial, moved, p.lanes, skew.first, skew.step);
   };
   if (p.group)
-    return sums ? go(k_norm_grad<TI, TO, V, C, false, EDGE, true>) : go(k_norm_grad<TI, TO, V, C, false, EDGE, false>);
-  return sums ? go(k_norm_grad<TI, TO, V, C, true, EDGE, true>) : go(k_norm_grad<TI, TO, V, C, true, EDGE, false>);
+    return sums ? go(k_norm_grad<TI, TO, V, GC, false, EDGE, true>) : go(k_norm_grad<TI, TO, V, GC, false, EDGE, false>);
+  return sums ? go(k_norm_grad<TI, TO, V, CC, true, EDGE, true>) : go(k_norm_grad<TI, TO, V, CC, true, EDGE, false>);
 }
 
 }  // namespace
@@ -354,14 +433,15 @@ cudaError_t launch_as(const mlt_norm_args& a, const mlt_norm_grads& g, const Pla
 size_t norm_grad_workspace(long long rows, int dim, int sms) {
   if (rows == 0) return 0;
   // whichever way the rows will lie
-  long long most = 0;
+  size_t most = 0;
   for (int pack : {1, 4, 8})
     for (int edges = 0; edges < 2; ++edges)
-      for (int period = 1; period <= pack; period *= 2) {
-        const long long teams = plan_of(rows, dim, pack, edges != 0, period, true, sms).teams;
-        if (teams > most) most = teams;
-      }
-  return up256(static_cast<size_t>(most) * 2 * dim * sizeof(float));
+      for (int period = 1; period <= pack; period *= 2)
+        for (int scaled = 0; scaled < 2; ++scaled) {
+          const size_t n = plan_of(rows, dim, pack, edges != 0, period, scaled != 0, sms).bytes;
+          if (n > most) most = n;
+        }
+  return most;
 }
 
 cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, void* ws, int sms, long long* launches,
@@ -385,19 +465,29 @@ cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, vo
                              a.weight != nullptr, sms);
       teams = p.teams;
       if (p.far) {
-        // the sums first: gx may be written over gy
-        if (sums) {
+        auto both = [&](auto pack, const Skew& k) -> cudaError_t {
+          constexpr int P = decltype(pack)::value;
+          // the sums first: gx may be written over gy
+          if (sums) {
+            ++*launches;
+            // columns keep their places in packs only where rows begin at boundaries
+            auto columns = [&](auto width) {
+              constexpr int W = decltype(width)::value;
+              return launch_pdl(k_norm_cols_long<TI, TO, W>,
+                                dim3((a.dim + 256 * W - 1) / (256 * W), static_cast<unsigned>(p.teams)), dim3(256), 0, st, a,
+                                g, partial, (a.rows + p.teams - 1) / p.teams);
+            };
+            const cudaError_t r = k.first == 0 && k.step == 0 ? columns(pack) : columns(std::integral_constant<int, 1>());
+            if (r != cudaSuccess) return r;
+          }
+          if (g.gx == nullptr) return cudaSuccess;
+          const long long most = 2LL * sms;
           ++*launches;
-          const cudaError_t r =
-              launch_pdl(k_norm_cols_long<TI, TO>, dim3((a.dim + 255) / 256, static_cast<unsigned>(p.teams)), dim3(256),
-                         0, st, a, g, partial, (a.rows + p.teams - 1) / p.teams);
-          if (r != cudaSuccess) return r;
-        }
-        if (g.gx == nullptr) return cudaSuccess;
-        const long long most = 4LL * sms;
-        ++*launches;
-        return launch_cluster(k_norm_grad_long<TI, TO>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMostThreads,
-                              1, 0, st, a, g);
+          return launch_rows(k_norm_grad_long<TI, TO, P>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMostThreads,
+                             0, st, a, g, k.first, k.step);
+        };
+        return skew.same ? both(std::integral_constant<int, V>(), skew)
+                         : both(std::integral_constant<int, 1>(), Skew{true, 0, 0});
       }
       ++*launches;
       if (!skew.same) return launch_as<TI, TO, 1, false>(a, g, p, Skew{true, 0, 0}, partial, sums, st);
