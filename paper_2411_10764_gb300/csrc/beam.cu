@@ -33,6 +33,7 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kSlots = 4;
+constexpr int kRowQueue = 1024;  // packs that are looked at again
 constexpr int kRowList = 2048;   // collected scores of a CTA's share of a row
 constexpr int kMostCands = 8192;
 constexpr int kItemThreads = 1024;
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kRowThreads, 4)
     k_beam_rows(const __grid_constant__ mlt_beam_args a, int parts, int k, RowPart* found, u64* lists) {
   __shared__ float warp_top[kRowWarps];
   __shared__ Two warp_sum[kRowWarps];
-  __shared__ int total[2], listed;
+  __shared__ int total[2], listed, queued, queue[kRowQueue];
   __shared__ u64 list[kRowList];
   pdl_wait();
   pdl_trigger();
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kRowThreads, 4)
     for (int o = 16; o > 0; o /= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
     __syncthreads();
     if (lane == 0) warp_top[warp] = high;
-    if (tid == 0) listed = total[0] = total[1] = 0;
+    if (tid == 0) listed = queued = total[0] = total[1] = 0;
     __syncthreads();
     high = -INFINITY;
 #pragma unroll
@@ -406,15 +407,24 @@ __global__ void __launch_bounds__(kRowThreads, 4)
       if (at < kRowList) list[at] = row_key(s, i);
     }
   };
+  // which packs these are, for all threads to share (each in its own slots: 64 x 8 rows of 50,021 12 us for 3)
 #pragma unroll
   for (int u = 0; u < kSlots; ++u)
     if (slot[u] > -INFINITY && slot[u] >= from)
       for (int q = sh.first + tid + u * kRowThreads; q < sh.last; q += kSlots * kRowThreads) {
-        Pack<T, V> p;
-        sh.load(q, p);
-#pragma unroll
-        for (int e = 0; e < V; ++e) keep(clean(to_f32(p.v[e])), q * V + e);
+        const int at = atomicAdd(&queued, 1);
+        if (at < kRowQueue) queue[at] = q;
       }
+  __syncthreads();
+  const bool few = queued <= kRowQueue;
+  const int packs_again = few ? queued : sh.last - sh.first;
+  for (int i = tid; i < packs_again; i += kRowThreads) {
+    const int q = few ? queue[i] : sh.first + i;
+    Pack<T, V> p;
+    sh.load(q, p);
+#pragma unroll
+    for (int e = 0; e < V; ++e) keep(clean(to_f32(p.v[e])), q * V + e);
+  }
   __syncthreads();
   int count = listed;
   if (count > kRowList) {
@@ -508,41 +518,49 @@ __device__ __forceinline__ void write_none(const mlt_beam_args& a, int b, int at
   a.out_done[o] = 0;
 }
 
-// Up to kCountSort candidates an item, out of the rows' lists.
-__global__ void __launch_bounds__(kCountSort)
+// Up to kCountSort candidates an item, out of the rows' lists: a thread forms one, several count together how many
+// are larger.
+constexpr int kFewThreads = 256;
+__global__ void __launch_bounds__(kFewThreads)
     k_beam_few(const __grid_constant__ mlt_beam_args a, int parts, int k, const RowPart* found, const u64* lists) {
   __shared__ Cand list[kCountSort];
+  __shared__ int ranks[kCountSort];
   pdl_wait();
   pdl_trigger();
   const int b = blockIdx.x, tid = threadIdx.x, each = parts * k, cands = a.beams * each;
-  const int w = min(tid / each, a.beams - 1), at = tid - w * each;
-  const long long r = static_cast<long long>(b) * a.beams + w, o = r * parts + min(at / k, parts - 1);
-  const float lp = a.logp[r];
-  const bool ended = a.done != nullptr && a.done[r] != 0;
-  const u64 key = tid < cands ? lists[o * k + at % k] : 0;
-  bool valid = tid < cands && lp > -INFINITY;
-  Cand mine{0, 0};
-  if (valid) {
-    if (ended) {
-      valid = at == 0;
-      mine = candidate_of(w, 0.0f, static_cast<int>(a.eos), lp);
-    } else {
-      const double z = join_parts(found + r * parts, parts, a.normalised != 0);
-      valid = at % k < found[o].count;
-      const float s = from_ordered(static_cast<unsigned>(key >> 32));
-      mine = candidate_of(w, s, ~static_cast<int>(key), lp + (static_cast<double>(s) - z));
+  int wide = 32;
+  while (wide < cands) wide *= 2;
+  bool ended = false;
+  if (tid < wide) {
+    const int w = min(tid / each, a.beams - 1), at = tid - w * each;
+    const long long r = static_cast<long long>(b) * a.beams + w, o = r * parts + min(at / k, parts - 1);
+    const float lp = a.logp[r];
+    const u64 key = tid < cands ? lists[o * k + at % k] : 0;
+    ended = a.done != nullptr && a.done[r] != 0;
+    Cand mine{0, 0};
+    if (tid < cands && lp > -INFINITY) {
+      if (ended) {
+        if (at == 0) mine = candidate_of(w, 0.0f, static_cast<int>(a.eos), lp);
+      } else if (at % k < found[o].count) {
+        const double z = join_parts(found + r * parts, parts, a.normalised != 0);
+        const float s = from_ordered(static_cast<unsigned>(key >> 32));
+        mine = candidate_of(w, s, ~static_cast<int>(key), lp + (static_cast<double>(s) - z));
+      }
     }
-    if (!valid) mine = Cand{0, 0};
+    list[tid] = mine;
+    ranks[tid] = 0;
   }
-  list[tid] = mine;
-  const int count = __syncthreads_count(valid);
-  if (valid) {
-    int rank = 0;
+  const int count = __syncthreads_count(tid < wide && list[tid].total != 0);
+  const Cand mine = list[tid % wide];
+  if (mine.total != 0) {
+    int larger = 0;
 #pragma unroll 4
-    for (int j = 0; j < cands; ++j) rank += less(mine, list[j]);
-    if (rank < a.m) write(a, b, rank, mine, ended);
+    for (int j = tid / wide; j < cands; j += kFewThreads / wide) larger += less(mine, list[j]);
+    if (larger > 0) atomicAdd(&ranks[tid % wide], larger);
   }
-  for (int i = count + tid; i < a.m; i += blockDim.x) write_none(a, b, i);
+  __syncthreads();
+  if (tid < wide && mine.total != 0 && ranks[tid] < a.m) write(a, b, ranks[tid], mine, ended);
+  for (int i = count + tid; i < a.m; i += kFewThreads) write_none(a, b, i);
 }
 
 // T: the scores' type where candidates are all scores; else the rows' lists are read (FROM_ROWS).
@@ -750,7 +768,7 @@ Plan plan_of(const mlt_beam_args& a, int sms) {
   if (!p.direct) {
     // parts of a row until the GPU is full, none shorter than eight scores a thread
     const int least = kRowThreads * 8;
-    while (p.parts < 64 && rows * p.parts < 4LL * sms && a.n / (2 * p.parts) >= least &&
+    while (p.parts < 64 && rows * p.parts < 2LL * sms && a.n / (2 * p.parts) >= least &&
            static_cast<long long>(a.beams) * p.k * p.parts * 2 <= kMostCands)
       p.parts *= 2;
     cands = static_cast<long long>(a.beams) * p.k * p.parts;
@@ -872,7 +890,7 @@ cudaError_t launch_beam(const mlt_beam_args& a, void* ws, int sms, long long* la
     if (e != cudaSuccess) return e;
     ++*launches;
     if (a.beams * p.parts * p.k <= kCountSort)
-      return launch_pdl(k_beam_few, dim3(a.batch), dim3(kCountSort), 0, st, a, p.parts, p.k,
+      return launch_pdl(k_beam_few, dim3(a.batch), dim3(kFewThreads), 0, st, a, p.parts, p.k,
                         static_cast<const RowPart*>(found), static_cast<const u64*>(lists));
     return launch_items<float, true>(a, p, found, lists, st);
   });
