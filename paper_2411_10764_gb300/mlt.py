@@ -927,6 +927,78 @@ def _per_tensor(value, count: int, name: str):
     return [value] * count
 
 
+def _adamw_rows(params, grads, copies, rates, decays, device):
+    """mlt_adamw_tensor records of a few tensors as 64-bit words, the blocks of their moments, and what has
+    to live until the launch."""
+    words, blocks, kept = [], 0, []
+    for p, g, rate, decay, copy in zip(params, grads, rates, decays, copies or [None] * len(params)):
+        n = p.numel()
+        blocks += -(-n // ADAMW_BLOCK)
+        if g is None:
+            words += (0, 0, 0, n, 0, 0)
+            continue
+        if p.get_device() != device or g.get_device() != device:
+            raise ValueError("parameters, gradients, copies and moments must lie on one CUDA device")
+        if not p.is_contiguous():
+            raise ValueError("parameters and copies must be contiguous")
+        if g.shape != p.shape:
+            raise ValueError("a gradient and a copy must have their parameter's shape")
+        if not g.is_contiguous():
+            g = g.contiguous()
+            kept.append(g)
+        kinds, to = _dtype_code(p) | _dtype_code(g) << 16, 0
+        if copy is not None:
+            kinds |= _dtype_code(copy) << 32
+            if copy.shape != p.shape or copy.get_device() != device:
+                raise ValueError("a copy must be of its parameter's shape and device")
+            if not copy.is_contiguous():
+                raise ValueError("parameters and copies must be contiguous")
+            to = copy.data_ptr()
+        words += (p.data_ptr(), g.data_ptr(), to, n, kinds, _rate_words.get((rate, decay)) or _rate_word(rate, decay))
+    return array("q", words), blocks, kept
+
+
+def _adamw_columns(params, grads, copies, rates, decays, device):
+    """The same for many tensors, column by column."""
+    Tensor, count = _torch.Tensor, len(params)
+    missing = [k for k, g in enumerate(grads) if g is None]
+    if missing:  # their parameters stand in for them, and have no address below
+        grads = [p if g is None else g for p, g in zip(params, grads)]
+    given = [params, grads] if copies is None else [params, grads, copies]
+    for some in given:
+        if any(d != device for d in map(Tensor.get_device, some)):
+            raise ValueError("parameters, gradients, copies and moments must lie on one CUDA device")
+    if not all(map(Tensor.is_contiguous, params)) or not (copies is None or all(map(Tensor.is_contiguous, copies))):
+        raise ValueError("parameters and copies must be contiguous")
+    shapes = [p.shape for p in params]
+    if any([t.shape for t in some] != shapes for some in given[1:]):
+        raise ValueError("a gradient and a copy must have their parameter's shape")
+    if not all(map(Tensor.is_contiguous, grads)):
+        grads = given[1] = [g.contiguous() for g in grads]
+    kinds, mixed = 0, None
+    for k, some in enumerate(given):
+        types = {t.dtype for t in some}
+        if not types <= _DTYPES.keys():
+            raise TypeError(f"float32, bfloat16 or float16 wanted, got {(types - _DTYPES.keys()).pop()}")
+        if len(types) == 1:
+            kinds += _DTYPES[types.pop()] << 16 * k
+        elif types:
+            mixed = [x + (_DTYPES[t.dtype] << 16 * k) for x, t in zip(mixed or [0] * count, some)]
+    words = list(map(_rate_words.get, zip(rates, decays)))
+    if None in words:
+        words = [_rate_word(a, b) for a, b in zip(rates, decays)]
+    table = array("q", bytes(48 * count))
+    for k, some in enumerate(given):
+        table[k::6] = array("q", map(Tensor.data_ptr, some))
+    table[3::6] = sizes = array("q", map(Tensor.numel, params))
+    table[4::6] = array("q", [kinds] * count if mixed is None else [x + kinds for x in mixed])
+    table[5::6] = array("q", words)
+    blocks = int((-(-np.frombuffer(sizes, np.int64) // ADAMW_BLOCK)).sum()) if count else 0
+    for k in missing:
+        table[6 * k + 1] = 0
+    return table, blocks, given
+
+
 def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
           copies=None, grad_scale=None, seed: int = 0, lr_scale=1.0, stream=None) -> None:
     """mlt_adamw: one AdamW step over the tensors of `params`, in place, with `state` (adamw_state
@@ -967,45 +1039,11 @@ def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), e
     decays = _per_tensor(weight_decay, count, "weight_decay")
     if isinstance(lr_scale, (list, tuple)) or lr_scale != 1.0:
         rates = [a * b for a, b in zip(rates, _per_tensor(lr_scale, count, "lr_scale"))]
-    device, Tensor = m.get_device(), torch.Tensor
-    missing = [k for k, g in enumerate(grads) if g is None]
-    if missing:  # their parameters stand in for them, and have no address below
-        grads = [p if g is None else g for p, g in zip(params, grads)]
-    given = [params, grads] if copies is None else [params, grads, copies]
-    for some in given:
-        if any(d != device for d in map(Tensor.get_device, some)):
-            raise ValueError("parameters, gradients, copies and moments must lie on one CUDA device")
-    if not all(map(Tensor.is_contiguous, params)) or not (copies is None or all(map(Tensor.is_contiguous, copies))):
-        raise ValueError("parameters and copies must be contiguous")
-    shapes = [p.shape for p in params]
-    if any([t.shape for t in some] != shapes for some in given[1:]):
-        raise ValueError("a gradient and a copy must have their parameter's shape")
-    if not all(map(Tensor.is_contiguous, grads)):
-        grads = given[1] = [g.contiguous() for g in grads]  # kept until the launch
-    kinds, mixed = 0, None
-    for k, some in enumerate(given):
-        types = {t.dtype for t in some}
-        if not types <= _DTYPES.keys():
-            raise TypeError(f"float32, bfloat16 or float16 wanted, got {(types - _DTYPES.keys()).pop()}")
-        if len(types) == 1:
-            kinds += _DTYPES[types.pop()] << 16 * k
-        elif types:
-            mixed = [x + (_DTYPES[t.dtype] << 16 * k) for x, t in zip(mixed or [0] * count, some)]
-    words = list(map(_rate_words.get, zip(rates, decays)))
-    if None in words:
-        words = [_rate_word(a, b) for a, b in zip(rates, decays)]
-    table = array("q", bytes(48 * count))
-    for k, some in enumerate(given):
-        table[k::6] = array("q", map(Tensor.data_ptr, some))
-    table[3::6] = sizes = array("q", map(Tensor.numel, params))
-    table[4::6] = array("q", [kinds] * count if mixed is None else [x + kinds for x in mixed])
-    table[5::6] = array("q", words)
-    blocks = int((-(-np.frombuffer(sizes, np.int64) // ADAMW_BLOCK)).sum()) if count else 0
-    for k in missing:
-        table[6 * k + 1] = 0
+    device = m.get_device()
+    table, blocks, kept = (_adamw_rows if count <= 32 else _adamw_columns)(params, grads, copies, rates, decays, device)
     _need(m.numel() == v.numel() == blocks * ADAMW_BLOCK and (ms is None or ms.numel() == vs.numel() == blocks),
           "the moments are of other parameters")
-    _one_device(m, v, ms, vs, *[t for t in (step, lr, grad_scale) if isinstance(t, Tensor)])
+    _one_device(m, v, ms, vs, *[t for t in (step, lr, grad_scale) if isinstance(t, torch.Tensor)])
     rule = AdamWRule(betas[0], betas[1], eps, 0 if scalars[0] is not None else int(step), *scalars, bits, seed & 0xFFFFFFFF)
     rc = L.mlt_adamw(_raw_stream(device), table.buffer_info()[0], count, C.byref(rule), m.data_ptr(), v.data_ptr(),
                      None if ms is None else ms.data_ptr(), None if vs is None else vs.data_ptr())

@@ -275,6 +275,24 @@ def test_rounding_to_8_bits_has_no_bias():
     assert np.corrcoef(v, want_v)[0, 1] > 0.8
 
 
+def test_more_than_32_bits_of_values():
+    """The second tensor's moments begin past 2^32 values; both tensors' ends get their step."""
+    import torch
+
+    n = (1 << 32) + 1000
+    big, small = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(300, device="cuda")
+    g, h = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.ones(300, device="cuda")
+    g[-1000:] = 1.0
+    state = mlt.adamw_state([big, small], 8)
+    mlt.adamw([big, small], [g, h], state, 1, lr=0.5)
+    # the first step of a gradient of 1 is lr, but for eps and some roundings
+    assert (big[-1000:] == -0.5).all() and (big[-1256:-1000] == 0).all() and (big[:1000] == 0).all()
+    assert ((small + 0.5).abs() <= 12 * U * 0.5 + 1e-8).all()
+    first = -(-n // BLOCK)
+    assert (state.m_scale[first:] == state.m_scale[first]).all() and state.m_scale[first] > 0
+    assert (state.m[first * BLOCK:first * BLOCK + 300].float() > 0).all()
+
+
 def test_another_stream_and_refusals():
     import torch
 

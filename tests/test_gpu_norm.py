@@ -283,6 +283,23 @@ def test_backward_strides_and_in_place(dim, kind):
     _check_backward(row, x, stats, w, None, mlt.layer_norm_grad(row, x, stats, w, b), kind, "f32")
 
 
+def test_more_than_32_bits_of_values():
+    """The last row of 4.6 billion values is normed, and its gradient lands there."""
+    import torch
+
+    rows, dim = 70001, 65536
+    x = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(3)
+    last = torch.randn(1, dim, device="cuda", generator=gen).bfloat16()
+    x[-1:] = last
+    want, _, stats = mlt.layer_norm(last)
+    g = mlt.layer_norm_grad(last, last, stats)["x"]
+    y, _, s = mlt.layer_norm(x)
+    assert torch.equal(y[-1:], want) and torch.equal(s[-1:], stats) and (y[-2] == 0).all()
+    out = mlt.layer_norm_grad(x, x, s, out=x)["x"]
+    assert torch.equal(out[-1:], g) and (out[-2] == 0).all()
+
+
 def test_no_rows():
     import torch
 
