@@ -871,6 +871,7 @@ struct Move {
   unsigned first_cta;
 };
 constexpr int kMostMoves = 64;
+constexpr int kHeldRows = 8;
 struct Moves {
   Move t[kMostMoves];
   int count, beams;
@@ -884,6 +885,19 @@ template <typename U>
 __device__ __forceinline__ void move_slice(const Move& t, unsigned char* base, long long from, int bytes, const int* to,
                                            const int* of, int count, unsigned char* mem) {
   const int units = bytes / static_cast<int>(sizeof(U)), all = units * count;
+  if (count <= kHeldRows) {  // each thread its columns, in registers (64 x 8 rows of 143 KB 21 us through shared memory)
+    for (int c = threadIdx.x; c < units; c += blockDim.x) {
+      unsigned char* at = base + from + c * sizeof(U);
+      U v[kHeldRows];
+#pragma unroll
+      for (int i = 0; i < kHeldRows; ++i)
+        if (i < count) v[i] = *reinterpret_cast<const U*>(at + of[i] * t.row_stride);
+#pragma unroll
+      for (int i = 0; i < kHeldRows; ++i)
+        if (i < count) *reinterpret_cast<U*>(at + to[i] * t.row_stride) = v[i];
+    }
+    return;
+  }
   U* held = reinterpret_cast<U*>(mem);
 #pragma unroll 4
   for (int i = threadIdx.x; i < all; i += blockDim.x) {
@@ -972,7 +986,7 @@ cudaError_t launch_reorder(const int64_t* parent, int batch, int beams, const ml
   // 48 KB for all beams' slices, at least 128 bytes of each
   int most = 48 * 1024 / beams / 16 * 16;
   if (most < 128) most = 128;
-  if (most > 8192) most = 8192;
+  if (most >= 4096) most = 4096;  // a 16-byte access for each of 256 threads
   unsigned long long ctas = 0;
   int widest = 0;
   for (int i = 0; i < count; ++i) {
