@@ -852,7 +852,7 @@ Plan plan_of(const mlt_beam_args& a, int sms) {
 
 template <typename T, bool FROM_ROWS>
 cudaError_t launch_items(const mlt_beam_args& a, const Plan& p, const RowPart* found, const u64* lists, cudaStream_t st) {
-  if (p.smem > 48 * 1024) {
+  if (p.smem > 40 * 1024) {  // with the static part past what a kernel has unasked, 48 KB
     const cudaError_t e = cudaFuncSetAttribute(k_beam_items<T, FROM_ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                static_cast<int>(p.smem));
     if (e != cudaSuccess) return e;
@@ -1008,7 +1008,7 @@ cudaError_t launch_reorder(const int64_t* parent, int batch, int beams, const ml
   }
   if (ctas == 0) return cudaSuccess;
   const size_t smem = (2 * beams * sizeof(int) + 15) / 16 * 16 + static_cast<size_t>(widest) * beams;
-  if (smem > 48 * 1024) {
+  if (smem > 40 * 1024) {  // with the static part past what a kernel has unasked, 48 KB
     const cudaError_t e =
         cudaFuncSetAttribute(k_beam_reorder, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;

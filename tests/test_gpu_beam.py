@@ -104,6 +104,15 @@ def test_step(batch, beams, n, m, kind):
     _check(scores, logp, m, got, normalised=True)
 
 
+@pytest.mark.parametrize("beams", [950, 960, 970, 1000, 1024])
+def test_lists_around_48_kb(beams):
+    """2,048 candidates of 16 bytes and the beams' numbers in shared memory."""
+    rng = np.random.default_rng(beams)
+    for n in (2, 3):
+        scores, logp, d = _make(rng, 2, beams, n, done=0.1)
+        _check(scores, logp, 300, mlt.beam_step(scores, logp, 300, done=d, eos=0), d, 0)
+
+
 def test_one_item_and_uint8():
     import torch
 
@@ -264,6 +273,19 @@ def test_reorder(batch, beams):
         mlt.beam_reorder(parent, *tensors)
         assert all(torch.equal(a, b) for a, b in zip(tensors, want)), kind
     mlt.sync_status()
+
+
+@pytest.mark.parametrize("beams", [9, 11, 12, 13, 100, 300, 350, 384, 400])
+def test_reorder_around_48_kb(beams):
+    """Slices of all beams in shared memory beside their parents."""
+    import torch
+
+    g = torch.Generator("cuda").manual_seed(beams)
+    t = torch.randint(0, 1 << 40, (beams, 3001), device="cuda", generator=g)
+    parent = torch.randint(0, beams, (1, beams), device="cuda", generator=g)
+    want = _moved(t, parent)
+    mlt.beam_reorder(parent, t)
+    assert torch.equal(t, want)
 
 
 def test_reorder_strides_and_bad_parents():

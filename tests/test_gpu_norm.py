@@ -92,6 +92,21 @@ def test_forward(rows, dim, kinds):
     _check_forward(x, None, None, b, 1e-5, mlt.layer_norm(x, None, b, out_dtype=_type(kout)), kin, kout)
 
 
+@pytest.mark.parametrize("kind,dims", [("bf16", (6000, 6100, 6144, 8184, 8185, 16384, 114000, 114689)),
+                                       ("f32", (3000, 3056, 4096, 4097, 12224, 12288, 57300, 57345))])
+def test_sizes_of_shared_memory(kind, dims):
+    """Weights, rows ahead and whole rows in shared memory: just below and above what fits unasked (48 KB with a
+    kernel's own part) and at all (224 KB)."""
+    rng = np.random.default_rng(0)
+    for dim in dims:
+        x, gy = _rand(rng, (3, dim), kind, 1.5, 0.7), _rand(rng, (3, dim), kind)
+        w, b = _rand(rng, (dim,), "f32", 0.1, 1.0), _rand(rng, (dim,), "f32", 0.1)
+        got = mlt.layer_norm(x, w, b, residual=gy)
+        _check_forward(x, gy, w, b, 1e-5, got, kind, kind)
+        g = mlt.layer_norm_grad(gy, got[1], got[2], w, b, g_total=gy)
+        _check_backward(gy, got[1], got[2], w, gy, g, kind, "f32")
+
+
 def test_many_rows_and_large_means():
     """More rows than all CTAs hold at once; a mean a thousand times the spread."""
     rng = np.random.default_rng(1)
