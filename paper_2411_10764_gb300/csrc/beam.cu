@@ -62,9 +62,8 @@ __device__ __forceinline__ double double_from_ordered(u64 k) {
 __device__ __forceinline__ float clean(float x) { return x > -INFINITY ? fminf(fmaxf(x, -FLT_MAX), FLT_MAX) : -INFINITY; }
 
 // exp(x) / 2^unit: the product by log2 e is exact inside the sum, so all there is are the sum's rounding and
-// that of log2 e itself, a factor 1 + kLogE on x that the normaliser takes back for its largest terms.
+// that of log2 e itself, 1.3e-8 of x, of which the distance from the largest score counts.
 constexpr float kLog2E = 1.44269504f;
-constexpr double kLogE = 1.44269502162933349609375 / 1.44269504088896340736 - 1;
 __device__ __forceinline__ float power(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -104,9 +103,9 @@ struct Two {
   }
 };
 
-// ln(sum 2^unit) for terms up to exp(top), by ln f = 2 atanh((f - 1) / (f + 1)) of the sum's fraction f in
-// [0.7, 1.42): the leading term in two numbers, the rest of the series (below 0.004) in fp32.  Off by some 2^-32.
-__device__ __forceinline__ double log_sum(float top, float unit, Two sum) {
+// ln(sum), by ln f = 2 atanh((f - 1) / (f + 1)) of its fraction f in [0.7, 1.42): the leading term in two
+// numbers, the rest of the series (below 0.004) in fp32.  Off by some 2^-32.
+__device__ __forceinline__ double log_sum(Two sum) {
   float hi = __fadd_rn(sum.hi, sum.lo);
   float lo = __fadd_rn(__fsub_rn(sum.hi, hi), sum.lo);
   int e = (__float_as_int(hi) >> 23) - 127;
@@ -126,15 +125,15 @@ __device__ __forceinline__ double log_sum(float top, float unit, Two sum) {
   r = fmaf(q, r, 2.0f / 5);
   r = fmaf(q, r, 2.0f / 3);
   r = r * q * s + 2.0f * s_lo;
-  const float back = static_cast<float>(-kLogE) * top;
-  return fma(static_cast<double>(unit) + e, 0.693147180559945309417,
-             static_cast<double>(2.0f * s) + static_cast<double>(r + back));
+  return fma(static_cast<double>(e), 0.693147180559945309417, static_cast<double>(2.0f * s) + static_cast<double>(r));
 }
 
-// The normaliser: ln of a sum of terms up to exp(top), top finite.
+// The normaliser: ln of a sum of terms up to exp(top), top finite, as top + ln(sum / its own term): what that
+// term is off by falls out, and a row of one score has exactly that score as its normaliser.
 __device__ __forceinline__ double normaliser(float top, Two sum) {
-  if (is_huge(top)) return top + log_sum(0.0f, 0.0f, sum);
-  return log_sum(top, unit_of(top), sum);
+  const float one = term(top, top, unit_of(top));
+  const float q = __fdiv_rn(sum.hi, one);
+  return top + log_sum(Two{q, __fdividef(__fmaf_rn(-q, one, sum.hi) + sum.lo, one)});
 }
 
 // What a CTA found in its share of a row.

@@ -147,6 +147,24 @@ def test_ties(beams, n):
                 assert abs(out[j] - (-3.0 + x[c] - z)) <= 2.0 ** -21 + U * abs(out[j])
 
 
+@pytest.mark.parametrize("n", [3, 9000])
+def test_rows_of_one_score(n):
+    """A beam's only continuation has the beam's own log-probability exactly, whatever its score: equal ones tie."""
+    import torch
+
+    rng = np.random.default_rng(n)
+    x = torch.full((4, 8, n), -math.inf, device="cuda")
+    at = rng.integers(0, n, (4, 8))
+    for b in range(4):
+        for w in range(8):
+            x[b, w, at[b, w]] = float(rng.standard_normal() * 10.0 ** rng.integers(-3, 4))
+    logp = torch.full((4, 8), -11.3, device="cuda")
+    parent, token, out, _ = mlt.beam_step(x, logp, 8)
+    assert (out == logp[0, 0]).all()
+    assert torch.equal(parent, torch.arange(8, device="cuda").expand(4, 8))
+    assert torch.equal(token.cpu(), torch.from_numpy(at))
+
+
 def test_scores_that_one_total_cannot_tell_apart():
     """Within a beam the scores decide even where totals are equal in 64 bits."""
     import torch
