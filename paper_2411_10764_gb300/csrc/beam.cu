@@ -13,7 +13,7 @@
 //                 maxima is at most the k-th largest score, so scores from it on are collected, from the few
 //                 slots that reach it, and the k best of them are kept for the item.  Sums that are not
 //                 finite (NaN, infinite or huge scores) are formed again score by score.
-//   k_beam_few    up to 128 candidates an item: a thread each, which finds its beam's normaliser by itself;
+//   k_beam_few    up to 256 candidates an item: a thread each, which finds its beam's normaliser by itself;
 //   k_beam_items  more: a CTA an item, the normalisers, then all candidates (the rows' lists, or all
 //                 scores where there are at most 8,192).  Each candidate's total is bounded from both
 //                 sides in fp32; m lower bounds reach some threshold, and those whose upper bound does
@@ -557,13 +557,13 @@ __device__ __forceinline__ void write_none(const mlt_beam_args& a, int b, int at
   a.out_done[o] = 0;
 }
 
-// Up to kCountSort candidates an item, out of the rows' lists: a thread forms one, several count together how many
+// Up to kFewMost candidates an item, out of the rows' lists: a thread forms one, several count together how many
 // are larger.
-constexpr int kFewThreads = 256;
+constexpr int kFewMost = 256, kFewThreads = 512;
 __global__ void __launch_bounds__(kFewThreads)
     k_beam_few(const __grid_constant__ mlt_beam_args a, int parts, int k, const RowPart* found, const u64* lists) {
-  __shared__ Cand list[kCountSort];
-  __shared__ int ranks[kCountSort];
+  __shared__ Cand list[kFewMost];
+  __shared__ int ranks[kFewMost];
   pdl_wait();
   pdl_trigger();
   const int b = blockIdx.x, tid = threadIdx.x, each = parts * k, cands = a.beams * each;
@@ -969,7 +969,7 @@ cudaError_t launch_beam(const mlt_beam_args& a, void* ws, int sms, long long* la
                                      a, p.parts, p.k, found, lists);
     if (e != cudaSuccess) return e;
     ++*launches;
-    if (a.beams * p.parts * p.k <= kCountSort)
+    if (a.beams * p.parts * p.k <= kFewMost)
       return launch_pdl(k_beam_few, dim3(a.batch), dim3(kFewThreads), 0, st, a, p.parts, p.k,
                         static_cast<const RowPart*>(found), static_cast<const u64*>(lists));
     return launch_items<float, true>(a, p, found, lists, st);

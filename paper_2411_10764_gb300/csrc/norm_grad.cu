@@ -338,24 +338,27 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// The teams' sums of 32 columns: 32 threads a column take every 32nd team, then a tree.
+// The teams' sums of 16 columns: 64 threads a column take every 64th team, then a tree.
+constexpr int kColumns = 16;
 __global__ void __launch_bounds__(1024)
     k_norm_cols(const float* partial, int teams, int dim, void* gweight, void* gbias, int dtype) {
-  __shared__ float s[32][33];
+  __shared__ float s[64][kColumns + 1];
   pdl_wait();
   pdl_trigger();
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+  const int x = threadIdx.x % kColumns, y = threadIdx.x / kColumns, col = blockIdx.x * kColumns + x;
   void* to = blockIdx.y == 0 ? gweight : gbias;
   if (to == nullptr) return;
   float sum = 0.0f, c = 0.0f;
   if (col < dim)
 #pragma unroll 8
-    for (int t = y; t < teams; t += 32) add_exactly(sum, c, partial[(t * 2LL + blockIdx.y) * dim + col]);
+    for (int t = y; t < teams; t += 64) add_exactly(sum, c, partial[(t * 2LL + blockIdx.y) * dim + col]);
   s[y][x] = sum + c;
   __syncthreads();
-  float v[1] = {s[x][y]};
+  const int lane = threadIdx.x & 31, of = threadIdx.x >> 5;
+  if (of >= kColumns) return;
+  float v[1] = {s[lane][of] + s[lane + 32][of]};
   warp_sums(v);
-  if (x == 0 && blockIdx.x * 32 + y < dim) store_from_f32(to, dtype, blockIdx.x * 32 + y, v[0]);
+  if (lane == 0 && blockIdx.x * kColumns + of < dim) store_from_f32(to, dtype, blockIdx.x * kColumns + of, v[0]);
 }
 
 struct Plan {
@@ -496,7 +499,7 @@ cudaError_t launch_norm_grad(const mlt_norm_args& a, const mlt_norm_grads& g, vo
     });
   if (e != cudaSuccess || !sums) return e;
   ++*launches;
-  return launch_pdl(k_norm_cols, dim3((a.dim + 31) / 32, 2), dim3(1024), 0, st, static_cast<const float*>(partial),
+  return launch_pdl(k_norm_cols, dim3((a.dim + kColumns - 1) / kColumns, 2), dim3(1024), 0, st, static_cast<const float*>(partial),
                     static_cast<int>(teams), a.dim, g.gweight, g.gbias, a.w_dtype);
 }
 
