@@ -678,6 +678,8 @@ int mlt_scan_grad_workspace(const mlt_scan_args *args, size_t *bytes_out);
  *   stats     device [rows][2] fp32: mean and rstd, for the gradient
  * residual, weight, bias, total and stats may be NULL.  y and total may each be
  * x or residual themselves (same address and stride), not both the same one.
+ * A row's result depends on its values and on where they lie towards 16-byte
+ * boundaries (the order of its sums), on nothing else.
  *   rows 0 .. 2^31-1;  dim 1 .. 2^20;  eps >= 0 */
 typedef struct {
     int32_t dtype, y_dtype, w_dtype, dim;
@@ -764,7 +766,7 @@ typedef struct {
 typedef struct {
     double beta1, beta2, eps;
     int64_t step;              /* 1 for the first one                        */
-    const int64_t *step_device; /* read instead of `step` if not NULL, so
+    const int64_t *step_device; /* read instead of `step` if not NULL (at least 1), so
                                   that a captured step may be replayed       */
     const float *lr;           /* device, one value, or NULL                 */
     const float *grad_scale;   /* device, one value, or NULL: 1              */

@@ -7,8 +7,8 @@
 // tensor by bisection over the table.  A warp takes a block at a time, each lane 2 x 4
 // elements 128 apart, so every access of a warp is one contiguous run.
 //
-// Bound: memory.  32 bits: 28 bytes an element of fp32 parameters and gradients; 8 bits: 16, and some 70
-// instructions.
+// Bound, for fp32 parameters with bf16 gradients and copies: 32 bits memory, 28 bytes an element (118 M of them
+// 484 us, 6.8 TB/s); 8 bits 16 bytes, and 80 instructions (368 us, 5.2 TB/s at 77 % of the issue slots).
 //
 // 8 bits: scales are powers of two, so scaling is exact and a value that a code stands for
 // stays where it is while the block's largest one keeps its octave.  Codes are cut from the bits of the value
@@ -41,7 +41,7 @@ struct Tensor {
   unsigned first_cta;  // of this launch
   float rate, keep;    // lr / (1 - beta1^step) and 1 - lr weight_decay; both of lr 1, the latter without
                        // the 1 -, where lr is on the device
-  uint8_t dtype, grad_dtype, copy_dtype, wide;
+  uint8_t dtype, grad_dtype, copy_dtype, wide;  // wide: four values at once are aligned everywhere
 };
 struct Common {
   float beta1, one_beta1, beta2, one_beta2, eps, root;  // root: 1 / sqrt(1 - beta2^step)

@@ -19,7 +19,8 @@
 //                 sides in fp32; m lower bounds reach some threshold, and those whose upper bound does
 //                 are formed in 64 bits and sorted.
 //
-// Bound: memory for the scores, else the latency of two launches and some twenty barriers.
+// Bound: memory for the scores, else the latency of two launches and some twenty barriers: 64 x 8 rows of 50,021
+// bf16 scores 27 us (17 of them the pass, 51 MB), 4 rows of fp32 14, 256 beams of 8 options 16 on one SM.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>

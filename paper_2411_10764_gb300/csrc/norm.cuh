@@ -7,14 +7,15 @@
 //   the rest        a CTA a row that keeps it in shared memory or reads it again out of L2.  (Clusters of CTAs with
 //                   a row in their registers wait for all their stores at each of two barriers a row:
 //                   4,096 x 16,384 bf16 154 us by two CTAs a row, 216 by four.)
-// What costs beside memory is the work for each row and thread (shuffles, barrier, addresses: some 100
-// instructions), so threads take many values: 16,384 x 4,096 bf16 with eight a thread 136 us and 46
-// instructions a value, with 32 see norm.cu.
+// What costs beside memory is the work for each row and thread (shuffles, barrier, addresses: some 200
+// instructions), so threads take as many values as registers allow: 16,384 x 4,096 bf16 with eight a thread
+// 136 us and 46 instructions a value, with sixteen 85 and 33.
 //
 // Threads take packs of 16 bytes wherever all tensors' rows lie alike towards 16-byte boundaries, as
 // contiguous tensors of any dim do: packs are counted from the boundary before the row (`skew` values before
-// its first), and the two at its ends are taken value by value.  A team takes
+// its first), the two at its ends are read whole and written value by value.  A team takes
 // rows whose skew is the same, so its columns stay its own.  Else packs are single values.
+// Packs or not, and how many values a thread, follow from addresses, strides and dim alone.
 #pragma once
 
 #include <type_traits>

@@ -3,7 +3,9 @@
 // With h = (t - mean) rstd and gw = gy weight, two sums over the row (gw and gw h) give the
 // input's gradient.  Each thread keeps its columns' sums of gy h and gy in registers over
 // all rows of its team; the teams' sums go to the workspace and a second
-// kernel adds them up in a fixed order.  Bound: memory (x and gy read, gx written, once).
+// kernel adds them up in a fixed order.  Bound: memory (x and gy read, gx written, once), and
+// instructions: 32,768 x 2,048 bf16 with g_total 104 us, 5.2 TB/s, at 62 % of the issue slots (34 instructions a value;
+// the sums' 32 registers leave 15 warps an SM); 1,048,573 x 61 fp32 155 us, 4.9 TB/s.
 // Of n equal terms in a plain sum the error grows with n: where a thread has more than kPlainRows rows, every
 // so many its sums move on to pairs of numbers in the workspace (Knuth's exact addition), 32 bytes a
 // column that stay in L2.  (In shared memory they halved the warps that fit.)
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(1024)
 }
 
 struct Plan {
-  bool far;  // rows that no cluster holds
+  bool far;  // rows that registers do not hold
   bool group;
   int lanes, threads;
   long long teams;  // of rows, and of partial sums
