@@ -62,7 +62,8 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
   for (; base < a.rows; base += step) {
     const long long row = base + sub;
     const bool live = row < a.rows;
-    float t[C][V], total[1] = {0.0f};
+    constexpr int E = C * V;
+    float2 t[E / 2], s = both(0.0f);
     if (add && live) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -76,31 +77,24 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
 #pragma unroll
       for (int c = 0; c < C; ++c) cols.store(px[c], static_cast<TI*>(a.total) + row * a.total_stride, c);
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float s = 0.0f;
-      cols.template each<CTA>(c, [&](int c, int v, bool on) {
-        t[c][v] = on && live ? px[c].get(v) : 0.0f;
-        s += t[c][v];
-      });
-      total[0] += s;
-    }
+    cols.template pairs<CTA>([&](int i, bool on0, bool on1) {
+      const bool all = CTA || live;
+      t[i / 2] = masked(two_of(px, i), on0 && all, on1 && all);
+      s = __fadd2_rn(s, t[i / 2]);
+    });
+    float total[1] = {s.x + s.y};
     if (base + step < a.rows) fetch(row + step);
     if (CTA)
       row_sums(total, sums, slot);
     else
       group_sums(total, lanes);
     const float mean = total[0] / a.dim;
-    total[0] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float s = 0.0f;
-      cols.template each<CTA>(c, [&](int c, int v, bool on) {
-        t[c][v] = on ? t[c][v] - mean : 0.0f;
-        s = fmaf(t[c][v], t[c][v], s);
-      });
-      total[0] += s;
-    }
+    s = both(0.0f);
+    cols.template pairs<CTA>([&](int i, bool on0, bool on1) {
+      t[i / 2] = masked(__fadd2_rn(t[i / 2], both(-mean)), on0, on1);
+      s = __ffma2_rn(t[i / 2], t[i / 2], s);
+    });
+    total[0] = s.x + s.y;
     if (CTA)
       row_sums(total, sums, slot);
     else
@@ -116,10 +110,20 @@ __global__ void __maxnreg__(registers(CTA, EDGE))
         bs.get(b[c], c);
       }
       float f[V];
+      auto value = [&](int i) {
+        const float2 h = __fmul2_rn(t[i / 2], both(rstd));
+        return !CTA || scaled ? __ffma2_rn(h, two_of(w, i), two_of(b, i)) : h;
+      };
+      if constexpr (V == 1) {
+        const float h = one_of(t, c) * rstd;
+        f[0] = !CTA || scaled ? fmaf(h, w[c][0], b[c][0]) : h;
+      } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float h = t[c][v] * rstd;
-        f[v] = !CTA || scaled ? fmaf(h, w[c][v], b[c][v]) : h;
+        for (int v = 0; v < V; v += 2) {
+          const float2 d = value(c * V + v);
+          f[v] = d.x;
+          f[v + 1] = d.y;
+        }
       }
       Vec<TO, V> q;
       q.put(f);

@@ -192,6 +192,24 @@ struct Vec {
   }
 };
 
+// Places i and i + 1 of packs, of numbers by pack, and one of numbers by two.
+template <typename T, int V, int C>
+__device__ __forceinline__ float2 two_of(const Vec<T, V> (&p)[C], int i) {
+  return make_float2(p[i / V].get(i % V), p[(i + 1) / V].get((i + 1) % V));
+}
+template <int V, int C>
+__device__ __forceinline__ float2 two_of(const float (&w)[C][V], int i) {
+  return make_float2(w[i / V][i % V], w[(i + 1) / V][(i + 1) % V]);
+}
+template <int N>
+__device__ __forceinline__ float& one_of(float2 (&x)[N], int i) {
+  return i & 1 ? x[i / 2].y : x[i / 2].x;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 masked(float2 v, bool on0, bool on1) {
+  return make_float2(on0 ? v.x : 0.0f, on1 ? v.y : 0.0f);
+}
+
 // The columns of a thread: C packs of V, `hop` values apart.
 template <int V, int C, bool EDGE>
 struct Columns {
@@ -245,15 +263,24 @@ struct Columns {
       }
     }
   }
-  // f(c, v, whether it is a value of the row) for each place.  BRANCH: whole packs apart, where few have edges.
+  // f(i, whether the places i and i + 1 of the thread's C * V are values of the row) for each two places, which
+  // go through two-wide operations together.  BRANCH: whole packs apart, where few have edges.
   template <bool BRANCH, typename F>
-  __device__ __forceinline__ void each(int c, F f) const {
-    if ((BRANCH || !EDGE) && whole(c)) {
+  __device__ __forceinline__ void pairs(F f) const {
+    if constexpr (V == 1) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) f(c, v, true);
+      for (int c = 0; c < C; c += 2) f(c, mask[c] != 0, mask[c + 1] != 0);
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) f(c, v, EDGE && on(c, v));
+      for (int c = 0; c < C; ++c) {
+        if ((BRANCH || !EDGE) && whole(c)) {
+#pragma unroll
+          for (int v = 0; v < V; v += 2) f(c * V + v, true, true);
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; v += 2) f(c * V + v, EDGE && on(c, v), EDGE && on(c, v + 1));
+        }
+      }
     }
   }
   template <typename T>

@@ -55,7 +55,8 @@ __global__ void __maxnreg__(registers(CTA, V))
   const Columns<V, C, EDGE> cols(j * V, lanes * V, skew, a.dim);
   const bool scaled = a.weight != nullptr;
   const Kept<V, C> ws{mem};
-  float w[C][V], sw[C][V], sb[C][V];
+  float w[C][V];
+  float2 sw[E / 2], sb[E / 2];
   const bool more = g.g_total != nullptr;
   const float inv_dim = 1.0f / a.dim;
   const TI *x0 = static_cast<const TI*>(a.x), *t0 = static_cast<const TI*>(g.g_total);
@@ -93,9 +94,7 @@ __global__ void __maxnreg__(registers(CTA, V))
     if (CTA) ws.put(w);
   }
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int v = 0; v < V; ++v) sw[c][v] = sb[c][v] = 0.0f;
+  for (int i = 0; i < E / 2; ++i) sw[i] = sb[i] = both(0.0f);
   if (CTA) sums.clear();
   __syncthreads();
   float* own = moved + blockIdx.x * 4LL * E * blockDim.x + threadIdx.x;
@@ -112,11 +111,11 @@ __global__ void __maxnreg__(registers(CTA, V))
         if (!first_move)
 #pragma unroll
           for (int k = 0; k < 4; ++k) s[k] = at[k * hop];
-        add_exactly(s[0], s[1], sw[c][v]);
-        add_exactly(s[2], s[3], sb[c][v]);
+        add_exactly(s[0], s[1], one_of(sw, c * V + v));
+        add_exactly(s[2], s[3], one_of(sb, c * V + v));
 #pragma unroll
         for (int k = 0; k < 4; ++k) at[k * hop] = s[k];
-        sw[c][v] = sb[c][v] = 0.0f;
+        one_of(sw, c * V + v) = one_of(sb, c * V + v) = 0.0f;
       }
     }
     first_move = false;
@@ -133,30 +132,30 @@ __global__ void __maxnreg__(registers(CTA, V))
       cols.load(pt, t0 + row * g.g_total_stride, t0, t1);
     }
     const float mean = next.x, rstd = next.y;
-    float h[C][V], gw[C][V], total[2] = {0.0f, 0.0f};
+    if constexpr (kInRing)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (CTA && scaled) ws.get(w[c], c);
-      if constexpr (kInRing) {
+      for (int c = 0; c < C; ++c) {
         px[c] = ring.template get<TI>(stage, 0, c);
         pg[c] = ring.template get<TO>(stage, 1, c);
       }
-      float s0 = 0.0f, s1 = 0.0f;
-      cols.template each<CTA>(c, [&](int c, int v, bool on) {
-        on = on && live;
-        h[c][v] = on ? (px[c].get(v) - mean) * rstd : 0.0f;
-        const float gy = on ? pg[c].get(v) : 0.0f;
-        if (SUMS) {
-          sw[c][v] = fmaf(gy, h[c][v], sw[c][v]);
-          sb[c][v] += gy;
-        }
-        gw[c][v] = !CTA || scaled ? gy * w[c][v] : gy;
-        s0 += gw[c][v];
-        s1 = fmaf(gw[c][v], h[c][v], s1);
-      });
-      total[0] += s0;
-      total[1] += s1;
-    }
+    if (CTA && scaled)
+#pragma unroll
+      for (int c = 0; c < C; ++c) ws.get(w[c], c);
+    float2 h[E / 2], gw[E / 2], s0 = both(0.0f), s1 = both(0.0f);
+    cols.template pairs<CTA>([&](int i, bool on0, bool on1) {
+      const bool all = CTA || live;
+      const float2 x = __fmul2_rn(__fadd2_rn(two_of(px, i), both(-mean)), both(rstd));
+      h[i / 2] = masked(x, on0 && all, on1 && all);
+      const float2 gy = masked(two_of(pg, i), on0 && all, on1 && all);
+      if (SUMS) {
+        sw[i / 2] = __ffma2_rn(gy, h[i / 2], sw[i / 2]);
+        sb[i / 2] = __fadd2_rn(sb[i / 2], gy);
+      }
+      gw[i / 2] = !CTA || scaled ? __fmul2_rn(gy, two_of(w, i)) : gy;
+      s0 = __fadd2_rn(s0, gw[i / 2]);
+      s1 = __ffma2_rn(gw[i / 2], h[i / 2], s1);
+    });
+    float total[2] = {s0.x + s0.y, s1.x + s1.y};
     if (!kInRing && base + step < a.rows) fetch(row + step, 0);
     if (CTA)
       row_sums(total, sums, slot);
@@ -177,10 +176,20 @@ __global__ void __maxnreg__(registers(CTA, V))
         if (more) pt[c] = ring.template get<TI>(now, 2, c);
       }
       float f[V];
+      auto value = [&](int i) {
+        const float2 d = __fmul2_rn(__ffma2_rn(h[i / 2], both(-m1), __fadd2_rn(gw[i / 2], both(-m0))), both(rstd));
+        return more ? __fadd2_rn(d, two_of(pt, i)) : d;
+      };
+      if constexpr (V == 1) {
+        const float2 d = value(c & ~1);
+        f[0] = c & 1 ? d.y : d.x;
+      } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float d = fmaf(-h[c][v], m1, gw[c][v] - m0) * rstd;
-        f[v] = more ? d + pt[c].get(v) : d;
+        for (int v = 0; v < V; v += 2) {
+          const float2 d = value(c * V + v);
+          f[v] = d.x;
+          f[v + 1] = d.y;
+        }
       }
       Vec<TI, V> q;
       q.put(f);
@@ -195,8 +204,8 @@ __global__ void __maxnreg__(registers(CTA, V))
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float* at = own + (c * V + v) * blockDim.x;
-        sw[c][v] = at[0] + at[hop];
-        sb[c][v] = at[2 * hop] + at[3 * hop];
+        one_of(sw, c * V + v) = at[0] + at[hop];
+        one_of(sb, c * V + v) = at[2 * hop] + at[3 * hop];
       }
   }
   if (CTA) {
@@ -207,8 +216,8 @@ __global__ void __maxnreg__(registers(CTA, V))
       for (int v = 0; v < V; ++v)
         if (cols.on(c, v)) {
           const int col = cols.first + c * cols.hop + v;
-          out[col] = sw[c][v];
-          out[a.dim + col] = sb[c][v];
+          out[col] = one_of(sw, c * V + v);
+          out[a.dim + col] = one_of(sb, c * V + v);
         }
     return;
   }
@@ -222,7 +231,7 @@ __global__ void __maxnreg__(registers(CTA, V))
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int v = 0; v < V; ++v) mem[group * places + c * cols.hop + j * V + v] = k == 0 ? sw[c][v] : sb[c][v];
+      for (int v = 0; v < V; ++v) mem[group * places + c * cols.hop + j * V + v] = k == 0 ? one_of(sw, c * V + v) : one_of(sb, c * V + v);
     __syncthreads();
     float s = 0.0f, rest = 0.0f;
     for (int col = threadIdx.x % wide; col < a.dim; col += kGroupThreads) {
