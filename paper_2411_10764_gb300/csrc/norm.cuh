@@ -9,7 +9,7 @@
 //                   4,096 x 16,384 bf16 154 us by two CTAs a row, 216 by four.)
 // What costs beside memory is the work for each row and thread (shuffles, barrier, addresses: some 200
 // instructions), so threads take as many values as registers allow: 16,384 x 4,096 bf16 with eight a thread
-// 136 us and 46 instructions a value, with sixteen 85 and 33.
+// 136 us and 46 instructions a value, with sixteen 86 and, two-wide where they can be, 24.
 //
 // Threads take packs of 16 bytes wherever all tensors' rows lie alike towards 16-byte boundaries, as
 // contiguous tensors of any dim do: packs are counted from the boundary before the row (`skew` values before

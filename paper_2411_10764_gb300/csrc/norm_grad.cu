@@ -4,12 +4,13 @@
 // input's gradient.  Each thread keeps its columns' sums of gy h and gy in registers over
 // all rows of its team; the teams' sums go to the workspace and a second
 // kernel adds them up in a fixed order.  Bound: memory (x and gy read, gx written, once), and
-// instructions: 32,768 x 2,048 bf16 with g_total 104 us, 5.2 TB/s, at 62 % of the issue slots (34 instructions a value;
-// the sums' 32 registers leave 15 warps an SM); 1,048,573 x 61 fp32 155 us, 4.9 TB/s.
+// instructions and latency: 32,768 x 2,048 bf16 with g_total 97 us, 5.5 TB/s, at 52 % of the issue slots (27
+// instructions a value, two-wide where they can be; the sums' 32 registers leave 15 warps an SM);
+// 1,048,573 x 61 fp32 155 us, 4.9 TB/s.
 // Of n equal terms in a plain sum the error grows with n: where a thread has more than kPlainRows rows, every
 // so many its sums move on to pairs of numbers in the workspace (Knuth's exact addition), 32 bytes a
 // column that stay in L2.  (In shared memory they halved the warps that fit.)
-// Rows are on their way two ahead, in shared memory: in registers, one ahead, 32,768 x 2,048 took 145 us.
+// Rows are on their way two ahead, in shared memory: in registers, one ahead, 32,768 x 2,048 took 145 us for 104.
 #include <utility>
 
 #include "norm.cuh"
