@@ -71,8 +71,10 @@ __device__ __forceinline__ float power(float x) {
   return r;
 }
 __device__ __forceinline__ float exp_in(float x, float unit) { return power(fmaf(x, kLog2E, -unit)); }
-// Scores of 1e37 and more: next to such a one only its equals count, and the unit is exp of it.
-__device__ __forceinline__ bool is_huge(float top) { return !(fabsf(top) < 1e37f); }
+// Scores of 2^30 and more, whose neighbours are 64 and more apart: next to such a one only its equals count (2^22
+// others are 2^-70 of it), and the unit is exp of it.  Below, the product by log2 e is off by at most 64 when it is rounded
+// to a unit, so terms are at most 2^64 and sums finite; above 2^31 it is off by more than fp32's exponents hold.
+__device__ __forceinline__ bool is_huge(float top) { return !(fabsf(top) < 0x1p30f); }
 // The unit for terms up to exp(top); 0 where there are none.
 __device__ __forceinline__ float unit_of(float top) { return is_huge(top) ? 0.0f : rintf(top * kLog2E); }
 // exp(x) for x <= top, both finite or -infinity, in these units.
@@ -93,7 +95,8 @@ struct Two {
     add(o.hi);
     lo = __fadd_rn(lo, o.lo);
   }
-  // to another unit; an empty sum's may lie at any distance
+  // to another unit; an empty sum's may lie at any distance.  A NaN or infinite sum may not become a finite one:
+  // it is what a row is looked at again for
   __device__ __forceinline__ void scale(float f) {
     const float g = hi > 0.0f ? f : 0.0f;
     hi *= g;
