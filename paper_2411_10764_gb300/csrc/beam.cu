@@ -856,8 +856,7 @@ Plan plan_of(const mlt_beam_args& a, int sms) {
 template <typename T, bool FROM_ROWS>
 cudaError_t launch_items(const mlt_beam_args& a, const Plan& p, const RowPart* found, const u64* lists, cudaStream_t st) {
   if (p.smem > 40 * 1024) {  // with the static part past what a kernel has unasked, 48 KB
-    const cudaError_t e = cudaFuncSetAttribute(k_beam_items<T, FROM_ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               static_cast<int>(p.smem));
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_beam_items<T, FROM_ROWS>), p.smem);
     if (e != cudaSuccess) return e;
   }
   return launch_pdl(k_beam_items<T, FROM_ROWS>, dim3(a.batch), dim3(p.threads), p.smem, st, a, p.parts, p.k, found, lists,
@@ -1012,8 +1011,7 @@ cudaError_t launch_reorder(const int64_t* parent, int batch, int beams, const ml
   if (ctas == 0) return cudaSuccess;
   const size_t smem = (2 * beams * sizeof(int) + 15) / 16 * 16 + static_cast<size_t>(widest) * beams;
   if (smem > 40 * 1024) {  // with the static part past what a kernel has unasked, 48 KB
-    const cudaError_t e =
-        cudaFuncSetAttribute(k_beam_reorder, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_beam_reorder), smem);
     if (e != cudaSuccess) return e;
   }
   ++*launches;

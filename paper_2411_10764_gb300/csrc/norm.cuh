@@ -472,8 +472,7 @@ int resident_ctas(int threads, size_t smem) {
 template <typename... K, typename... A>
 cudaError_t launch_rows(void (*kernel)(K...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, A&&... args) {
   if (smem > 40 * 1024) {  // with the static part past what a kernel has unasked, 48 KB
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
   }
   return launch_pdl(kernel, dim3(grid), dim3(block), smem, st, std::forward<A>(args)...);
