@@ -961,9 +961,14 @@ def _adamw_rows(params, grads, copies, rates, decays, device):
 def _adamw_columns(params, grads, copies, rates, decays, device):
     """The same for many tensors, column by column."""
     Tensor, count = _torch.Tensor, len(params)
-    missing = [k for k, g in enumerate(grads) if g is None]
-    if missing:  # their parameters stand in for them, and have no address below
-        grads = [p if g is None else g for p, g in zip(params, grads)]
+    sizes = array("q", map(Tensor.numel, params))
+    have = [k for k, g in enumerate(grads) if g is not None]
+    if len(have) < count:  # the others' rows hold a size alone
+        params, grads, copies, rates, decays = (q if q is None else [q[k] for k in have]
+                                                for q in (params, grads, copies, rates, decays))
+    bare = () if copies is None else [k for k, c in enumerate(copies) if c is None]
+    if bare:  # the parameter stands in, and has no address below
+        copies = [p if c is None else c for p, c in zip(params, copies)]
     given = [params, grads] if copies is None else [params, grads, copies]
     for some in given:
         if any(d != device for d in map(Tensor.get_device, some)):
@@ -983,19 +988,25 @@ def _adamw_columns(params, grads, copies, rates, decays, device):
         if len(types) == 1:
             kinds += _DTYPES[types.pop()] << 16 * k
         elif types:
-            mixed = [x + (_DTYPES[t.dtype] << 16 * k) for x, t in zip(mixed or [0] * count, some)]
+            mixed = [x + (_DTYPES[t.dtype] << 16 * k) for x, t in zip(mixed or [0] * len(some), some)]
     words = list(map(_rate_words.get, zip(rates, decays)))
     if None in words:
         words = [_rate_word(a, b) for a, b in zip(rates, decays)]
+    columns = [array("q", map(Tensor.data_ptr, some)) for some in given] + [None] * (3 - len(given))
+    for k in bare:
+        columns[2][k] = 0
+    columns += [sizes, array("q", [kinds] * len(have) if mixed is None else [x + kinds for x in mixed]), array("q", words)]
     table = array("q", bytes(48 * count))
-    for k, some in enumerate(given):
-        table[k::6] = array("q", map(Tensor.data_ptr, some))
-    table[3::6] = sizes = array("q", map(Tensor.numel, params))
-    table[4::6] = array("q", [kinds] * count if mixed is None else [x + kinds for x in mixed])
-    table[5::6] = array("q", words)
+    for k, column in enumerate(columns):
+        if column is None:
+            continue
+        if len(column) < count:
+            whole = array("q", bytes(8 * count))
+            for i, x in zip(have, column):
+                whole[i] = x
+            column = whole
+        table[k::6] = column
     blocks = int((-(-np.frombuffer(sizes, np.int64) // ADAMW_BLOCK)).sum()) if count else 0
-    for k in missing:
-        table[6 * k + 1] = 0
     return table, blocks, given
 
 
@@ -1006,8 +1017,8 @@ def adamw(params, grads, state: AdamWState, step, lr=1e-3, betas=(0.9, 0.999), e
     None: that one is left as it is.  `step` counts from 1: a number or an int64 CUDA
     tensor of one value; `lr`: a number, a list of one for each tensor or an fp32 CUDA tensor of one
     value (tensors are read when the step runs, so a captured one may be replayed with others).
-    `lr_scale` multiplies it; `weight_decay`, `lr_scale`: a number or a list.  `copies`: a list of tensors
-    (or None) of the parameters' shapes that receive them in their types.  `grad_scale`: an
+    `lr_scale` multiplies it; `weight_decay`, `lr_scale`: a number or a list.  `copies`: None, or a list that has
+    for each parameter a tensor of its shape, which receives it in its own type, or None.  `grad_scale`: an
     fp32 CUDA tensor of one value that multiplies the gradients.  `seed`: of the rounding of moments in
     8 bits, 32 bits of it."""
     L = _setup()
