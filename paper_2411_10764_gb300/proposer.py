@@ -32,6 +32,19 @@ from . import mlt
 TAPS = 4
 
 
+def most_beams(radices) -> int:
+    """How many beams a search over knobs of these radices may keep: mlt.beam_step takes 1,024, and
+    8,192 continuations of which each beam has as many as are kept or its knob has options."""
+    return int(min(1024, max(90, 8192 // max(1, *radices))))  # w min(w, r) <= 8192, and 90 * 90 is below it
+
+
+def _check_beams(beams: int, radices) -> int:
+    most = most_beams(radices)
+    if not 1 <= beams <= most:
+        raise ValueError(f"between 1 and {most} beams can be kept over knobs of up to {max(1, *radices)} options, got {beams}")
+    return beams
+
+
 class Proposer:
     """Embedding -> selective scan with gate -> residual (-> layer norm) -> scores of digits, in fp32.
 
@@ -184,15 +197,14 @@ class Proposer:
             token = digit + self.offsets[j]
         return index, logp
 
-
     def search(self, m: int, beams: int | None = None):
-        """The m most probable candidates that a beam of `beams` (default: m) finds, best first:
-        (indices int64 [m], -1 where there are fewer; log-probabilities [m])."""
+        """The m most probable candidates that a beam of `beams` (default: m; no fewer than m are kept) finds, best
+        first: (indices int64 [m], -1 where there are fewer; log-probabilities [m]).  At most most_beams(radices)."""
         import torch
 
+        w = _check_beams(max(m, beams or m), self.radices)
         P = self.params
         device = P["table"].device
-        w = max(m, beams or m)
         state = torch.zeros((w, self.inner, self.states), device=device)
         conv = torch.zeros((w, TAPS - 1, self.inner), device=device)
         token = torch.full((w, 1), self.vocab - 1, dtype=torch.int64, device=device)
@@ -215,10 +227,13 @@ def explore(decoder, thr: float, first: int, n: int, keep: int = 256, chains: in
     """One round over a knob space whose V and P models are loaded: screen candidates first ..
     first + n - 1, draw `keep` of the valid ones by their scores, train a proposer on them, and
     anneal one step from its proposals, the first up to `beams` of them its most probable
-    candidates, the others drawn.  Returns a dict of tensors and the losses."""
+    candidates, the others drawn (at most most_beams(decoder.radices), 0: all drawn).  Returns a dict of tensors and
+    the losses."""
     import torch
 
     r, ov, prog = decoder.radices, decoder.option_values, decoder.program
+    if beams:
+        _check_beams(min(beams, chains), r)
     _, perf, topk = mlt.screen_decoded(r, ov, prog, first, n, thr, keep)
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
@@ -248,7 +263,8 @@ def main(argv=()) -> None:
     p = argparse.ArgumentParser(prog="python -m paper_2411_10764_gb300.proposer", description=__doc__.splitlines()[0])
     p.add_argument("--norm", action="store_true", help="end the block in a layer norm")
     p.add_argument("--adamw", action="store_true", help="train with AdamW")
-    p.add_argument("--beams", type=int, default=0, help="anneal from so many most probable candidates too")
+    p.add_argument("--beams", type=int, default=0, help="anneal from so many most probable candidates too (up to 1024; "
+                   "fewer where a knob has more than 8 options)")
     args = p.parse_args(argv)
     w = W.make_workload(4, seed=1, n=65536)
     mlt.load_workload_models(w)

@@ -129,3 +129,16 @@ def test_a_round_with_everything():
 def test_command(capsys):
     proposer.main(["--norm", "--adamw", "--beams", "64"])
     assert "annealed proposals valid" in capsys.readouterr().out
+
+
+def test_search_keeps_as_many_beams_as_may_be():
+    import torch
+
+    for radices in ([9, 16, 9], [91, 3], [2, 3]):
+        model = Proposer(radices, dim=16, inner=16, seed=6)
+        most = proposer.most_beams(radices)
+        index, logp = model.search(most)
+        found, count = index[index >= 0], min(most, math.prod(radices))
+        assert found.numel() == count and found.unique().numel() == count
+        assert (logp[1:count] <= logp[:count - 1]).all() and (logp[count:] == -math.inf).all()
+        assert torch.equal(model.search(3, 0)[0], model.search(3)[0])
