@@ -677,9 +677,10 @@ int mlt_scan_grad_workspace(const mlt_scan_args *args, size_t *bytes_out);
  *   weight, bias  device [dim] of `w_dtype`
  *   stats     device [rows][2] fp32: mean and rstd, for the gradient
  * residual, weight, bias, total and stats may be NULL.  y and total may each be
- * x or residual themselves (same address and stride), not both the same one.
- * A row's result depends on its values and on where they lie towards 16-byte
- * boundaries (the order of its sums), on nothing else.
+ * x or residual themselves (same address, type and stride; at that address others
+ * are refused), not both the same one.
+ * A row's result depends on its values and on where it lies, in each of the tensors,
+ * towards 16-byte boundaries (the order of its sums), on nothing else.
  *   rows 0 .. 2^31-1;  dim 1 .. 2^20;  eps >= 0 */
 typedef struct {
     int32_t dtype, y_dtype, w_dtype, dim;
@@ -700,8 +701,8 @@ int mlt_layer_norm(void *stream, const mlt_norm_args *args);
  * are not used.
  *   h  = (t - mean) rstd;  gw = gy weight
  *   gx = round(rstd (gw - mean(gw) - h mean(gw h)) + g_total), the gradient of x
- *        and of residual alike;  gx may be gy or g_total themselves where the
- *        types are the same
+ *        and of residual alike;  gx may be x, g_total or, where the types are
+ *        the same, gy themselves (same address and stride)
  *   gweight = round(sum over rows of gy h), gbias = round(sum over rows of gy), of
  *        `w_dtype`, summed in a fixed order; 0 without rows
  * Each output may be NULL. */

@@ -107,6 +107,12 @@ int check_norm(const mlt_norm_args* a) {
   return MLT_OK;
 }
 
+// Whether an output of rows that begins where an input does is that input, of its type and stride.
+bool is_itself(const void* out, int out_dtype, int64_t out_stride, const void* in, int in_dtype, int64_t in_stride,
+               int64_t rows) {
+  return out == nullptr || out != in || (out_dtype == in_dtype && (rows <= 1 || out_stride == in_stride));
+}
+
 int check_tensors(const mlt_adamw_tensor* tensors, int count) {
   if (count < 0 || count > (1 << 20)) return api_fail(MLT_EINVAL, "count must lie in [0, 2^20], got %d", count);
   if (count > 0 && tensors == nullptr) return api_fail(MLT_EINVAL, "tensors must be non-NULL");
@@ -348,6 +354,14 @@ int mlt_layer_norm(void* stream, const mlt_norm_args* args) {
       (args->total != nullptr && !stride_ok(args->total_stride, args->dim, args->rows)))
     return api_fail(MLT_EINVAL, "rows must be at least dim elements apart");
   if (args->total != nullptr && args->total == args->y) return api_fail(MLT_EINVAL, "y and total must differ");
+  struct {
+    const void* p;
+    int64_t stride;
+  } in[] = {{args->x, args->x_stride}, {args->residual, args->residual_stride}};
+  for (const auto& t : in)
+    if (!is_itself(args->y, args->y_dtype, args->y_stride, t.p, args->dtype, t.stride, args->rows) ||
+        !is_itself(args->total, args->dtype, args->total_stride, t.p, args->dtype, t.stride, args->rows))
+      return api_fail(MLT_EINVAL, "y and total over an input must be of its type and stride");
   if (!aligned_to(args->residual, dtype_size(args->dtype)) || !aligned_to(args->total, dtype_size(args->dtype)) ||
       !aligned_to(args->y, dtype_size(args->y_dtype)))
     return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
@@ -385,6 +399,10 @@ int mlt_layer_norm_grad(void* stream, const mlt_norm_args* args, const mlt_norm_
       !aligned_to(grads->gx, dtype_size(args->dtype)) || !aligned_to(grads->gweight, dtype_size(args->w_dtype)) ||
       !aligned_to(grads->gbias, dtype_size(args->w_dtype)))
     return api_fail(MLT_EINVAL, "buffers must be aligned to their elements");
+  if (!is_itself(grads->gx, args->dtype, grads->gx_stride, grads->gy, args->y_dtype, grads->gy_stride, args->rows) ||
+      !is_itself(grads->gx, args->dtype, grads->gx_stride, grads->g_total, args->dtype, grads->g_total_stride, args->rows) ||
+      !is_itself(grads->gx, args->dtype, grads->gx_stride, args->x, args->dtype, args->x_stride, args->rows))
+    return api_fail(MLT_EINVAL, "gx over an input must be of its type and stride");
   const bool sums = grads->gweight != nullptr || grads->gbias != nullptr;
   const int sms = api_sm_count();
   rc = check_ws(workspace, workspace_bytes, sums ? norm_grad_workspace(args->rows, args->dim, sms) : 0);

@@ -834,7 +834,7 @@ def layer_norm_grad(gy, x, stats, weight=None, bias=None, g_total=None, out=None
     """mlt_layer_norm_grad: the gradients of layer_norm's inputs from those of y (`gy`) and of
     total (`g_total`, or None).  `x` is what was normed: the total where a residual was added.
     Returns a dict: "x" (x's type, also the residual's gradient), "weight" and
-    "bias" (their types; None where they were not given).  `out` receives "x" and may be g_total, or
+    "bias" (their types; None where they were not given).  `out` receives "x" and may be x, g_total, or
     gy where the types are the same."""
     L = _setup()
     if stream is not None:

@@ -54,3 +54,19 @@ def test_gradient(L):
     assert L.mlt_layer_norm_grad_workspace(3, 8, None) == -1
     for rows, dim in ((-1, 8), (3, 0), (3, (1 << 20) + 1)):
         assert L.mlt_layer_norm_grad_workspace(rows, dim, C.byref(size)) == -1
+
+
+def test_outputs_over_inputs(L):
+    """Where an output begins at an input's address it has to be that input, or rows would be written before others
+    have read theirs."""
+    for bad in (dict(x_stride=0), dict(y_stride=16), dict(y_dtype=1), dict(rows=1, y_dtype=2),
+                dict(y=512, residual=512), dict(y=512, total=256, total_stride=16), dict(y=512, total=1024, residual=1024),
+                dict(y=512, residual=512, residual_stride=8, y_dtype=1)):
+        assert L.mlt_layer_norm(None, _args(**bad)) == -1 and b"over an input" in L.mlt_last_error(), bad
+    for bad, args in ((dict(gy=512, g_total=256, g_total_stride=0), {}), (dict(gy_stride=0), {}), (dict(gx_stride=16), {}),
+                      (dict(), dict(y_dtype=1)), (dict(gy=512), dict(x_stride=0))):
+        g = mlt.NormGrads(256, None, 8, 8, 256, 8, 256, 256)
+        for k, v in bad.items():
+            setattr(g, k, v)
+        assert L.mlt_layer_norm_grad(None, _args(**args), C.byref(g), None, 0) == -1
+        assert b"over an input" in L.mlt_last_error(), (bad, args)
