@@ -827,7 +827,8 @@ int mlt_beam_step_workspace(const mlt_beam_args *args, size_t *bytes_out);
  * their own parents are not touched.
  *   tensors  host, [count], 0 .. 64 of them, read before the call returns:
  *            [batch * beams] rows of row_bytes bytes, row_stride bytes apart;
- *            they must not overlap each other or parent (compared and refused)
+ *            they must not overlap each other or parent (compared and refused; columns
+ *            of one buffer, at one row_stride, do not)
  *   parent   device [batch][beams] int64
  *   batch 0 .. 65535;  beams 1 .. 1024 */
 typedef struct {

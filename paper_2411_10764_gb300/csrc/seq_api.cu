@@ -141,6 +141,16 @@ void add_range(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges, const void*
   if (p != nullptr && bytes > 0) ranges.emplace_back(at, at + static_cast<uintptr_t>(bytes));
 }
 
+// Whether two states of so many rows have no byte in common: one behind the other, or columns of one buffer.
+bool apart(const mlt_beam_state& s, const mlt_beam_state& t, int64_t rows) {
+  const mlt_beam_state &a = s.data < t.data ? s : t, &b = s.data < t.data ? t : s;
+  const uintptr_t far = reinterpret_cast<uintptr_t>(b.data) - reinterpret_cast<uintptr_t>(a.data);
+  if (far >= static_cast<uintptr_t>((rows - 1) * a.row_stride + a.row_bytes)) return true;
+  if (rows == 1 || a.row_stride != b.row_stride) return false;
+  const int64_t column = static_cast<int64_t>(far % static_cast<uintptr_t>(a.row_stride));
+  return column >= a.row_bytes && column + b.row_bytes <= a.row_stride;
+}
+
 int check_beam(const mlt_beam_args* a) {
   if (a == nullptr) return api_fail(MLT_EINVAL, "args must be non-NULL");
   if (!dtype_ok(a->dtype)) return api_fail(MLT_EINVAL, "unknown element type %d", a->dtype);
@@ -508,7 +518,7 @@ int mlt_beam_step(void* stream, const mlt_beam_args* args, void* workspace, size
 }
 
 int mlt_beam_reorder(void* stream, const int64_t* parent, int batch, int beams, const mlt_beam_state* tensors,
-                     int count) try {
+                     int count) {
   if (batch < 0 || batch > 65535) return api_fail(MLT_EINVAL, "batch must lie in [0, 65535], got %d", batch);
   if (beams < 1 || beams > kBeamMostBeams)
     return api_fail(MLT_EINVAL, "beams must lie in [1, %d], got %d", kBeamMostBeams, beams);
@@ -516,7 +526,8 @@ int mlt_beam_reorder(void* stream, const int64_t* parent, int batch, int beams, 
     return api_fail(MLT_EINVAL, "count must lie in [0, %d], got %d", kBeamMostStates, count);
   if (count > 0 && tensors == nullptr) return api_fail(MLT_EINVAL, "tensors must be non-NULL");
   const int64_t rows = static_cast<int64_t>(batch) * beams;
-  std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+  int64_t moved = 0;
+  const mlt_beam_state list{const_cast<int64_t*>(parent), 8, 8};
   for (int i = 0; i < count; ++i) {
     const mlt_beam_state& t = tensors[i];
     if (t.row_bytes < 0 || t.row_bytes > (1LL << 40) || t.row_stride > (1LL << 40))
@@ -525,12 +536,17 @@ int mlt_beam_reorder(void* stream, const int64_t* parent, int batch, int beams, 
     if (t.data == nullptr) return api_fail(MLT_EINVAL, "tensor %d: data must be non-NULL", i);
     if (!stride_ok(t.row_stride, t.row_bytes, rows))
       return api_fail(MLT_EINVAL, "tensor %d: rows must be at least row_bytes apart", i);
-    add_range(ranges, t.data, (rows - 1) * t.row_stride + t.row_bytes);
+    if (rows > 1 && t.row_stride > (1LL << 60) / rows) return api_fail(MLT_EINVAL, "tensor %d: longer than 2^60 bytes", i);
+    ++moved;
   }
-  if (ranges.empty()) return MLT_OK;
+  if (moved == 0) return MLT_OK;
   if (parent == nullptr || !aligned_to(parent, 8)) return api_fail(MLT_EINVAL, "parent must be non-NULL, aligned to 8 bytes");
-  add_range(ranges, parent, rows * 8);
-  if (overlap(ranges)) return api_fail(MLT_EINVAL, "tensors must not overlap each other or parent");
+  for (int i = 0; i < count; ++i) {
+    if (tensors[i].row_bytes == 0) continue;
+    bool ok = apart(tensors[i], list, rows);
+    for (int j = 0; j < i; ++j) ok = ok && (tensors[j].row_bytes == 0 || apart(tensors[i], tensors[j], rows));
+    if (!ok) return api_fail(MLT_EINVAL, "tensors must not overlap each other or parent");
+  }
   int rc = MLT_OK;
   unsigned* err = api_error_word(&rc);
   if (err == nullptr) return rc;
@@ -538,8 +554,6 @@ int mlt_beam_reorder(void* stream, const int64_t* parent, int batch, int beams, 
   const cudaError_t e =
       launch_reorder(parent, batch, beams, tensors, count, err, &launches, static_cast<cudaStream_t>(stream));
   return launched(e, launches, "beam reorder launch");
-} catch (const std::bad_alloc&) {
-  return api_fail(MLT_ENOMEM, "out of host memory for %d tensors", count);
 }
 
 }  // extern "C"

@@ -53,3 +53,17 @@ def test_reorder(L):
         assert reorder(bad) == -1, bad
     assert reorder(one, (4096 + 448, 64, 64)) == -1  # the other's last row
     assert reorder() == 0 and reorder(one, batch=0) == 0 and reorder((4096, 0, 0), parent=None) == 0
+
+
+def test_states_side_by_side(L):
+    """Columns of one buffer that share a byte, or lie at different strides, are refused; so is what ends past 2^60 bytes."""
+    def reorder(*states, parent=1 << 30, batch=2, beams=4):
+        t = (mlt.BeamState * len(states))(*[mlt.BeamState(*s) for s in states])
+        return L.mlt_beam_reorder(None, parent, batch, beams, t, len(states))
+
+    one = (4096, 16, 64)
+    for other in ((4096 + 15, 8, 64), (4096 + 48, 17, 64), (4096 + 64, 16, 64), (4096 - 8, 9, 64), (4096 - 64 + 8, 8, 64),
+                  (4096 + 16, 16, 128), (4096, 16, 64), (4096 + 7 * 64 + 15, 1, 64), (4096 - 20, 30, 64)):
+        assert reorder(one, other) == -1 and b"overlap" in L.mlt_last_error(), other
+        assert reorder(other, one) == -1 and b"overlap" in L.mlt_last_error(), other
+    assert reorder((4096, 1, 1 << 40), batch=65535, beams=1024) == -1 and b"2^60" in L.mlt_last_error()
