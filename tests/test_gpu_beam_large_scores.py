@@ -55,7 +55,9 @@ def _check(x, logp, m, got):
         for j in range(have):
             total = want[j][0]
             tol = 2 * max(c[1] for c in want[max(0, j - 1):j + 2]) + 2.0 ** -50 * abs(total)
-            assert abs(out[b, j] - total) <= tol + U * abs(total) if total >= -FMAX else out[b, j] == -np.inf, (b, j)
+            # below the lowest float by half a step and more a total is -infinity
+            lowest = total <= -(FMAX + 2.0 ** 103)
+            assert out[b, j] == -np.inf if lowest else abs(out[b, j] - total) <= tol + U * abs(total), (b, j)
             near = [(c[2], c[4]) for c in want if abs(c[0] - total) <= tol]
             assert (parent[b, j], token[b, j]) in near, (b, j)
         assert len(set(zip(parent[b, :have].tolist(), token[b, :have].tolist()))) == have
