@@ -785,9 +785,14 @@ int mlt_adamw_blocks(const mlt_adamw_tensor *tensors, int count, int64_t *blocks
  * beams, the m best by their total log-probability.
  *   s       = score clamped to the finite floats; a NaN or -infinity score is no
  *             continuation
- *   lse[w]  = ln(sum over the continuations of beam w of exp s), or 0 with
- *             normalised != 0 (scores are log-probabilities)
- *   total   = logp[w] + (s - lse[w]), compared in more than 32 bits
+ *   lse[w]  = ln(sum over the continuations of beam w of exp s), a number of 64
+ *             bits, or 0 with normalised != 0 (scores are log-probabilities)
+ *   total   = logp[w] + (s - lse[w]), compared in 64 bits
+ * The terms of lse's sum are approximate powers in 32 bits: lse was off by 2^-24 to
+ * 2^-26 on average and by 2^-22.6 at most over 4,800 rows of 700 to 262,144 normal
+ * scores, so beams that are nearer than that may change places; equal rows have equal
+ * ones.  Where all of a row's best scores are large, the 64 bits round its ln:
+ * to 2e-6 at 1e10, to nothing from some 1e17 on.
  * Order: the larger total; then the lower beam, of one beam the higher score, then
  * the lower token.  A beam whose logp is NaN or -infinity has no continuations (a
  * search starts from logp 0 and -infinity for the other beams); a finished one
